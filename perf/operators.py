@@ -164,7 +164,8 @@ def _inputs(case, seed):
         h = normal(M, F, std=0.5)
         # rows without kept edges come out of the layer as zeros
         s["h"] = torch.where(torch.rand(M, 1, generator=gen, device=DEV) < 0.03, torch.zeros_like(h), h).to(TYPES[case["block"]])
-        s["gate"] = None if case["gate"] == "none" else normal(M if case["gate"] == "full" else 1, F, dtype=case["block"])
+        # a gate for every entry is the block's output, one for all rows is a parameter
+        s["gate"] = normal(M, F, dtype=case["block"]) if case["gate"] == "full" else normal(F) if case["gate"] == "row" else None
         s["post_w"], s["pre_w"] = 1.0 + normal(F, std=0.1), 1.0 + normal(F, std=0.1)
         s["post_b"], s["pre_b"] = (normal(F, std=0.1), normal(F, std=0.1)) if case["bias"] else (None, None)
         if op == "norm_grad":
@@ -220,7 +221,7 @@ def prepare(case, seed):
             if case["gate"] == "full":
                 s["dgate"] = torch.zeros((M, F), dtype=block, device=DEV)
             elif case["gate"] == "row":
-                s["dgate"] = torch.zeros((1, F), dtype=torch.float32, device=DEV)
+                s["dgate"] = torch.zeros(F, dtype=torch.float32, device=DEV)
             for k in ("dpost_w", "dpre_w"):
                 s[k] = torch.zeros(F, dtype=torch.float32, device=DEV)
             for k in ("dpost_b", "dpre_b"):
@@ -377,7 +378,7 @@ def _plain_norm_grad(s):
     out = [(c["beta"] * d).to(TYPES[c["stream"]]), dh.to(TYPES[c["block"]])]
     if a is not None:
         dg = t * n * da
-        out.append(dg.to(TYPES[c["block"]]) if c["gate"] == "full" else dg.sum(0, keepdim=True))
+        out.append(dg.to(TYPES[c["block"]]) if c["gate"] == "full" else dg.sum(0))
     out.append((dn * hat).sum(0))
     if c["bias"]:
         out.append(dn.sum(0))
