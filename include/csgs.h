@@ -69,7 +69,8 @@ enum {
     CSGS_ST_ADJ_OVERFLOW = 8,     /* sampled adjacency needs more than adj_cap entries */
     CSGS_ST_BAD_NODE_ID = 16,     /* an entry of S is outside [0, n_nodes) */
     CSGS_ST_EDGE_OVERFLOW = 32,   /* the rows of S hold more edges than the workspace was sized for */
-    CSGS_ST_INTERNAL = 64         /* a bounded wait between blocks ran out (should not happen) */
+    CSGS_ST_INTERNAL = 64,        /* a bounded wait between blocks ran out (should not happen) */
+    CSGS_ST_NONFINITE_GRAD = 128  /* the global gradient norm is NaN or infinite */
 };
 
 enum { CSGS_F32 = 0, CSGS_BF16 = 1 };
@@ -458,6 +459,138 @@ int csgs_aggregate_grad(const int32_t *adj_rowptr, const int32_t *adj_col, const
                         const int32_t *n_cols_dev, const float *dZ, int64_t lddz, int32_t F,
                         const float *H_prev, int64_t ldh, float *dH_prev, int64_t ldd, void *scratch,
                         size_t scratch_bytes, void *stream);
+
+/*
+ * Rows of a learned table (graphs whose nodes have no features learn a row per node; a layer that adds its nodes' own
+ * rows looks them up once more):
+ *     out[t, 0..F) = scale * T[ids[t], 0..F)     for t < n; a row of zeros where ids[t] is outside [0, rows)
+ * T [rows x F] of `dtype`, out [n x F] of `out_dtype` (CSGS_F32 or CSGS_BF16 each), leading dimensions ld and ldo in
+ * elements; rows start on any element.  Computed in fp32, one rounding.  n up to 2^31 - 1; n_dev as everywhere (rows of out
+ * past the device count are left untouched).
+ * Host errors: CSGS_EINVAL, CSGS_EUNSUPPORTED.
+ */
+int csgs_embed(const void *T, int64_t ld, int64_t rows, int32_t F, int dtype, const int32_t *ids, int64_t n,
+               const int32_t *n_dev, float scale, void *out, int64_t ldo, int out_dtype, void *stream);
+
+/*
+ * Gradient of csgs_embed: with G = dL/d out [n x F] of `g_dtype`, leading dimension ldg,
+ *     dT[v] = scale * sum of G[t] over the t < n with ids[t] = v
+ * Positions are sorted by id (stable); a row's sum is formed in ascending position over pieces of a fixed number of
+ * positions that are then added in order, in double, and rounded once: two calls on the same input give the same bits.  Ids
+ * outside [0, rows) contribute nothing, whatever their rows of G hold.
+ *
+ * csgs_embed_grad: the whole table's gradient, dT [rows x F] of `d_dtype`, leading dimension ldd.  accumulate = 0: every row is
+ *   written, zeros where no id points.  accumulate = 1: the sums are added to what dT holds (one rounding); other rows are
+ *   left untouched.
+ * csgs_embed_grad_rows: the rows that were looked up alone (a mini-batch looks up few of a graph's nodes):
+ *   uniq [n] out: the different ids inside [0, rows), ascending; *n_uniq of them; dR [n x F] of `d_dtype`, leading dimension
+ *   ldd: row j is the gradient of row uniq[j].  Entries past *n_uniq are left untouched.
+ * scratch: device, 256-byte aligned, csgs_embed_grad_scratch_bytes(n, rows, F) bytes (0 on bad input); nothing in it needs to
+ *   be kept or cleared between calls.
+ * Host errors: CSGS_EINVAL, CSGS_EWORKSPACE, CSGS_EUNSUPPORTED (dtype; n or rows above 2^31 - 1).
+ */
+size_t csgs_embed_grad_scratch_bytes(int64_t n, int64_t rows, int32_t F);
+int csgs_embed_grad(const int32_t *ids, int64_t n, const int32_t *n_dev, const void *G, int64_t ldg, int32_t F, int g_dtype,
+                    float scale, int accumulate, void *dT, int64_t ldd, int64_t rows, int d_dtype, void *scratch,
+                    size_t scratch_bytes, void *stream);
+int csgs_embed_grad_rows(const int32_t *ids, int64_t n, const int32_t *n_dev, const void *G, int64_t ldg, int32_t F,
+                         int g_dtype, float scale, int64_t rows, int32_t *uniq, int32_t *n_uniq, void *dR, int64_t ldd,
+                         int d_dtype, void *scratch, size_t scratch_bytes, void *stream);
+
+/*
+ * The end of a residual block and the norm in front of the next one, in one kernel:
+ *     y = beta x + alpha a(gate) .* N(h; post_w, post_b)          u = N(y; pre_w, pre_b)
+ * per row, where x is the residual stream, h the block's output (of the layer product, say) and
+ *     N(v; w, b) = w .* (v - m) / sqrt(mean((v - m)^2) + eps) + b
+ * with m = mean(v) for CSGS_NORM_LAYER and m = 0 for CSGS_NORM_RMS; CSGS_NORM_NONE (post only): N(v) = v.  a is the
+ * identity, the logistic function s(g), or g s(g).  u is formed from y before its rounding.
+ */
+enum { CSGS_NORM_NONE = 0, CSGS_NORM_RMS = 1, CSGS_NORM_LAYER = 2 };
+enum { CSGS_GATE_LINEAR = 0, CSGS_GATE_SIGMOID = 1, CSGS_GATE_SILU = 2 };
+
+typedef struct csgs_residual {
+    int32_t M, F;               /* rows (capacity if M_dev is given), width */
+    const int32_t *M_dev;       /* nullable */
+    const void *x;              /* [M x F] of x_dtype, nullable: no residual (beta x is absent) */
+    const void *h;              /* [M x F] of h_dtype, nullable: y = beta x.  One of the two is needed */
+    const void *gate;           /* nullable: 1.  ldg > 0: [M x F] of h_dtype; ldg = 0: one float row [F] for all rows */
+    int64_t ldx, ldh, ldg;      /* leading dimensions in elements */
+    const float *post_w, *post_b, *pre_w, *pre_b; /* [F] each, nullable: ones / zeros */
+    int32_t x_dtype, h_dtype;   /* stream (x, y, and their gradients) and block (h, gate, u, and theirs): both CSGS_F32, both
+                                   CSGS_BF16, or stream CSGS_F32 with block CSGS_BF16 */
+    int32_t post, pre;          /* CSGS_NORM_* */
+    int32_t gate_act;           /* CSGS_GATE_* */
+    float eps, alpha, beta;     /* eps >= 0 */
+} csgs_residual;
+
+/* y [M x F] of x_dtype, leading dimension ldy, nullable; u [M x F] of h_dtype, ldu, nullable (pre = CSGS_NORM_NONE: must be
+ * NULL); one of the two is needed.  An output may be an input of the same type at the same address with the same leading dimension (y = x,
+ * u = h); other overlaps are not allowed.  A row depends on its own rows of x, h and gate alone.  fp32, one rounding per output.
+ * Host errors: CSGS_EINVAL, CSGS_EUNSUPPORTED (types). */
+int csgs_norm_residual(const csgs_residual *r /*host*/, void *y, int64_t ldy, void *u, int64_t ldu, void *stream);
+
+/* Gradients of csgs_norm_residual from dy = dL/dy [M x F] of x_dtype (nullable: 0) and du = dL/du [M x F] of h_dtype
+ * (nullable: 0); `r` as in the forward call (nothing has to be kept from it but its inputs).
+ *   dx    [M x F] of x_dtype, nullable          dh [M x F] of h_dtype, nullable
+ *   dgate nullable: [M x F] of h_dtype with leading dimension lddg, or, where r->ldg = 0, a float row [F] (lddg ignored)
+ *   dpost_w, dpost_b, dpre_w, dpre_b  [F] float, nullable: sums over the rows
+ * Sums over rows are formed in fp32 over a fixed share of them and joined in double in a fixed order.  dx may be dy, dh may be
+ * du or h, dgate may be gate (same type, address and leading dimension); other overlaps are not allowed.
+ * scratch: device, 256-byte aligned, csgs_norm_residual_grad_scratch_bytes(M, F) bytes.
+ * Host errors: CSGS_EINVAL (also: an output whose input is absent), CSGS_EWORKSPACE, CSGS_EUNSUPPORTED. */
+size_t csgs_norm_residual_grad_scratch_bytes(int32_t M, int32_t F);
+int csgs_norm_residual_grad(const csgs_residual *r /*host*/, const void *dy, int64_t lddy, const void *du, int64_t lddu,
+                            void *dx, int64_t lddx, void *dh, int64_t lddh, void *dgate, int64_t lddg, float *dpost_w,
+                            float *dpost_b, float *dpre_w, float *dpre_b, void *scratch, size_t scratch_bytes, void *stream);
+
+/*
+ * Global norm over the gradients of a whole network, and clipping by it:
+ *     total = sqrt(sum |g|^2),  sum |g|  or  max |g|  over all entries of all tensors
+ *     c = min(1, max_norm / (total + 1e-6)),      out = c g
+ *
+ * The tensors are described once, in device memory that the caller owns, and the list is used as long as the buffers stay where
+ * they are (calls read whatever the tensors hold then): csgs_grad_list_bytes() bytes, 256-byte aligned, filled by
+ * csgs_grad_list_init, whose host array `t` may be freed after it returns.  Calls that share a list must be ordered on one stream.
+ */
+enum { CSGS_GRAD_L2 = 0, CSGS_GRAD_L1 = 1, CSGS_GRAD_MAX = 2 };
+
+typedef struct csgs_grad_tensor {
+    const void *g;            /* [rows x cols] of dtype, leading dimension ldg */
+    void *out;                /* the same type, leading dimension ldo; may be g (same leading dimension).  Nullable: the tensor counts in the norm alone */
+    int64_t rows, cols, ldg, ldo;
+    const int32_t *rows_dev;  /* nullable: min(max(*rows_dev, 0), rows) rows count, the others are left untouched */
+    int32_t dtype;            /* CSGS_F32 or CSGS_BF16 */
+    int32_t reserved;
+} csgs_grad_tensor;
+
+typedef struct csgs_grad_list {
+    void *base;               /* device buffer */
+    size_t bytes;
+    /* owned by the library: */
+    int64_t tiles;
+    int32_t n, ready;
+} csgs_grad_list;
+
+/* Bytes of device memory for a list of these tensors; 0 on bad input (n outside [1, 2^20], a tensor that csgs_grad_list_init
+ * would refuse). */
+size_t csgs_grad_list_bytes(const csgs_grad_tensor *t /*host*/, int32_t n);
+/* Writes the descriptions of the n tensors into l->base (kernels that carry them as arguments: safe under graph capture).
+ * Host errors: CSGS_EINVAL (null g, non-positive rows or cols, ld < cols, n), CSGS_EWORKSPACE, CSGS_EUNSUPPORTED (dtype, more than
+ * 2^40 entries). */
+int csgs_grad_list_init(csgs_grad_list *l /*host*/, const csgs_grad_tensor *t /*host*/, int32_t n, void *stream);
+
+/* total (device double) = sum |g|^2 (CSGS_GRAD_L2: not yet its root), sum |g|, or max |g|, over the list.  Sums are formed in double in a
+ * fixed order; a NaN anywhere makes each of them NaN.  The halves of csgs_grad_clip, for gradients that lie on several GPUs:
+ * totals are added (CSGS_GRAD_MAX: their maximum taken) between the two calls. */
+int csgs_grad_norm(const csgs_grad_list *l /*host*/, int kind, double *total, void *stream);
+/* out = c g for every tensor with an out, from such a total.  norm (device float, nullable) receives the norm.  Where c = 1, tensors
+ * that are their own output are not written.  A total that is NaN or infinite gives c = NaN or 0 by the formula and sets CSGS_ST_NONFINITE_GRAD in
+ * *status (nullable): a caller that then skips its step keeps its weights.
+ * Host errors: CSGS_EINVAL (also max_norm <= 0 or NaN; +infinity: nothing is clipped). */
+int csgs_grad_scale(const csgs_grad_list *l /*host*/, int kind, const double *total, float max_norm, float *norm,
+                    int32_t *status, void *stream);
+/* Both: csgs_grad_norm then csgs_grad_scale, without the total passing through the caller's memory. */
+int csgs_grad_clip(const csgs_grad_list *l /*host*/, int kind, float max_norm, float *norm, int32_t *status, void *stream);
 
 /* Static string for a CSGS_E* code. */
 const char *csgs_strerror(int code);

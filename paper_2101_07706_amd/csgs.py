@@ -17,13 +17,19 @@ LIB_PATH = os.path.join(_HERE, "libcsgs.so")
 
 OK, EINVAL, EWORKSPACE, EUNSUPPORTED, ERANGE, ELAUNCH = 0, -1, -2, -3, -4, -5
 ST_CAND_OVERFLOW, ST_BAD_EDGE_VALUE, ST_EMPTY_CANDIDATES, ST_ADJ_OVERFLOW, ST_BAD_NODE_ID = 1, 2, 4, 8, 16
-ST_EDGE_OVERFLOW, ST_INTERNAL = 32, 64
+ST_EDGE_OVERFLOW, ST_INTERNAL, ST_NONFINITE_GRAD = 32, 64, 128
 F32, BF16 = 0, 1
+NORM_NONE, NORM_RMS, NORM_LAYER = 0, 1, 2
+GATE_LINEAR, GATE_SIGMOID, GATE_SILU = 0, 1, 2
+GRAD_L2, GRAD_L1, GRAD_MAX = 0, 1, 2
 
 EXPORTS = ["csgs_workspace_bytes", "csgs_workspace_clean_bytes", "csgs_workspace_init", "csgs_workspace_wait_limit", "csgs_fixed_point", "csgs_build_probs", "csgs_build_probs_auto",
            "csgs_sample_layer", "csgs_draw_nodes", "csgs_sampled_adjacency", "csgs_remote_count", "csgs_aggregate", "csgs_gather_rows",
            "csgs_layer_gemm", "csgs_aggregate_n", "csgs_gather_rows_n", "csgs_layer_gemm_n", "csgs_layer_forward", "csgs_layer_forward_n", "csgs_layer_forward_supported", "csgs_layer_gemm_grad_w_scratch_bytes", "csgs_layer_gemm_grad_w", "csgs_layer_gemm_grad_w_static", "csgs_layer_gemm_grad_z",
            "csgs_aggregate_grad_scratch_bytes", "csgs_aggregate_grad", "csgs_strerror",
+           "csgs_embed", "csgs_embed_grad_scratch_bytes", "csgs_embed_grad", "csgs_embed_grad_rows", "csgs_norm_residual",
+           "csgs_norm_residual_grad_scratch_bytes", "csgs_norm_residual_grad", "csgs_grad_list_bytes", "csgs_grad_list_init", "csgs_grad_norm",
+           "csgs_grad_scale", "csgs_grad_clip",
            "csgs_profile_enable", "csgs_profile_kernel_count", "csgs_profile_kernel_name", "csgs_profile_collect", "csgs_profile_samples",
            "csgs_calib_copy", "csgs_calib_atomics", "csgs_calib_mfma_f64", "csgs_calib_lookups"]
 
@@ -67,6 +73,25 @@ class ProbStats(C.Structure):
     _fields_ = [("n_cand", C.c_int64), ("n_local", C.c_int64), ("n_remote", C.c_int64),
                 ("edges_scanned", C.c_int64), ("w_local", C.c_uint64), ("w_remote", C.c_uint64),
                 ("total", C.c_uint64), ("shift", C.c_int32), ("skew_fx", C.c_int32)]
+
+
+class Residual(C.Structure):
+    """csgs_residual: host struct of the inputs of csgs_norm_residual and its gradient."""
+    _fields_ = [("M", C.c_int32), ("F", C.c_int32), ("M_dev", C.c_void_p), ("x", C.c_void_p), ("h", C.c_void_p), ("gate", C.c_void_p),
+                ("ldx", C.c_int64), ("ldh", C.c_int64), ("ldg", C.c_int64), ("post_w", C.c_void_p), ("post_b", C.c_void_p),
+                ("pre_w", C.c_void_p), ("pre_b", C.c_void_p), ("x_dtype", C.c_int32), ("h_dtype", C.c_int32), ("post", C.c_int32),
+                ("pre", C.c_int32), ("gate_act", C.c_int32), ("eps", C.c_float), ("alpha", C.c_float), ("beta", C.c_float)]
+
+
+class GradTensor(C.Structure):
+    """csgs_grad_tensor: one gradient of a list."""
+    _fields_ = [("g", C.c_void_p), ("out", C.c_void_p), ("rows", C.c_int64), ("cols", C.c_int64), ("ldg", C.c_int64), ("ldo", C.c_int64),
+                ("rows_dev", C.c_void_p), ("dtype", C.c_int32), ("reserved", C.c_int32)]
+
+
+class GradList(C.Structure):
+    """csgs_grad_list: host descriptor of a prepared list of gradients."""
+    _fields_ = [("base", C.c_void_p), ("bytes", C.c_size_t), ("tiles", C.c_int64), ("n", C.c_int32), ("ready", C.c_int32)]
 
 
 _lib = None
@@ -115,6 +140,21 @@ def lib():
         L.csgs_aggregate_grad_scratch_bytes.restype = sz
         L.csgs_aggregate_grad_scratch_bytes.argtypes = [i32, i64]
         L.csgs_aggregate_grad.argtypes = [vp, vp, vp, i64, i32, vp, i32, vp, vp, i64, i32, vp, i64, vp, i64, vp, sz, vp]
+        L.csgs_embed.argtypes = [vp, i64, i64, i32, C.c_int, vp, i64, vp, f32, vp, i64, C.c_int, vp]
+        L.csgs_embed_grad_scratch_bytes.restype = sz
+        L.csgs_embed_grad_scratch_bytes.argtypes = [i64, i64, i32]
+        L.csgs_embed_grad.argtypes = [vp, i64, vp, vp, i64, i32, C.c_int, f32, C.c_int, vp, i64, i64, C.c_int, vp, sz, vp]
+        L.csgs_embed_grad_rows.argtypes = [vp, i64, vp, vp, i64, i32, C.c_int, f32, i64, vp, vp, vp, i64, C.c_int, vp, sz, vp]
+        L.csgs_norm_residual.argtypes = [C.POINTER(Residual), vp, i64, vp, i64, vp]
+        L.csgs_norm_residual_grad_scratch_bytes.restype = sz
+        L.csgs_norm_residual_grad_scratch_bytes.argtypes = [i32, i32]
+        L.csgs_norm_residual_grad.argtypes = [C.POINTER(Residual), vp, i64, vp, i64, vp, i64, vp, i64, vp, i64, vp, vp, vp, vp, vp, sz, vp]
+        L.csgs_grad_list_bytes.restype = sz
+        L.csgs_grad_list_bytes.argtypes = [C.POINTER(GradTensor), i32]
+        L.csgs_grad_list_init.argtypes = [C.POINTER(GradList), C.POINTER(GradTensor), i32, vp]
+        L.csgs_grad_norm.argtypes = [C.POINTER(GradList), C.c_int, vp, vp]
+        L.csgs_grad_scale.argtypes = [C.POINTER(GradList), C.c_int, vp, f32, vp, vp, vp]
+        L.csgs_grad_clip.argtypes = [C.POINTER(GradList), C.c_int, f32, vp, vp, vp]
         L.csgs_strerror.restype = C.c_char_p
         L.csgs_strerror.argtypes = [C.c_int]
         L.csgs_calib_copy.argtypes = [vp, vp, sz, vp]
@@ -439,6 +479,163 @@ def csgs_gather_rows(X, ids, n_dev, out, stream=None, inst=None):
     suffix, lead = _inst(inst)
     _call("csgs_gather_rows" + suffix, *lead, _ptr(X), X.stride(0), X.shape[0], X.shape[1], dtype, _ptr(ids), ids.numel(),
                                 _ptr(n_dev), _ptr(out), out.stride(0), _stream(stream))
+
+
+def _elem(t):
+    """CSGS_* type of a tensor's elements."""
+    if t.dtype == torch.float32:
+        return F32
+    if t.dtype == torch.bfloat16:
+        return BF16
+    raise TypeError(f"float32 or bfloat16, not {t.dtype}")
+
+
+def _ld(t, cols):
+    """Leading dimension of a matrix whose rows are contiguous (what a tensor says of the step between rows it has one of, does not count)."""
+    assert t.dim() == 2 and t.shape[1] == cols and (cols == 1 or t.stride(1) == 1), "rows of a matrix, contiguous"
+    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), cols)
+
+
+def _i32(t):
+    assert t is None or isinstance(t, C._SimpleCData) or (t.dtype == torch.int32 and (t.dim() == 0 or t.numel() == 1 or t.is_contiguous())), "int32, contiguous"
+    return _ptr(t)
+
+
+def _f32(t, n):
+    """A contiguous float vector of n entries, or None."""
+    assert t is None or (t.dtype == torch.float32 and t.numel() == n and t.is_contiguous()), f"float32, {n} entries, contiguous"
+    return _ptr(t)
+
+
+def _scratch(t):
+    assert t.is_contiguous()
+    return _ptr(t), t.numel() * t.element_size()
+
+
+def csgs_embed(T, ids, out, scale=1.0, n_dev=None, stream=None):
+    """out[t] = scale * T[ids[t]] (float32 or bfloat16 each); zeros where an id is outside the table."""
+    F = T.shape[1]
+    assert out.shape[0] >= ids.numel()
+    _call("csgs_embed", _ptr(T), _ld(T, F), T.shape[0], F, _elem(T), _i32(ids), ids.numel(), _i32(n_dev), scale, _ptr(out), _ld(out, F), _elem(out),
+          _stream(stream))
+
+
+def csgs_embed_grad_scratch_bytes(n, rows, F) -> int:
+    return int(lib().csgs_embed_grad_scratch_bytes(n, rows, F))
+
+
+def csgs_embed_grad(ids, G, dT, scratch, scale=1.0, accumulate=False, n_dev=None, stream=None):
+    """dT[v] = scale * sum of G[t] over ids[t] = v, zeros elsewhere; accumulate: added to what dT holds.
+    scratch: a tensor of at least csgs_embed_grad_scratch_bytes(len(ids), len(dT), F) bytes."""
+    F = G.shape[1]
+    assert G.shape[0] >= ids.numel()
+    ptr, nbytes = _scratch(scratch)
+    _call("csgs_embed_grad", _i32(ids), ids.numel(), _i32(n_dev), _ptr(G), _ld(G, F), F, _elem(G), scale, 1 if accumulate else 0, _ptr(dT),
+          _ld(dT, F), dT.shape[0], _elem(dT), ptr, nbytes, _stream(stream))
+
+
+def csgs_embed_grad_rows(ids, G, rows, uniq, n_uniq, dR, scratch, scale=1.0, n_dev=None, stream=None):
+    """The rows of that gradient that some id points to alone: uniq ascending, *n_uniq of them, dR[j] the gradient of row uniq[j]."""
+    F = G.shape[1]
+    assert G.shape[0] >= ids.numel() and uniq.numel() >= ids.numel() and dR.shape[0] >= ids.numel()
+    ptr, nbytes = _scratch(scratch)
+    _call("csgs_embed_grad_rows", _i32(ids), ids.numel(), _i32(n_dev), _ptr(G), _ld(G, F), F, _elem(G), scale, rows, _i32(uniq), _i32(n_uniq),
+          _ptr(dR), _ld(dR, F), _elem(dR), ptr, nbytes, _stream(stream))
+
+
+def _residual(x, h, stream_type, block_type, gate, gate_act, post, post_w, post_b, pre, pre_w, pre_b, eps, alpha, beta, M_dev):
+    M, F = (x if x is not None else h).shape
+    assert x is None or h is None or x.shape == h.shape
+    types = [_elem(t) for t in (stream_type, block_type)]
+    assert (x is None or _elem(x) == types[0]) and (h is None or _elem(h) == types[1])
+    ldg = 0
+    if gate is not None:
+        if gate.dim() == 1:
+            _f32(gate, F)
+        else:
+            assert gate.shape == (M, F) and _elem(gate) == types[1]
+            ldg = _ld(gate, F)
+    return Residual(M, F, _i32(M_dev), _ptr(x), _ptr(h), _ptr(gate), _ld(x, F) if x is not None else 0, _ld(h, F) if h is not None else 0, ldg,
+                    _f32(post_w, F), _f32(post_b, F), _f32(pre_w, F), _f32(pre_b, F), types[0], types[1], post, pre, gate_act, eps, alpha, beta)
+
+
+def _out(t, shape, elem):
+    """Address and leading dimension of a matrix that may be absent."""
+    if t is None:
+        return None, 0
+    assert tuple(t.shape) == tuple(shape) and _elem(t) == elem
+    return _ptr(t), _ld(t, shape[1])
+
+
+def csgs_norm_residual(x, h, y, u, gate=None, gate_act=GATE_LINEAR, post=NORM_RMS, post_w=None, post_b=None, pre=NORM_RMS, pre_w=None, pre_b=None,
+                       eps=1e-5, alpha=1.0, beta=1.0, M_dev=None, stream=None):
+    """y = beta x + alpha a(gate) .* N(h; post_w, post_b), u = N(y; pre_w, pre_b).  x or h, y or u may be None.
+    gate: None, a float32 vector for all rows, or a matrix like h."""
+    a = x if x is not None else y if y is not None else h     # a tensor of the stream's type, of the block's
+    b = h if h is not None else u if u is not None else x
+    r = _residual(x, h, a, b, gate, gate_act, post, post_w, post_b, pre, pre_w, pre_b, eps, alpha, beta, M_dev)
+    _call("csgs_norm_residual", C.byref(r), *_out(y, (r.M, r.F), r.x_dtype), *_out(u, (r.M, r.F), r.h_dtype), _stream(stream))
+
+
+def csgs_norm_residual_grad_scratch_bytes(M, F) -> int:
+    return int(lib().csgs_norm_residual_grad_scratch_bytes(M, F))
+
+
+def csgs_norm_residual_grad(x, h, dy, du, dx, dh, dgate, dpost_w, dpost_b, dpre_w, dpre_b, scratch, gate=None, gate_act=GATE_LINEAR, post=NORM_RMS,
+                            post_w=None, post_b=None, pre=NORM_RMS, pre_w=None, pre_b=None, eps=1e-5, alpha=1.0, beta=1.0, M_dev=None, stream=None):
+    """Gradients of csgs_norm_residual from dy and du (one may be None); outputs may be None.
+    scratch: a tensor of at least csgs_norm_residual_grad_scratch_bytes(M, F) bytes."""
+    first = lambda *ts: next(t for t in ts if t is not None)
+    r = _residual(x, h, first(x, dy, dx, h), first(h, du, dh, x), gate, gate_act, post, post_w, post_b, pre, pre_w, pre_b, eps, alpha, beta, M_dev)
+    M, F = r.M, r.F
+    dg = (_f32(dgate, F), 0) if gate is None or gate.dim() == 1 else _out(dgate, (M, F), r.h_dtype)
+    ptr, nbytes = _scratch(scratch)
+    _call("csgs_norm_residual_grad", C.byref(r), *_out(dy, (M, F), r.x_dtype), *_out(du, (M, F), r.h_dtype), *_out(dx, (M, F), r.x_dtype),
+          *_out(dh, (M, F), r.h_dtype), *dg, _f32(dpost_w, F), _f32(dpost_b, F), _f32(dpre_w, F), _f32(dpre_b, F), ptr, nbytes, _stream(stream))
+
+
+def make_grad_list(grads, outs=None, rows_dev=None, stream=None) -> GradList:
+    """A list of gradients for csgs_grad_norm / _scale / _clip, described once in device memory.  outs: where the clipped gradients go (None: in
+    place; entries may be None); rows_dev: per gradient, a device int32 with the number of rows that count, or None.
+    The list keeps the tensors; they must not be resized or freed by other means."""
+    outs = grads if outs is None else outs
+    rows_dev = [None] * len(grads) if rows_dev is None else rows_dev
+    assert len(grads) > 0 and len(outs) == len(grads) and len(rows_dev) == len(grads)
+    assert _recording is None, "a list is made once, not by a recorded call"
+
+    def matrix(t):   # as rows x cols
+        return t if t.dim() == 2 else t.reshape(1, -1) if t.is_contiguous() else t.unsqueeze(0)
+
+    ts = (GradTensor * len(grads))()
+    for i, (g, o, n) in enumerate(zip(grads, outs, rows_dev)):
+        assert o is None or (o.shape == g.shape and o.dtype == g.dtype)
+        assert n is None or g.dim() == 2, "rows are those of a matrix"
+        m = matrix(g)
+        ts[i] = GradTensor(_ptr(g), _ptr(o), m.shape[0], m.shape[1], _ld(m, m.shape[1]), 0 if o is None else _ld(matrix(o), m.shape[1]), _i32(n), _elem(g), 0)
+    nbytes = int(lib().csgs_grad_list_bytes(ts, len(grads)))
+    if nbytes == 0:
+        raise CsgsError(EINVAL, "csgs_grad_list_bytes")
+    buf = torch.empty(nbytes // 8, dtype=torch.int64, device=grads[0].device)
+    l = GradList(buf.data_ptr(), nbytes, 0, 0, 0)
+    _call("csgs_grad_list_init", C.byref(l), ts, len(grads), _stream(stream))
+    l._keep = (buf, list(grads), list(outs), list(rows_dev))
+    return l
+
+
+def csgs_grad_norm(l, kind, total, stream=None):
+    """total: float64 tensor of one entry; receives the sum of squares, of absolute values, or the largest of these."""
+    assert total.dtype == torch.float64
+    _call("csgs_grad_norm", C.byref(l), kind, _ptr(total), _stream(stream))
+
+
+def csgs_grad_scale(l, kind, total, max_norm, norm=None, status=None, stream=None):
+    assert total.dtype == torch.float64
+    _call("csgs_grad_scale", C.byref(l), kind, _ptr(total), max_norm, _f32(norm, 1), _i32(status), _stream(stream))
+
+
+def csgs_grad_clip(l, kind, max_norm, norm=None, status=None, stream=None):
+    """out = min(1, max_norm / (total + 1e-6)) g over the list; norm receives the total before clipping."""
+    _call("csgs_grad_clip", C.byref(l), kind, max_norm, _f32(norm, 1), _i32(status), _stream(stream))
 
 
 def csgs_profile_enable(on: bool):

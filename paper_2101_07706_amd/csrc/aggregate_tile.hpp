@@ -3,89 +3,9 @@
 // kernel and by the kernel that goes on to the layer product without writing Z to memory.
 #pragma once
 #include "common.hpp"
+#include "row_pieces.hpp"
 
 namespace csgs {
-
-template <int V>
-struct Vec {
-    float x[V];
-};
-
-// Rows of the gathered tables are read through pointers that come out of LDS or a lane exchange as plain
-// integers; the loads say that they go to global memory (a pointer of unknown kind would be read with the
-// slower flat instructions, which every wait for LDS data would then wait for as well).
-#define CSGS_GLOBAL __attribute__((address_space(1)))
-typedef float f32x2 __attribute__((ext_vector_type(2)));
-typedef float f32x4 __attribute__((ext_vector_type(4)));
-typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
-typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-// A value in a table whose rows start on any element of ALIGN bytes: global loads and stores of any width take any address on this
-// part, but the compiler has to know that they are asked to.  (A struct, whose alignment is part of the type: that of a typedef is
-// dropped where it is a template argument, and the access then claims the vector's own.)
-template <typename U, int ALIGN>
-struct __attribute__((packed, aligned(ALIGN))) Piece {
-    U v;
-};
-template <typename U, int ALIGN = (int)alignof(U)>
-__device__ inline U load_global(const void *p)
-{
-    static_assert(alignof(Piece<U, ALIGN>) == ALIGN && sizeof(Piece<U, ALIGN>) == sizeof(U), "the claim on the address");
-    return reinterpret_cast<const CSGS_GLOBAL Piece<U, ALIGN> *>((uintptr_t)p)->v;
-}
-template <typename U, int ALIGN = (int)alignof(U)>
-__device__ inline void store_global(void *p, U v)
-{
-    static_assert(alignof(Piece<U, ALIGN>) == ALIGN && sizeof(Piece<U, ALIGN>) == sizeof(U), "the claim on the address");
-    reinterpret_cast<CSGS_GLOBAL Piece<U, ALIGN> *>((uintptr_t)p)->v = v;
-}
-
-template <typename T, int V>
-__device__ inline Vec<V> load_row(const T *p);
-
-template <>
-__device__ inline Vec<1> load_row<float, 1>(const float *p) { return Vec<1>{{load_global<float>(p)}}; }
-template <>
-__device__ inline Vec<2> load_row<float, 2>(const float *p)
-{
-    const f32x2 v = load_global<f32x2, 4>(p);
-    return Vec<2>{{v.x, v.y}};
-}
-template <>
-__device__ inline Vec<4> load_row<float, 4>(const float *p)
-{
-    const f32x4 v = load_global<f32x4, 4>(p);
-    return Vec<4>{{v.x, v.y, v.z, v.w}};
-}
-template <>
-__device__ inline Vec<8> load_row<float, 8>(const float *p)   // two 16-byte loads
-{
-    const f32x4 a = load_global<f32x4, 4>(p), b = load_global<f32x4, 4>(p + 4);
-    return Vec<8>{{a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w}};
-}
-// bfloat16 bit patterns: widening is a 16-bit left shift
-template <>
-__device__ inline Vec<1> load_row<uint16_t, 1>(const uint16_t *p) { return Vec<1>{{__uint_as_float((uint32_t)load_global<uint16_t>(p) << 16)}}; }
-template <>
-__device__ inline Vec<2> load_row<uint16_t, 2>(const uint16_t *p)
-{
-    const uint32_t v = load_global<uint32_t, 2>(p);
-    return Vec<2>{{__uint_as_float(v << 16), __uint_as_float(v & 0xFFFF0000u)}};
-}
-template <>
-__device__ inline Vec<4> load_row<uint16_t, 4>(const uint16_t *p)
-{
-    const u32x2 v = load_global<u32x2, 2>(p);
-    return Vec<4>{{__uint_as_float(v.x << 16), __uint_as_float(v.x & 0xFFFF0000u), __uint_as_float(v.y << 16),
-                   __uint_as_float(v.y & 0xFFFF0000u)}};
-}
-template <>
-__device__ inline Vec<8> load_row<uint16_t, 8>(const uint16_t *p)
-{
-    const u32x4 v = load_global<u32x4, 2>(p);
-    return Vec<8>{{__uint_as_float(v.x << 16), __uint_as_float(v.x & 0xFFFF0000u), __uint_as_float(v.y << 16),
-                   __uint_as_float(v.y & 0xFFFF0000u), __uint_as_float(v.z << 16), __uint_as_float(v.z & 0xFFFF0000u),
-                   __uint_as_float(v.w << 16), __uint_as_float(v.w & 0xFFFF0000u)}};
-}
 
 // Rows with more kept edges than LONG_ROW are taken by the whole block, after its tiles.  With 32 or 64 lanes per row, where a
 // wavefront walks through a long row nearly alone, so are rows of more than long_row<G>() (us, 256 everywhere / this: F = 100

@@ -1,0 +1,263 @@
+// Global norm over the gradients of a network, and clipping by it.
+//
+// total = (sum |g|^p)^(1/p) or max |g|; c = min(1, max_norm / (total + 1e-6)); out = c g.  Two launches for any number of
+// tensors: their entries are cut into tiles of GRAD_TILE, the first kernel leaves one sum per block (in double, each
+// thread's entries in ascending order, joined by a fixed tree), every block of the second adds those sums up for itself,
+// in the same order, and scales its tiles.
+#include <math.h>
+#include "common.hpp"
+#include "row_pieces.hpp"
+
+namespace csgs {
+
+constexpr int64_t GRAD_TILE = 8192;
+constexpr int GRAD_BLOCKS = 2048;      // most blocks of either kernel
+constexpr int64_t GRAD_ENTRIES = 1ll << 40;
+
+// A tensor as the kernels see it.  Rows that lie side by side are one row of all entries; `per` is then the entries of a row
+// that a device count counts.
+struct GradDesc {
+    const void *g;
+    void *out;
+    const int32_t *rows_dev;
+    int64_t rows, cols, ldg, ldo, first_tile;
+    int32_t dtype, flat;
+};
+struct GradMem {
+    double *partial;      // [GRAD_BLOCKS]
+    GradDesc *desc;       // [n]
+    int32_t *tile_tensor; // [tiles]
+    size_t bytes;
+};
+__host__ __device__ inline GradMem carve_grads(void *base, int32_t n, int64_t tiles)
+{
+    GradMem m;
+    size_t off = align_up(sizeof(double) * GRAD_BLOCKS, 256);
+    m.partial = (double *)base;
+    m.desc = (GradDesc *)((char *)base + off);
+    off = align_up(off + sizeof(GradDesc) * (size_t)n, 256);
+    m.tile_tensor = (int32_t *)((char *)base + off);
+    m.bytes = align_up(off + sizeof(int32_t) * (size_t)tiles, 256);
+    return m;
+}
+
+constexpr int DESC_PER_LAUNCH = 32;
+struct DescBatch {
+    GradDesc d[DESC_PER_LAUNCH];
+    int64_t end_tile[DESC_PER_LAUNCH];
+};
+__global__ __launch_bounds__(256) void grad_list_k(DescBatch b, int32_t first, GradDesc *__restrict__ desc, int32_t *__restrict__ tile_tensor)
+{
+    const int k = (int)blockIdx.x;
+    if (threadIdx.x == 0) desc[first + k] = b.d[k];
+    for (int64_t t = b.d[k].first_tile + threadIdx.x; t < b.end_tile[k]; t += blockDim.x) tile_tensor[t] = first + k;
+}
+
+__device__ inline int64_t live_entries(const GradDesc &d)
+{
+    int64_t rows = d.rows;
+    if (d.rows_dev) {
+        const int64_t r = *d.rows_dev;
+        rows = r < 0 ? 0 : (r < rows ? r : rows);
+    }
+    return rows * d.cols;
+}
+
+__device__ inline float load_entry(const void *p, int32_t dtype, int64_t at)
+{
+    return dtype == CSGS_F32 ? load_row<float, 1>((const float *)p + at).x[0] : load_row<uint16_t, 1>((const uint16_t *)p + at).x[0];
+}
+__device__ inline void store_entry(void *p, int32_t dtype, int64_t at, float v)
+{
+    if (dtype == CSGS_F32) store_row<float, 1>((float *)p + at, Vec<1>{{v}});
+    else store_row<uint16_t, 1>((uint16_t *)p + at, Vec<1>{{v}});
+}
+
+// The sum, or the larger one with NaN above everything.
+__device__ inline double add_or_max(double a, double b, int kind)
+{
+    if (kind != CSGS_GRAD_MAX) return a + b;
+    return !(a >= b) && !(a != a) ? b : a;
+}
+__device__ inline double term(float x, int kind)
+{
+    const double v = (double)x;
+    return kind == CSGS_GRAD_L2 ? v * v : fabs(v);
+}
+
+// Joined over the block's 256 threads by a fixed tree; the result in every thread.
+__device__ inline double block_join(double v, int kind, double *lds /*[256]*/)
+{
+    const int tid = (int)threadIdx.x;
+    lds[tid] = v;
+    __syncthreads();
+    for (int s = 128; s > 0; s >>= 1) {
+        if (tid < s) lds[tid] = add_or_max(lds[tid], lds[tid + s], kind);
+        __syncthreads();
+    }
+    const double r = lds[0];
+    __syncthreads();
+    return r;
+}
+
+__global__ __launch_bounds__(256) void grad_norm_k(GradMem m, int64_t tiles, int kind)
+{
+    __shared__ double lds[256];
+    double sum = 0.0;
+    for (int64_t t = blockIdx.x; t < tiles; t += gridDim.x) {
+        const GradDesc d = m.desc[m.tile_tensor[t]];
+        const int64_t beg = (t - d.first_tile) * GRAD_TILE, live = live_entries(d);
+        const int64_t end = beg + GRAD_TILE < live ? beg + GRAD_TILE : live;
+        for (int64_t e = beg + threadIdx.x; e < end; e += 256) {
+            const int64_t at = d.flat ? e : e / d.cols * d.ldg + e % d.cols;
+            sum = add_or_max(sum, term(load_entry(d.g, d.dtype, at), kind), kind);
+        }
+    }
+    sum = block_join(sum, kind, lds);
+    if (threadIdx.x == 0) m.partial[blockIdx.x] = sum;
+}
+
+__device__ inline double join_partials(const double *__restrict__ partial, int blocks, int kind, double *lds)
+{
+    double s = 0.0;
+    for (int b = (int)threadIdx.x; b < blocks; b += 256) s = add_or_max(s, partial[b], kind);
+    return block_join(s, kind, lds);
+}
+
+__global__ __launch_bounds__(256) void grad_total_k(GradMem m, int blocks, int kind, double *__restrict__ total)
+{
+    __shared__ double lds[256];
+    const double s = join_partials(m.partial, blocks, kind, lds);
+    if (threadIdx.x == 0) *total = s;
+}
+
+__global__ __launch_bounds__(256) void grad_scale_k(GradMem m, int64_t tiles, int blocks, int kind, const double *total, float max_norm, float *norm_out,
+                                                    int32_t *status)
+{
+    __shared__ double lds[256];
+    const double s = total ? *total : join_partials(m.partial, blocks, kind, lds);
+    const double norm = kind == CSGS_GRAD_L2 ? sqrt(s) : s;
+    double coef = (double)max_norm / (norm + 1e-6);
+    if (coef > 1.0) coef = 1.0;
+    if (blockIdx.x == 0 && threadIdx.x == 0) {
+        if (norm_out) *norm_out = (float)norm;
+        if (status && !(norm <= 1.7976931348623157e308)) atomicOr(status, CSGS_ST_NONFINITE_GRAD);
+    }
+    for (int64_t t = blockIdx.x; t < tiles; t += gridDim.x) {
+        const GradDesc d = m.desc[m.tile_tensor[t]];
+        if (!d.out || (coef == 1.0 && d.out == d.g)) continue;
+        const int64_t beg = (t - d.first_tile) * GRAD_TILE, live = live_entries(d);
+        const int64_t end = beg + GRAD_TILE < live ? beg + GRAD_TILE : live;
+        for (int64_t e = beg + threadIdx.x; e < end; e += 256) {
+            const int64_t r = d.flat ? 0 : e / d.cols, f = d.flat ? e : e % d.cols;
+            store_entry(d.out, d.dtype, r * d.ldo + f, (float)(coef * (double)load_entry(d.g, d.dtype, r * d.ldg + f)));
+        }
+    }
+}
+
+// Checks a tensor and describes it; tiles counted on from *tiles.
+static int describe(const csgs_grad_tensor &t, int64_t *tiles, GradDesc *d)
+{
+    if (!t.g || t.rows <= 0 || t.cols <= 0 || t.ldg < t.cols || (t.out && t.ldo < t.cols) || (t.out == t.g && t.ldo != t.ldg)) return CSGS_EINVAL;
+    if ((t.dtype != CSGS_F32 && t.dtype != CSGS_BF16) || t.rows > GRAD_ENTRIES / t.cols) return CSGS_EUNSUPPORTED;
+    d->g = t.g;
+    d->out = t.out;
+    d->rows_dev = t.rows_dev;
+    d->rows = t.rows;
+    d->cols = t.cols;
+    d->ldg = t.ldg;
+    d->ldo = t.out ? t.ldo : t.ldg;
+    d->first_tile = *tiles;
+    d->dtype = t.dtype;
+    d->flat = t.rows == 1 || (t.ldg == t.cols && d->ldo == t.cols) ? 1 : 0;
+    *tiles += (t.rows * t.cols + GRAD_TILE - 1) / GRAD_TILE;
+    return *tiles > GRAD_ENTRIES / GRAD_TILE ? CSGS_EUNSUPPORTED : CSGS_OK;
+}
+
+static int grad_blocks(int64_t tiles) { return (int)(tiles < GRAD_BLOCKS ? tiles : GRAD_BLOCKS); }
+static bool list_ok(const csgs_grad_list *l, int kind)
+{
+    return l && l->base && l->ready && l->n > 0 && l->tiles > 0 && kind >= CSGS_GRAD_L2 && kind <= CSGS_GRAD_MAX;
+}
+
+static int launch_scale(const csgs_grad_list *l, int kind, const double *total, float max_norm, float *norm, int32_t *status, hipStream_t st)
+{
+    const GradMem m = carve_grads(l->base, l->n, l->tiles);
+    const int blocks = grad_blocks(l->tiles);
+    CSGS_LAUNCH(K_GRAD_SCALE, grad_scale_k, dim3((unsigned)blocks), dim3(256), st, m, l->tiles, blocks, kind, total, max_norm, norm, status);
+    CSGS_LAUNCH_CHECK();
+    return CSGS_OK;
+}
+static int launch_norm(const csgs_grad_list *l, int kind, hipStream_t st)
+{
+    const GradMem m = carve_grads(l->base, l->n, l->tiles);
+    CSGS_LAUNCH(K_GRAD_NORM, grad_norm_k, dim3((unsigned)grad_blocks(l->tiles)), dim3(256), st, m, l->tiles, kind);
+    CSGS_LAUNCH_CHECK();
+    return CSGS_OK;
+}
+
+}  // namespace csgs
+
+using namespace csgs;
+
+extern "C" size_t csgs_grad_list_bytes(const csgs_grad_tensor *t, int32_t n)
+{
+    if (!t || n < 1 || n > 1 << 20) return 0;
+    int64_t tiles = 0;
+    GradDesc d;
+    for (int32_t i = 0; i < n; ++i)
+        if (describe(t[i], &tiles, &d) != CSGS_OK) return 0;
+    return carve_grads(nullptr, n, tiles).bytes;
+}
+
+extern "C" int csgs_grad_list_init(csgs_grad_list *l, const csgs_grad_tensor *t, int32_t n, void *stream)
+{
+    if (!l || !l->base || ((uintptr_t)l->base & 255) || !t || n < 1 || n > 1 << 20) return CSGS_EINVAL;
+    l->ready = 0;
+    int64_t tiles = 0;
+    GradDesc d;
+    for (int32_t i = 0; i < n; ++i) {
+        const int rc = describe(t[i], &tiles, &d);
+        if (rc != CSGS_OK) return rc;
+    }
+    const GradMem m = carve_grads(l->base, n, tiles);
+    if (l->bytes < m.bytes) return CSGS_EWORKSPACE;
+    int64_t at = 0;
+    for (int32_t first = 0; first < n; first += DESC_PER_LAUNCH) {
+        DescBatch b;
+        const int32_t k = n - first < DESC_PER_LAUNCH ? n - first : DESC_PER_LAUNCH;
+        for (int32_t i = 0; i < k; ++i) {
+            (void)describe(t[first + i], &at, &b.d[i]);
+            b.end_tile[i] = at;
+        }
+        CSGS_LAUNCH(K_GRAD_LIST, grad_list_k, dim3((unsigned)k), dim3(256), (hipStream_t)stream, b, first, m.desc, m.tile_tensor);
+        CSGS_LAUNCH_CHECK();
+    }
+    l->n = n;
+    l->tiles = tiles;
+    l->ready = 1;
+    return CSGS_OK;
+}
+
+extern "C" int csgs_grad_norm(const csgs_grad_list *l, int kind, double *total, void *stream)
+{
+    if (!list_ok(l, kind) || !total) return CSGS_EINVAL;
+    const int rc = launch_norm(l, kind, (hipStream_t)stream);
+    if (rc != CSGS_OK) return rc;
+    CSGS_LAUNCH(K_GRAD_TOTAL, grad_total_k, dim3(1), dim3(256), (hipStream_t)stream, carve_grads(l->base, l->n, l->tiles), grad_blocks(l->tiles), kind, total);
+    CSGS_LAUNCH_CHECK();
+    return CSGS_OK;
+}
+
+extern "C" int csgs_grad_scale(const csgs_grad_list *l, int kind, const double *total, float max_norm, float *norm, int32_t *status, void *stream)
+{
+    if (!list_ok(l, kind) || !total || !(max_norm > 0.0f)) return CSGS_EINVAL;
+    return launch_scale(l, kind, total, max_norm, norm, status, (hipStream_t)stream);
+}
+
+extern "C" int csgs_grad_clip(const csgs_grad_list *l, int kind, float max_norm, float *norm, int32_t *status, void *stream)
+{
+    if (!list_ok(l, kind) || !(max_norm > 0.0f)) return CSGS_EINVAL;
+    const int rc = launch_norm(l, kind, (hipStream_t)stream);
+    return rc != CSGS_OK ? rc : launch_scale(l, kind, nullptr, max_norm, norm, status, (hipStream_t)stream);
+}
