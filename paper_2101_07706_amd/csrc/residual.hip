@@ -29,7 +29,7 @@ struct Gate {
 __device__ inline Gate gate_of(float g, int32_t act)
 {
     if (act == CSGS_GATE_LINEAR) return Gate{g, 1.0f};
-    const float s = 1.0f / (1.0f + __expf(-g));
+    const float s = __builtin_amdgcn_rcpf(1.0f + __expf(-g));   // (1 / infinity is 0)
     if (act == CSGS_GATE_SIGMOID) return Gate{s, s * (1.0f - s)};
     return Gate{g * s, s * (1.0f + g * (1.0f - s))};
 }
@@ -109,6 +109,177 @@ __global__ __launch_bounds__(RES_BLOCK) void residual_k(ResidualArgs a, TS *y, i
     }
 }
 
+// ---------------------------------------------------------------- rows in registers
+// G lanes take a row, N pieces of V columns each; what a lane holds of the vectors (weights, sums over rows) stays in registers
+// from row to row.  Rows start on any element.  RAGGED: V does not divide the width; the last piece then ends with the row and
+// overlaps the one before: the values that both hold are computed twice, alike, and count once in sums.
+
+// Sum over the G lanes of a row, the same bits in each of them: every step adds two lanes' values that are each other's
+// counterparts.  Rotations inside rows of 16 lanes, then rows and halves of the wavefront exchanged.
+template <int CTRL>
+__device__ inline float add_rotated(float v)
+{
+    return v + __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(v), CTRL, 0xF, 0xF, true));
+}
+template <int G>
+__device__ inline float lanes_sum(float v)
+{
+    v = add_rotated<0x128>(v);   // row_ror:8
+    v = add_rotated<0x124>(v);
+    v = add_rotated<0x122>(v);
+    v = add_rotated<0x121>(v);
+    if constexpr (G >= 32) {
+        const auto p = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+        v = __uint_as_float(p[0]) + __uint_as_float(p[1]);
+    }
+    if constexpr (G >= 64) {
+        const auto p = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+        v = __uint_as_float(p[0]) + __uint_as_float(p[1]);
+    }
+    return v;
+}
+// Sums of K values over a row's lanes; with G = 256 over the block, through LDS (turn: the two halves of `lds` in turn, so that one barrier a
+// sum is enough).
+template <int G, int K>
+__device__ inline void row_sums(float (&v)[K], float *lds /*[2][RES_BLOCK / WAVE][2]*/, int &turn)
+{
+#pragma unroll
+    for (int k = 0; k < K; ++k) v[k] = lanes_sum<G>(v[k]);
+    if constexpr (G > WAVE) {
+        float *l = lds + turn * (2 * RES_BLOCK / WAVE);
+        turn ^= 1;
+        if (lane_id() == 0)
+#pragma unroll
+            for (int k = 0; k < K; ++k) l[2 * (threadIdx.x / WAVE) + k] = v[k];
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            v[k] = l[k];
+#pragma unroll
+            for (int w = 1; w < RES_BLOCK / WAVE; ++w) v[k] += l[2 * w + k];
+        }
+    }
+}
+
+// The columns that a lane holds: piece n begins at col(n); its first skip(n) values belong to the piece before.
+template <int V, int G, int N, bool RAGGED>
+struct Cols {
+    int32_t F;
+    int lane;   // of the row's
+    __device__ int32_t begin(int n) const { return (lane + n * G) * V; }
+    __device__ bool active(int n) const { return begin(n) < F; }
+    __device__ int32_t col(int n) const { return RAGGED && begin(n) > F - V ? F - V : begin(n); }
+    __device__ int32_t skip(int n) const { return RAGGED ? begin(n) - col(n) : 0; }
+    template <typename T>
+    __device__ void load(float (&v)[N * V], const T *row) const
+    {
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            Vec<V> p{};
+            if (active(n)) p = load_row<T, V>(row + col(n));
+#pragma unroll
+            for (int i = 0; i < V; ++i) v[n * V + i] = p.x[i];
+        }
+    }
+    __device__ void load_or(float (&v)[N * V], const float *row, float otherwise) const
+    {
+        if (row) return load(v, row);
+#pragma unroll
+        for (int i = 0; i < N * V; ++i) v[i] = otherwise;
+    }
+    template <typename T>
+    __device__ void store(T *row, const float (&v)[N * V]) const
+    {
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            Vec<V> p;
+#pragma unroll
+            for (int i = 0; i < V; ++i) p.x[i] = v[n * V + i];
+            if (active(n)) store_row<T, V>(row + col(n), p);
+        }
+    }
+    // Sum of term(i) over the lane's own values.
+    template <typename T>
+    __device__ float sum(T term) const
+    {
+        float s = 0.0f;
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            float p = 0.0f;
+            const int32_t sk = skip(n);
+#pragma unroll
+            for (int i = 0; i < V; ++i) p += RAGGED && i < sk ? 0.0f : term(n * V + i);
+            s += active(n) ? p : 0.0f;
+        }
+        return s;
+    }
+};
+
+// Mean and 1 / deviation of a row.
+template <int G, typename C, int NV>
+__device__ inline Stats stats_of(const float (&v)[NV], const C &c, float inv_F, int32_t kind, float eps, float *lds, int &turn)
+{
+    if (kind == CSGS_NORM_NONE) return Stats{0.0f, 1.0f};
+    float m[1] = {0.0f}, q[1];
+    if (kind == CSGS_NORM_LAYER) {
+        m[0] = c.sum([&](int i) { return v[i]; });
+        row_sums<G>(m, lds, turn);
+        m[0] *= inv_F;
+    }
+    q[0] = c.sum([&](int i) { return (v[i] - m[0]) * (v[i] - m[0]); });
+    row_sums<G>(q, lds, turn);
+    return Stats{m[0], rsqrtf(q[0] * inv_F + eps)};
+}
+
+template <typename TS, typename TB, int V, int G, int N, bool RAGGED>
+__global__ __launch_bounds__(RES_BLOCK) void residual_rows_k(ResidualArgs a, TS *y, int64_t ldy, TB *u, int64_t ldu)
+{
+    constexpr int NV = N * V;
+    __shared__ float lds[4 * RES_BLOCK / WAVE];
+    int turn = 0;
+    const int32_t M = resolve_count(a.M, a.M_dev);
+    const Cols<V, G, N, RAGGED> c{a.F, (int)threadIdx.x % G};
+    const float inv_F = 1.0f / (float)a.F;
+    float pw[NV], pb[NV], qw[NV], qb[NV], gv[NV];
+    c.load_or(pw, a.post_w, 1.0f);
+    c.load_or(pb, a.post_b, 0.0f);
+    c.load_or(qw, a.pre_w, 1.0f);
+    c.load_or(qb, a.pre_b, 0.0f);
+    c.load_or(gv, a.gate && !a.ldg ? (const float *)a.gate : nullptr, 0.0f);
+    constexpr int ROWS = RES_BLOCK / G;
+    const int group = (int)threadIdx.x / G;
+    for (int64_t r0 = (int64_t)blockIdx.x * ROWS; r0 < M; r0 += (int64_t)gridDim.x * ROWS) {
+        const bool live = r0 + group < M;
+        const int64_t r = live ? r0 + group : M - 1;
+        float v[NV], h[NV];
+        if (a.x) c.load(v, (const TS *)a.x + r * a.ldx);
+        if (a.h) {
+            c.load(h, (const TB *)a.h + r * a.ldh);
+            if (a.ldg) c.load(gv, (const TB *)a.gate + r * a.ldg);
+        }
+#pragma unroll
+        for (int i = 0; i < NV; ++i) v[i] = a.x ? a.beta * v[i] : 0.0f;
+        if (a.h) {
+            const Stats s = stats_of<G>(h, c, inv_F, a.post, a.eps, lds, turn);
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                const float n = (h[i] - s.m) * s.r * pw[i] + pb[i];
+                v[i] += a.alpha * (a.gate ? gate_of(gv[i], a.act).a * n : n);
+            }
+        }
+        Stats s{0.0f, 1.0f};
+        if (u) s = stats_of<G>(v, c, inv_F, a.pre, a.eps, lds, turn);
+        if (G > WAVE) __syncthreads();   // an output may lie on an input: everybody has read the row
+        if (!live) continue;
+        if (y) c.store(y + r * ldy, v);
+        if (u) {
+#pragma unroll
+            for (int i = 0; i < NV; ++i) v[i] = (v[i] - s.m) * s.r * qw[i] + qb[i];
+            c.store(u + r * ldu, v);
+        }
+    }
+}
+
 // Sums over rows: every block leaves one row of sums per vector, which a second kernel adds up.
 enum { COL_POST_W = 0, COL_POST_B, COL_PRE_W, COL_PRE_B, COL_GATE, COL_KINDS };
 constexpr int COL_BLOCKS = 512;   // most blocks
@@ -184,16 +355,162 @@ __global__ __launch_bounds__(RES_BLOCK) void residual_grad_k(ResidualArgs a, Res
     }
 }
 
+// The same with the row in registers.  BIAS: sums of post_b or pre_b are wanted; GATE_ROW: those of a gate for all rows.
+template <typename TS, typename TB, int V, int G, int N, bool RAGGED, bool BIAS, bool GATE_ROW>
+__global__ __launch_bounds__(RES_BLOCK) void residual_grad_rows_k(ResidualArgs a, ResidualGrad g)
+{
+    constexpr int NV = N * V, ROWS = RES_BLOCK / G;
+    __shared__ float lds[4 * RES_BLOCK / WAVE];
+    __shared__ float sums[ROWS > 1 ? ROWS : 1][ROWS > 1 ? G * NV : 1];
+    int turn = 0;
+    const int32_t M = resolve_count(a.M, a.M_dev);
+    const Cols<V, G, N, RAGGED> c{a.F, (int)threadIdx.x % G};
+    const float inv_F = 1.0f / (float)a.F;
+    float pw[NV], pb[NV], qw[NV], gv[NV], s_pw[NV], s_pb[BIAS ? NV : 1], s_qw[NV], s_qb[BIAS ? NV : 1], s_g[GATE_ROW ? NV : 1];
+    c.load_or(pw, a.post_w, 1.0f);
+    c.load_or(pb, a.post_b, 0.0f);
+    c.load_or(qw, a.pre_w, 1.0f);
+    c.load_or(gv, a.gate && !a.ldg ? (const float *)a.gate : nullptr, 0.0f);
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        s_pw[i] = s_qw[i] = 0.0f;
+        if constexpr (BIAS) s_pb[i] = s_qb[i] = 0.0f;
+        if constexpr (GATE_ROW) s_g[i] = 0.0f;
+    }
+    const int group = (int)threadIdx.x / G;
+    for (int64_t r0 = (int64_t)blockIdx.x * ROWS; r0 < M; r0 += (int64_t)gridDim.x * ROWS) {
+        const bool live = r0 + group < M;
+        const int64_t r = live ? r0 + group : M - 1;
+        float v[NV], h[NV], du[NV], d[NV];
+        if (a.x) c.load(v, (const TS *)a.x + r * a.ldx);
+        if (a.h) c.load(h, (const TB *)a.h + r * a.ldh);
+        if (a.ldg) c.load(gv, (const TB *)a.gate + r * a.ldg);
+        if (g.du) c.load(du, (const TB *)g.du + r * g.lddu);
+        if (g.dy) c.load(d, (const TS *)g.dy + r * g.lddy);
+        else
+#pragma unroll
+            for (int i = 0; i < NV; ++i) d[i] = 0.0f;
+        Stats hs{0.0f, 1.0f};
+        if (a.h) hs = stats_of<G>(h, c, inv_F, a.post, a.eps, lds, turn);
+#pragma unroll
+        for (int i = 0; i < NV; ++i) h[i] = a.h ? (h[i] - hs.m) * hs.r : 0.0f;   // from here on hat(h)
+        if (g.du) {
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                v[i] = a.x ? a.beta * v[i] : 0.0f;
+                if (a.h) {
+                    const float n = h[i] * pw[i] + pb[i];
+                    v[i] += a.alpha * (a.gate ? gate_of(gv[i], a.act).a * n : n);
+                }
+            }
+            const Stats s = stats_of<G>(v, c, inv_F, a.pre, a.eps, lds, turn);
+#pragma unroll
+            for (int i = 0; i < NV; ++i) v[i] = (v[i] - s.m) * s.r;              // hat(y)
+            float t[2];
+            t[0] = c.sum([&](int i) { return du[i] * qw[i] * v[i]; });
+            t[1] = a.pre == CSGS_NORM_LAYER ? c.sum([&](int i) { return du[i] * qw[i]; }) : 0.0f;
+            row_sums<G>(t, lds, turn);
+            t[0] *= inv_F;
+            t[1] *= inv_F;
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                d[i] += s.r * (du[i] * qw[i] - t[1] - v[i] * t[0]);
+                s_qw[i] += live ? du[i] * v[i] : 0.0f;
+                if constexpr (BIAS) s_qb[i] += live ? du[i] : 0.0f;
+            }
+        }
+        float t[2] = {0.0f, 0.0f};
+        if (a.h) {
+            // dn in v (hat(y) is done with), dgate in du
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                const float e = a.alpha * d[i];
+                Gate gt{1.0f, 0.0f};
+                if (a.gate) gt = gate_of(gv[i], a.act);
+                v[i] = e * gt.a;
+                du[i] = e * (h[i] * pw[i] + pb[i]) * gt.da;
+                s_pw[i] += live ? v[i] * h[i] : 0.0f;
+                if constexpr (BIAS) s_pb[i] += live ? v[i] : 0.0f;
+                if constexpr (GATE_ROW) s_g[i] += live ? du[i] : 0.0f;
+                v[i] *= pw[i];
+            }
+            if (a.post != CSGS_NORM_NONE) {
+                t[0] = c.sum([&](int i) { return v[i] * h[i]; });
+                t[1] = a.post == CSGS_NORM_LAYER ? c.sum([&](int i) { return v[i]; }) : 0.0f;
+                row_sums<G>(t, lds, turn);
+                t[0] *= inv_F;
+                t[1] *= inv_F;
+            }
+        }
+        if (G > WAVE) __syncthreads();
+        if (!live) continue;
+        if (a.h) {
+            if (g.dgate && a.ldg) c.store((TB *)g.dgate + r * g.lddg, du);
+            if (g.dh) {
+#pragma unroll
+                for (int i = 0; i < NV; ++i) v[i] = hs.r * (v[i] - t[1] - h[i] * t[0]);
+                c.store((TB *)g.dh + r * g.lddh, v);
+            }
+        }
+        if (g.dx) {
+#pragma unroll
+            for (int i = 0; i < NV; ++i) d[i] *= a.beta;
+            c.store((TS *)g.dx + r * g.lddx, d);
+        }
+    }
+    // sums over the block's rows
+    auto leave = [&](int k, const float (&v)[NV]) {
+        if (!g.want[k]) return;
+        float *part = g.part + ((int64_t)k * gridDim.x + blockIdx.x) * a.F;
+        if constexpr (ROWS == 1) {
+            c.store(part, v);
+        } else {
+            __syncthreads();
+#pragma unroll
+            for (int n = 0; n < N; ++n)
+#pragma unroll
+                for (int i = 0; i < V; ++i)
+                    if (c.active(n)) sums[group][c.col(n) + i] = v[n * V + i];
+            __syncthreads();
+            for (int32_t f = (int32_t)threadIdx.x; f < a.F; f += RES_BLOCK) {
+                float s = sums[0][f];
+#pragma unroll
+                for (int w = 1; w < ROWS; ++w) s += sums[w][f];
+                part[f] = s;
+            }
+        }
+    };
+    leave(COL_POST_W, s_pw);
+    leave(COL_PRE_W, s_qw);
+    if constexpr (BIAS) {
+        leave(COL_POST_B, s_pb);
+        leave(COL_PRE_B, s_qb);
+    }
+    if constexpr (GATE_ROW) leave(COL_GATE, s_g);
+}
+
 struct ColOut {
     float *out[COL_KINDS];
 };
-__global__ __launch_bounds__(256) void col_sums_k(const float *__restrict__ part, int blocks, int32_t F, ColOut o)
+// A block takes 64 columns of a vector; its wavefronts take the parts in turn.
+constexpr int COL_WAVES = 16;
+__global__ __launch_bounds__(COL_WAVES * WAVE) void col_sums_k(const float *__restrict__ part, int blocks, int32_t F, ColOut o)
 {
-    const int k = (int)blockIdx.y;
-    const int32_t f = (int32_t)(blockIdx.x * blockDim.x + threadIdx.x);
-    if (!o.out[k] || f >= F) return;
+    __shared__ double lds[COL_WAVES][WAVE];
+    const int k = (int)blockIdx.y, wave = (int)threadIdx.x / WAVE, lane = lane_id();
+    if (!o.out[k]) return;
+    const int32_t f = (int32_t)blockIdx.x * WAVE + lane;
     double s = 0.0;
-    for (int b = 0; b < blocks; ++b) s += (double)part[((int64_t)k * blocks + b) * F + f];
+    if (f < F) {
+        const float *p = part + (int64_t)k * blocks * F + f;
+#pragma unroll 8
+        for (int b = wave; b < blocks; b += COL_WAVES) s += (double)p[(int64_t)b * F];
+    }
+    lds[wave][lane] = s;
+    __syncthreads();
+    if (wave != 0 || f >= F) return;
+#pragma unroll
+    for (int w = 1; w < COL_WAVES; ++w) s += lds[w][lane];
     o.out[k][f] = (float)s;
 }
 
@@ -212,16 +529,62 @@ static int open_residual(const csgs_residual *r, ResidualArgs *a)
     return CSGS_OK;
 }
 
+// Calls f with the row's layout as constants: lanes, pieces a lane, and whether the width is no multiple of a piece.
+template <int V, typename F>
+static bool with_layout(int32_t width, F f)
+{
+    if (width < V) return false;
+    const bool ragged = width % V != 0;
+    auto go = [&](auto lanes, auto pieces) {
+        if (ragged) f(lanes, pieces, std::true_type{});
+        else f(lanes, pieces, std::false_type{});
+        return true;
+    };
+    using std::integral_constant;
+    const int pieces = (width + V - 1) / V;
+    if (pieces <= 16) return go(integral_constant<int, 16>{}, integral_constant<int, 1>{});
+    if (pieces <= 32) return go(integral_constant<int, 32>{}, integral_constant<int, 1>{});
+    if (pieces <= 64) return go(integral_constant<int, 64>{}, integral_constant<int, 1>{});
+    if (pieces <= 128) return go(integral_constant<int, 64>{}, integral_constant<int, 2>{});
+    if (pieces <= 192) return go(integral_constant<int, 64>{}, integral_constant<int, 3>{});
+    if (pieces <= 256) return go(integral_constant<int, 64>{}, integral_constant<int, 4>{});
+    if (pieces <= 512) return go(integral_constant<int, 256>{}, integral_constant<int, 2>{});
+    if (pieces <= 1024) return go(integral_constant<int, 256>{}, integral_constant<int, 4>{});
+    return false;
+}
+
 template <typename TS, typename TB>
 static void launch_residual(const ResidualArgs &a, void *y, int64_t ldy, void *u, int64_t ldu, hipStream_t st)
 {
+    const bool done = with_layout<4>(a.F, [&](auto lanes, auto pieces, auto ragged) {
+        constexpr int G = decltype(lanes)::value, N = decltype(pieces)::value;
+        const int64_t need = ((int64_t)a.M + RES_BLOCK / G - 1) / (RES_BLOCK / G);
+        const unsigned blocks = (unsigned)(need < 2048 ? need : 2048);
+        CSGS_LAUNCH(K_RESIDUAL, (residual_rows_k<TS, TB, 4, G, N, decltype(ragged)::value>), dim3(blocks), dim3(RES_BLOCK), st, a, (TS *)y, ldy, (TB *)u, ldu);
+    });
+    if (done) return;
     const unsigned blocks = (unsigned)(a.M < 4096 ? a.M : 4096);
     CSGS_LAUNCH(K_RESIDUAL, (residual_k<TS, TB>), dim3(blocks), dim3(RES_BLOCK), st, a, (TS *)y, ldy, (TB *)u, ldu);
 }
+// Returns the number of blocks, each of which has left a row of sums.
 template <typename TS, typename TB>
-static void launch_residual_grad(const ResidualArgs &a, const ResidualGrad &g, hipStream_t st)
+static int launch_residual_grad(const ResidualArgs &a, const ResidualGrad &g, hipStream_t st)
 {
-    CSGS_LAUNCH(K_RESIDUAL_GRAD, (residual_grad_k<TS, TB>), dim3((unsigned)col_blocks(a.M)), dim3(RES_BLOCK), st, a, g);
+    int blocks = col_blocks(a.M);
+    const bool done = with_layout<4>(a.F, [&](auto lanes, auto pieces, auto ragged) {
+        constexpr int G = decltype(lanes)::value, N = decltype(pieces)::value, ROWS = RES_BLOCK / G;
+        constexpr bool R = decltype(ragged)::value;
+        const int64_t need = ((int64_t)a.M + ROWS - 1) / ROWS;
+        blocks = (int)(need < COL_BLOCKS ? need : COL_BLOCKS);
+        const dim3 grid((unsigned)blocks), block(RES_BLOCK);
+        const bool bias = g.want[COL_POST_B] || g.want[COL_PRE_B], row = g.want[COL_GATE];
+        if (bias && row) CSGS_LAUNCH(K_RESIDUAL_GRAD, (residual_grad_rows_k<TS, TB, 4, G, N, R, true, true>), grid, block, st, a, g);
+        else if (bias) CSGS_LAUNCH(K_RESIDUAL_GRAD, (residual_grad_rows_k<TS, TB, 4, G, N, R, true, false>), grid, block, st, a, g);
+        else if (row) CSGS_LAUNCH(K_RESIDUAL_GRAD, (residual_grad_rows_k<TS, TB, 4, G, N, R, false, true>), grid, block, st, a, g);
+        else CSGS_LAUNCH(K_RESIDUAL_GRAD, (residual_grad_rows_k<TS, TB, 4, G, N, R, false, false>), grid, block, st, a, g);
+    });
+    if (!done) CSGS_LAUNCH(K_RESIDUAL_GRAD, (residual_grad_k<TS, TB>), dim3((unsigned)blocks), dim3(RES_BLOCK), st, a, g);
+    return blocks;
 }
 
 }  // namespace csgs
@@ -265,12 +628,12 @@ extern "C" int csgs_norm_residual_grad(const csgs_residual *r, const void *dy, i
     ColOut o{{dpost_w, dpost_b, dpre_w, dpre_b, dgate && !a.ldg ? (float *)dgate : nullptr}};
     bool any = false;
     for (int k = 0; k < COL_KINDS; ++k) any |= (g.want[k] = o.out[k] ? 1 : 0) != 0;
-    if (r->h_dtype == CSGS_F32) launch_residual_grad<float, float>(a, g, st);
-    else if (r->x_dtype == CSGS_F32) launch_residual_grad<float, uint16_t>(a, g, st);
-    else launch_residual_grad<uint16_t, uint16_t>(a, g, st);
+    const int blocks = r->h_dtype == CSGS_F32   ? launch_residual_grad<float, float>(a, g, st)
+                       : r->x_dtype == CSGS_F32 ? launch_residual_grad<float, uint16_t>(a, g, st)
+                                                : launch_residual_grad<uint16_t, uint16_t>(a, g, st);
     CSGS_LAUNCH_CHECK();
     if (any) {
-        CSGS_LAUNCH(K_COL_SUMS, col_sums_k, dim3((unsigned)((a.F + 255) / 256), COL_KINDS), dim3(256), st, (const float *)scratch, col_blocks(a.M), a.F, o);
+        CSGS_LAUNCH(K_COL_SUMS, col_sums_k, dim3((unsigned)((a.F + WAVE - 1) / WAVE), COL_KINDS), dim3(COL_WAVES * WAVE), st, (const float *)scratch, blocks, a.F, o);
         CSGS_LAUNCH_CHECK();
     }
     return CSGS_OK;
