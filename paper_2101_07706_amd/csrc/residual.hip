@@ -170,20 +170,29 @@ struct Cols {
     __device__ bool active(int n) const { return begin(n) < F; }
     __device__ int32_t col(int n) const { return RAGGED && begin(n) > F - V ? F - V : begin(n); }
     __device__ int32_t skip(int n) const { return RAGGED ? begin(n) - col(n) : 0; }
+    // Lanes without a piece read the row's last one again.
+    __device__ int32_t load_col(int n) const { return begin(n) > F - V ? F - V : begin(n); }
     template <typename T>
-    __device__ void load(float (&v)[N * V], const T *row) const
+    __device__ void ask(RawPiece<T, V> (&p)[N], const T *row) const
     {
 #pragma unroll
-        for (int n = 0; n < N; ++n) {
-            Vec<V> p{};
-            if (active(n)) p = load_row<T, V>(row + col(n));
+        for (int n = 0; n < N; ++n) p[n].load(row + load_col(n));
+    }
+    template <typename T>
+    __device__ void widen(float (&v)[N * V], const RawPiece<T, V> (&p)[N]) const
+    {
 #pragma unroll
-            for (int i = 0; i < V; ++i) v[n * V + i] = p.x[i];
-        }
+        for (int n = 0; n < N; ++n)
+#pragma unroll
+            for (int i = 0; i < V; ++i) v[n * V + i] = p[n].value(i);
     }
     __device__ void load_or(float (&v)[N * V], const float *row, float otherwise) const
     {
-        if (row) return load(v, row);
+        if (row) {
+            RawPiece<float, V> p[N];
+            ask(p, row);
+            return widen(v, p);
+        }
 #pragma unroll
         for (int i = 0; i < N * V; ++i) v[i] = otherwise;
     }
@@ -252,11 +261,14 @@ __global__ __launch_bounds__(RES_BLOCK) void residual_rows_k(ResidualArgs a, TS 
         const bool live = r0 + group < M;
         const int64_t r = live ? r0 + group : M - 1;
         float v[NV], h[NV];
-        if (a.x) c.load(v, (const TS *)a.x + r * a.ldx);
-        if (a.h) {
-            c.load(h, (const TB *)a.h + r * a.ldh);
-            if (a.ldg) c.load(gv, (const TB *)a.gate + r * a.ldg);
-        }
+        RawPiece<TS, V> rx[N];
+        RawPiece<TB, V> rh[N], rg[N];
+        if (a.h) c.ask(rh, (const TB *)a.h + r * a.ldh);
+        if (a.ldg) c.ask(rg, (const TB *)a.gate + r * a.ldg);
+        if (a.x) c.ask(rx, (const TS *)a.x + r * a.ldx);
+        c.widen(h, rh);
+        if (a.ldg) c.widen(gv, rg);
+        c.widen(v, rx);
 #pragma unroll
         for (int i = 0; i < NV; ++i) v[i] = a.x ? a.beta * v[i] : 0.0f;
         if (a.h) {
@@ -382,12 +394,19 @@ __global__ __launch_bounds__(RES_BLOCK) void residual_grad_rows_k(ResidualArgs a
         const bool live = r0 + group < M;
         const int64_t r = live ? r0 + group : M - 1;
         float v[NV], h[NV], du[NV], d[NV];
-        if (a.x) c.load(v, (const TS *)a.x + r * a.ldx);
-        if (a.h) c.load(h, (const TB *)a.h + r * a.ldh);
-        if (a.ldg) c.load(gv, (const TB *)a.gate + r * a.ldg);
-        if (g.du) c.load(du, (const TB *)g.du + r * g.lddu);
-        if (g.dy) c.load(d, (const TS *)g.dy + r * g.lddy);
-        else
+        RawPiece<TS, V> rx[N], rdy[N];
+        RawPiece<TB, V> rh[N], rg[N], rdu[N];
+        if (a.h) c.ask(rh, (const TB *)a.h + r * a.ldh);
+        if (a.ldg) c.ask(rg, (const TB *)a.gate + r * a.ldg);
+        if (a.x) c.ask(rx, (const TS *)a.x + r * a.ldx);
+        if (g.du) c.ask(rdu, (const TB *)g.du + r * g.lddu);
+        if (g.dy) c.ask(rdy, (const TS *)g.dy + r * g.lddy);
+        c.widen(h, rh);
+        if (a.ldg) c.widen(gv, rg);
+        c.widen(v, rx);
+        c.widen(du, rdu);
+        c.widen(d, rdy);
+        if (!g.dy)
 #pragma unroll
             for (int i = 0; i < NV; ++i) d[i] = 0.0f;
         Stats hs{0.0f, 1.0f};

@@ -86,6 +86,34 @@ __device__ inline Vec<8> load_row<uint16_t, 8>(const uint16_t *p)
                    __uint_as_float(v.w << 16), __uint_as_float(v.w & 0xFFFF0000u)}};
 }
 
+// A piece as it lies in memory: what is asked for in one place and widened in another, so that many can be on their way (a value
+// that is widened where it is loaded is waited for there, at the end of the branch at the latest).
+template <typename T, int V>
+struct RawPiece {
+    static constexpr int WORDS = (int)sizeof(T) * V / 4;
+    static_assert(WORDS * 4 == (int)sizeof(T) * V && (WORDS == 1 || WORDS == 2 || WORDS == 4 || WORDS == 8), "whole words");
+    uint32_t w[WORDS];
+    __device__ void load(const T *p)
+    {
+        if constexpr (WORDS == 1) w[0] = load_global<uint32_t, (int)sizeof(T)>(p);
+        if constexpr (WORDS == 2) {
+            const u32x2 a = load_global<u32x2, (int)sizeof(T)>(p);
+            w[0] = a.x; w[1] = a.y;
+        }
+        if constexpr (WORDS >= 4)
+#pragma unroll
+            for (int k = 0; k < WORDS; k += 4) {
+                const u32x4 a = load_global<u32x4, (int)sizeof(T)>((const uint32_t *)p + k);
+                w[k] = a.x; w[k + 1] = a.y; w[k + 2] = a.z; w[k + 3] = a.w;
+            }
+    }
+    __device__ float value(int i) const
+    {
+        if constexpr (sizeof(T) == 4) return __uint_as_float(w[i]);
+        return __uint_as_float(i & 1 ? w[i / 2] & 0xFFFF0000u : w[i / 2] << 16);
+    }
+};
+
 // The same the other way: a row's values to memory, bfloat16 by rounding to nearest even (NaN stays NaN).
 __device__ inline uint32_t bf16_bits(float x) { return (uint32_t)__builtin_bit_cast(uint16_t, (__bf16)x); }
 template <typename T, int V>
