@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 
 import torch
 
@@ -145,10 +146,10 @@ def lib():
         L.csgs_embed_grad_scratch_bytes.argtypes = [i64, i64, i32]
         L.csgs_embed_grad.argtypes = [vp, i64, vp, vp, i64, i32, C.c_int, f32, C.c_int, vp, i64, i64, C.c_int, vp, sz, vp]
         L.csgs_embed_grad_rows.argtypes = [vp, i64, vp, vp, i64, i32, C.c_int, f32, i64, vp, vp, vp, i64, C.c_int, vp, sz, vp]
-        L.csgs_norm_residual.argtypes = [C.POINTER(Residual), vp, i64, vp, i64, vp]
+        L.csgs_norm_residual.argtypes = [vp, vp, i64, vp, i64, vp]
         L.csgs_norm_residual_grad_scratch_bytes.restype = sz
         L.csgs_norm_residual_grad_scratch_bytes.argtypes = [i32, i32]
-        L.csgs_norm_residual_grad.argtypes = [C.POINTER(Residual), vp, i64, vp, i64, vp, i64, vp, i64, vp, i64, vp, vp, vp, vp, vp, sz, vp]
+        L.csgs_norm_residual_grad.argtypes = [vp, vp, i64, vp, i64, vp, i64, vp, i64, vp, i64, vp, vp, vp, vp, vp, sz, vp]
         L.csgs_grad_list_bytes.restype = sz
         L.csgs_grad_list_bytes.argtypes = [C.POINTER(GradTensor), i32]
         L.csgs_grad_list_init.argtypes = [C.POINTER(GradList), C.POINTER(GradTensor), i32, vp]
@@ -481,13 +482,15 @@ def csgs_gather_rows(X, ids, n_dev, out, stream=None, inst=None):
                                 _ptr(n_dev), _ptr(out), out.stride(0), _stream(stream))
 
 
+_ELEM = {torch.float32: F32, torch.bfloat16: BF16}
+
+
 def _elem(t):
     """CSGS_* type of a tensor's elements."""
-    if t.dtype == torch.float32:
-        return F32
-    if t.dtype == torch.bfloat16:
-        return BF16
-    raise TypeError(f"float32 or bfloat16, not {t.dtype}")
+    e = _ELEM.get(t.dtype)
+    if e is None:
+        raise TypeError(f"float32 or bfloat16, not {t.dtype}")
+    return e
 
 
 def _ld(t, cols):
@@ -496,27 +499,51 @@ def _ld(t, cols):
     return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), cols)
 
 
+# The calls below describe up to a dozen tensors, and what torch is asked about each of them is the time of a small one: the usual tensor is contiguous
+# and takes four questions (us of host time, a Structure per call and strides, types and sizes asked for one by one / this: residual 12.4 / 4.6,
+# its gradient 21 / 7.6).
+def _mat(t, shape, dtype):
+    """Address and leading dimension of a matrix of this shape and type, or of none."""
+    if t is None:
+        return None, 0
+    assert t.dtype is dtype and t.shape == shape, f"{dtype} of shape {tuple(shape)}, not {t.dtype} of shape {tuple(t.shape)}"
+    return t.data_ptr(), shape[1] if t.is_contiguous() else _ld(t, shape[1])
+
+
 def _i32(t):
-    assert t is None or isinstance(t, C._SimpleCData) or (t.dtype == torch.int32 and (t.dim() == 0 or t.numel() == 1 or t.is_contiguous())), "int32, contiguous"
-    return _ptr(t)
+    if t is None or isinstance(t, C._SimpleCData):
+        return t
+    assert t.dtype is torch.int32 and (t.is_contiguous() or t.numel() == 1), "int32, contiguous"
+    return t.data_ptr()
 
 
 def _f32(t, n):
     """A contiguous float vector of n entries, or None."""
-    assert t is None or (t.dtype == torch.float32 and t.numel() == n and t.is_contiguous()), f"float32, {n} entries, contiguous"
-    return _ptr(t)
+    if t is None:
+        return None
+    assert t.dtype is torch.float32 and t.numel() == n and t.is_contiguous(), f"float32, {n} entries, contiguous"
+    return t.data_ptr()
 
 
 def _scratch(t):
     assert t.is_contiguous()
-    return _ptr(t), t.numel() * t.element_size()
+    return t.data_ptr(), t.numel() * t.element_size()
+
+
+def _rows_of(t, at_least):
+    """Address, leading dimension and width of a matrix of at least so many rows."""
+    rows, cols = t.shape
+    assert rows >= at_least, f"at least {at_least} rows"
+    return t.data_ptr(), cols if t.is_contiguous() else _ld(t, cols), cols
 
 
 def csgs_embed(T, ids, out, scale=1.0, n_dev=None, stream=None):
     """out[t] = scale * T[ids[t]] (float32 or bfloat16 each); zeros where an id is outside the table."""
-    F = T.shape[1]
-    assert out.shape[0] >= ids.numel()
-    _call("csgs_embed", _ptr(T), _ld(T, F), T.shape[0], F, _elem(T), _i32(ids), ids.numel(), _i32(n_dev), scale, _ptr(out), _ld(out, F), _elem(out),
+    n = ids.numel()
+    rows, F = T.shape
+    op, ldo, cols = _rows_of(out, n)
+    assert cols == F, "as wide as the table"
+    _call("csgs_embed", T.data_ptr(), F if T.is_contiguous() else _ld(T, F), rows, F, _elem(T), _i32(ids), n, _i32(n_dev), scale, op, ldo, _elem(out),
           _stream(stream))
 
 
@@ -527,44 +554,48 @@ def csgs_embed_grad_scratch_bytes(n, rows, F) -> int:
 def csgs_embed_grad(ids, G, dT, scratch, scale=1.0, accumulate=False, n_dev=None, stream=None):
     """dT[v] = scale * sum of G[t] over ids[t] = v, zeros elsewhere; accumulate: added to what dT holds.
     scratch: a tensor of at least csgs_embed_grad_scratch_bytes(len(ids), len(dT), F) bytes."""
-    F = G.shape[1]
-    assert G.shape[0] >= ids.numel()
+    n = ids.numel()
+    gp, ldg, F = _rows_of(G, n)
+    rows, cols = dT.shape
+    assert cols == F, "as wide as the table"
     ptr, nbytes = _scratch(scratch)
-    _call("csgs_embed_grad", _i32(ids), ids.numel(), _i32(n_dev), _ptr(G), _ld(G, F), F, _elem(G), scale, 1 if accumulate else 0, _ptr(dT),
-          _ld(dT, F), dT.shape[0], _elem(dT), ptr, nbytes, _stream(stream))
+    _call("csgs_embed_grad", _i32(ids), n, _i32(n_dev), gp, ldg, F, _elem(G), scale, 1 if accumulate else 0, dT.data_ptr(),
+          F if dT.is_contiguous() else _ld(dT, F), rows, _elem(dT), ptr, nbytes, _stream(stream))
 
 
 def csgs_embed_grad_rows(ids, G, rows, uniq, n_uniq, dR, scratch, scale=1.0, n_dev=None, stream=None):
     """The rows of that gradient that some id points to alone: uniq ascending, *n_uniq of them, dR[j] the gradient of row uniq[j]."""
-    F = G.shape[1]
-    assert G.shape[0] >= ids.numel() and uniq.numel() >= ids.numel() and dR.shape[0] >= ids.numel()
+    n = ids.numel()
+    gp, ldg, F = _rows_of(G, n)
+    dp, ldd, cols = _rows_of(dR, n)
+    assert cols == F and uniq.numel() >= n, "a row and an id for every position"
     ptr, nbytes = _scratch(scratch)
-    _call("csgs_embed_grad_rows", _i32(ids), ids.numel(), _i32(n_dev), _ptr(G), _ld(G, F), F, _elem(G), scale, rows, _i32(uniq), _i32(n_uniq),
-          _ptr(dR), _ld(dR, F), _elem(dR), ptr, nbytes, _stream(stream))
+    _call("csgs_embed_grad_rows", _i32(ids), n, _i32(n_dev), gp, ldg, F, _elem(G), scale, rows, _i32(uniq), _i32(n_uniq), dp, ldd, _elem(dR), ptr, nbytes,
+          _stream(stream))
 
 
-def _residual(x, h, stream_type, block_type, gate, gate_act, post, post_w, post_b, pre, pre_w, pre_b, eps, alpha, beta, M_dev):
-    M, F = (x if x is not None else h).shape
-    assert x is None or h is None or x.shape == h.shape
-    types = [_elem(t) for t in (stream_type, block_type)]
-    assert (x is None or _elem(x) == types[0]) and (h is None or _elem(h) == types[1])
-    ldg = 0
-    if gate is not None:
-        if gate.dim() == 1:
-            _f32(gate, F)
-        else:
-            assert gate.shape == (M, F) and _elem(gate) == types[1]
-            ldg = _ld(gate, F)
-    return Residual(M, F, _i32(M_dev), _ptr(x), _ptr(h), _ptr(gate), _ld(x, F) if x is not None else 0, _ld(h, F) if h is not None else 0, ldg,
-                    _f32(post_w, F), _f32(post_b, F), _f32(pre_w, F), _f32(pre_b, F), types[0], types[1], post, pre, gate_act, eps, alpha, beta)
+_residual_layout = struct.Struct("<iiQQQQqqqQQQQiiiiifff")     # csgs_residual
 
 
-def _out(t, shape, elem):
-    """Address and leading dimension of a matrix that may be absent."""
-    if t is None:
-        return None, 0
-    assert tuple(t.shape) == tuple(shape) and _elem(t) == elem
-    return _ptr(t), _ld(t, shape[1])
+def _residual(x, h, stream, block, gate, gate_act, post, post_w, post_b, pre, pre_w, pre_b, eps, alpha, beta, M_dev):
+    """csgs_residual, its shape, and the tensors' types; `stream` and `block`: a tensor of each of the two."""
+    shape = (x if x is not None else h).shape
+    M, F = shape
+    ts, tb = stream.dtype, block.dtype
+    xp, ldx = _mat(x, shape, ts)
+    hp, ldh = _mat(h, shape, tb)
+    if gate is None:
+        gp, ldg = 0, 0
+    elif gate.dim() == 1:
+        gp, ldg = _f32(gate, F), 0
+    else:
+        gp, ldg = _mat(gate, shape, tb)
+    if M_dev is not None:
+        assert M_dev.dtype is torch.int32
+        M_dev = M_dev.data_ptr()
+    r = _residual_layout.pack(M, F, M_dev or 0, xp or 0, hp or 0, gp, ldx, ldh, ldg, _f32(post_w, F) or 0, _f32(post_b, F) or 0, _f32(pre_w, F) or 0,
+                              _f32(pre_b, F) or 0, _elem(stream), _elem(block), post, pre, gate_act, eps, alpha, beta)
+    return r, shape, ts, tb
 
 
 def csgs_norm_residual(x, h, y, u, gate=None, gate_act=GATE_LINEAR, post=NORM_RMS, post_w=None, post_b=None, pre=NORM_RMS, pre_w=None, pre_b=None,
@@ -573,8 +604,8 @@ def csgs_norm_residual(x, h, y, u, gate=None, gate_act=GATE_LINEAR, post=NORM_RM
     gate: None, a float32 vector for all rows, or a matrix like h."""
     a = x if x is not None else y if y is not None else h     # a tensor of the stream's type, of the block's
     b = h if h is not None else u if u is not None else x
-    r = _residual(x, h, a, b, gate, gate_act, post, post_w, post_b, pre, pre_w, pre_b, eps, alpha, beta, M_dev)
-    _call("csgs_norm_residual", C.byref(r), *_out(y, (r.M, r.F), r.x_dtype), *_out(u, (r.M, r.F), r.h_dtype), _stream(stream))
+    r, shape, ts, tb = _residual(x, h, a, b, gate, gate_act, post, post_w, post_b, pre, pre_w, pre_b, eps, alpha, beta, M_dev)
+    _call("csgs_norm_residual", r, *_mat(y, shape, ts), *_mat(u, shape, tb), _stream(stream))
 
 
 def csgs_norm_residual_grad_scratch_bytes(M, F) -> int:
@@ -585,13 +616,14 @@ def csgs_norm_residual_grad(x, h, dy, du, dx, dh, dgate, dpost_w, dpost_b, dpre_
                             post_w=None, post_b=None, pre=NORM_RMS, pre_w=None, pre_b=None, eps=1e-5, alpha=1.0, beta=1.0, M_dev=None, stream=None):
     """Gradients of csgs_norm_residual from dy and du (one may be None); outputs may be None.
     scratch: a tensor of at least csgs_norm_residual_grad_scratch_bytes(M, F) bytes."""
-    first = lambda *ts: next(t for t in ts if t is not None)
-    r = _residual(x, h, first(x, dy, dx, h), first(h, du, dh, x), gate, gate_act, post, post_w, post_b, pre, pre_w, pre_b, eps, alpha, beta, M_dev)
-    M, F = r.M, r.F
-    dg = (_f32(dgate, F), 0) if gate is None or gate.dim() == 1 else _out(dgate, (M, F), r.h_dtype)
+    a = x if x is not None else dy if dy is not None else dx if dx is not None else h
+    b = h if h is not None else du if du is not None else dh if dh is not None else x
+    r, shape, ts, tb = _residual(x, h, a, b, gate, gate_act, post, post_w, post_b, pre, pre_w, pre_b, eps, alpha, beta, M_dev)
+    F = shape[1]
+    dg, lddg = (_f32(dgate, F), 0) if gate is None or gate.dim() == 1 else _mat(dgate, shape, tb)
     ptr, nbytes = _scratch(scratch)
-    _call("csgs_norm_residual_grad", C.byref(r), *_out(dy, (M, F), r.x_dtype), *_out(du, (M, F), r.h_dtype), *_out(dx, (M, F), r.x_dtype),
-          *_out(dh, (M, F), r.h_dtype), *dg, _f32(dpost_w, F), _f32(dpost_b, F), _f32(dpre_w, F), _f32(dpre_b, F), ptr, nbytes, _stream(stream))
+    _call("csgs_norm_residual_grad", r, *_mat(dy, shape, ts), *_mat(du, shape, tb), *_mat(dx, shape, ts), *_mat(dh, shape, tb), dg, lddg, _f32(dpost_w, F),
+          _f32(dpost_b, F), _f32(dpre_w, F), _f32(dpre_b, F), ptr, nbytes, _stream(stream))
 
 
 def make_grad_list(grads, outs=None, rows_dev=None, stream=None) -> GradList:

@@ -90,12 +90,13 @@ __device__ inline Vec<8> load_row<uint16_t, 8>(const uint16_t *p)
 // that is widened where it is loaded is waited for there, at the end of the branch at the latest).
 template <typename T, int V>
 struct RawPiece {
-    static constexpr int WORDS = (int)sizeof(T) * V / 4;
-    static_assert(WORDS * 4 == (int)sizeof(T) * V && (WORDS == 1 || WORDS == 2 || WORDS == 4 || WORDS == 8), "whole words");
-    uint32_t w[WORDS];
+    static constexpr int WORDS = ((int)sizeof(T) * V + 3) / 4;
+    static_assert(WORDS == 1 || WORDS == 2 || WORDS == 4 || WORDS == 8, "piece widths");
+    uint32_t w[WORDS];   // (a single bfloat16: the lower half of one)
     __device__ void load(const T *p)
     {
-        if constexpr (WORDS == 1) w[0] = load_global<uint32_t, (int)sizeof(T)>(p);
+        if constexpr (sizeof(T) * V == 2) w[0] = load_global<uint16_t>(p);
+        else if constexpr (WORDS == 1) w[0] = load_global<uint32_t, (int)sizeof(T)>(p);
         if constexpr (WORDS == 2) {
             const u32x2 a = load_global<u32x2, (int)sizeof(T)>(p);
             w[0] = a.x; w[1] = a.y;
