@@ -28,11 +28,13 @@ __global__ __launch_bounds__(256) void embed_k(const TI *T, int64_t ld, int64_t 
 }
 
 // ---------------------------------------------------------------- positions sorted by id
-// A pass sorts by one digit of up to 8 bits.  At most SORT_TILES blocks take consecutive tiles of the entries: the first kernel
-// counts a tile's digits, the second one adds up what lies before its own (the counts of all tiles, at most 64 K of them)
-// and places its entries.  No block waits for another.
+// An entry is an id and its position, id << 32 | position.  A pass sorts by one digit of up to 8 bits.  At most SORT_TILES blocks
+// take consecutive tiles of the entries: the first kernel counts a tile's digits, the second one adds up what lies before its own
+// (the counts of all tiles, at most 64 K of them) and places its entries.  No block waits for another.
 constexpr int SORT_TILES = 256, SORT_BLOCK = 256, SORT_WAVES = SORT_BLOCK / WAVE, DIGITS = 256;
-constexpr int32_t SORT_TILE_MIN = 2048;
+static_assert(DIGITS == SORT_BLOCK, "a thread per digit");
+constexpr int SORT_ITEMS = 8;                              // entries that a thread places at a time
+constexpr int32_t SORT_STEP = SORT_BLOCK * SORT_ITEMS;     // a tile is a number of these
 
 // Sorted positions are summed in chunks of a fixed number, whatever ids they hold (see chunk_sums_k): as many as leave a
 // million values of the sums at a time (1024 wavefronts of 16 bytes a lane), 8 to 64, no more than the lanes that take a row.
@@ -45,9 +47,10 @@ __host__ inline int32_t chunk_of(int64_t n, int32_t F)
 }
 
 struct EmbedScratch {
-    uint32_t *key[2], *pos[2];   // [n] entries, used in turn
-    uint32_t *hist;              // [DIGITS * SORT_TILES] of a pass
-    uint32_t *heads;             // [SORT_TILES] different ids that begin in a tile
+    uint64_t *entry[2];          // [n] entries, used in turn
+    uint32_t *hist;              // [SORT_TILES][DIGITS] of a pass
+    uint32_t *heads;             // [SORT_TILES] different ids that begin in a tile; of every range
+    int32_t *n_valid;            // positions whose id is in the table
     uint32_t *rank;              // [n] of an entry's id among the different ones
     double *part;                // [chunks][2][F] sums of rows that go on across chunks
     size_t bytes;
@@ -61,12 +64,10 @@ __host__ inline EmbedScratch carve_embed(void *base, int64_t n, int32_t F)
         off = align_up(off + bytes, 256);
         return (char *)base + o;
     };
-    for (int i = 0; i < 2; ++i) {
-        s.key[i] = (uint32_t *)take((size_t)n * 4);
-        s.pos[i] = (uint32_t *)take((size_t)n * 4);
-    }
+    for (int i = 0; i < 2; ++i) s.entry[i] = (uint64_t *)take((size_t)n * 8);
     s.hist = (uint32_t *)take(sizeof(uint32_t) * DIGITS * SORT_TILES);
     s.heads = (uint32_t *)take(sizeof(uint32_t) * SORT_TILES);
+    s.n_valid = (int32_t *)take(4);
     s.rank = (uint32_t *)take((size_t)n * 4);
     const int32_t chunk = chunk_of(n, F);
     s.part = (double *)take(sizeof(double) * 2 * (size_t)((n + chunk - 1) / chunk) * (size_t)F);
@@ -76,25 +77,16 @@ __host__ inline EmbedScratch carve_embed(void *base, int64_t n, int32_t F)
 
 // Where the entries of a pass come from: the caller's ids in the first one (ids outside the table take the key `rows`, behind
 // all others), the entries of the pass before in the others.
+__device__ inline uint32_t key_of(uint64_t entry) { return (uint32_t)(entry >> 32); }
 struct SortIn {
     const int32_t *ids;
-    const uint32_t *key, *pos;
+    const uint64_t *entry;
     uint32_t rows;
-    __device__ uint32_t get(int64_t i, uint32_t *p) const
+    __device__ uint64_t get(int64_t i) const
     {
-        if (ids) {
-            const uint32_t id = (uint32_t)ids[i];
-            *p = (uint32_t)i;
-            return id < rows ? id : rows;
-        }
-        *p = pos[i];
-        return key[i];
-    }
-    __device__ uint32_t get(int64_t i) const
-    {
-        if (!ids) return key[i];
+        if (!ids) return entry[i];
         const uint32_t id = (uint32_t)ids[i];
-        return id < rows ? id : rows;
+        return (uint64_t)(id < rows ? id : rows) << 32 | (uint32_t)i;
     }
 };
 
@@ -107,9 +99,9 @@ __global__ __launch_bounds__(SORT_BLOCK) void sort_count_k(SortIn in, int32_t n_
     const int64_t end = beg + tile < n ? beg + tile : n;
     count[threadIdx.x] = 0;
     __syncthreads();
-    for (int64_t i = beg + threadIdx.x; i < end; i += SORT_BLOCK) atomicAdd(&count[(in.get(i) >> shift) & mask], 1u);
+    for (int64_t i = beg + threadIdx.x; i < end; i += SORT_BLOCK) atomicAdd(&count[(key_of(in.get(i)) >> shift) & mask], 1u);
     __syncthreads();
-    hist[threadIdx.x * SORT_TILES + blockIdx.x] = count[threadIdx.x];
+    hist[blockIdx.x * DIGITS + threadIdx.x] = count[threadIdx.x];
 }
 
 // The lanes of the wavefront whose digit is this lane's own (lanes that take part).
@@ -124,63 +116,375 @@ __device__ inline uint64_t same_digit(uint32_t digit, bool active, int bits)
     return peers;
 }
 
-__global__ __launch_bounds__(SORT_BLOCK) void sort_place_k(SortIn in, int32_t n_cap, const int32_t *__restrict__ n_dev, int32_t tile, int tiles,
-                                                           int shift, int bits, const uint32_t *__restrict__ hist,
-                                                           uint32_t *__restrict__ key_out, uint32_t *__restrict__ pos_out)
+__device__ inline uint32_t digit_of(uint64_t e, uint32_t least, int shift, int bits) { return ((key_of(e) - least) >> shift) & ((1u << bits) - 1u); }
+__device__ inline int bits_of(uint32_t x) { return x ? 32 - __clz((int)x) : 0; }
+
+// A wavefront's entries of a step: rank[u] = entries before that one with its digit in the wavefront's share, `count` [DIGITS] (zeros before) = how
+// many there are of each.  Entries u * 64 + lane, of which those with `active` count.
+template <int ITEMS>
+__device__ inline void rank_digits(const uint64_t (&e)[ITEMS], const bool (&active)[ITEMS], int shift, int bits, volatile uint32_t *count, uint32_t (&rank)[ITEMS],
+                                   uint32_t least = 0)
 {
-    __shared__ uint32_t at[SORT_WAVES][DIGITS];   // a wavefront's entries by digit, then the next place of each
+    const uint64_t below = (1ull << lane_id()) - 1ull;
+#pragma unroll
+    for (int u = 0; u < ITEMS; ++u) {
+        const uint32_t digit = digit_of(e[u], least, shift, bits);
+        const uint64_t peers = same_digit(digit, active[u], bits);
+        const uint32_t before = (uint32_t)__popcll(peers & below);
+        uint32_t seen = 0;
+        if (active[u]) seen = count[digit];
+        __builtin_amdgcn_wave_barrier();
+        if (active[u] && before == 0) count[digit] = seen + (uint32_t)__popcll(peers);
+        __builtin_amdgcn_wave_barrier();
+        rank[u] = seen + before;
+    }
+}
+
+__global__ __launch_bounds__(SORT_BLOCK) void sort_place_k(SortIn in, int32_t n_cap, const int32_t *__restrict__ n_dev, int32_t tile, int tiles,
+                                                           int shift, int bits, const uint32_t *__restrict__ hist, uint64_t *__restrict__ out)
+{
+    __shared__ uint32_t at[SORT_WAVES][DIGITS];   // a wavefront's entries by digit, then the place of its first
     __shared__ uint32_t scan[17];
     const int32_t n = resolve_count(n_cap, n_dev);
     const int64_t beg = (int64_t)blockIdx.x * tile;
     const int64_t end = beg + tile < n ? beg + tile : n;
     if (beg >= end) return;
     const uint32_t mask = (1u << bits) - 1;
-    const int tid = (int)threadIdx.x, lane = lane_id(), wave = tid / WAVE;
-    const int64_t share = tile / SORT_WAVES;   // a multiple of 64
-    const int64_t w_beg = beg + wave * share, w_end = w_beg + share < end ? w_beg + share : end;
-    for (int w = 0; w < SORT_WAVES; ++w) at[w][tid] = 0;
+    const int tid = (int)threadIdx.x, wave = tid / WAVE;
+    auto load = [&](int64_t i0, uint64_t (&e)[SORT_ITEMS], bool (&active)[SORT_ITEMS]) {
+#pragma unroll
+        for (int u = 0; u < SORT_ITEMS; ++u) {
+            const int64_t i = i0 + wave * (SORT_ITEMS * WAVE) + u * WAVE + lane_id();
+            active[u] = i < end;
+            e[u] = in.get(active[u] ? i : end - 1);
+        }
+    };
+    uint64_t e[SORT_ITEMS];
+    bool active[SORT_ITEMS];
+    load(beg, e, active);
     // entries with a smaller digit, and of this digit in earlier tiles
-    uint32_t before = 0, all = 0;
+    uint32_t before = 0, all = 0, total;
+#pragma unroll 8
     for (int t = 0; t < tiles; ++t) {
-        const uint32_t c = hist[tid * SORT_TILES + t];
+        const uint32_t c = hist[t * DIGITS + tid];
         before += t < (int)blockIdx.x ? c : 0u;
         all += c;
     }
-    __syncthreads();
-    for (int64_t i = w_beg + lane; i < w_end; i += WAVE) atomicAdd(&at[wave][(in.get(i) >> shift) & mask], 1u);
-    uint32_t total;
-    const uint32_t smaller = block_exclusive_scan<uint32_t>(all, scan, &total);   // (its barriers: the counts are complete)
-    uint32_t next = smaller + before;
-    for (int w = 0; w < SORT_WAVES; ++w) {
-        const uint32_t c = at[w][tid];
-        at[w][tid] = next;
-        next += c;
-    }
-    __syncthreads();
-    for (int64_t i0 = w_beg; i0 < w_end; i0 += WAVE) {
-        const int64_t i = i0 + lane;
-        const bool active = i < w_end;
-        uint32_t p = 0;
-        const uint32_t k = active ? in.get(i, &p) : 0u;
-        const uint32_t digit = (k >> shift) & mask;
-        const uint64_t peers = same_digit(digit, active, bits);
-        const uint32_t rank = (uint32_t)__popcll(peers & ((1ull << lane) - 1ull));
-        uint32_t dst = 0;
-        if (active) dst = *(volatile uint32_t *)&at[wave][digit] + rank;
-        __builtin_amdgcn_wave_barrier();
-        if (active && rank == 0) *(volatile uint32_t *)&at[wave][digit] = dst + (uint32_t)__popcll(peers);
-        __builtin_amdgcn_wave_barrier();
-        if (active && dst < (uint32_t)n) {
-            key_out[dst] = k;
-            pos_out[dst] = p;
+    uint32_t next = block_exclusive_scan<uint32_t>(all, scan, &total) + before;   // of the thread's digit
+    for (int64_t i0 = beg; i0 < end; i0 += SORT_STEP) {
+        if (i0 > beg) load(i0, e, active);
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < SORT_WAVES; ++w) at[w][tid] = 0;
+        __syncthreads();
+        uint32_t rank[SORT_ITEMS];
+        rank_digits(e, active, shift, bits, at[wave], rank);
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < SORT_WAVES; ++w) {
+            const uint32_t c = at[w][tid];
+            at[w][tid] = next;
+            next += c;
         }
+        __syncthreads();
+#pragma unroll
+        for (int u = 0; u < SORT_ITEMS; ++u)
+            if (active[u]) {
+                const uint32_t dst = at[wave][(key_of(e[u]) >> shift) & mask] + rank[u];
+                if (dst < (uint32_t)n) out[dst] = e[u];
+            }
     }
 }
 
-// ---------------------------------------------------------------- the different ids
-__device__ inline bool is_head(const uint32_t *__restrict__ key, int64_t i, uint32_t rows) { return key[i] < rows && (i == 0 || key[i - 1] != key[i]); }
+// ---------------------------------------------------------------- a block's own sort
+constexpr int WIDE = 1024, WIDE_WAVES = WIDE / WAVE, WIDE_ITEMS = 8;
+constexpr int LDS_ENTRIES = WIDE * WIDE_ITEMS;   // most entries that a block sorts in LDS
+struct SortLds {
+    uint32_t at[WIDE_WAVES][DIGITS];   // a wavefront's entries by digit, then the place of its first
+    uint32_t scan[17];
+};
 
-__global__ __launch_bounds__(SORT_BLOCK) void heads_count_k(const uint32_t *__restrict__ key, int32_t n_cap, const int32_t *__restrict__ n_dev,
+// Places of a step of at most WIDE * ITEMS entries of which thread `digit` knows the place of its digit's next one: at[][] is left holding
+// each wavefront's first places.  Barriers: the caller's entries are loaded when it returns, and nothing is stored yet.
+template <int ITEMS>
+__device__ inline void step_places(const uint64_t (&e)[ITEMS], const bool (&active)[ITEMS], uint32_t least, int shift, int bits, SortLds &l,
+                                   uint32_t (&rank)[ITEMS])
+{
+    const int tid = (int)threadIdx.x, wave = tid / WAVE;
+    __syncthreads();
+    for (int x = tid; x < WIDE_WAVES * DIGITS; x += WIDE) (&l.at[0][0])[x] = 0;
+    __syncthreads();
+    rank_digits(e, active, shift, bits, l.at[wave], rank, least);
+    __syncthreads();
+}
+__device__ inline uint32_t wave_prefixes(SortLds &l, uint32_t next)   // thread = digit
+{
+#pragma unroll
+    for (int w = 0; w < WIDE_WAVES; ++w) {
+        const uint32_t c = l.at[w][threadIdx.x];
+        l.at[w][threadIdx.x] = next;
+        next += c;
+    }
+    return next;
+}
+
+// Sorts m <= WIDE * ITEMS entries in LDS by key, stable, where keys lie in [least, least + span].
+template <int ITEMS>
+__device__ inline void sort_in_lds(uint64_t *e, int m, uint32_t least, uint32_t span, SortLds &l)
+{
+    const int key_bits = bits_of(span), passes = (key_bits + 7) / 8, bits = passes ? (key_bits + passes - 1) / passes : 0;
+    const int tid = (int)threadIdx.x, wave = tid / WAVE, steps = (m + WIDE - 1) / WIDE;
+    for (int p = 0; p < passes; ++p) {
+        uint64_t v[ITEMS];
+        bool active[ITEMS];
+        uint32_t rank[ITEMS];
+#pragma unroll
+        for (int u = 0; u < ITEMS; ++u) {
+            const int i = (wave * steps + u) * WAVE + lane_id();
+            active[u] = u < steps && i < m;
+            v[u] = active[u] ? e[i] : 0ull;
+        }
+        step_places(v, active, least, p * bits, bits, l, rank);
+        uint32_t all = 0, total;
+        if (tid < DIGITS) all = wave_prefixes(l, 0);
+        const uint32_t first = block_exclusive_scan<uint32_t>(all, l.scan, &total);
+        if (tid < DIGITS)
+#pragma unroll
+            for (int w = 0; w < WIDE_WAVES; ++w) l.at[w][tid] += first;
+        __syncthreads();
+#pragma unroll
+        for (int u = 0; u < ITEMS; ++u)
+            if (active[u]) e[l.at[wave][digit_of(v[u], least, p * bits, bits)] + rank[u]] = v[u];
+        __syncthreads();
+    }
+}
+
+// The same for any number of entries in global memory, from a to b and back; returns where they are in the end (a or b).
+__device__ inline uint64_t *sort_in_memory(uint64_t *a, uint64_t *b, int64_t m, uint32_t least, uint32_t span, SortLds &l)
+{
+    constexpr int ITEMS = 4;
+    const int key_bits = bits_of(span), passes = (key_bits + 7) / 8, bits = passes ? (key_bits + passes - 1) / passes : 0;
+    const int tid = (int)threadIdx.x, wave = tid / WAVE;
+    for (int p = 0; p < passes; ++p) {
+        __syncthreads();
+        if (tid < DIGITS) l.at[0][tid] = 0;
+        __syncthreads();
+        for (int64_t i = tid; i < m; i += WIDE) atomicAdd(&l.at[0][digit_of(a[i], least, p * bits, bits)], 1u);
+        __syncthreads();
+        const uint32_t all = tid < DIGITS ? l.at[0][tid] : 0u;
+        uint32_t total, next = block_exclusive_scan<uint32_t>(all, l.scan, &total);
+        for (int64_t i0 = 0; i0 < m; i0 += WIDE * ITEMS) {
+            uint64_t v[ITEMS];
+            bool active[ITEMS];
+            uint32_t rank[ITEMS];
+#pragma unroll
+            for (int u = 0; u < ITEMS; ++u) {
+                const int64_t i = i0 + (wave * ITEMS + u) * WAVE + lane_id();
+                active[u] = i < m;
+                v[u] = active[u] ? a[i] : 0ull;
+            }
+            step_places(v, active, least, p * bits, bits, l, rank);
+            if (tid < DIGITS) next = wave_prefixes(l, next);
+            __syncthreads();
+#pragma unroll
+            for (int u = 0; u < ITEMS; ++u)
+                if (active[u]) b[l.at[wave][digit_of(v[u], least, p * bits, bits)] + rank[u]] = v[u];
+        }
+        __syncthreads();
+        uint64_t *t = a;
+        a = b;
+        b = t;
+    }
+    return a;
+}
+
+// ---------------------------------------------------------------- zeros
+// Rows of `row` bytes (a multiple of 2), `ld` bytes apart, by worker `me` of `workers` wavefronts.
+struct ZeroRows {
+    void *d;
+    int64_t rows, row, ld;   // rows = 0: none
+};
+__device__ inline void zero_rows(const ZeroRows &z, int64_t me, int64_t workers)
+{
+    const bool flat = z.row == z.ld;   // then one row of everything, in pieces of 16 KB
+    const int64_t rows = flat ? (z.rows * z.row + 16383) / 16384 : z.rows, ld = flat ? 16384 : z.ld;
+    for (int64_t r = me; r < rows; r += workers) {
+        char *p = (char *)z.d + r * ld;
+        const int64_t len = !flat ? z.row : (r + 1 < rows ? 16384 : z.rows * z.row - r * 16384);
+        for (int64_t at = lane_id() * 16; at < len; at += WAVE * 16) {
+            if (at + 16 <= len) store_global<u32x4, 2>(p + at, u32x4{0, 0, 0, 0});
+            else
+                for (int64_t b = at; b < len; b += 2) store_global<uint16_t>(p + b, (uint16_t)0);
+        }
+    }
+}
+__global__ __launch_bounds__(256) void rows_zero_k(ZeroRows z)
+{
+    zero_rows(z, ((int64_t)blockIdx.x * blockDim.x + threadIdx.x) / WAVE, (int64_t)gridDim.x * blockDim.x / WAVE);
+}
+
+// ---------------------------------------------------------------- positions sorted by id, in one launch
+// A block owns a range of ids, looks at all ids itself and lists those of its range in order of position; how many lie below the range
+// says where its list belongs among the sorted entries, so that no block waits for another.  Ranges hold about as many positions
+// each: every block sorts the same sample of the ids and takes its bounds from there.  An id that fills bounds by itself has a
+// range of its own, which needs no sorting however many positions it holds; a list that outgrows LDS all the same (a sample that misses) is
+// sorted in memory.  Further blocks clear the gradient's rows meanwhile.
+constexpr int RANGES = 256, SAMPLE = WIDE, RANGE_CACHED = 32;
+constexpr int64_t RANGE_CACHED_MAX = (int64_t)WIDE * RANGE_CACHED;
+template <bool CACHED>   // at most RANGE_CACHED_MAX positions: the ids stay in registers between counting and listing
+__global__ __launch_bounds__(WIDE) void sort_ranges_k(const int32_t *__restrict__ ids, int32_t n_cap, const int32_t *__restrict__ n_dev, uint32_t rows,
+                                                      uint64_t *out, uint64_t *other, uint32_t *__restrict__ rank, uint32_t *__restrict__ distinct,
+                                                      int32_t *__restrict__ n_valid, ZeroRows z)
+{
+    constexpr int U = 8;
+    __shared__ uint64_t e[LDS_ENTRIES];
+    __shared__ SortLds l;
+    __shared__ uint32_t w_below[WIDE_WAVES], w_own[WIDE_WAVES];
+    const int tid = (int)threadIdx.x, lane = lane_id(), wave = tid / WAVE, b = (int)blockIdx.x;
+    if (b >= RANGES) return zero_rows(z, (int64_t)(b - RANGES) * WIDE_WAVES + wave, (int64_t)(gridDim.x - RANGES) * WIDE_WAVES);
+    const int32_t n = resolve_count(n_cap, n_dev);
+    if (n == 0) {
+        if (tid == 0) {
+            distinct[b] = 0;
+            if (b == 0) *n_valid = 0;
+        }
+        return;
+    }
+    auto key_at = [&](int64_t i) {
+        const uint32_t id = (uint32_t)ids[i];
+        return id < rows ? id : rows;
+    };
+    const int32_t share = (n + WIDE - 1) / WIDE * WAVE;   // positions of a wavefront
+    const int32_t w_beg = wave * share, w_end = w_beg + share < n ? w_beg + share : n;
+    uint32_t held[CACHED ? RANGE_CACHED : 1];
+    if constexpr (CACHED) {
+#pragma unroll
+        for (int u = 0; u < RANGE_CACHED; ++u) {
+            const int32_t i = w_beg + u * WAVE + lane;
+            held[u] = u * WAVE < share && i < w_end ? (uint32_t)ids[i] : 0xFFFFFFFFu;
+        }
+    }
+    // bounds
+    const int samples = n < SAMPLE ? n : SAMPLE;
+    if (tid < samples) e[tid] = (uint64_t)key_at((int64_t)tid * n / samples) << 32;
+    __syncthreads();
+    sort_in_lds<1>(e, samples, 0, rows, l);
+    auto bound = [&](int r) { return r <= 0 ? 0u : key_of(e[(int64_t)r * samples / RANGES]); };
+    uint32_t lo = bound(b), hi = b + 1 < RANGES ? bound(b + 1) : rows;   // [lo, hi)
+    const bool again = b > 0 && bound(b - 1) == lo;   // the id `lo` is another block's
+    if (lo == hi && !again) hi = lo + 1;              // ... this one's, alone
+    else if (again) ++lo;
+    if (hi > rows) hi = rows;
+    if (lo > hi) lo = hi;
+    __syncthreads();
+    const uint32_t width = hi - lo;
+    // ids below the range and in it
+    uint32_t n_below = 0, n_own = 0;
+    auto count = [&](uint32_t id) {
+        n_below += (uint32_t)__popcll(__ballot(id < lo));
+        n_own += (uint32_t)__popcll(__ballot(id - lo < width));
+    };
+    if constexpr (CACHED) {
+#pragma unroll
+        for (int u = 0; u < RANGE_CACHED; ++u)
+            if (u * WAVE < share) count(held[u]);
+    } else {
+        for (int32_t i0 = w_beg; i0 < w_end; i0 += U * WAVE) {
+            uint32_t id[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int32_t i = i0 + u * WAVE + lane;
+                id[u] = i < w_end ? (uint32_t)ids[i] : 0xFFFFFFFFu;
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u) count(id[u]);
+        }
+    }
+    if (lane == 0) {
+        w_below[wave] = n_below;
+        w_own[wave] = n_own;
+    }
+    __syncthreads();
+    uint32_t below = 0, own = 0, at = 0;
+    for (int w = 0; w < WIDE_WAVES; ++w) {
+        below += w_below[w];
+        if (w == wave) at = own;
+        own += w_own[w];
+    }
+    if (b == RANGES - 1 && tid == 0) *n_valid = (int32_t)(below + own);
+    if (own == 0) {
+        if (tid == 0) distinct[b] = 0;
+        return;
+    }
+    // the list
+    const bool alone = width == 1, in_lds = !alone && own <= LDS_ENTRIES;
+    const int passes = (bits_of(width - 1) + 7) / 8;
+    uint64_t *mine = alone || passes % 2 == 0 ? out : other;   // the sorted list has to end in `out`
+    auto list = [&](uint32_t id, int32_t i) {
+        const bool is = id - lo < width;
+        const uint64_t m = __ballot(is);
+        const uint32_t dst = at + (uint32_t)__popcll(m & ((1ull << lane) - 1ull));
+        const uint64_t entry = (uint64_t)id << 32 | (uint32_t)i;
+        if (is) {
+            if (in_lds) e[dst] = entry;
+            else if (below + dst < (uint32_t)n) mine[below + dst] = entry;
+        }
+        at += (uint32_t)__popcll(m);
+    };
+    if constexpr (CACHED) {
+#pragma unroll
+        for (int u = 0; u < RANGE_CACHED; ++u)
+            if (u * WAVE < share) list(held[u], w_beg + u * WAVE + lane);
+    } else {
+        for (int32_t i0 = w_beg; i0 < w_end; i0 += U * WAVE) {
+            uint32_t id[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int32_t i = i0 + u * WAVE + lane;
+                id[u] = i < w_end ? (uint32_t)ids[i] : 0xFFFFFFFFu;
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u) list(id[u], i0 + u * WAVE + lane);
+        }
+    }
+    __syncthreads();
+    if (in_lds) sort_in_lds<WIDE_ITEMS>(e, (int)own, lo, width - 1, l);
+    else if (!alone) sort_in_memory(mine + below, (mine == out ? other : out) + below, own, lo, width - 1, l);
+    // entries out, with their id's rank in the list
+    uint32_t base = 0;
+    for (uint32_t i0 = 0; i0 < own; i0 += WIDE) {
+        const uint32_t i = i0 + (uint32_t)tid;
+        if (in_lds && i < own) out[below + i] = e[i];
+        if (!rank) continue;
+        if (alone) {
+            if (i < own) rank[below + i] = (uint32_t)b << 24;
+            continue;
+        }
+        bool head = false;
+        if (i < own) head = i == 0 || (in_lds ? key_of(e[i]) != key_of(e[i - 1]) : key_of(out[below + i]) != key_of(out[below + i - 1]));
+        uint32_t total;
+        const uint32_t before = base + block_exclusive_scan<uint32_t>(head ? 1u : 0u, l.scan, &total);
+        base += total;
+        if (i < own) rank[below + i] = (uint32_t)b << 24 | (before + (head ? 1u : 0u) - 1u);
+    }
+    if (tid == 0) distinct[b] = alone ? 1u : base;
+}
+constexpr int64_t RANGES_MAX = 1 << 18;   // most positions of this form
+static_assert(RANGES_MAX <= 1 << 24 && RANGES <= 256, "a block and a rank in 32 bits");
+
+// ---------------------------------------------------------------- the different ids
+// The keys of sorted entries.
+struct Keys {
+    const uint64_t *entry;
+    __device__ uint32_t operator[](int64_t i) const { return (uint32_t)(entry[i] >> 32); }
+};
+__device__ inline bool is_head(const Keys &key, int64_t i, uint32_t rows)
+{
+    const uint32_t k = key[i], before = key[i > 0 ? i - 1 : 0];
+    return k < rows && (i == 0 || before != k);
+}
+
+__global__ __launch_bounds__(SORT_BLOCK) void heads_count_k(Keys key, int32_t n_cap, const int32_t *__restrict__ n_dev,
                                                             int32_t tile, uint32_t rows, uint32_t *__restrict__ heads)
 {
     __shared__ uint32_t scan[17];
@@ -193,9 +497,9 @@ __global__ __launch_bounds__(SORT_BLOCK) void heads_count_k(const uint32_t *__re
     if (threadIdx.x == 0) heads[blockIdx.x] = total;
 }
 
-__global__ __launch_bounds__(SORT_BLOCK) void heads_place_k(const uint32_t *__restrict__ key, int32_t n_cap, const int32_t *__restrict__ n_dev,
+__global__ __launch_bounds__(SORT_BLOCK) void heads_place_k(Keys key, int32_t n_cap, const int32_t *__restrict__ n_dev,
                                                             int32_t tile, int tiles, uint32_t rows, const uint32_t *__restrict__ heads,
-                                                            uint32_t *__restrict__ rank, int32_t *__restrict__ uniq, int32_t *__restrict__ n_uniq)
+                                                            uint32_t *__restrict__ rank, int32_t *__restrict__ n_uniq)
 {
     __shared__ uint32_t scan[17];
     const int32_t n = resolve_count(n_cap, n_dev);
@@ -212,20 +516,11 @@ __global__ __launch_bounds__(SORT_BLOCK) void heads_place_k(const uint32_t *__re
         const bool head = i < end && is_head(key, i, rows);
         const uint32_t before = base + block_exclusive_scan<uint32_t>(head ? 1u : 0u, scan, &total);
         base += total;
-        if (head) uniq[before] = (int32_t)key[i];
         if (i < end) rank[i] = before + (head ? 1u : 0u) - 1u;
     }
 }
 
 // ---------------------------------------------------------------- sums
-template <typename TD>
-__global__ __launch_bounds__(256) void rows_zero_k(TD *d, int64_t ldd, int64_t rows, int32_t F)
-{
-    const int64_t waves = (int64_t)gridDim.x * (blockDim.x / WAVE);
-    for (int64_t r = ((int64_t)blockIdx.x * blockDim.x + threadIdx.x) / WAVE; r < rows; r += waves)
-        for (int32_t f = lane_id(); f < F; f += WAVE) store_row<TD, 1>(d + r * ldd + f, Vec<1>{{0.0f}});
-}
-
 // The piece of V columns that a lane holds; where V does not divide F, the row's last piece is read from F - V on and its first `skip`
 // values are the piece's before.
 template <int V>
@@ -242,7 +537,9 @@ struct Piece1 {
 
 // Where the sums go: row `rank` of the compact form, row `key` of the dense one.
 struct SumOut {
-    const uint32_t *rank;   // null: dense
+    const uint32_t *rank;       // null: dense
+    const uint32_t *distinct;   // the different ids of every range (rank: range << 24 | rank in it); null: ranks are ranks
+    int32_t *uniq, *n_uniq;
     void *d;
     int64_t ldd;
     float scale;
@@ -277,6 +574,16 @@ __device__ inline void write_part(double *part, const Piece1<V> &pc, const doubl
     for (int i = 0; i < V; ++i) part[pc.col + i] = acc[i];   // (values of two pieces: the same from both)
 }
 
+// Rows of the output before each range's.  All threads of a block of 256 or more.
+__device__ inline void range_bases(const SumOut &o, uint32_t *base /*[RANGES]*/, uint32_t *scan /*[17]*/, uint32_t *total)
+{
+    const int tid = (int)threadIdx.x;
+    const uint32_t first = block_exclusive_scan<uint32_t>(tid < RANGES ? o.distinct[tid] : 0u, scan, total);
+    if (tid < RANGES) base[tid] = first;
+    __syncthreads();
+}
+__device__ inline uint32_t row_of_rank(const SumOut &o, uint32_t rank, const uint32_t *base) { return o.distinct ? base[rank >> 24] + (rank & 0xFFFFFFu) : rank; }
+
 // Value of lane `from` of the G lanes that work together.
 template <int G>
 __device__ inline uint32_t from_lane(uint32_t v, int from)
@@ -289,12 +596,18 @@ __device__ inline uint32_t from_lane(uint32_t v, int from)
 // table row all of whose positions lie in the chunk is written at once, parts of others go to `part`.  The work per chunk does not
 // depend on how often an id occurs.
 template <typename TG, typename TD, int V, int G>
-__global__ __launch_bounds__(256) void chunk_sums_k(const TG *g, int64_t ldg, int32_t F, const uint32_t *__restrict__ key, const uint32_t *__restrict__ pos,
+__global__ __launch_bounds__(256) void chunk_sums_k(const TG *g, int64_t ldg, int32_t F, const uint64_t *__restrict__ entry,
                                                     int32_t n_cap, const int32_t *__restrict__ n_dev, uint32_t rows, int32_t chunk,
                                                     double *__restrict__ part, SumOut o)
 {
     constexpr int U = 8;
+    __shared__ uint32_t base[RANGES], scan[17];
     const int32_t n = resolve_count(n_cap, n_dev);
+    if (o.distinct) {
+        uint32_t total;
+        range_bases(o, base, scan, &total);
+        if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) *o.n_uniq = (int32_t)total;
+    }
     const int lane = (int)threadIdx.x % G;
     const int64_t c = ((int64_t)blockIdx.x * 256 + threadIdx.x) / G;
     const int64_t beg = c * chunk;
@@ -303,17 +616,20 @@ __global__ __launch_bounds__(256) void chunk_sums_k(const TG *g, int64_t ldg, in
     const uint32_t NONE = 0xFFFFFFFFu;
     uint32_t k = NONE, p = 0, rk = 0;
     if (lane < len) {
-        k = key[beg + lane];
-        p = pos[beg + lane];
-        if (o.rank) rk = o.rank[beg + lane];
+        const uint64_t e = entry[beg + lane];
+        k = key_of(e);
+        p = (uint32_t)e;
+        if (o.rank) rk = row_of_rank(o, o.rank[beg + lane], base);
     }
     const uint32_t row = o.rank ? rk : k;
+    const Keys key{entry};
     const uint32_t before = len > 0 && beg > 0 ? key[beg - 1] : NONE, after = len > 0 && end < n ? key[end] : NONE;
     const uint32_t prev = (uint32_t)__shfl_up((int)k, 1, G);
     const uint32_t next = (uint32_t)__shfl_down((int)k, 1, G);
     const bool valid = lane < len && k < rows;
     const bool last = valid && (lane == len - 1 ? after != k : next != k);      // the row's last position
     const bool first = valid && (lane == 0 ? before != k : prev != k);
+    if (first && o.rank && blockIdx.y == 0) o.uniq[rk] = (int32_t)k;
     const int shift = (int)(threadIdx.x & (WAVE - 1)) / G * G;
     const uint64_t lanes = G == WAVE ? ~0ull : (1ull << (G % WAVE)) - 1ull;
     const uint64_t m_valid = (__ballot(valid) >> shift) & lanes, m_last = (__ballot(last) >> shift) & lanes, m_first = (__ballot(first) >> shift) & lanes;
@@ -353,34 +669,44 @@ __global__ __launch_bounds__(256) void chunk_sums_k(const TG *g, int64_t ldg, in
 
 // Table rows that go on across chunks: a wavefront per chunk looks whether one begins in it, and adds up its parts in order; one
 // of more than JOIN_LONG chunks is left to the whole block, whose groups of G lanes take consecutive shares of the parts.
-constexpr int JOIN_WAVES = 16, JOIN_LONG = 32;
+constexpr int JOIN_WAVES = 16, JOIN_LONG = 16;
 template <typename TD, int V, int G>
-__global__ __launch_bounds__(JOIN_WAVES * WAVE) void chunk_join_k(int32_t F, const uint32_t *__restrict__ key, int32_t n_cap,
-                                                                  const int32_t *__restrict__ n_dev, uint32_t rows, int32_t chunk,
-                                                                  const double *__restrict__ part, SumOut o)
+__global__ __launch_bounds__(JOIN_WAVES * WAVE) void chunk_join_k(int32_t F, Keys key, int32_t n_cap, const int32_t *__restrict__ n_dev, uint32_t rows,
+                                                                  int32_t chunk, const double *__restrict__ part, SumOut o)
 {
-    constexpr int GROUPS = JOIN_WAVES * WAVE / G, U = 8;
+    constexpr int GROUPS = JOIN_WAVES * WAVE / G;
     __shared__ int64_t long_parts[JOIN_WAVES];
     __shared__ double lds[GROUPS][G * V];
+    __shared__ uint32_t base[RANGES], scan[17];
     const int32_t n = resolve_count(n_cap, n_dev);
     const int lane = lane_id(), wave = (int)threadIdx.x / WAVE, sub = lane % G, group = (int)threadIdx.x / G;
     const Piece1<V> pc((int32_t)(blockIdx.y * G + sub), F);
     const int64_t c0 = (int64_t)blockIdx.x * JOIN_WAVES, c = c0 + wave;
+    if (c0 * chunk >= n) return;
     const int64_t beg = c * chunk, end = beg + chunk;
     int64_t parts = 0;     // chunks after c that the row is in
     uint32_t k = 0;
     if (end < n) {
+        // (all asked for at once; lane t: the first position of chunk c + 1 + t)
+        const int64_t mine = (c + 1 + lane) * chunk;
+        const uint32_t first = key[beg], before = key[beg > 0 ? beg - 1 : 0], here = key[mine < n ? mine : n - 1];
         k = key[end - 1];
-        const bool begins = key[beg] != k || beg == 0 || key[beg - 1] != k;
-        if (k < rows && begins && key[end] == k) {
+        const bool begins = first != k || beg == 0 || before != k;
+        if (k < rows && begins) {
+            uint64_t m = __ballot(mine < n && here == k);
             for (;;) {
-                const int64_t at = (c + 1 + parts + lane) * chunk;
-                const uint64_t m = __ballot(at < n && key[at < n ? at : n - 1] == k);
                 const int run = m == ~0ull ? WAVE : __ffsll((unsigned long long)~m) - 1;
                 parts += run;
                 if (run < WAVE) break;
+                const int64_t at = (c + 1 + parts + lane) * chunk;
+                m = __ballot(at < n && key[at < n ? at : n - 1] == k);
             }
         }
+    }
+    if (o.distinct) {
+        if (!__syncthreads_or(parts > 0 ? 1 : 0)) return;
+        uint32_t total;
+        range_bases(o, base, scan, &total);
     }
     auto add = [&](double (&acc)[V], const double *p) {
 #pragma unroll
@@ -393,7 +719,7 @@ __global__ __launch_bounds__(JOIN_WAVES * WAVE) void chunk_join_k(int32_t F, con
         add(acc, part + (2 * c + 1) * F);
 #pragma unroll 4
         for (int64_t t = 1; t <= parts; ++t) add(acc, part + 2 * (c + t) * F);
-        write_sum<TD, V>(o, o.rank ? o.rank[end - 1] : k, pc, acc);
+        write_sum<TD, V>(o, o.rank ? row_of_rank(o, o.rank[end - 1], base) : k, pc, acc);
     }
     if (lane == 0) long_parts[wave] = parts > JOIN_LONG ? parts : 0;
     __syncthreads();
@@ -405,17 +731,18 @@ __global__ __launch_bounds__(JOIN_WAVES * WAVE) void chunk_join_k(int32_t F, con
 #pragma unroll
         for (int i = 0; i < V; ++i) acc[i] = 0.0;
         if (group == 0) add(acc, part + (2 * cw + 1) * F);
-#pragma unroll U
+#pragma unroll 4
         for (int64_t t = t0; t < t1; ++t) add(acc, part + 2 * (cw + t) * F);
 #pragma unroll
         for (int i = 0; i < V; ++i) lds[group][sub * V + i] = acc[i];
         __syncthreads();
         if (group == 0) {
+#pragma unroll 1
             for (int q = 1; q < GROUPS; ++q)
 #pragma unroll
                 for (int i = 0; i < V; ++i) acc[i] += lds[q][sub * V + i];
             const int64_t at = (cw + 1) * chunk - 1;
-            write_sum<TD, V>(o, o.rank ? o.rank[at] : key[at], pc, acc);
+            write_sum<TD, V>(o, o.rank ? row_of_rank(o, o.rank[at], base) : key[at], pc, acc);
         }
         __syncthreads();
     }
@@ -433,7 +760,7 @@ struct SumIn {
     const void *g;
     int64_t ldg;
     int32_t F;
-    const uint32_t *key, *pos;
+    const uint64_t *entry;
     int32_t n;
     const int32_t *n_dev;
     uint32_t rows;
@@ -446,17 +773,13 @@ static void launch_sums(const SumIn &in, const SumOut &o, hipStream_t st)
     const int64_t chunks = ((int64_t)in.n + chunk - 1) / chunk;
     const unsigned slices = (unsigned)((in.F + G * V - 1) / (G * V));
     CSGS_LAUNCH(K_EMBED_SUM, (chunk_sums_k<TG, TD, V, G>), dim3((unsigned)((chunks * G + 255) / 256), slices), dim3(256), st, (const TG *)in.g, in.ldg, in.F,
-                in.key, in.pos, in.n, in.n_dev, in.rows, chunk, in.part, o);
-    CSGS_LAUNCH(K_EMBED_JOIN, (chunk_join_k<TD, V, G>), dim3((unsigned)((chunks + JOIN_WAVES - 1) / JOIN_WAVES), slices), dim3(JOIN_WAVES * WAVE), st, in.F, in.key,
+                in.entry, in.n, in.n_dev, in.rows, chunk, in.part, o);
+    CSGS_LAUNCH(K_EMBED_JOIN, (chunk_join_k<TD, V, G>), dim3((unsigned)((chunks + JOIN_WAVES - 1) / JOIN_WAVES), slices), dim3(JOIN_WAVES * WAVE), st, in.F, Keys{in.entry},
                 in.n, in.n_dev, in.rows, chunk, in.part, o);
 }
 template <typename TG, typename TD>
 static int embed_grad_sums(const SumIn &in, const SumOut &o, hipStream_t st)
 {
-    if (!o.rank && !o.accumulate) {
-        CSGS_LAUNCH(K_EMBED_ZERO, rows_zero_k<TD>, dim3(wave_blocks(in.rows)), dim3(256), st, (TD *)o.d, o.ldd, (int64_t)in.rows, in.F);
-        CSGS_LAUNCH_CHECK();
-    }
     constexpr int V = sizeof(TG) == 4 ? 4 : 8;
     if (in.F < V) launch_sums<TG, TD, 1, 16>(in, o, st);
     else if (in.F <= 16 * V) launch_sums<TG, TD, V, 16>(in, o, st);
@@ -475,27 +798,43 @@ static int embed_grad(const int32_t *ids, int64_t n, const int32_t *n_dev, const
     const EmbedScratch s = carve_embed(scratch, n, F);
     if (scratch_bytes < s.bytes) return CSGS_EWORKSPACE;
     hipStream_t st = (hipStream_t)stream;
-    const int64_t even = ((n + SORT_TILES - 1) / SORT_TILES + SORT_BLOCK - 1) / SORT_BLOCK * SORT_BLOCK;
-    const int32_t tile = (int32_t)(even < SORT_TILE_MIN ? SORT_TILE_MIN : even);
-    const int tiles = (int)((n + tile - 1) / tile);
-    int key_bits = 0;
-    while ((rows >> key_bits) != 0) ++key_bits;   // the key `rows` too
-    const int passes = (key_bits + 7) / 8, bits = (key_bits + passes - 1) / passes;
-    for (int p = 0; p < passes; ++p) {
-        const SortIn in{p == 0 ? ids : nullptr, p == 0 ? nullptr : s.key[(p + 1) & 1], p == 0 ? nullptr : s.pos[(p + 1) & 1], (uint32_t)rows};
-        CSGS_LAUNCH(K_EMBED_COUNT, sort_count_k, dim3((unsigned)tiles), dim3(SORT_BLOCK), st, in, (int32_t)n, n_dev, tile, p * bits, (1u << bits) - 1, s.hist);
-        CSGS_LAUNCH(K_EMBED_PLACE, sort_place_k, dim3((unsigned)tiles), dim3(SORT_BLOCK), st, in, (int32_t)n, n_dev, tile, tiles, p * bits, bits, s.hist, s.key[p & 1], s.pos[p & 1]);
+    const int64_t elt = d_dtype == CSGS_F32 ? 4 : 2;
+    const ZeroRows z{d, uniq || accumulate ? 0 : rows, F * elt, ldd * elt};
+    SumIn in{G, ldg, F, nullptr, (int32_t)n, n_dev, (uint32_t)rows, s.part};
+    SumOut o{uniq ? s.rank : nullptr, nullptr, uniq, n_uniq, d, ldd, scale, accumulate};
+    if (n <= RANGES_MAX) {
+        const dim3 grid(RANGES + (z.rows ? RANGES : 0)), block(WIDE);
+        if (n <= RANGE_CACHED_MAX)
+            CSGS_LAUNCH(K_EMBED_RANGES, sort_ranges_k<true>, grid, block, st, ids, (int32_t)n, n_dev, (uint32_t)rows, s.entry[0], s.entry[1], uniq ? s.rank : nullptr,
+                        s.heads, s.n_valid, z);
+        else
+            CSGS_LAUNCH(K_EMBED_RANGES, sort_ranges_k<false>, grid, block, st, ids, (int32_t)n, n_dev, (uint32_t)rows, s.entry[0], s.entry[1], uniq ? s.rank : nullptr,
+                        s.heads, s.n_valid, z);
         CSGS_LAUNCH_CHECK();
+        in.entry = s.entry[0];
+        in.n_dev = s.n_valid;
+        if (uniq) o.distinct = s.heads;
+    } else {
+        const int32_t tile = (int32_t)(((n + SORT_TILES - 1) / SORT_TILES + SORT_STEP - 1) / SORT_STEP * SORT_STEP);
+        const int tiles = (int)((n + tile - 1) / tile);
+        int key_bits = 0;
+        while ((rows >> key_bits) != 0) ++key_bits;   // the key `rows` too
+        const int passes = (key_bits + 7) / 8, bits = (key_bits + passes - 1) / passes;
+        if (z.rows) CSGS_LAUNCH(K_EMBED_ZERO, rows_zero_k, dim3(wave_blocks(z.rows)), dim3(256), st, z);
+        for (int p = 0; p < passes; ++p) {
+            const SortIn si{p == 0 ? ids : nullptr, p == 0 ? nullptr : s.entry[(p + 1) & 1], (uint32_t)rows};
+            CSGS_LAUNCH(K_EMBED_COUNT, sort_count_k, dim3((unsigned)tiles), dim3(SORT_BLOCK), st, si, (int32_t)n, n_dev, tile, p * bits, (1u << bits) - 1, s.hist);
+            CSGS_LAUNCH(K_EMBED_PLACE, sort_place_k, dim3((unsigned)tiles), dim3(SORT_BLOCK), st, si, (int32_t)n, n_dev, tile, tiles, p * bits, bits, s.hist, s.entry[p & 1]);
+            CSGS_LAUNCH_CHECK();
+        }
+        in.entry = s.entry[(passes - 1) & 1];
+        if (uniq) {
+            CSGS_LAUNCH(K_EMBED_HEADS, heads_count_k, dim3((unsigned)tiles), dim3(SORT_BLOCK), st, Keys{in.entry}, (int32_t)n, n_dev, tile, (uint32_t)rows, s.heads);
+            CSGS_LAUNCH(K_EMBED_HEADS, heads_place_k, dim3((unsigned)tiles), dim3(SORT_BLOCK), st, Keys{in.entry}, (int32_t)n, n_dev, tile, tiles, (uint32_t)rows, s.heads,
+                        s.rank, n_uniq);
+            CSGS_LAUNCH_CHECK();
+        }
     }
-    const int last = (passes - 1) & 1;
-    if (uniq) {
-        CSGS_LAUNCH(K_EMBED_HEADS, heads_count_k, dim3((unsigned)tiles), dim3(SORT_BLOCK), st, s.key[last], (int32_t)n, n_dev, tile, (uint32_t)rows, s.heads);
-        CSGS_LAUNCH(K_EMBED_HEADS, heads_place_k, dim3((unsigned)tiles), dim3(SORT_BLOCK), st, s.key[last], (int32_t)n, n_dev, tile, tiles, (uint32_t)rows, s.heads,
-                    s.rank, uniq, n_uniq);
-        CSGS_LAUNCH_CHECK();
-    }
-    const SumIn in{G, ldg, F, s.key[last], s.pos[last], (int32_t)n, n_dev, (uint32_t)rows, s.part};
-    const SumOut o{uniq ? s.rank : nullptr, d, ldd, scale, accumulate};
     if (g_dtype == CSGS_F32) return d_dtype == CSGS_F32 ? embed_grad_sums<float, float>(in, o, st) : embed_grad_sums<float, uint16_t>(in, o, st);
     return d_dtype == CSGS_F32 ? embed_grad_sums<uint16_t, float>(in, o, st) : embed_grad_sums<uint16_t, uint16_t>(in, o, st);
 }

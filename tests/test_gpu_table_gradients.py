@@ -134,6 +134,30 @@ def test_gradient_of_many_positions(env, n, rows, F, dist):
     check_grad(run_grad(csgs, dev, ids, G, rows, 1.0, torch.float32), ids, G, rows, 1.0)
 
 
+@pytest.mark.parametrize("n,rows", [(1 << 15, 1 << 24), (1 << 15, 1 << 17), (1 << 18, 1 << 24), (1 << 18, 1 << 17), (50_000, 1 << 20)])
+def test_ids_that_a_sample_misses(env, n, rows):
+    """Every (n / 1024)-th position holds an id from all over the table, all the others one of a narrow range between two of those."""
+    csgs, dev = env
+    rng = np.random.default_rng(n)
+    step = rows // 1024
+    ids = 5 * step + 1 + rng.integers(0, step - 1, n)
+    at = np.arange(1024) * n // 1024
+    ids[at] = np.arange(1024) * step
+    ids = torch.from_numpy(ids.astype(np.int32))
+    G = torch.randn(n, 2, generator=torch.Generator().manual_seed(7)).to(dev)
+    check_grad(run_grad(csgs, dev, ids, G, rows, 1.0, torch.float32), ids, G, rows, 1.0)
+
+
+@pytest.mark.parametrize("n", [2048, 2049, 32768, 32769, 262_144, 262_145])
+@pytest.mark.parametrize("dist", ["steep", "half", "one", "none", "ascending"])
+def test_gradient_around_the_forms_of_the_sort(env, n, dist):
+    csgs, dev = env
+    rows = 1000 if dist != "half" else 70_000
+    ids = make_ids(n, rows, dist, n)
+    G = torch.randn(n, 5, generator=torch.Generator().manual_seed(8)).to(dev)
+    check_grad(run_grad(csgs, dev, ids, G, rows, 1.0, torch.float32), ids, G, rows, 1.0)
+
+
 @pytest.mark.parametrize("n", [300, 9000, 70000])
 @pytest.mark.parametrize("share", [0.0, 0.004, 0.5, 2.0])
 def test_gradient_up_to_a_device_count(env, n, share):
