@@ -104,16 +104,23 @@ __global__ __launch_bounds__(SORT_BLOCK) void sort_count_k(SortIn in, int32_t n_
     hist[blockIdx.x * DIGITS + threadIdx.x] = count[threadIdx.x];
 }
 
-// The lanes of the wavefront whose digit is this lane's own (lanes that take part).
-__device__ inline uint64_t same_digit(uint32_t digit, bool active, int bits)
+// The lanes of the wavefront whose digit (of up to 8 bits) is this lane's own, among those that take part.
+struct Lanes {
+    uint32_t lo, hi;
+    __device__ uint32_t count() const { return (uint32_t)(__popc(lo) + __popc(hi)); }
+    __device__ uint32_t before() const { return (uint32_t)__builtin_amdgcn_mbcnt_hi(hi, __builtin_amdgcn_mbcnt_lo(lo, 0)); }   // lower lanes
+};
+__device__ inline Lanes same_digit(uint32_t digit, uint64_t active)
 {
-    uint64_t peers = __ballot(active);
-    for (int b = 0; b < bits; ++b) {
-        const bool bit = (digit >> b) & 1u;
-        const uint64_t with = __ballot(active && bit);
-        peers &= bit ? with : ~with;
+    Lanes p{(uint32_t)active, (uint32_t)(active >> 32)};
+#pragma unroll
+    for (int b = 0; b < 8; ++b) {
+        const uint32_t all = (uint32_t)((int32_t)(digit << (31 - b)) >> 31);   // the bit, 32 times
+        const uint64_t with = __ballot(all != 0);
+        p.lo &= ~((uint32_t)with ^ all);
+        p.hi &= ~((uint32_t)(with >> 32) ^ all);
     }
-    return peers;
+    return p;
 }
 
 __device__ inline uint32_t digit_of(uint64_t e, uint32_t least, int shift, int bits) { return ((key_of(e) - least) >> shift) & ((1u << bits) - 1u); }
@@ -121,20 +128,25 @@ __device__ inline int bits_of(uint32_t x) { return x ? 32 - __clz((int)x) : 0; }
 
 // A wavefront's entries of a step: rank[u] = entries before that one with its digit in the wavefront's share, `count` [DIGITS] (zeros before) = how
 // many there are of each.  Entries u * 64 + lane, of which those with `active` count.
+// (The counts are read and written through a pointer that says that it is one to LDS: through a generic one they would be flat accesses, and volatile
+// ones past all caches at that, 2 us a pass.)
+typedef volatile __attribute__((address_space(3))) uint32_t *LdsCounts;
 template <int ITEMS>
-__device__ inline void rank_digits(const uint64_t (&e)[ITEMS], const bool (&active)[ITEMS], int shift, int bits, volatile uint32_t *count, uint32_t (&rank)[ITEMS],
+__device__ inline void rank_digits(const uint64_t (&e)[ITEMS], const bool (&active)[ITEMS], int shift, int bits, LdsCounts count, uint32_t (&rank)[ITEMS],
                                    uint32_t least = 0)
 {
-    const uint64_t below = (1ull << lane_id()) - 1ull;
 #pragma unroll
     for (int u = 0; u < ITEMS; ++u) {
+        rank[u] = 0;
+        const uint64_t some = __ballot(active[u]);
+        if (some == 0) continue;
         const uint32_t digit = digit_of(e[u], least, shift, bits);
-        const uint64_t peers = same_digit(digit, active[u], bits);
-        const uint32_t before = (uint32_t)__popcll(peers & below);
+        const Lanes peers = same_digit(digit, some);
+        const uint32_t before = peers.before();
         uint32_t seen = 0;
         if (active[u]) seen = count[digit];
         __builtin_amdgcn_wave_barrier();
-        if (active[u] && before == 0) count[digit] = seen + (uint32_t)__popcll(peers);
+        if (active[u] && before == 0) count[digit] = seen + peers.count();
         __builtin_amdgcn_wave_barrier();
         rank[u] = seen + before;
     }
@@ -178,7 +190,7 @@ __global__ __launch_bounds__(SORT_BLOCK) void sort_place_k(SortIn in, int32_t n_
         for (int w = 0; w < SORT_WAVES; ++w) at[w][tid] = 0;
         __syncthreads();
         uint32_t rank[SORT_ITEMS];
-        rank_digits(e, active, shift, bits, at[wave], rank);
+        rank_digits(e, active, shift, bits, (LdsCounts)at[wave], rank);
         __syncthreads();
 #pragma unroll
         for (int w = 0; w < SORT_WAVES; ++w) {
@@ -197,35 +209,60 @@ __global__ __launch_bounds__(SORT_BLOCK) void sort_place_k(SortIn in, int32_t n_
 }
 
 // ---------------------------------------------------------------- a block's own sort
-constexpr int WIDE = 1024, WIDE_WAVES = WIDE / WAVE, WIDE_ITEMS = 8;
-constexpr int LDS_ENTRIES = WIDE * WIDE_ITEMS;   // most entries that a block sorts in LDS
-struct SortLds {
+constexpr int WIDE = 1024, WIDE_WAVES = WIDE / WAVE, WIDE_ITEMS = 7;
+constexpr int LDS_ENTRIES = WIDE * WIDE_ITEMS;   // most entries that a block sorts in LDS (two such blocks fit on a compute unit)
+struct __attribute__((aligned(16))) SortLds {
     uint32_t at[WIDE_WAVES][DIGITS];   // a wavefront's entries by digit, then the place of its first
     uint32_t scan[17];
 };
 
-// Places of a step of at most WIDE * ITEMS entries of which thread `digit` knows the place of its digit's next one: at[][] is left holding
-// each wavefront's first places.  Barriers: the caller's entries are loaded when it returns, and nothing is stored yet.
+// Ranks of a step of at most WIDE * ITEMS entries among those of their wavefront and digit, which at[][] is left counting, for
+// the first `waves` wavefronts (the others hold no entry).  The caller's entries are loaded when it returns, and nothing is stored yet.
 template <int ITEMS>
-__device__ inline void step_places(const uint64_t (&e)[ITEMS], const bool (&active)[ITEMS], uint32_t least, int shift, int bits, SortLds &l,
-                                   uint32_t (&rank)[ITEMS])
+__device__ inline void step_ranks(const uint64_t (&e)[ITEMS], const bool (&active)[ITEMS], uint32_t least, int shift, int bits, int waves, SortLds &l,
+                                  uint32_t (&rank)[ITEMS])
 {
-    const int tid = (int)threadIdx.x, wave = tid / WAVE;
+    const int tid = (int)threadIdx.x;
     __syncthreads();
-    for (int x = tid; x < WIDE_WAVES * DIGITS; x += WIDE) (&l.at[0][0])[x] = 0;
+    for (int x = tid; x < waves * DIGITS; x += WIDE) (&l.at[0][0])[x] = 0;
     __syncthreads();
-    rank_digits(e, active, shift, bits, l.at[wave], rank, least);
+    rank_digits(e, active, shift, bits, (LdsCounts)l.at[tid / WAVE], rank, least);
     __syncthreads();
 }
-__device__ inline uint32_t wave_prefixes(SortLds &l, uint32_t next)   // thread = digit
-{
+// Threads 0 .. 255, thread = digit: each wavefront's entries of it, then (places()) the place of each wavefront's first, from `next` on.
+struct DigitCounts {
+    uint32_t c[WIDE_WAVES], all;
+    __device__ DigitCounts(const SortLds &l, int waves)
+    {
+        all = 0;
 #pragma unroll
-    for (int w = 0; w < WIDE_WAVES; ++w) {
-        const uint32_t c = l.at[w][threadIdx.x];
-        l.at[w][threadIdx.x] = next;
-        next += c;
+        for (int w = 0; w < WIDE_WAVES; ++w) c[w] = w < waves ? l.at[w][threadIdx.x % DIGITS] : 0u;
+#pragma unroll
+        for (int w = 0; w < WIDE_WAVES; ++w) all += c[w];
     }
-    return next;
+    __device__ void places(SortLds &l, int waves, uint32_t next) const
+    {
+#pragma unroll
+        for (int w = 0; w < WIDE_WAVES; ++w) {
+            if (w < waves) l.at[w][threadIdx.x] = next;
+            next += c[w];
+        }
+    }
+};
+// Exclusive sum over threads 0 .. 255 (a thread per digit); all threads call it.
+__device__ inline uint32_t digits_scan(uint32_t v, uint32_t *lds /*[DIGITS / WAVE]*/)
+{
+    const int wave = (int)threadIdx.x / WAVE;
+    uint32_t incl = 0;
+    if (wave < DIGITS / WAVE) {
+        incl = wave_inclusive_scan(v);
+        if (lane_id() == WAVE - 1) lds[wave] = incl;
+    }
+    __syncthreads();
+    uint32_t before = 0;
+#pragma unroll
+    for (int w = 0; w < DIGITS / WAVE; ++w) before += w < wave ? lds[w] : 0u;
+    return before + incl - v;
 }
 
 // Sorts m <= WIDE * ITEMS entries in LDS by key, stable, where keys lie in [least, least + span].
@@ -233,7 +270,7 @@ template <int ITEMS>
 __device__ inline void sort_in_lds(uint64_t *e, int m, uint32_t least, uint32_t span, SortLds &l)
 {
     const int key_bits = bits_of(span), passes = (key_bits + 7) / 8, bits = passes ? (key_bits + passes - 1) / passes : 0;
-    const int tid = (int)threadIdx.x, wave = tid / WAVE, steps = (m + WIDE - 1) / WIDE;
+    const int tid = (int)threadIdx.x, wave = tid / WAVE, steps = (m + WIDE - 1) / WIDE, waves = (m + steps * WAVE - 1) / (steps * WAVE);
     for (int p = 0; p < passes; ++p) {
         uint64_t v[ITEMS];
         bool active[ITEMS];
@@ -244,18 +281,107 @@ __device__ inline void sort_in_lds(uint64_t *e, int m, uint32_t least, uint32_t 
             active[u] = u < steps && i < m;
             v[u] = active[u] ? e[i] : 0ull;
         }
-        step_places(v, active, least, p * bits, bits, l, rank);
-        uint32_t all = 0, total;
-        if (tid < DIGITS) all = wave_prefixes(l, 0);
-        const uint32_t first = block_exclusive_scan<uint32_t>(all, l.scan, &total);
-        if (tid < DIGITS)
-#pragma unroll
-            for (int w = 0; w < WIDE_WAVES; ++w) l.at[w][tid] += first;
+        step_ranks(v, active, least, p * bits, bits, waves, l, rank);
+        const DigitCounts dc(l, waves);   // (threads past the digits: not used)
+        const uint32_t first = digits_scan(dc.all, l.scan);
+        if (tid < DIGITS) dc.places(l, waves, first);
         __syncthreads();
 #pragma unroll
         for (int u = 0; u < ITEMS; ++u)
             if (active[u]) e[l.at[wave][digit_of(v[u], least, p * bits, bits)] + rank[u]] = v[u];
         __syncthreads();
+    }
+}
+
+// Sorts m <= COUNTED entries in LDS by key, stable, where keys lie less than COUNTED_SPAN above `least`, by the number of smaller ones: a power of
+// two of threads for the entries, as many sets of them as there are threads, each looking at its share.
+constexpr int COUNTED_BITS = 9, COUNTED = 1 << COUNTED_BITS;
+constexpr uint32_t COUNTED_SPAN = 1u << (32 - COUNTED_BITS);
+__device__ inline void sort_by_counting(uint64_t *e, int m, uint32_t least, SortLds &l)
+{
+    uint32_t *order = &l.at[0][0], *smaller = order + COUNTED;   // key and place of an entry in 32 bits; what is counted
+    const int tid = (int)threadIdx.x;
+    int width = WAVE;
+    while (width < m) width *= 2;
+    const int i = tid & (width - 1), sets = WIDE / width, share = ((m + sets - 1) / sets + 3) / 4 * 4;
+    const int j0 = tid / width * share, j1 = j0 + share < m ? j0 + share : m;
+    const uint64_t mine = i < m ? e[i] : 0ull;
+    if (tid < COUNTED) {
+        order[tid] = tid < m ? (key_of(e[tid]) - least) << COUNTED_BITS | (uint32_t)tid : 0xFFFFFFFFu;   // (none: no smaller than any)
+        smaller[tid] = 0;
+    }
+    __syncthreads();
+    const uint32_t own = order[i];
+    uint32_t c = 0;
+#pragma unroll 4
+    for (int j = j0; j < j1; j += 4) {
+        const uint4 q = *reinterpret_cast<const uint4 *>(order + j);
+        c += (q.x < own ? 1u : 0u) + (q.y < own ? 1u : 0u) + (q.z < own ? 1u : 0u) + (q.w < own ? 1u : 0u);
+    }
+    if (c && i < m) atomicAdd(&smaller[i], c);
+    __syncthreads();
+    if (tid < m) e[smaller[tid]] = mine;
+    __syncthreads();
+}
+
+// Order statistics of a sample, SAMPLES of whose keys a thread holds (has[i]: it does): found[t] = the one that target[t] others precede, by
+// digits from the top.  A level counts the samples that share what is known of a target by their next digit; targets of which the same is
+// known share the counts.  Keys of up to key_bits bits.
+constexpr int TARGETS = 3;
+struct SelectLds {
+    uint32_t count[TARGETS][DIGITS];
+    uint32_t key[TARGETS], left[TARGETS];
+};
+template <int SAMPLES>
+__device__ inline void select_samples(const uint32_t (&sample)[SAMPLES], const bool (&has)[SAMPLES], int key_bits, const int (&target)[TARGETS], SelectLds &l,
+                                      uint32_t (&found)[TARGETS])
+{
+    const int tid = (int)threadIdx.x, wave = tid / WAVE, lane = lane_id();
+    uint32_t left[TARGETS];
+#pragma unroll
+    for (int t = 0; t < TARGETS; ++t) {
+        found[t] = 0;
+        left[t] = (uint32_t)target[t];
+    }
+    for (int v = (key_bits + 7) / 8 - 1; v >= 0; --v) {
+        const uint64_t known = ~0ull << (8 * v + 8);
+        int counts[TARGETS];   // whose counts a target uses
+#pragma unroll
+        for (int t = 0; t < TARGETS; ++t) counts[t] = t > 0 && ((found[t] ^ found[t - 1]) & known) == 0 ? counts[t - 1] : t;
+        if (tid < DIGITS)
+#pragma unroll
+            for (int t = 0; t < TARGETS; ++t) l.count[t][tid] = 0;
+        __syncthreads();
+#pragma unroll
+        for (int t = 0; t < TARGETS; ++t)
+            if (counts[t] == t)
+#pragma unroll
+                for (int i = 0; i < SAMPLES; ++i)
+                    if (has[i] && ((sample[i] ^ found[t]) & known) == 0) atomicAdd(&l.count[t][(sample[i] >> (8 * v)) & (DIGITS - 1)], 1u);
+        __syncthreads();
+        if (wave < TARGETS) {   // a wavefront a target, four digits a lane
+            uint32_t want = left[0], key = found[0];
+            int from = counts[0];
+#pragma unroll
+            for (int t = 1; t < TARGETS; ++t)
+                if (wave == t) { want = left[t]; key = found[t]; from = counts[t]; }
+            const uint4 c = *reinterpret_cast<const uint4 *>(&l.count[from][4 * lane]);
+            const uint32_t sum = c.x + c.y + c.z + c.w, before = wave_inclusive_scan(sum) - sum;
+            if (before <= want && want < before + sum) {   // one lane
+                uint32_t r = want - before, d = 0;
+                if (r >= c.x) { r -= c.x; d = 1;
+                    if (r >= c.y) { r -= c.y; d = 2;
+                        if (r >= c.z) { r -= c.z; d = 3; } } }
+                l.key[wave] = key | (uint32_t)(4 * lane + (int)d) << (8 * v);
+                l.left[wave] = r;
+            }
+        }
+        __syncthreads();
+#pragma unroll
+        for (int t = 0; t < TARGETS; ++t) {
+            found[t] = l.key[t];
+            left[t] = l.left[t];
+        }
     }
 }
 
@@ -283,8 +409,12 @@ __device__ inline uint64_t *sort_in_memory(uint64_t *a, uint64_t *b, int64_t m, 
                 active[u] = i < m;
                 v[u] = active[u] ? a[i] : 0ull;
             }
-            step_places(v, active, least, p * bits, bits, l, rank);
-            if (tid < DIGITS) next = wave_prefixes(l, next);
+            step_ranks(v, active, least, p * bits, bits, WIDE_WAVES, l, rank);
+            if (tid < DIGITS) {
+                const DigitCounts dc(l, WIDE_WAVES);
+                dc.places(l, WIDE_WAVES, next);
+                next += dc.all;
+            }
             __syncthreads();
 #pragma unroll
             for (int u = 0; u < ITEMS; ++u)
@@ -329,16 +459,37 @@ __global__ __launch_bounds__(256) void rows_zero_k(ZeroRows z)
 // each: every block sorts the same sample of the ids and takes its bounds from there.  An id that fills bounds by itself has a
 // range of its own, which needs no sorting however many positions it holds; a list that outgrows LDS all the same (a sample that misses) is
 // sorted in memory.  Further blocks clear the gradient's rows meanwhile.
-constexpr int RANGES = 256, SAMPLE = WIDE, RANGE_CACHED = 32;
+constexpr int RANGES = 256, SAMPLE = 4 * WIDE, RANGE_CACHED = 32;
+constexpr uint32_t OWN_LIST = LDS_ENTRIES / WIDE_WAVES;   // entries of its range that a wavefront lists in LDS
 constexpr int64_t RANGE_CACHED_MAX = (int64_t)WIDE * RANGE_CACHED;
+// Block b's ids are [lo, lo + width): bounds are, of the sorted samples, the (r samples / RANGES)-th.  All threads call it.
+struct Range {
+    uint32_t lo, width;
+};
+template <int SAMPLES>
+__device__ inline Range range_of(int b, const uint32_t (&sample)[SAMPLES], const bool (&has)[SAMPLES], int samples, uint32_t rows, SelectLds &sel)
+{
+    auto target = [&](int r) { return (int)((int64_t)(r < 0 ? 0 : r < RANGES ? r : RANGES - 1) * samples / RANGES); };
+    const int targets[TARGETS] = {target(b - 1), target(b), target(b + 1)};
+    uint32_t bound[TARGETS];
+    select_samples(sample, has, bits_of(rows), targets, sel, bound);
+    uint32_t lo = b > 0 ? bound[1] : 0u, hi = b + 1 < RANGES ? bound[2] : rows;
+    const bool again = b > 0 && (b > 1 ? bound[0] : 0u) == lo;   // the id `lo` is another block's
+    if (lo == hi && !again) hi = lo + 1;                         // ... this one's, alone
+    else if (again) ++lo;
+    if (hi > rows) hi = rows;
+    if (lo > hi) lo = hi;
+    return Range{lo, hi - lo};
+}
 template <bool CACHED>   // at most RANGE_CACHED_MAX positions: the ids stay in registers between counting and listing
 __global__ __launch_bounds__(WIDE) void sort_ranges_k(const int32_t *__restrict__ ids, int32_t n_cap, const int32_t *__restrict__ n_dev, uint32_t rows,
                                                       uint64_t *out, uint64_t *other, uint32_t *__restrict__ rank, uint32_t *__restrict__ distinct,
                                                       int32_t *__restrict__ n_valid, ZeroRows z)
 {
-    constexpr int U = 8;
+    constexpr int U = 8;   // ids on their way per lane
     __shared__ uint64_t e[LDS_ENTRIES];
     __shared__ SortLds l;
+    __shared__ __attribute__((aligned(16))) SelectLds sel;
     __shared__ uint32_t w_below[WIDE_WAVES], w_own[WIDE_WAVES];
     const int tid = (int)threadIdx.x, lane = lane_id(), wave = tid / WAVE, b = (int)blockIdx.x;
     if (b >= RANGES) return zero_rows(z, (int64_t)(b - RANGES) * WIDE_WAVES + wave, (int64_t)(gridDim.x - RANGES) * WIDE_WAVES);
@@ -356,100 +507,118 @@ __global__ __launch_bounds__(WIDE) void sort_ranges_k(const int32_t *__restrict_
     };
     const int32_t share = (n + WIDE - 1) / WIDE * WAVE;   // positions of a wavefront
     const int32_t w_beg = wave * share, w_end = w_beg + share < n ? w_beg + share : n;
-    uint32_t held[CACHED ? RANGE_CACHED : 1];
-    if constexpr (CACHED) {
-#pragma unroll
-        for (int u = 0; u < RANGE_CACHED; ++u) {
-            const int32_t i = w_beg + u * WAVE + lane;
-            held[u] = u * WAVE < share && i < w_end ? (uint32_t)ids[i] : 0xFFFFFFFFu;
-        }
-    }
-    // bounds
     const int samples = n < SAMPLE ? n : SAMPLE;
-    if (tid < samples) e[tid] = (uint64_t)key_at((int64_t)tid * n / samples) << 32;
-    __syncthreads();
-    sort_in_lds<1>(e, samples, 0, rows, l);
-    auto bound = [&](int r) { return r <= 0 ? 0u : key_of(e[(int64_t)r * samples / RANGES]); };
-    uint32_t lo = bound(b), hi = b + 1 < RANGES ? bound(b + 1) : rows;   // [lo, hi)
-    const bool again = b > 0 && bound(b - 1) == lo;   // the id `lo` is another block's
-    if (lo == hi && !again) hi = lo + 1;              // ... this one's, alone
-    else if (again) ++lo;
-    if (hi > rows) hi = rows;
-    if (lo > hi) lo = hi;
-    __syncthreads();
-    const uint32_t width = hi - lo;
-    // ids below the range and in it
-    uint32_t n_below = 0, n_own = 0;
-    auto count = [&](uint32_t id) {
-        n_below += (uint32_t)__popcll(__ballot(id < lo));
-        n_own += (uint32_t)__popcll(__ballot(id - lo < width));
+    uint32_t sample[SAMPLE / WIDE];
+    bool has[SAMPLE / WIDE];
+#pragma unroll
+    for (int i = 0; i < SAMPLE / WIDE; ++i) {
+        const int k = i * WIDE + tid;
+        has[i] = k < samples;
+        sample[i] = key_at((int64_t)(has[i] ? k : 0) * n / samples);
+    }
+    // the ids from position i0 on, a wavefront's 64 at a time, and what lies past its share as none
+    auto ask = [&](int32_t i0, uint32_t (&id)[U]) {
+        if (i0 + U * WAVE <= w_end) {
+#pragma unroll
+            for (int u = 0; u < U; ++u) id[u] = (uint32_t)ids[i0 + lane + u * WAVE];
+            return;
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int32_t i = i0 + u * WAVE + lane;
+            id[u] = (uint32_t)ids[i < n ? i : n - 1];
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (i0 + u * WAVE + lane >= w_end) id[u] = 0xFFFFFFFFu;
     };
+    uint32_t held[CACHED ? RANGE_CACHED / U : 1][U];
     if constexpr (CACHED) {
 #pragma unroll
-        for (int u = 0; u < RANGE_CACHED; ++u)
-            if (u * WAVE < share) count(held[u]);
-    } else {
-        for (int32_t i0 = w_beg; i0 < w_end; i0 += U * WAVE) {
-            uint32_t id[U];
-#pragma unroll
-            for (int u = 0; u < U; ++u) {
-                const int32_t i = i0 + u * WAVE + lane;
-                id[u] = i < w_end ? (uint32_t)ids[i] : 0xFFFFFFFFu;
-            }
-#pragma unroll
-            for (int u = 0; u < U; ++u) count(id[u]);
-        }
+        for (int q = 0; q < RANGE_CACHED / U; ++q)
+            if (q * U * WAVE < share) ask(w_beg + q * U * WAVE, held[q]);
     }
+    // f(ids, first position), over the wavefront's share
+    auto each = [&](auto f) {
+        if constexpr (CACHED) {
+#pragma unroll
+            for (int q = 0; q < RANGE_CACHED / U; ++q)
+                if (q * U * WAVE < share) f(held[q], w_beg + q * U * WAVE);
+        } else {
+            for (int32_t i0 = w_beg; i0 < w_end; i0 += U * WAVE) {
+                uint32_t id[U];
+                ask(i0, id);
+                f(id, i0);
+            }
+        }
+    };
+    const Range range = range_of(b, sample, has, samples, rows, sel);
+    const uint32_t lo = range.lo;
+    const uint32_t width = range.width;
+    // ids below the range, and those in it: each wavefront lists its own in its part of LDS as far as that goes
+    const uint64_t lanes_below = (1ull << lane) - 1ull;
+    uint32_t n_below = 0, n_own = 0;
+    each([&](const uint32_t (&id)[U], int32_t i0) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            n_below += (uint32_t)__popcll(__ballot(id[u] < lo));
+            const bool is = id[u] - lo < width;
+            const uint64_t m = __ballot(is);
+            if (m == 0) continue;
+            const uint32_t dst = n_own + (uint32_t)__popcll(m & lanes_below);
+            if (is && dst < OWN_LIST) e[wave * OWN_LIST + dst] = (uint64_t)id[u] << 32 | (uint32_t)(i0 + u * WAVE + lane);
+            n_own += (uint32_t)__popcll(m);
+        }
+    });
     if (lane == 0) {
         w_below[wave] = n_below;
         w_own[wave] = n_own;
     }
     __syncthreads();
-    uint32_t below = 0, own = 0, at = 0;
+    uint32_t below = 0, own = 0, at = 0, most = 0;
     for (int w = 0; w < WIDE_WAVES; ++w) {
+        const uint32_t c = w_own[w];
         below += w_below[w];
         if (w == wave) at = own;
-        own += w_own[w];
+        own += c;
+        most = c > most ? c : most;
     }
     if (b == RANGES - 1 && tid == 0) *n_valid = (int32_t)(below + own);
     if (own == 0) {
         if (tid == 0) distinct[b] = 0;
         return;
     }
-    // the list
-    const bool alone = width == 1, in_lds = !alone && own <= LDS_ENTRIES;
-    const int passes = (bits_of(width - 1) + 7) / 8;
-    uint64_t *mine = alone || passes % 2 == 0 ? out : other;   // the sorted list has to end in `out`
-    auto list = [&](uint32_t id, int32_t i) {
-        const bool is = id - lo < width;
-        const uint64_t m = __ballot(is);
-        const uint32_t dst = at + (uint32_t)__popcll(m & ((1ull << lane) - 1ull));
-        const uint64_t entry = (uint64_t)id << 32 | (uint32_t)i;
-        if (is) {
-            if (in_lds) e[dst] = entry;
-            else if (below + dst < (uint32_t)n) mine[below + dst] = entry;
-        }
-        at += (uint32_t)__popcll(m);
-    };
-    if constexpr (CACHED) {
+    const bool alone = width == 1, in_lds = most <= OWN_LIST;
+    if (in_lds) {
+        // the wavefronts' lists after each other
+        uint64_t v[OWN_LIST / WAVE];
 #pragma unroll
-        for (int u = 0; u < RANGE_CACHED; ++u)
-            if (u * WAVE < share) list(held[u], w_beg + u * WAVE + lane);
+        for (int u = 0; u < OWN_LIST / WAVE; ++u)
+            if (u * WAVE + lane < (int)n_own) v[u] = e[wave * OWN_LIST + u * WAVE + lane];
+        __syncthreads();
+#pragma unroll
+        for (int u = 0; u < OWN_LIST / WAVE; ++u)
+            if (u * WAVE + lane < (int)n_own) e[at + u * WAVE + lane] = v[u];
+        __syncthreads();
+        if (alone) {
+        } else if (own <= COUNTED && width <= COUNTED_SPAN) sort_by_counting(e, (int)own, lo, l);
+        else sort_in_lds<WIDE_ITEMS>(e, (int)own, lo, width - 1, l);
     } else {
-        for (int32_t i0 = w_beg; i0 < w_end; i0 += U * WAVE) {
-            uint32_t id[U];
+        const int passes = (bits_of(width - 1) + 7) / 8;
+        uint64_t *mine = passes % 2 == 0 ? out : other;   // the sorted list has to end in `out`
+        each([&](const uint32_t (&id)[U], int32_t i0) {
 #pragma unroll
             for (int u = 0; u < U; ++u) {
-                const int32_t i = i0 + u * WAVE + lane;
-                id[u] = i < w_end ? (uint32_t)ids[i] : 0xFFFFFFFFu;
+                const bool is = id[u] - lo < width;
+                const uint64_t m = __ballot(is);
+                const uint32_t dst = below + at + (uint32_t)__popcll(m & lanes_below);
+                if (is && dst < (uint32_t)n) mine[dst] = (uint64_t)id[u] << 32 | (uint32_t)(i0 + u * WAVE + lane);
+                at += (uint32_t)__popcll(m);
             }
-#pragma unroll
-            for (int u = 0; u < U; ++u) list(id[u], i0 + u * WAVE + lane);
-        }
+        });
+        __syncthreads();
+        sort_in_memory(mine + below, (mine == out ? other : out) + below, own, lo, width - 1, l);   // (an id alone: no pass)
     }
-    __syncthreads();
-    if (in_lds) sort_in_lds<WIDE_ITEMS>(e, (int)own, lo, width - 1, l);
-    else if (!alone) sort_in_memory(mine + below, (mine == out ? other : out) + below, own, lo, width - 1, l);
     // entries out, with their id's rank in the list
     uint32_t base = 0;
     for (uint32_t i0 = 0; i0 < own; i0 += WIDE) {
@@ -717,7 +886,7 @@ __global__ __launch_bounds__(JOIN_WAVES * WAVE) void chunk_join_k(int32_t F, Key
 #pragma unroll
         for (int i = 0; i < V; ++i) acc[i] = 0.0;
         add(acc, part + (2 * c + 1) * F);
-#pragma unroll 4
+#pragma unroll 8
         for (int64_t t = 1; t <= parts; ++t) add(acc, part + 2 * (c + t) * F);
         write_sum<TD, V>(o, o.rank ? row_of_rank(o, o.rank[end - 1], base) : k, pc, acc);
     }
@@ -731,7 +900,7 @@ __global__ __launch_bounds__(JOIN_WAVES * WAVE) void chunk_join_k(int32_t F, Key
 #pragma unroll
         for (int i = 0; i < V; ++i) acc[i] = 0.0;
         if (group == 0) add(acc, part + (2 * cw + 1) * F);
-#pragma unroll 4
+#pragma unroll 8
         for (int64_t t = t0; t < t1; ++t) add(acc, part + 2 * (cw + t) * F);
 #pragma unroll
         for (int i = 0; i < V; ++i) lds[group][sub * V + i] = acc[i];
@@ -743,6 +912,188 @@ __global__ __launch_bounds__(JOIN_WAVES * WAVE) void chunk_join_k(int32_t F, Key
                 for (int i = 0; i < V; ++i) acc[i] += lds[q][sub * V + i];
             const int64_t at = (cw + 1) * chunk - 1;
             write_sum<TD, V>(o, o.rank ? row_of_rank(o, o.rank[at], base) : key[at], pc, acc);
+        }
+        __syncthreads();
+    }
+}
+
+// ---------------------------------------------------------------- few positions: everything in one launch
+// Ranges as above, but a block also adds up the rows of its range: all positions of an id are in one block, and so few in all that the
+// block which an often repeated id falls to is no slower for it.  Groups of G lanes take consecutive shares of the sorted list; a row within a share
+// is written at once, parts of one that goes on across shares are joined in LDS.  The rank of a range's first id is the number of different ids
+// below it, which every block counts with a hash table.  Rows without positions are cleared in even shares of the table.
+constexpr int FEW = 2 * WIDE;
+constexpr int FEW_TABLE = 2 * FEW, FEW_ROWS = 1 << 15;   // hash table; rows whose being met a block notes at a time
+template <typename TG, typename TD, int V, int G>
+__global__ __launch_bounds__(WIDE) void few_sums_k(const TG *g, int64_t ldg, int32_t F, const int32_t *__restrict__ ids, int32_t n_cap,
+                                                   const int32_t *__restrict__ n_dev, uint32_t rows, ZeroRows z, SumOut o)
+{
+    constexpr int PER = FEW / WIDE, GROUPS = WIDE / G;
+    __shared__ uint64_t e[FEW];
+    __shared__ SortLds l;
+    __shared__ __attribute__((aligned(16))) SelectLds sel;
+    __shared__ double slot[2][GROUPS][G * V];
+    __shared__ uint16_t local_rank[FEW];
+    __shared__ uint32_t w_own[WIDE_WAVES], n_met;
+    static_assert(sizeof(slot) >= FEW_TABLE * 4 && sizeof(slot) >= FEW_ROWS / 8, "what else is kept in its place");
+    const int tid = (int)threadIdx.x, lane = lane_id(), wave = tid / WAVE, b = (int)blockIdx.x;
+    const int32_t n = resolve_count(n_cap, n_dev);
+    const int32_t steps = (n + WIDE - 1) / WIDE;   // of 64 positions of a wavefront
+    uint32_t id[PER], sample[PER];
+    bool has[PER];
+#pragma unroll
+    for (int u = 0; u < PER; ++u) {
+        const int32_t i = (wave * steps + u) * WAVE + lane;
+        has[u] = u < steps && i < n;
+        id[u] = has[u] ? (uint32_t)ids[i] : 0xFFFFFFFFu;
+        sample[u] = id[u] < rows ? id[u] : rows;
+    }
+    if (z.rows) {
+        uint32_t *met = (uint32_t *)&slot[0][0][0];
+        const int64_t r_beg = z.rows * b / RANGES, r_end = z.rows * (b + 1) / RANGES;
+        for (int64_t r0 = r_beg; r0 < r_end; r0 += FEW_ROWS) {
+            const int32_t len = (int32_t)(r_end - r0 < FEW_ROWS ? r_end - r0 : FEW_ROWS);
+            for (int x = tid; x < FEW_ROWS / 32; x += WIDE) met[x] = 0;
+            __syncthreads();
+#pragma unroll
+            for (int u = 0; u < PER; ++u) {
+                const int64_t r = (int64_t)id[u] - r0;
+                if (id[u] < rows && r >= 0 && r < len) atomicOr(&met[r >> 5], 1u << (r & 31));
+            }
+            __syncthreads();
+            for (int32_t r = wave; r < len; r += WIDE_WAVES)
+                if (!((met[r >> 5] >> (r & 31)) & 1u)) zero_rows(ZeroRows{(char *)z.d + (r0 + r) * z.ld, 1, z.row, z.ld + 2}, 0, 1);
+            __syncthreads();
+        }
+    }
+    if (n == 0) {
+        if (o.rank && b == 0 && tid == 0) *o.n_uniq = 0;
+        return;
+    }
+    const Range range = range_of(b, sample, has, n, rows, sel);
+    const uint32_t lo = range.lo, width = range.width;
+    uint32_t n_own = 0;
+#pragma unroll
+    for (int u = 0; u < PER; ++u) n_own += (uint32_t)__popcll(__ballot(id[u] - lo < width));
+    if (lane == 0) w_own[wave] = n_own;
+    uint32_t base = 0;
+    if (o.rank) {
+        uint32_t *table = (uint32_t *)&slot[0][0][0];
+        for (int x = tid; x < FEW_TABLE; x += WIDE) table[x] = 0xFFFFFFFFu;
+        if (tid == 0) n_met = 0;
+        __syncthreads();
+        uint32_t added = 0;
+#pragma unroll
+        for (int u = 0; u < PER; ++u)
+            if (id[u] < lo) {
+                for (uint32_t h = id[u] * 0x9E3779B1u >> 20;; h = (h + 1) & (FEW_TABLE - 1)) {   // at least half of the table stays free
+                    const uint32_t old = atomicCAS(&table[h & (FEW_TABLE - 1)], 0xFFFFFFFFu, id[u]);
+                    if (old == id[u]) break;
+                    if (old == 0xFFFFFFFFu) { ++added; break; }
+                }
+            }
+        if (added) atomicAdd(&n_met, added);
+    }
+    __syncthreads();
+    if (o.rank) base = n_met;
+    uint32_t own = 0, at = 0;
+    for (int w = 0; w < WIDE_WAVES; ++w) {
+        if (w == wave) at = own;
+        own += w_own[w];
+    }
+#pragma unroll
+    for (int u = 0; u < PER; ++u) {
+        const bool is = id[u] - lo < width;
+        const uint64_t m = __ballot(is);
+        if (is) e[at + (uint32_t)__popcll(m & ((1ull << lane) - 1ull))] = (uint64_t)id[u] << 32 | (uint32_t)((wave * steps + u) * WAVE + lane);
+        at += (uint32_t)__popcll(m);
+    }
+    __syncthreads();
+    if (width > 1 && own > 1) {
+        if (own <= COUNTED && width <= COUNTED_SPAN) sort_by_counting(e, (int)own, lo, l);
+        else sort_in_lds<PER>(e, (int)own, lo, width - 1, l);
+    }
+    if (o.rank) {
+        uint32_t met = 0;
+        for (uint32_t i0 = 0; i0 < own; i0 += WIDE) {
+            const uint32_t i = i0 + (uint32_t)tid;
+            const bool head = i < own && (i == 0 || key_of(e[i]) != key_of(e[i - 1]));
+            uint32_t total;
+            const uint32_t before = met + block_exclusive_scan<uint32_t>(head ? 1u : 0u, l.scan, &total);
+            met += total;
+            if (head) o.uniq[base + before] = (int32_t)key_of(e[i]);
+            if (i < own) local_rank[i] = (uint16_t)(before + (head ? 1u : 0u) - 1u);
+        }
+        if (b == RANGES - 1 && tid == 0) *o.n_uniq = (int32_t)(base + met);
+    }
+    __syncthreads();
+    if (own == 0) return;
+    auto row_of = [&](int i) { return o.rank ? base + local_rank[i] : key_of(e[i]); };
+    const int share = ((int)own + GROUPS - 1) / GROUPS, groups = ((int)own + share - 1) / share, q = tid / G, sub = tid % G;
+    struct Share {
+        int beg, end;
+        bool open, goes_on, one;   // its first row began before it; its last one goes on after it; it holds one row
+    };
+    auto share_of = [&](int k) {
+        Share s;
+        s.beg = k * share;
+        s.end = s.beg + share < (int)own ? s.beg + share : (int)own;
+        const uint32_t first = key_of(e[s.beg]), last = key_of(e[s.end - 1]);
+        s.open = s.beg > 0 && key_of(e[s.beg > 0 ? s.beg - 1 : 0]) == first;
+        s.goes_on = s.end < (int)own && key_of(e[s.end < (int)own ? s.end : s.end - 1]) == last;
+        s.one = first == last;
+        return s;
+    };
+    for (int32_t slice = 0; slice * (G * V) < F; ++slice) {
+        const Piece1<V> pc(slice * G + sub, F);
+        if (q < groups) {
+            constexpr int U = 4;
+            const Share s = share_of(q);
+            double acc[V];
+#pragma unroll
+            for (int i = 0; i < V; ++i) acc[i] = 0.0;
+            bool open = s.open;
+            for (int i0 = s.beg; i0 < s.end; i0 += U) {
+                RawPiece<TG, V> r[U];
+#pragma unroll
+                for (int u = 0; u < U; ++u) r[u].load(g + (int64_t)(uint32_t)e[i0 + u < s.end ? i0 + u : s.end - 1] * ldg + pc.col);
+#pragma unroll
+                for (int u = 0; u < U; ++u) {
+                    const int i = i0 + u;
+                    if (i < s.end) {
+#pragma unroll
+                        for (int j = 0; j < V; ++j) acc[j] += (double)r[u].value(j);
+                        const bool last = i == s.end - 1;
+                        if (last || key_of(e[i + 1]) != key_of(e[i])) {
+                            if (open || (last && s.goes_on))
+#pragma unroll
+                                for (int j = 0; j < V; ++j) slot[open ? 0 : 1][q][sub * V + j] = acc[j];
+                            else write_sum<TD, V>(o, row_of(i), pc, acc);
+#pragma unroll
+                            for (int j = 0; j < V; ++j) acc[j] = 0.0;
+                            open = false;
+                        }
+                    }
+                }
+            }
+        }
+        __syncthreads();
+        if (q == 0 && groups > 1) {
+            double acc[V];
+#pragma unroll
+            for (int i = 0; i < V; ++i) acc[i] = 0.0;
+#pragma unroll 1
+            for (int k = 0; k < groups; ++k) {
+                const Share s = share_of(k);
+                if (s.open) {
+#pragma unroll
+                    for (int j = 0; j < V; ++j) acc[j] += slot[0][k][sub * V + j];
+                    if (!(s.one && s.goes_on)) write_sum<TD, V>(o, row_of(s.beg), pc, acc);
+                }
+                if (s.goes_on && !(s.open && s.one))
+#pragma unroll
+                    for (int j = 0; j < V; ++j) acc[j] = slot[1][k][sub * V + j];
+            }
         }
         __syncthreads();
     }
@@ -774,9 +1125,31 @@ static void launch_sums(const SumIn &in, const SumOut &o, hipStream_t st)
     const unsigned slices = (unsigned)((in.F + G * V - 1) / (G * V));
     CSGS_LAUNCH(K_EMBED_SUM, (chunk_sums_k<TG, TD, V, G>), dim3((unsigned)((chunks * G + 255) / 256), slices), dim3(256), st, (const TG *)in.g, in.ldg, in.F,
                 in.entry, in.n, in.n_dev, in.rows, chunk, in.part, o);
+}
+template <typename TD, int V, int G>
+static void launch_join(const SumIn &in, const SumOut &o, hipStream_t st)
+{
+    const int32_t chunk = chunk_of(in.n, in.F);
+    const int64_t chunks = ((int64_t)in.n + chunk - 1) / chunk;
+    const unsigned slices = (unsigned)((in.F + G * V - 1) / (G * V));
     CSGS_LAUNCH(K_EMBED_JOIN, (chunk_join_k<TD, V, G>), dim3((unsigned)((chunks + JOIN_WAVES - 1) / JOIN_WAVES), slices), dim3(JOIN_WAVES * WAVE), st, in.F, Keys{in.entry},
                 in.n, in.n_dev, in.rows, chunk, in.part, o);
 }
+template <typename TG, typename TD>
+static int embed_grad_few(const SumIn &in, const int32_t *ids, const ZeroRows &z, const SumOut &o, hipStream_t st)
+{
+    auto launch = [&](auto pieces, auto lanes) {
+        constexpr int V = decltype(pieces)::value, G = decltype(lanes)::value;
+        CSGS_LAUNCH(K_EMBED_FEW, (few_sums_k<TG, TD, V, G>), dim3(RANGES), dim3(WIDE), st, (const TG *)in.g, in.ldg, in.F, ids, in.n, in.n_dev, in.rows, z, o);
+    };
+    using std::integral_constant;
+    if (in.F < 4) launch(integral_constant<int, 1>{}, integral_constant<int, 16>{});
+    else if (in.F <= 64) launch(integral_constant<int, 4>{}, integral_constant<int, 16>{});
+    else launch(integral_constant<int, 4>{}, integral_constant<int, 64>{});
+    CSGS_LAUNCH_CHECK();
+    return CSGS_OK;
+}
+
 template <typename TG, typename TD>
 static int embed_grad_sums(const SumIn &in, const SumOut &o, hipStream_t st)
 {
@@ -785,6 +1158,11 @@ static int embed_grad_sums(const SumIn &in, const SumOut &o, hipStream_t st)
     else if (in.F <= 16 * V) launch_sums<TG, TD, V, 16>(in, o, st);
     else if (in.F <= 32 * V) launch_sums<TG, TD, V, 32>(in, o, st);
     else launch_sums<TG, TD, V, 64>(in, o, st);
+    // (parts are doubles: pieces of two are 16 bytes)
+    if (in.F < 2) launch_join<TD, 1, 16>(in, o, st);
+    else if (in.F <= 32) launch_join<TD, 2, 16>(in, o, st);
+    else if (in.F <= 64) launch_join<TD, 2, 32>(in, o, st);
+    else launch_join<TD, 2, 64>(in, o, st);
     CSGS_LAUNCH_CHECK();
     return CSGS_OK;
 }
@@ -802,6 +1180,10 @@ static int embed_grad(const int32_t *ids, int64_t n, const int32_t *n_dev, const
     const ZeroRows z{d, uniq || accumulate ? 0 : rows, F * elt, ldd * elt};
     SumIn in{G, ldg, F, nullptr, (int32_t)n, n_dev, (uint32_t)rows, s.part};
     SumOut o{uniq ? s.rank : nullptr, nullptr, uniq, n_uniq, d, ldd, scale, accumulate};
+    if (n <= FEW) {
+        if (g_dtype == CSGS_F32) return d_dtype == CSGS_F32 ? embed_grad_few<float, float>(in, ids, z, o, st) : embed_grad_few<float, uint16_t>(in, ids, z, o, st);
+        return d_dtype == CSGS_F32 ? embed_grad_few<uint16_t, float>(in, ids, z, o, st) : embed_grad_few<uint16_t, uint16_t>(in, ids, z, o, st);
+    }
     if (n <= RANGES_MAX) {
         const dim3 grid(RANGES + (z.rows ? RANGES : 0)), block(WIDE);
         if (n <= RANGE_CACHED_MAX)

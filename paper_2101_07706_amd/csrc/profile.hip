@@ -26,7 +26,7 @@ static const char *const kNames[K_COUNT] = {"row_prefix", "scan_edges", "cand_pa
                                             "layer_gemm", "gather_rows", "gemm_grad_z", "gemm_grad_w", "gemm_grad_w_reduce",
                                             "adjT_count", "adjT_prefix", "adjT_fill", "adjT_order", "aggregate_grad", "fill_zero", "copy", "atomics", "mfma_f64", "lookups", "layer_forward",
                                             "layer_gemm_digits", "gemm_grad_z_digits",
-                                            "embed", "embed_count", "embed_place", "embed_heads", "embed_zero", "embed_ranges", "embed_sum", "embed_join", "residual", "residual_grad",
+                                            "embed", "embed_count", "embed_place", "embed_heads", "embed_zero", "embed_few", "embed_ranges", "embed_sum", "embed_join", "residual", "residual_grad",
                                             "col_sums", "grad_list", "grad_norm", "grad_total", "grad_scale"};
 
 bool next_pair(int kid, hipEvent_t *start, hipEvent_t *stop)

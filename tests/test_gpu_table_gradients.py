@@ -135,14 +135,15 @@ def test_gradient_of_many_positions(env, n, rows, F, dist):
 
 
 @pytest.mark.parametrize("n,rows", [(1 << 15, 1 << 24), (1 << 15, 1 << 17), (1 << 18, 1 << 24), (1 << 18, 1 << 17), (50_000, 1 << 20)])
-def test_ids_that_a_sample_misses(env, n, rows):
-    """Every (n / 1024)-th position holds an id from all over the table, all the others one of a narrow range between two of those."""
+@pytest.mark.parametrize("sample", [1024, 4096])
+def test_ids_that_a_sample_misses(env, n, rows, sample):
+    """Every (n / sample)-th position holds an id from all over the table, all the others one of a narrow range between two of those."""
     csgs, dev = env
     rng = np.random.default_rng(n)
-    step = rows // 1024
+    step = rows // sample
     ids = 5 * step + 1 + rng.integers(0, step - 1, n)
-    at = np.arange(1024) * n // 1024
-    ids[at] = np.arange(1024) * step
+    at = np.arange(sample) * n // sample
+    ids[at] = np.arange(sample) * step
     ids = torch.from_numpy(ids.astype(np.int32))
     G = torch.randn(n, 2, generator=torch.Generator().manual_seed(7)).to(dev)
     check_grad(run_grad(csgs, dev, ids, G, rows, 1.0, torch.float32), ids, G, rows, 1.0)
