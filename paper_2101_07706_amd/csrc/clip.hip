@@ -63,36 +63,71 @@ __device__ inline int64_t live_entries(const GradDesc &d)
     return rows * d.cols;
 }
 
-__device__ inline float load_entry(const void *p, int32_t dtype, int64_t at)
+// A tile's entries [beg, end) by the block's threads: f(piece, output address, V) on pieces of V entries of a flat tensor, a quarter
+// of a tile's pieces on their way per thread, and entry by entry at its end and where rows lie apart.
+template <typename T, typename F>
+__device__ inline void each_piece(const GradDesc &d, int64_t beg, int64_t end, F f)
 {
-    return dtype == CSGS_F32 ? load_row<float, 1>((const float *)p + at).x[0] : load_row<uint16_t, 1>((const uint16_t *)p + at).x[0];
-}
-__device__ inline void store_entry(void *p, int32_t dtype, int64_t at, float v)
-{
-    if (dtype == CSGS_F32) store_row<float, 1>((float *)p + at, Vec<1>{{v}});
-    else store_row<uint16_t, 1>((uint16_t *)p + at, Vec<1>{{v}});
+    constexpr int V = 16 / (int)sizeof(T), U = (int)(GRAD_TILE / (256 * V));
+    static_assert(U * V * 256 == GRAD_TILE, "a tile");
+    const T *g = (const T *)d.g;
+    T *out = (T *)d.out;
+    if (d.flat) {
+        const int64_t whole = end - (end - beg) % V;
+        RawPiece<T, V> r[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int64_t e = beg + (u * 256 + (int)threadIdx.x) * V;
+            if (e < whole) r[u].load(g + e);
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int64_t e = beg + (u * 256 + (int)threadIdx.x) * V;
+            if (e < whole) {
+                Vec<V> v;
+#pragma unroll
+                for (int i = 0; i < V; ++i) v.x[i] = r[u].value(i);
+                f(v, out + e);
+            }
+        }
+        const int64_t e = whole + threadIdx.x;
+        if (e < end) f(load_row<T, 1>(g + e), out + e);
+        return;
+    }
+    // (a row and a column of the tile's first entry by one division, the others from there in 32 bits)
+    const int64_t r0 = beg / d.cols, c0 = beg - r0 * d.cols;
+    for (int32_t x = (int32_t)threadIdx.x; x < (int32_t)(end - beg); x += 256) {
+        const int64_t c = c0 + x;
+        const int64_t dr = c < d.cols ? 0 : d.cols > GRAD_TILE ? 1 : (int64_t)((uint32_t)c / (uint32_t)d.cols);
+        const int64_t r = r0 + dr, col = c - dr * d.cols;
+        f(load_row<T, 1>(g + r * d.ldg + col), out + r * d.ldo + col);
+    }
 }
 
 // The sum, or the larger one with NaN above everything.
-__device__ inline double add_or_max(double a, double b, int kind)
+template <int KIND>
+__device__ inline double add_or_max(double a, double b)
 {
-    if (kind != CSGS_GRAD_MAX) return a + b;
+    if (KIND != CSGS_GRAD_MAX) return a + b;
     return !(a >= b) && !(a != a) ? b : a;
 }
-__device__ inline double term(float x, int kind)
+template <int KIND>
+__device__ inline double take_in(double a, float x)
 {
     const double v = (double)x;
-    return kind == CSGS_GRAD_L2 ? v * v : fabs(v);
+    if (KIND == CSGS_GRAD_L2) return fma(v, v, a);   // (a float's square is exact in double)
+    return add_or_max<KIND>(a, fabs(v));
 }
 
 // Joined over the block's 256 threads by a fixed tree; the result in every thread.
-__device__ inline double block_join(double v, int kind, double *lds /*[256]*/)
+template <int KIND>
+__device__ inline double block_join(double v, double *lds /*[256]*/)
 {
     const int tid = (int)threadIdx.x;
     lds[tid] = v;
     __syncthreads();
     for (int s = 128; s > 0; s >>= 1) {
-        if (tid < s) lds[tid] = add_or_max(lds[tid], lds[tid + s], kind);
+        if (tid < s) lds[tid] = add_or_max<KIND>(lds[tid], lds[tid + s]);
         __syncthreads();
     }
     const double r = lds[0];
@@ -100,28 +135,43 @@ __device__ inline double block_join(double v, int kind, double *lds /*[256]*/)
     return r;
 }
 
-__global__ __launch_bounds__(256) void grad_norm_k(GradMem m, int64_t tiles, int kind)
+template <int KIND>
+__global__ __launch_bounds__(256) void grad_norm_k(GradMem m, int64_t tiles)
 {
     __shared__ double lds[256];
-    double sum = 0.0;
+    double sum[4] = {0.0, 0.0, 0.0, 0.0};
     for (int64_t t = blockIdx.x; t < tiles; t += gridDim.x) {
         const GradDesc d = m.desc[m.tile_tensor[t]];
         const int64_t beg = (t - d.first_tile) * GRAD_TILE, live = live_entries(d);
         const int64_t end = beg + GRAD_TILE < live ? beg + GRAD_TILE : live;
-        for (int64_t e = beg + threadIdx.x; e < end; e += 256) {
-            const int64_t at = d.flat ? e : e / d.cols * d.ldg + e % d.cols;
-            sum = add_or_max(sum, term(load_entry(d.g, d.dtype, at), kind), kind);
-        }
+        if (end <= beg) continue;
+        auto take = [&](const auto &v, auto *) {
+            constexpr int V = (int)(sizeof(v.x) / sizeof(float));
+#pragma unroll
+            for (int i = 0; i < V; ++i) sum[i % 4] = take_in<KIND>(sum[i % 4], v.x[i]);
+        };
+        if (d.dtype == CSGS_F32) each_piece<float>(d, beg, end, take);
+        else each_piece<uint16_t>(d, beg, end, take);
     }
-    sum = block_join(sum, kind, lds);
-    if (threadIdx.x == 0) m.partial[blockIdx.x] = sum;
+    const double own = add_or_max<KIND>(add_or_max<KIND>(sum[0], sum[1]), add_or_max<KIND>(sum[2], sum[3]));
+    const double all = block_join<KIND>(own, lds);
+    if (threadIdx.x == 0) m.partial[blockIdx.x] = all;
 }
 
+template <int KIND>
+__device__ inline double join_partials(const double *__restrict__ partial, int blocks, double *lds)
+{
+    double p[GRAD_BLOCKS / 256], s = 0.0;
+#pragma unroll
+    for (int k = 0; k < GRAD_BLOCKS / 256; ++k) p[k] = k * 256 + (int)threadIdx.x < blocks ? partial[k * 256 + (int)threadIdx.x] : 0.0;
+#pragma unroll
+    for (int k = 0; k < GRAD_BLOCKS / 256; ++k) s = add_or_max<KIND>(s, p[k]);
+    return block_join<KIND>(s, lds);
+}
+// (kind: the same for all threads)
 __device__ inline double join_partials(const double *__restrict__ partial, int blocks, int kind, double *lds)
 {
-    double s = 0.0;
-    for (int b = (int)threadIdx.x; b < blocks; b += 256) s = add_or_max(s, partial[b], kind);
-    return block_join(s, kind, lds);
+    return kind == CSGS_GRAD_MAX ? join_partials<CSGS_GRAD_MAX>(partial, blocks, lds) : join_partials<CSGS_GRAD_L2>(partial, blocks, lds);
 }
 
 __global__ __launch_bounds__(256) void grad_total_k(GradMem m, int blocks, int kind, double *__restrict__ total)
@@ -131,6 +181,8 @@ __global__ __launch_bounds__(256) void grad_total_k(GradMem m, int blocks, int k
     if (threadIdx.x == 0) *total = s;
 }
 
+// PAST: outputs too long for the caches go past them, so that what the next pass over the gradients reads is not pushed out.
+template <bool PAST>
 __global__ __launch_bounds__(256) void grad_scale_k(GradMem m, int64_t tiles, int blocks, int kind, const double *total, float max_norm, float *norm_out,
                                                     int32_t *status)
 {
@@ -143,15 +195,21 @@ __global__ __launch_bounds__(256) void grad_scale_k(GradMem m, int64_t tiles, in
         if (norm_out) *norm_out = (float)norm;
         if (status && !(norm <= 1.7976931348623157e308)) atomicOr(status, CSGS_ST_NONFINITE_GRAD);
     }
-    for (int64_t t = blockIdx.x; t < tiles; t += gridDim.x) {
+    // (from the last tile back: those are still in the cache from the pass before)
+    for (int64_t t = tiles - 1 - blockIdx.x; t >= 0; t -= gridDim.x) {
         const GradDesc d = m.desc[m.tile_tensor[t]];
         if (!d.out || (coef == 1.0 && d.out == d.g)) continue;
         const int64_t beg = (t - d.first_tile) * GRAD_TILE, live = live_entries(d);
         const int64_t end = beg + GRAD_TILE < live ? beg + GRAD_TILE : live;
-        for (int64_t e = beg + threadIdx.x; e < end; e += 256) {
-            const int64_t r = d.flat ? 0 : e / d.cols, f = d.flat ? e : e % d.cols;
-            store_entry(d.out, d.dtype, r * d.ldo + f, (float)(coef * (double)load_entry(d.g, d.dtype, r * d.ldg + f)));
-        }
+        if (end <= beg) continue;
+        auto give = [&](auto v, auto *out) {
+#pragma unroll
+            for (float &x : v.x) x = (float)(coef * (double)x);
+            if constexpr (PAST) store_row_past_caches(out, v);
+            else store_row(out, v);
+        };
+        if (d.dtype == CSGS_F32) each_piece<float>(d, beg, end, give);
+        else each_piece<uint16_t>(d, beg, end, give);
     }
 }
 
@@ -180,18 +238,26 @@ static bool list_ok(const csgs_grad_list *l, int kind)
     return l && l->base && l->ready && l->n > 0 && l->tiles > 0 && kind >= CSGS_GRAD_L2 && kind <= CSGS_GRAD_MAX;
 }
 
+// Entries from which outputs go past the caches: 256 MB of floats, the memory-side cache (us, through / past: 245 M floats 534 / 517).
+constexpr int64_t PAST_TILES = (1ll << 26) / GRAD_TILE;
 static int launch_scale(const csgs_grad_list *l, int kind, const double *total, float max_norm, float *norm, int32_t *status, hipStream_t st)
 {
     const GradMem m = carve_grads(l->base, l->n, l->tiles);
     const int blocks = grad_blocks(l->tiles);
-    CSGS_LAUNCH(K_GRAD_SCALE, grad_scale_k, dim3((unsigned)blocks), dim3(256), st, m, l->tiles, blocks, kind, total, max_norm, norm, status);
+    if (l->tiles >= PAST_TILES)
+        CSGS_LAUNCH(K_GRAD_SCALE, grad_scale_k<true>, dim3((unsigned)blocks), dim3(256), st, m, l->tiles, blocks, kind, total, max_norm, norm, status);
+    else
+        CSGS_LAUNCH(K_GRAD_SCALE, grad_scale_k<false>, dim3((unsigned)blocks), dim3(256), st, m, l->tiles, blocks, kind, total, max_norm, norm, status);
     CSGS_LAUNCH_CHECK();
     return CSGS_OK;
 }
 static int launch_norm(const csgs_grad_list *l, int kind, hipStream_t st)
 {
     const GradMem m = carve_grads(l->base, l->n, l->tiles);
-    CSGS_LAUNCH(K_GRAD_NORM, grad_norm_k, dim3((unsigned)grad_blocks(l->tiles)), dim3(256), st, m, l->tiles, kind);
+    const dim3 grid((unsigned)grad_blocks(l->tiles)), block(256);
+    if (kind == CSGS_GRAD_L2) CSGS_LAUNCH(K_GRAD_NORM, grad_norm_k<CSGS_GRAD_L2>, grid, block, st, m, l->tiles);
+    else if (kind == CSGS_GRAD_L1) CSGS_LAUNCH(K_GRAD_NORM, grad_norm_k<CSGS_GRAD_L1>, grid, block, st, m, l->tiles);
+    else CSGS_LAUNCH(K_GRAD_NORM, grad_norm_k<CSGS_GRAD_MAX>, grid, block, st, m, l->tiles);
     CSGS_LAUNCH_CHECK();
     return CSGS_OK;
 }

@@ -9,20 +9,35 @@
 namespace csgs {
 
 // ---------------------------------------------------------------- lookup
-template <typename TI, typename TO>
-__global__ __launch_bounds__(256) void embed_k(const TI *T, int64_t ld, int64_t rows, int32_t F, const int32_t *__restrict__ ids,
-                                               int32_t n_cap, const int32_t *__restrict__ n_dev, float scale, TO *out, int64_t ldo)
+// G lanes take a row in pieces of V columns, and several rows at a time: the rows are as far apart as the ids say, so what counts is how many
+// are asked for before the first is needed.  The last piece of a width that V does not divide ends with the row and overlaps the one before.
+template <typename TI, typename TO, int V, int G>
+__global__ __launch_bounds__(256) void embed_k(const TI *T, int64_t ld, int64_t rows, int32_t F, const int32_t *__restrict__ ids, int32_t n_cap,
+                                               const int32_t *__restrict__ n_dev, float scale, TO *out, int64_t ldo)
 {
+    constexpr int R = 4;
     const int32_t n = resolve_count(n_cap, n_dev);
-    const int lane = lane_id();
-    const int64_t waves = (int64_t)gridDim.x * (blockDim.x / WAVE);
-    for (int64_t t = ((int64_t)blockIdx.x * blockDim.x + threadIdx.x) / WAVE; t < n; t += waves) {
-        const int64_t id = ids[t];
-        const bool ok = id >= 0 && id < rows;
-        for (int32_t f = lane; f < F; f += WAVE) {
-            Vec<1> v{{0.0f}};
-            if (ok) v.x[0] = scale * load_row<TI, 1>(T + id * ld + f).x[0];
-            store_row<TO, 1>(out + t * ldo + f, v);
+    const int32_t begin = (int32_t)(blockIdx.y * G + threadIdx.x % G) * V, col = begin > F - V ? F - V : begin;
+    const int64_t groups = (int64_t)gridDim.x * (256 / G);
+    for (int64_t t0 = (int64_t)blockIdx.x * (256 / G) + threadIdx.x / G; t0 < n; t0 += groups * R) {
+        int32_t id[R];
+#pragma unroll
+        for (int k = 0; k < R; ++k) id[k] = ids[t0 + k * groups < n ? t0 + k * groups : t0];
+        if (begin >= F) continue;
+        RawPiece<TI, V> r[R];
+        bool ok[R];
+#pragma unroll
+        for (int k = 0; k < R; ++k) {
+            ok[k] = id[k] >= 0 && id[k] < rows;
+            r[k].load(T + (ok[k] ? id[k] : 0) * ld + col);
+        }
+#pragma unroll
+        for (int k = 0; k < R; ++k) {
+            const int64_t t = t0 + k * groups;
+            Vec<V> v;
+#pragma unroll
+            for (int i = 0; i < V; ++i) v.x[i] = ok[k] ? scale * r[k].value(i) : 0.0f;
+            if (t < n) store_row<TO, V>(out + t * ldo + col, v);
         }
     }
 }
@@ -1225,7 +1240,19 @@ template <typename TI, typename TO>
 static void launch_embed(const void *T, int64_t ld, int64_t rows, int32_t F, const int32_t *ids, int32_t n, const int32_t *n_dev, float scale, void *out,
                          int64_t ldo, hipStream_t st)
 {
-    CSGS_LAUNCH(K_EMBED, (embed_k<TI, TO>), dim3(wave_blocks(n)), dim3(256), st, (const TI *)T, ld, rows, F, ids, n, n_dev, scale, (TO *)out, ldo);
+    auto launch = [&](auto pieces, auto lanes) {
+        constexpr int V = decltype(pieces)::value, G = decltype(lanes)::value;
+        const int64_t blocks = ((int64_t)n + 256 / G - 1) / (256 / G);
+        const dim3 grid((unsigned)(blocks < 2048 ? blocks : 2048), (unsigned)(((int64_t)F + G * V - 1) / (G * V)));
+        CSGS_LAUNCH(K_EMBED, (embed_k<TI, TO, V, G>), grid, dim3(256), st, (const TI *)T, ld, rows, F, ids, n, n_dev, scale, (TO *)out, ldo);
+    };
+    using std::integral_constant;
+    constexpr int V = sizeof(TI) == 2 && sizeof(TO) == 2 ? 8 : 4;
+    if (F < V) launch(integral_constant<int, 1>{}, integral_constant<int, 8>{});
+    else if (F <= 8 * V) launch(integral_constant<int, V>{}, integral_constant<int, 8>{});
+    else if (F <= 16 * V) launch(integral_constant<int, V>{}, integral_constant<int, 16>{});
+    else if (F <= 32 * V) launch(integral_constant<int, V>{}, integral_constant<int, 32>{});
+    else launch(integral_constant<int, V>{}, integral_constant<int, 64>{});
 }
 
 }  // namespace csgs

@@ -137,21 +137,18 @@ __device__ inline void store_row(T *p, const Vec<V> &v)
         if constexpr (V == 8) store_global<u32x4, 2>(p, u32x4{two(0), two(2), two(4), two(6)});
     }
 }
-// The first n (1 .. V) values of a piece; the others are zero / are not written.
+// 16 bytes past the caches, for what is too long to be found there again.
+typedef u32x4 __attribute__((aligned(2))) u32x4_anywhere;
+__device__ inline void store_past_caches(void *p, u32x4 v) { __builtin_nontemporal_store(v, (CSGS_GLOBAL u32x4_anywhere *)(uintptr_t)p); }
 template <typename T, int V>
-__device__ inline Vec<V> load_part(const T *p, int n)
+__device__ inline void store_row_past_caches(T *p, const Vec<V> &v)
 {
-    Vec<V> v;
-#pragma unroll
-    for (int i = 0; i < V; ++i) v.x[i] = i < n ? load_row<T, 1>(p + i).x[0] : 0.0f;
-    return v;
+    if constexpr (sizeof(T) * V != 16) store_row<T, V>(p, v);
+    else if constexpr (sizeof(T) == 4)
+        store_past_caches(p, u32x4{__float_as_uint(v.x[0]), __float_as_uint(v.x[1]), __float_as_uint(v.x[2]), __float_as_uint(v.x[3])});
+    else {
+        auto two = [&](int i) { return bf16_bits(v.x[i]) | bf16_bits(v.x[i + 1]) << 16; };
+        store_past_caches(p, u32x4{two(0), two(2), two(4), two(6)});
+    }
 }
-template <typename T, int V>
-__device__ inline void store_part(T *p, const Vec<V> &v, int n)
-{
-#pragma unroll
-    for (int i = 0; i < V; ++i)
-        if (i < n) store_row<T, 1>(p + i, Vec<1>{{v.x[i]}});
-}
-
 }  // namespace csgs
