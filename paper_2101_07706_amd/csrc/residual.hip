@@ -294,8 +294,12 @@ __global__ __launch_bounds__(RES_BLOCK) void residual_rows_k(ResidualArgs a, TS 
 
 // Sums over rows: every block leaves one row of sums per vector, which a second kernel adds up.
 enum { COL_POST_W = 0, COL_POST_B, COL_PRE_W, COL_PRE_B, COL_GATE, COL_KINDS };
-constexpr int COL_BLOCKS = 512;   // most blocks
+constexpr int COL_BLOCKS = 1024;   // most blocks
 __host__ inline int col_blocks(int32_t M) { return M < COL_BLOCKS ? M : COL_BLOCKS; }
+// Blocks of the gradient with rows in registers: about as many as the device holds at a time, by the registers that N pieces take (us, 256 / 512 /
+// 1024 / 1536 blocks: 8192 rows of 256, a piece a lane, 21.7 / 19.0 / 19.2 / 22.2; 1999 rows of 602, three pieces, 16.9 / 17.6 / 17.8 / 17.8).
+template <int G, int N>
+constexpr int grad_blocks() { return G > WAVE && N == 1 ? 1024 : (N >= 3 ? 256 : 512); }
 
 struct ResidualGrad {
     const void *dy, *du;
@@ -566,7 +570,7 @@ static bool with_layout(int32_t width, F f)
     if (pieces <= 64) return go(integral_constant<int, 64>{}, integral_constant<int, 1>{});
     if (pieces <= 128) return go(integral_constant<int, 64>{}, integral_constant<int, 2>{});
     if (pieces <= 192) return go(integral_constant<int, 64>{}, integral_constant<int, 3>{});
-    if (pieces <= 256) return go(integral_constant<int, 64>{}, integral_constant<int, 4>{});
+    if (pieces <= 256) return go(integral_constant<int, 256>{}, integral_constant<int, 1>{});
     if (pieces <= 512) return go(integral_constant<int, 256>{}, integral_constant<int, 2>{});
     if (pieces <= 1024) return go(integral_constant<int, 256>{}, integral_constant<int, 4>{});
     return false;
@@ -594,7 +598,9 @@ static int launch_residual_grad(const ResidualArgs &a, const ResidualGrad &g, hi
         constexpr int G = decltype(lanes)::value, N = decltype(pieces)::value, ROWS = RES_BLOCK / G;
         constexpr bool R = decltype(ragged)::value;
         const int64_t need = ((int64_t)a.M + ROWS - 1) / ROWS;
-        blocks = (int)(need < COL_BLOCKS ? need : COL_BLOCKS);
+        constexpr int MOST = grad_blocks<G, N>();
+        static_assert(MOST <= COL_BLOCKS, "room for the sums");
+        blocks = (int)(need < MOST ? need : MOST);
         const dim3 grid((unsigned)blocks), block(RES_BLOCK);
         const bool bias = g.want[COL_POST_B] || g.want[COL_PRE_B], row = g.want[COL_GATE];
         if (bias && row) CSGS_LAUNCH(K_RESIDUAL_GRAD, (residual_grad_rows_k<TS, TB, 4, G, N, R, true, true>), grid, block, st, a, g);
