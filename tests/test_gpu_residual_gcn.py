@@ -1,0 +1,126 @@
+"""The training step that runs lookups, gated residuals, their gradients and clipping together, against 64-bit automatic
+differentiation through the same sampled layers."""
+import math
+
+import numpy as np
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+
+from paper_2101_07706_amd import synth
+
+RTOL, ATOL = 1e-4, 1e-5      # of an entry, and of the largest one
+
+
+@pytest.fixture(scope="module")
+def env():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    from paper_2101_07706_amd import csgs, pipeline, residual_gcn
+    csgs.lib()
+    return csgs, pipeline, residual_gcn
+
+
+def close(got, want, what):
+    got, want = got.double().cpu(), want.detach()
+    tol = RTOL * want.abs() + ATOL * want.abs().max() + 1e-30
+    worst = ((got - want).abs() / tol).max().item()
+    assert worst <= 1.0, f"{what}: error {worst:.2f} times its tolerance"
+
+
+def reference(net, G):
+    """Gradients in float64 of sum(G . logits), and the logits, through the adjacency the step sampled."""
+    c = lambda t: t.detach().double().cpu()
+    p = {k: c(v).requires_grad_(True) for k, v in net.params.items()}
+    counts = [net.batch] + [int(lb.n_next) for lb in net.lbs]
+    ids = [net.ids[net.at[l]:net.at[l] + counts[l]].long().cpu() for l in range(net.L + 1)]
+    table = c(net.table).requires_grad_(True)
+    x = [net.scale * table[i] for i in ids]
+
+    def layer_norm(v, w, b):
+        m = v.mean(1, keepdim=True)
+        return (v - m) / torch.sqrt(((v - m) ** 2).mean(1, keepdim=True) + 1e-5) * w + b
+
+    u = layer_norm(x[-1], p["bottom.pre_w"], p["bottom.pre_b"])
+    for l in range(net.L - 1, -1, -1):
+        lb = net.lbs[l]
+        ptr, col, val = lb.adj_rowptr.cpu().long(), lb.adj_col.cpu().long(), c(lb.adj_val)
+        P = torch.zeros(counts[l], counts[l + 1], dtype=torch.float64)
+        for r in range(counts[l]):
+            P[r, col[ptr[r]:ptr[r + 1]]] = val[ptr[r]:ptr[r + 1]]
+        h = (P @ torch.relu(u)) @ p[f"{l}.w"]
+        n = h / torch.sqrt((h * h).mean(1, keepdim=True) + 1e-5) * p[f"{l}.post_w"] + p[f"{l}.post_b"]
+        u = layer_norm(net.beta * x[l] + torch.sigmoid(p[f"{l}.gate"]) * n, p[f"{l}.pre_w"], p[f"{l}.pre_b"])
+    logits = u @ p["w_out"]
+    (logits * c(G)).sum().backward()
+    return logits, {k: v.grad for k, v in p.items()}, table.grad
+
+
+def make(residual_gcn, pipeline, width, L=2, seed=3, **kw):
+    g = synth.make_sbm(1500, 4, 0.02, 0.002, 5)
+    dg = pipeline.DeviceGraph(g)
+    net = residual_gcn.ResidualGCN(dg, width, 5, L, 100, 128, 4.0, g.nnz, seed=seed, **kw)
+    for k, v in net.params.items():       # nothing at its neutral value
+        v.add_(torch.randn(v.shape, generator=torch.Generator().manual_seed(len(k))).to(v.device), alpha=0.1)
+    S0 = torch.from_numpy(synth.make_batch(g, 100, 1)).to(dg.device)
+    return g, net, S0
+
+
+@pytest.mark.parametrize("width,L", [(64, 2), (30, 1), (100, 3)])
+def test_gradients(env, width, L):
+    csgs, pipeline, residual_gcn = env
+    g, net, S0 = make(residual_gcn, pipeline, width, L)
+    for it in range(2):                   # the second step finds the first one's leftovers in every buffer
+        logits = net.forward(S0, it).clone()
+        G = torch.randn(logits.shape, generator=torch.Generator().manual_seed(it)).to(logits.device) / 100
+        net.backward(G)
+        torch.cuda.synchronize()
+        assert all(int(lb.status) == 0 for lb in net.lbs)
+        want, grads, table = reference(net, G)
+        close(logits, want, "logits")
+        for k, v in net.grads.items():
+            close(v, grads[k], k)
+        n = int(net.table_count)
+        ids = net.table_ids[:n].long().cpu()
+        met = torch.unique(torch.cat([net.ids[net.at[l]:net.at[l + 1]].cpu() for l in range(L + 1)]))
+        assert torch.equal(ids, met[met >= 0].long())
+        close(net.table_rows[:n], table[ids], "table")
+        rest = torch.ones(g.n_nodes, dtype=torch.bool)
+        rest[ids] = False
+        assert bool((table[rest] == 0).all())
+        # clipping: the norm over all of them, and every one of them shortened by the same factor
+        total = math.sqrt(sum(float((v.double() ** 2).sum()) for v in net.grads.values()) + float((net.table_rows[:n].double() ** 2).sum()))
+        before = {k: v.clone() for k, v in net.grads.items()}
+        rows = net.table_rows[:n].clone()
+        net.max_norm = 0.3 * total
+        net.clip()
+        assert abs(float(net.norm) - total) <= 1e-6 * total and int(net.status) == 0
+        for k, v in net.grads.items():
+            assert bool(((v - 0.3 * before[k]).abs() <= 1e-5 * before[k].abs()).all()), k
+        assert bool(((net.table_rows[:n] - 0.3 * rows).abs() <= 1e-5 * rows.abs()).all())
+
+
+def test_steps_learn(env):
+    csgs, pipeline, residual_gcn = env
+    g, net, S0 = make(residual_gcn, pipeline, 32, lr=0.2)
+    labels = torch.from_numpy((np.arange(100) % 5).astype(np.int64)).to(S0.device)
+    losses = [float(net.step(S0, labels, it)) for it in range(40)]
+    assert all(math.isfinite(x) for x in losses) and int(net.status) == 0
+    assert sum(losses[-5:]) < 0.5 * sum(losses[:5]), losses
+
+
+def test_steps_repeat(env):
+    """Two networks of one seed take the same steps, bit for bit, as far as the library goes (the gradients before descent)."""
+    csgs, pipeline, residual_gcn = env
+    a, b = (make(residual_gcn, pipeline, 48)[1:] for _ in range(2))
+    G = torch.randn(100, 5, device=a[1].device)
+    for net, S0 in (a, b):
+        net.forward(S0, 7)
+        net.backward(G)
+        net.clip()
+    torch.cuda.synchronize()
+    for k in a[0].grads:
+        assert torch.equal(a[0].grads[k], b[0].grads[k]), k
+    assert torch.equal(a[0].table_rows, b[0].table_rows) and torch.equal(a[0].table_ids, b[0].table_ids) and torch.equal(a[0].norm, b[0].norm)
