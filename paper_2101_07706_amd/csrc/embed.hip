@@ -506,7 +506,7 @@ __global__ __launch_bounds__(WIDE) void sort_ranges_k(const int32_t *__restrict_
     __shared__ SortLds l;
     __shared__ __attribute__((aligned(16))) SelectLds sel;
     __shared__ uint32_t w_below[WIDE_WAVES], w_own[WIDE_WAVES];
-    const int tid = (int)threadIdx.x, lane = lane_id(), wave = tid / WAVE, b = (int)blockIdx.x;
+    const int tid = (int)threadIdx.x, lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(tid / WAVE), b = (int)blockIdx.x;
     if (b >= RANGES) return zero_rows(z, (int64_t)(b - RANGES) * WIDE_WAVES + wave, (int64_t)(gridDim.x - RANGES) * WIDE_WAVES);
     const int32_t n = resolve_count(n_cap, n_dev);
     if (n == 0) {
@@ -535,7 +535,7 @@ __global__ __launch_bounds__(WIDE) void sort_ranges_k(const int32_t *__restrict_
     auto ask = [&](int32_t i0, uint32_t (&id)[U]) {
         if (i0 + U * WAVE <= w_end) {
 #pragma unroll
-            for (int u = 0; u < U; ++u) id[u] = (uint32_t)ids[i0 + lane + u * WAVE];
+            for (int u = 0; u < U; ++u) id[u] = (uint32_t)(ids + i0)[(uint32_t)(lane + u * WAVE)];
             return;
         }
 #pragma unroll
@@ -572,11 +572,11 @@ __global__ __launch_bounds__(WIDE) void sort_ranges_k(const int32_t *__restrict_
     const uint32_t width = range.width;
     // ids below the range, and those in it: each wavefront lists its own in its part of LDS as far as that goes
     const uint64_t lanes_below = (1ull << lane) - 1ull;
-    uint32_t n_below = 0, n_own = 0;
+    uint32_t n_below = 0, n_own = 0;   // (n_below: the lane's)
     each([&](const uint32_t (&id)[U], int32_t i0) {
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            n_below += (uint32_t)__popcll(__ballot(id[u] < lo));
+            n_below += id[u] < lo ? 1u : 0u;
             const bool is = id[u] - lo < width;
             const uint64_t m = __ballot(is);
             if (m == 0) continue;
@@ -585,6 +585,7 @@ __global__ __launch_bounds__(WIDE) void sort_ranges_k(const int32_t *__restrict_
             n_own += (uint32_t)__popcll(m);
         }
     });
+    n_below = wave_sum(n_below);
     if (lane == 0) {
         w_below[wave] = n_below;
         w_own[wave] = n_own;
@@ -949,7 +950,7 @@ __global__ __launch_bounds__(WIDE) void few_sums_k(const TG *g, int64_t ldg, int
     __shared__ __attribute__((aligned(16))) SelectLds sel;
     __shared__ double slot[2][GROUPS][G * V];
     __shared__ uint16_t local_rank[FEW];
-    __shared__ uint32_t w_own[WIDE_WAVES], n_met;
+    __shared__ uint32_t w_own[WIDE_WAVES], n_met, kinds[GROUPS], first_row[GROUPS];
     static_assert(sizeof(slot) >= FEW_TABLE * 4 && sizeof(slot) >= FEW_ROWS / 8, "what else is kept in its place");
     const int tid = (int)threadIdx.x, lane = lane_id(), wave = tid / WAVE, b = (int)blockIdx.x;
     const int32_t n = resolve_count(n_cap, n_dev);
@@ -976,6 +977,22 @@ __global__ __launch_bounds__(WIDE) void few_sums_k(const TG *g, int64_t ldg, int
                 if (id[u] < rows && r >= 0 && r < len) atomicOr(&met[r >> 5], 1u << (r & 31));
             }
             __syncthreads();
+            if (z.row == z.ld && z.row < 1024) {
+                // narrow rows side by side: 16 bytes a lane across rows, two bytes at a time where one of those rows was met
+                const uint32_t row = (uint32_t)z.row, bytes = (uint32_t)len * row;
+                char *p = (char *)z.d + r0 * z.ld;
+                for (uint32_t at = (uint32_t)tid * 16; at < bytes; at += WIDE * 16) {
+                    const uint32_t first = at / row, to = at + 16 <= bytes ? at + 16 : bytes, last = (to - 1) / row;
+                    bool any = to != at + 16;
+                    for (uint32_t r = first; r <= last; ++r) any |= (met[r >> 5] >> (r & 31)) & 1u;
+                    if (!any) store_global<u32x4, 2>(p + at, u32x4{0, 0, 0, 0});
+                    else
+                        for (uint32_t x = at; x < to; x += 2) {
+                            const uint32_t r = x / row;
+                            if (!((met[r >> 5] >> (r & 31)) & 1u)) store_global<uint16_t>(p + x, (uint16_t)0);
+                        }
+                }
+            } else
             for (int32_t r = wave; r < len; r += WIDE_WAVES)
                 if (!((met[r >> 5] >> (r & 31)) & 1u)) zero_rows(ZeroRows{(char *)z.d + (r0 + r) * z.ld, 1, z.row, z.ld + 2}, 0, 1);
             __syncthreads();
@@ -1044,7 +1061,8 @@ __global__ __launch_bounds__(WIDE) void few_sums_k(const TG *g, int64_t ldg, int
     __syncthreads();
     if (own == 0) return;
     auto row_of = [&](int i) { return o.rank ? base + local_rank[i] : key_of(e[i]); };
-    const int share = ((int)own + GROUPS - 1) / GROUPS, groups = ((int)own + share - 1) / share, q = tid / G, sub = tid % G;
+    constexpr int U = 4;   // rows on their way, and fewest of a share
+    const int even = ((int)own + GROUPS - 1) / GROUPS, share = even < U ? U : even, groups = ((int)own + share - 1) / share, q = tid / G, sub = tid % G;
     struct Share {
         int beg, end;
         bool open, goes_on, one;   // its first row began before it; its last one goes on after it; it holds one row
@@ -1062,8 +1080,11 @@ __global__ __launch_bounds__(WIDE) void few_sums_k(const TG *g, int64_t ldg, int
     for (int32_t slice = 0; slice * (G * V) < F; ++slice) {
         const Piece1<V> pc(slice * G + sub, F);
         if (q < groups) {
-            constexpr int U = 4;
             const Share s = share_of(q);
+            if (slice == 0 && sub == 0) {
+                kinds[q] = (s.open ? 1u : 0u) | (s.goes_on ? 2u : 0u) | (s.one ? 4u : 0u);
+                first_row[q] = row_of(s.beg);
+            }
             double acc[V];
 #pragma unroll
             for (int i = 0; i < V; ++i) acc[i] = 0.0;
@@ -1099,13 +1120,14 @@ __global__ __launch_bounds__(WIDE) void few_sums_k(const TG *g, int64_t ldg, int
             for (int i = 0; i < V; ++i) acc[i] = 0.0;
 #pragma unroll 1
             for (int k = 0; k < groups; ++k) {
-                const Share s = share_of(k);
-                if (s.open) {
+                const uint32_t kind = kinds[k];
+                const bool open = kind & 1u, goes_on = kind & 2u, one = kind & 4u;
+                if (open) {
 #pragma unroll
                     for (int j = 0; j < V; ++j) acc[j] += slot[0][k][sub * V + j];
-                    if (!(s.one && s.goes_on)) write_sum<TD, V>(o, row_of(s.beg), pc, acc);
+                    if (!(one && goes_on)) write_sum<TD, V>(o, first_row[k], pc, acc);
                 }
-                if (s.goes_on && !(s.open && s.one))
+                if (goes_on && !(open && one))
 #pragma unroll
                     for (int j = 0; j < V; ++j) acc[j] = slot[1][k][sub * V + j];
             }

@@ -299,7 +299,7 @@ __host__ inline int col_blocks(int32_t M) { return M < COL_BLOCKS ? M : COL_BLOC
 // Blocks of the gradient with rows in registers: about as many as the device holds at a time, by the registers that N pieces take (us, 256 / 512 /
 // 1024 / 1536 blocks: 8192 rows of 256, a piece a lane, 21.7 / 19.0 / 19.2 / 22.2; 1999 rows of 602, three pieces, 16.9 / 17.6 / 17.8 / 17.8).
 template <int G, int N>
-constexpr int grad_blocks() { return G > WAVE && N == 1 ? 1024 : (N >= 3 ? 256 : 512); }
+constexpr int grad_blocks() { return (G > WAVE && N == 1) || G < 32 ? 1024 : (N >= 3 ? 256 : 512); }
 
 struct ResidualGrad {
     const void *dy, *du;

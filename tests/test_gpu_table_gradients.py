@@ -270,3 +270,16 @@ def test_on_another_stream_and_replayed(env):
         torch.cuda.synchronize()
         for a, b in zip(got, [out, dT, n_uniq, dR[:int(n_uniq)]]):
             assert torch.equal(a, b), f"replay {k}"
+
+
+@pytest.mark.parametrize("rows,F,d_dtype", [(100_001, 1, "f32"), (100_001, 3, "bf16"), (300_000, 10, "f32"), (70_000, 255, "f32"), (70_000, 300, "bf16"), (33, 5, "f32")])
+def test_few_positions_of_a_long_table(env, rows, F, d_dtype):
+    """Rows that no position points to are cleared around those that are written, however narrow they are."""
+    csgs, dev = env
+    for n, dist in ((1, "one"), (500, "uniform"), (2000, "steep")):
+        ids = make_ids(n, rows, dist, n + rows)
+        if n > 1:
+            ids[0], ids[1] = 0, rows - 1
+        G = torch.randn(n, F, generator=torch.Generator().manual_seed(9)).to(dev)
+        for extra in (0, 3):
+            check_grad(run_grad(csgs, dev, ids, G, rows, 1.0, DTYPES[d_dtype], extra=extra), ids, G, rows, 1.0)
