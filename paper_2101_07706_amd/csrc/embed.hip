@@ -51,15 +51,19 @@ static_assert(DIGITS == SORT_BLOCK, "a thread per digit");
 constexpr int SORT_ITEMS = 8;                              // entries that a thread places at a time
 constexpr int32_t SORT_STEP = SORT_BLOCK * SORT_ITEMS;     // a tile is a number of these
 
-// Sorted positions are summed in chunks of a fixed number, whatever ids they hold (see chunk_sums_k): as many as leave a
-// million values of the sums at a time (1024 wavefronts of 16 bytes a lane), 8 to 64, no more than the lanes that take a row.
-__host__ inline int32_t chunk_of(int64_t n, int32_t F)
+// Sorted positions are summed in chunks of a fixed number, whatever ids they hold (see chunk_sums_k): a block takes a chunk, groups of G lanes
+// take equal shares of it.  A share is as many positions as leave a million values of the sums at a time (1024 wavefronts of 16 bytes a lane), 8
+// to 64, no more than the lanes that take a row.
+constexpr int SUM_BLOCK = 256;
+__host__ inline int32_t share_of(int64_t n, int32_t F)
 {
     const int32_t most = F <= 128 ? 16 : (F <= 256 ? 32 : 64);
     int32_t c = 8;
     while (c < most && n / (2 * c) * F >= 1 << 20) c *= 2;
     return c;
 }
+// Lanes that take a row in pieces of V columns.
+__host__ inline int sum_lanes(int32_t F, int V) { return F <= 16 * V ? 16 : (F <= 32 * V ? 32 : 64); }
 
 struct EmbedScratch {
     uint64_t *entry[2];          // [n] entries, used in turn
@@ -84,7 +88,7 @@ __host__ inline EmbedScratch carve_embed(void *base, int64_t n, int32_t F)
     s.heads = (uint32_t *)take(sizeof(uint32_t) * SORT_TILES);
     s.n_valid = (int32_t *)take(4);
     s.rank = (uint32_t *)take((size_t)n * 4);
-    const int32_t chunk = chunk_of(n, F);
+    const int32_t chunk = share_of(n, F) * (SUM_BLOCK / sum_lanes(F, 4));   // (the smallest of all types)
     s.part = (double *)take(sizeof(double) * 2 * (size_t)((n + chunk - 1) / chunk) * (size_t)F);
     s.bytes = off;
     return s;
@@ -750,7 +754,6 @@ __device__ inline void write_sum(const SumOut &o, uint32_t row, const Piece1<V> 
             }
     }
 }
-// Partial sums of chunk c: slot 1 of a row that begins in it and goes on, slot 0 of one that began before it.
 template <int V>
 __device__ inline void write_part(double *part, const Piece1<V> &pc, const double (&acc)[V])
 {
@@ -777,16 +780,19 @@ __device__ inline uint32_t from_lane(uint32_t v, int from)
     return (uint32_t)__shfl((int)v, from, G);
 }
 
-// G lanes take a chunk of sorted positions: the rows of G that they point to are added up in order, eight on their way at a time; a
-// table row all of whose positions lie in the chunk is written at once, parts of others go to `part`.  The work per chunk does not
-// depend on how often an id occurs.
+// G lanes take a share of a chunk of sorted positions: the rows of G that they point to are added up in order, eight on their way at a time; a
+// table row all of whose positions lie in the share is written at once.  Parts of rows that go on across shares are joined in LDS, in order, and written
+// there as far as they lie in the chunk; parts of others go to `part`, slot 1 of a row that begins in the chunk and goes on, slot 0 of one that
+// began before it.  The work per chunk does not depend on how often an id occurs.
 template <typename TG, typename TD, int V, int G>
 __global__ __launch_bounds__(256) void chunk_sums_k(const TG *g, int64_t ldg, int32_t F, const uint64_t *__restrict__ entry,
-                                                    int32_t n_cap, const int32_t *__restrict__ n_dev, uint32_t rows, int32_t chunk,
+                                                    int32_t n_cap, const int32_t *__restrict__ n_dev, uint32_t rows, int32_t share,
                                                     double *__restrict__ part, SumOut o)
 {
-    constexpr int U = 8;
-    __shared__ uint32_t base[RANGES], scan[17];
+    constexpr int U = 8, GROUPS = SUM_BLOCK / G;
+    constexpr uint32_t OPEN = 1, GOES_ON = 2, ONE = 4;   // a share's first row began before it; its last one goes on after it; it holds one row
+    __shared__ uint32_t base[RANGES], scan[17], kinds[GROUPS], first_row[GROUPS];
+    __shared__ double slot[2][GROUPS][G * V];
     const int32_t n = resolve_count(n_cap, n_dev);
     if (o.distinct) {
         uint32_t total;
@@ -794,9 +800,9 @@ __global__ __launch_bounds__(256) void chunk_sums_k(const TG *g, int64_t ldg, in
         if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) *o.n_uniq = (int32_t)total;
     }
     const int lane = (int)threadIdx.x % G;
-    const int64_t c = ((int64_t)blockIdx.x * 256 + threadIdx.x) / G;
-    const int64_t beg = c * chunk;
-    const int64_t end = beg + chunk < n ? beg + chunk : n;
+    const int q = (int)threadIdx.x / G;
+    const int64_t beg = ((int64_t)blockIdx.x * GROUPS + q) * share;
+    const int64_t end = beg + share < n ? beg + share : n;
     const int len = end > beg ? (int)(end - beg) : 0;
     const uint32_t NONE = 0xFFFFFFFFu;
     uint32_t k = NONE, p = 0, rk = 0;
@@ -823,8 +829,8 @@ __global__ __launch_bounds__(256) void chunk_sums_k(const TG *g, int64_t ldg, in
     double acc[V];
 #pragma unroll
     for (int i = 0; i < V; ++i) acc[i] = 0.0;
-    bool inside = true;    // the row's sum began in this chunk
-    for (int i0 = 0; i0 < chunk; i0 += U) {
+    bool inside = true;    // the row's sum began in this share
+    for (int i0 = 0; i0 < share; i0 += U) {
         if (__ballot(i0 < count) == 0) break;
         RawPiece<TG, V> r[U];
 #pragma unroll
@@ -843,12 +849,43 @@ __global__ __launch_bounds__(256) void chunk_sums_k(const TG *g, int64_t ldg, in
                 const bool ends = (m_last >> i) & 1ull;
                 if (ends || i == count - 1) {
                     if (ends && inside) write_sum<TD, V>(o, from_lane<G>(row, i), pc, acc);
-                    else write_part<V>(part + (2 * c + (inside ? 1 : 0)) * F, pc, acc);
+                    else
+#pragma unroll
+                        for (int j = 0; j < V; ++j) slot[inside ? 1 : 0][q][lane * V + j] = acc[j];
 #pragma unroll
                     for (int j = 0; j < V; ++j) acc[j] = 0.0;
                 }
             }
         }
+    }
+    if (lane == 0) {
+        const uint64_t own = m_first & ((2ull << (count > 0 ? count - 1 : 0)) - 1ull);   // where rows begin
+        kinds[q] = count == 0 ? 0u : ((own & 1ull) ? 0u : OPEN) | ((m_last >> (count - 1)) & 1ull ? 0u : GOES_ON) | ((own & ~1ull) ? 0u : ONE);
+        first_row[q] = row;
+    }
+    __syncthreads();
+    // a row that goes on is followed by the group in whose share it begins, one that began before the chunk by the first group
+    const uint32_t kind = kinds[q];
+    auto follow = [&](int k, bool ends) {   // from share k on; returns the share it ends in, GROUPS if it goes on
+        while (!ends && ++k < GROUPS) {
+#pragma unroll
+            for (int j = 0; j < V; ++j) acc[j] += slot[0][k][lane * V + j];
+            ends = (kinds[k] & (GOES_ON | ONE)) != (GOES_ON | ONE);
+        }
+        return k;
+    };
+    if (q == 0 && (kind & OPEN)) {
+#pragma unroll
+        for (int j = 0; j < V; ++j) acc[j] = slot[0][0][lane * V + j];
+        (void)follow(0, (kind & (GOES_ON | ONE)) != (GOES_ON | ONE));
+        write_part<V>(part + 2 * (int64_t)blockIdx.x * F, pc, acc);
+    }
+    if ((kind & GOES_ON) && (kind & (OPEN | ONE)) != (OPEN | ONE)) {
+#pragma unroll
+        for (int j = 0; j < V; ++j) acc[j] = slot[1][q][lane * V + j];
+        const int k = follow(q, false);
+        if (k < GROUPS) write_sum<TD, V>(o, first_row[k], pc, acc);
+        else write_part<V>(part + (2 * (int64_t)blockIdx.x + 1) * F, pc, acc);
     }
 }
 
@@ -878,14 +915,18 @@ __global__ __launch_bounds__(JOIN_WAVES * WAVE) void chunk_join_k(int32_t F, Key
         k = key[end - 1];
         const bool begins = first != k || beg == 0 || before != k;
         if (k < rows && begins) {
-            uint64_t m = __ballot(mine < n && here == k);
-            for (;;) {
-                const int run = m == ~0ull ? WAVE : __ffsll((unsigned long long)~m) - 1;
-                parts += run;
-                if (run < WAVE) break;
-                const int64_t at = (c + 1 + parts + lane) * chunk;
-                m = __ballot(at < n && key[at < n ? at : n - 1] == k);
+            const uint64_t m = __ballot(mine < n && here == k);
+            parts = m == ~0ull ? WAVE : __ffsll((unsigned long long)~m) - 1;
+            // a long one: its end by sixty-fourths of what is left
+            int64_t lo = c + 1 + parts, hi = ((int64_t)n + chunk - 1) / chunk;   // it is in the chunks before lo, and not in hi
+            while (parts >= WAVE && lo < hi) {
+                const int64_t step = (hi - lo + WAVE - 1) / WAVE, at = lo + (lane + 1) * step - 1;
+                const uint64_t in = __ballot(at < hi && key[at * chunk] == k);   // ascending: the lower lanes
+                const int full = in == ~0ull ? WAVE : __ffsll((unsigned long long)~in) - 1;
+                lo += full * step;
+                hi = lo + step - 1 < hi ? lo + step - 1 : hi;
             }
+            if (parts >= WAVE) parts = lo - (c + 1);
         }
     }
     if (o.distinct) {
@@ -1157,16 +1198,14 @@ struct SumIn {
 template <typename TG, typename TD, int V, int G>
 static void launch_sums(const SumIn &in, const SumOut &o, hipStream_t st)
 {
-    const int32_t chunk = chunk_of(in.n, in.F);
-    const int64_t chunks = ((int64_t)in.n + chunk - 1) / chunk;
+    const int32_t share = share_of(in.n, in.F), chunk = share * (SUM_BLOCK / G);
     const unsigned slices = (unsigned)((in.F + G * V - 1) / (G * V));
-    CSGS_LAUNCH(K_EMBED_SUM, (chunk_sums_k<TG, TD, V, G>), dim3((unsigned)((chunks * G + 255) / 256), slices), dim3(256), st, (const TG *)in.g, in.ldg, in.F,
-                in.entry, in.n, in.n_dev, in.rows, chunk, in.part, o);
+    CSGS_LAUNCH(K_EMBED_SUM, (chunk_sums_k<TG, TD, V, G>), dim3((unsigned)(((int64_t)in.n + chunk - 1) / chunk), slices), dim3(SUM_BLOCK), st, (const TG *)in.g, in.ldg,
+                in.F, in.entry, in.n, in.n_dev, in.rows, share, in.part, o);
 }
 template <typename TD, int V, int G>
-static void launch_join(const SumIn &in, const SumOut &o, hipStream_t st)
+static void launch_join(const SumIn &in, const SumOut &o, int32_t chunk, hipStream_t st)
 {
-    const int32_t chunk = chunk_of(in.n, in.F);
     const int64_t chunks = ((int64_t)in.n + chunk - 1) / chunk;
     const unsigned slices = (unsigned)((in.F + G * V - 1) / (G * V));
     CSGS_LAUNCH(K_EMBED_JOIN, (chunk_join_k<TD, V, G>), dim3((unsigned)((chunks + JOIN_WAVES - 1) / JOIN_WAVES), slices), dim3(JOIN_WAVES * WAVE), st, in.F, Keys{in.entry},
@@ -1191,15 +1230,18 @@ template <typename TG, typename TD>
 static int embed_grad_sums(const SumIn &in, const SumOut &o, hipStream_t st)
 {
     constexpr int V = sizeof(TG) == 4 ? 4 : 8;
+    const int lanes = in.F < V ? 16 : sum_lanes(in.F, V);
     if (in.F < V) launch_sums<TG, TD, 1, 16>(in, o, st);
-    else if (in.F <= 16 * V) launch_sums<TG, TD, V, 16>(in, o, st);
-    else if (in.F <= 32 * V) launch_sums<TG, TD, V, 32>(in, o, st);
+    else if (lanes == 16) launch_sums<TG, TD, V, 16>(in, o, st);
+    else if (lanes == 32) launch_sums<TG, TD, V, 32>(in, o, st);
     else launch_sums<TG, TD, V, 64>(in, o, st);
     // (parts are doubles: pieces of two are 16 bytes)
-    if (in.F < 2) launch_join<TD, 1, 16>(in, o, st);
-    else if (in.F <= 32) launch_join<TD, 2, 16>(in, o, st);
-    else if (in.F <= 64) launch_join<TD, 2, 32>(in, o, st);
-    else launch_join<TD, 2, 64>(in, o, st);
+    const int32_t chunk = share_of(in.n, in.F) * (SUM_BLOCK / lanes);
+    if (in.n <= chunk) {   // nothing goes on
+    } else if (in.F < 2) launch_join<TD, 1, 16>(in, o, chunk, st);
+    else if (in.F <= 32) launch_join<TD, 2, 16>(in, o, chunk, st);
+    else if (in.F <= 64) launch_join<TD, 2, 32>(in, o, chunk, st);
+    else launch_join<TD, 2, 64>(in, o, chunk, st);
     CSGS_LAUNCH_CHECK();
     return CSGS_OK;
 }
