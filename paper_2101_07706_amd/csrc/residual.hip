@@ -115,19 +115,20 @@ __global__ __launch_bounds__(RES_BLOCK) void residual_k(ResidualArgs a, TS *y, i
 // overlaps the one before: the values that both hold are computed twice, alike, and count once in sums.
 
 // Sum over the G lanes of a row, the same bits in each of them: every step adds two lanes' values that are each other's
-// counterparts.  Rotations inside rows of 16 lanes, then rows and halves of the wavefront exchanged.
+// counterparts, first in fours (quad_perm), then mirrored in eights and rows of 16, then rows and halves of the wavefront exchanged.
 template <int CTRL>
-__device__ inline float add_rotated(float v)
+__device__ inline float add_counterpart(float v)
 {
     return v + __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(v), CTRL, 0xF, 0xF, true));
 }
 template <int G>
 __device__ inline float lanes_sum(float v)
 {
-    v = add_rotated<0x128>(v);   // row_ror:8
-    v = add_rotated<0x124>(v);
-    v = add_rotated<0x122>(v);
-    v = add_rotated<0x121>(v);
+    static_assert(G >= 4, "lanes of a row");
+    v = add_counterpart<0xB1>(v);                            // quad_perm:[1,0,3,2]
+    v = add_counterpart<0x4E>(v);                            // quad_perm:[2,3,0,1]
+    if constexpr (G >= 8) v = add_counterpart<0x141>(v);     // row_half_mirror
+    if constexpr (G >= 16) v = add_counterpart<0x140>(v);    // row_mirror
     if constexpr (G >= 32) {
         const auto p = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
         v = __uint_as_float(p[0]) + __uint_as_float(p[1]);
@@ -141,12 +142,12 @@ __device__ inline float lanes_sum(float v)
 // Sums of K values over a row's lanes; with G = 256 over the block, through LDS (turn: the two halves of `lds` in turn, so that one barrier a
 // sum is enough).
 template <int G, int K>
-__device__ inline void row_sums(float (&v)[K], float *lds /*[2][RES_BLOCK / WAVE][2]*/, int &turn)
+__device__ inline void row_sums(float (&v)[K], float *lds /*[2][G / WAVE][2]*/, int &turn)
 {
 #pragma unroll
     for (int k = 0; k < K; ++k) v[k] = lanes_sum<G>(v[k]);
     if constexpr (G > WAVE) {
-        float *l = lds + turn * (2 * RES_BLOCK / WAVE);
+        float *l = lds + turn * (2 * G / WAVE);
         turn ^= 1;
         if (lane_id() == 0)
 #pragma unroll
@@ -156,10 +157,13 @@ __device__ inline void row_sums(float (&v)[K], float *lds /*[2][RES_BLOCK / WAVE
         for (int k = 0; k < K; ++k) {
             v[k] = l[k];
 #pragma unroll
-            for (int w = 1; w < RES_BLOCK / WAVE; ++w) v[k] += l[2 * w + k];
+            for (int w = 1; w < G / WAVE; ++w) v[k] += l[2 * w + k];
         }
     }
 }
+// Threads of a block: rows of up to 256 lanes share one.
+template <int G>
+constexpr int row_block() { return G > RES_BLOCK ? G : RES_BLOCK; }
 
 // The columns that a lane holds: piece n begins at col(n); its first skip(n) values belong to the piece before.
 template <int V, int G, int N, bool RAGGED>
@@ -241,10 +245,10 @@ __device__ inline Stats stats_of(const float (&v)[NV], const C &c, float inv_F, 
 }
 
 template <typename TS, typename TB, int V, int G, int N, bool RAGGED>
-__global__ __launch_bounds__(RES_BLOCK) void residual_rows_k(ResidualArgs a, TS *y, int64_t ldy, TB *u, int64_t ldu)
+__global__ __launch_bounds__(row_block<G>()) void residual_rows_k(ResidualArgs a, TS *y, int64_t ldy, TB *u, int64_t ldu)
 {
     constexpr int NV = N * V;
-    __shared__ float lds[4 * RES_BLOCK / WAVE];
+    __shared__ float lds[4 * row_block<G>() / WAVE];
     int turn = 0;
     const int32_t M = resolve_count(a.M, a.M_dev);
     const Cols<V, G, N, RAGGED> c{a.F, (int)threadIdx.x % G};
@@ -255,7 +259,7 @@ __global__ __launch_bounds__(RES_BLOCK) void residual_rows_k(ResidualArgs a, TS 
     c.load_or(qw, a.pre_w, 1.0f);
     c.load_or(qb, a.pre_b, 0.0f);
     c.load_or(gv, a.gate && !a.ldg ? (const float *)a.gate : nullptr, 0.0f);
-    constexpr int ROWS = RES_BLOCK / G;
+    constexpr int ROWS = row_block<G>() / G;
     const int group = (int)threadIdx.x / G;
     for (int64_t r0 = (int64_t)blockIdx.x * ROWS; r0 < M; r0 += (int64_t)gridDim.x * ROWS) {
         const bool live = r0 + group < M;
@@ -373,10 +377,10 @@ __global__ __launch_bounds__(RES_BLOCK) void residual_grad_k(ResidualArgs a, Res
 
 // The same with the row in registers.  BIAS: sums of post_b or pre_b are wanted; GATE_ROW: those of a gate for all rows.
 template <typename TS, typename TB, int V, int G, int N, bool RAGGED, bool BIAS, bool GATE_ROW>
-__global__ __launch_bounds__(RES_BLOCK) void residual_grad_rows_k(ResidualArgs a, ResidualGrad g)
+__global__ __launch_bounds__(row_block<G>()) void residual_grad_rows_k(ResidualArgs a, ResidualGrad g)
 {
-    constexpr int NV = N * V, ROWS = RES_BLOCK / G;
-    __shared__ float lds[4 * RES_BLOCK / WAVE];
+    constexpr int NV = N * V, ROWS = row_block<G>() / G;
+    __shared__ float lds[4 * row_block<G>() / WAVE];
     __shared__ float sums[ROWS > 1 ? ROWS : 1][ROWS > 1 ? G * NV : 1];
     int turn = 0;
     const int32_t M = resolve_count(a.M, a.M_dev);
@@ -497,7 +501,7 @@ __global__ __launch_bounds__(RES_BLOCK) void residual_grad_rows_k(ResidualArgs a
             __syncthreads();
             for (int32_t f = (int32_t)threadIdx.x; f < a.F; f += RES_BLOCK) {
                 float s = sums[0][f];
-#pragma unroll
+#pragma unroll 16
                 for (int w = 1; w < ROWS; ++w) s += sums[w][f];
                 part[f] = s;
             }
@@ -565,6 +569,8 @@ static bool with_layout(int32_t width, F f)
     };
     using std::integral_constant;
     const int pieces = (width + V - 1) / V;
+    if (pieces <= 4) return go(integral_constant<int, 4>{}, integral_constant<int, 1>{});
+    if (pieces <= 8) return go(integral_constant<int, 8>{}, integral_constant<int, 1>{});
     if (pieces <= 16) return go(integral_constant<int, 16>{}, integral_constant<int, 1>{});
     if (pieces <= 32) return go(integral_constant<int, 32>{}, integral_constant<int, 1>{});
     if (pieces <= 64) return go(integral_constant<int, 64>{}, integral_constant<int, 1>{});
@@ -572,7 +578,8 @@ static bool with_layout(int32_t width, F f)
     if (pieces <= 192) return go(integral_constant<int, 64>{}, integral_constant<int, 3>{});
     if (pieces <= 256) return go(integral_constant<int, 256>{}, integral_constant<int, 1>{});
     if (pieces <= 512) return go(integral_constant<int, 256>{}, integral_constant<int, 2>{});
-    if (pieces <= 1024) return go(integral_constant<int, 256>{}, integral_constant<int, 4>{});
+    if (pieces <= 1024) return go(integral_constant<int, 512>{}, integral_constant<int, 2>{});
+    if (pieces <= 2048) return go(integral_constant<int, 1024>{}, integral_constant<int, 2>{});
     return false;
 }
 
@@ -581,9 +588,10 @@ static void launch_residual(const ResidualArgs &a, void *y, int64_t ldy, void *u
 {
     const bool done = with_layout<4>(a.F, [&](auto lanes, auto pieces, auto ragged) {
         constexpr int G = decltype(lanes)::value, N = decltype(pieces)::value;
-        const int64_t need = ((int64_t)a.M + RES_BLOCK / G - 1) / (RES_BLOCK / G);
+        constexpr int ROWS = row_block<G>() / G;
+        const int64_t need = ((int64_t)a.M + ROWS - 1) / ROWS;
         const unsigned blocks = (unsigned)(need < 2048 ? need : 2048);
-        CSGS_LAUNCH(K_RESIDUAL, (residual_rows_k<TS, TB, 4, G, N, decltype(ragged)::value>), dim3(blocks), dim3(RES_BLOCK), st, a, (TS *)y, ldy, (TB *)u, ldu);
+        CSGS_LAUNCH(K_RESIDUAL, (residual_rows_k<TS, TB, 4, G, N, decltype(ragged)::value>), dim3(blocks), dim3(row_block<G>()), st, a, (TS *)y, ldy, (TB *)u, ldu);
     });
     if (done) return;
     const unsigned blocks = (unsigned)(a.M < 4096 ? a.M : 4096);
@@ -595,13 +603,13 @@ static int launch_residual_grad(const ResidualArgs &a, const ResidualGrad &g, hi
 {
     int blocks = col_blocks(a.M);
     const bool done = with_layout<4>(a.F, [&](auto lanes, auto pieces, auto ragged) {
-        constexpr int G = decltype(lanes)::value, N = decltype(pieces)::value, ROWS = RES_BLOCK / G;
+        constexpr int G = decltype(lanes)::value, N = decltype(pieces)::value, ROWS = row_block<G>() / G;
         constexpr bool R = decltype(ragged)::value;
         const int64_t need = ((int64_t)a.M + ROWS - 1) / ROWS;
         constexpr int MOST = grad_blocks<G, N>();
         static_assert(MOST <= COL_BLOCKS, "room for the sums");
         blocks = (int)(need < MOST ? need : MOST);
-        const dim3 grid((unsigned)blocks), block(RES_BLOCK);
+        const dim3 grid((unsigned)blocks), block(row_block<G>());
         const bool bias = g.want[COL_POST_B] || g.want[COL_PRE_B], row = g.want[COL_GATE];
         if (bias && row) CSGS_LAUNCH(K_RESIDUAL_GRAD, (residual_grad_rows_k<TS, TB, 4, G, N, R, true, true>), grid, block, st, a, g);
         else if (bias) CSGS_LAUNCH(K_RESIDUAL_GRAD, (residual_grad_rows_k<TS, TB, 4, G, N, R, true, false>), grid, block, st, a, g);
