@@ -63,46 +63,65 @@ __device__ inline int64_t live_entries(const GradDesc &d)
     return rows * d.cols;
 }
 
-// A tile's entries [beg, end) by the block's threads: f(piece, output address, V) on pieces of V entries of a flat tensor, a quarter
-// of a tile's pieces on their way per thread, and entry by entry at its end and where rows lie apart.
-template <typename T, typename F>
-__device__ inline void each_piece(const GradDesc &d, int64_t beg, int64_t end, F f)
-{
-    constexpr int V = 16 / (int)sizeof(T), U = (int)(GRAD_TILE / (256 * V));
-    static_assert(U * V * 256 == GRAD_TILE, "a tile");
-    const T *g = (const T *)d.g;
-    T *out = (T *)d.out;
-    if (d.flat) {
-        const int64_t whole = end - (end - beg) % V;
-        RawPiece<T, V> r[U];
+// A tile's entries [beg, end) by the block's threads.  Those of a flat tensor are asked for together, 16 bytes a piece and thread, before the first is
+// needed; the others, and what does not fill a piece at the end, one by one when they are.
+constexpr int TILE_PIECES = (int)(GRAD_TILE * 4 / (256 * 16));   // of a thread, of floats (half as many of bfloat16)
+struct Tile {
+    GradDesc d;
+    int64_t beg, end, whole;
+    u32x4 held[TILE_PIECES];
+
+    __device__ void ask(const GradMem &m, int64_t t)
+    {
+        d = m.desc[m.tile_tensor[t]];
+        const int64_t live = live_entries(d);
+        beg = (t - d.first_tile) * GRAD_TILE;
+        end = beg + GRAD_TILE < live ? beg + GRAD_TILE : live;
+        if (end < beg) end = beg;
+        const int V = d.dtype == CSGS_F32 ? 4 : 8;
+        whole = d.flat ? end - (end - beg) % V : beg;
+        const char *p = (const char *)d.g + beg * (16 / V);
+        const int pieces = (int)((whole - beg) / V);
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int64_t e = beg + (u * 256 + (int)threadIdx.x) * V;
-            if (e < whole) r[u].load(g + e);
+        for (int u = 0; u < TILE_PIECES; ++u) {
+            const int k = u * 256 + (int)threadIdx.x;
+            if (k < pieces) held[u] = load_global<u32x4, 2>(p + (int64_t)k * 16);
         }
+    }
+    // f(values, where they go)
+    template <typename T, typename F>
+    __device__ void each(F f) const
+    {
+        constexpr int V = 16 / (int)sizeof(T);
+        const T *g = (const T *)d.g;
+        T *out = (T *)d.out;
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
+        for (int u = 0; u < TILE_PIECES * 4 / V; ++u) {
             const int64_t e = beg + (u * 256 + (int)threadIdx.x) * V;
             if (e < whole) {
+                RawPiece<T, V> r;
+                r.w[0] = held[u].x; r.w[1] = held[u].y; r.w[2] = held[u].z; r.w[3] = held[u].w;
                 Vec<V> v;
 #pragma unroll
-                for (int i = 0; i < V; ++i) v.x[i] = r[u].value(i);
+                for (int i = 0; i < V; ++i) v.x[i] = r.value(i);
                 f(v, out + e);
             }
         }
-        const int64_t e = whole + threadIdx.x;
-        if (e < end) f(load_row<T, 1>(g + e), out + e);
-        return;
+        if (d.flat) {
+            const int64_t e = whole + threadIdx.x;
+            if (e < end) f(load_row<T, 1>(g + e), out + e);
+            return;
+        }
+        // (a row and a column of the tile's first entry by one division, the others from there in 32 bits)
+        const int64_t r0 = beg / d.cols, c0 = beg - r0 * d.cols;
+        for (int32_t x = (int32_t)threadIdx.x; x < (int32_t)(end - beg); x += 256) {
+            const int64_t c = c0 + x;
+            const int64_t dr = c < d.cols ? 0 : d.cols > GRAD_TILE ? 1 : (int64_t)((uint32_t)c / (uint32_t)d.cols);
+            const int64_t r = r0 + dr, col = c - dr * d.cols;
+            f(load_row<T, 1>(g + r * d.ldg + col), out + r * d.ldo + col);
+        }
     }
-    // (a row and a column of the tile's first entry by one division, the others from there in 32 bits)
-    const int64_t r0 = beg / d.cols, c0 = beg - r0 * d.cols;
-    for (int32_t x = (int32_t)threadIdx.x; x < (int32_t)(end - beg); x += 256) {
-        const int64_t c = c0 + x;
-        const int64_t dr = c < d.cols ? 0 : d.cols > GRAD_TILE ? 1 : (int64_t)((uint32_t)c / (uint32_t)d.cols);
-        const int64_t r = r0 + dr, col = c - dr * d.cols;
-        f(load_row<T, 1>(g + r * d.ldg + col), out + r * d.ldo + col);
-    }
-}
+};
 
 // The sum, or the larger one with NaN above everything.
 template <int KIND>
@@ -119,39 +138,32 @@ __device__ inline double take_in(double a, float x)
     return add_or_max<KIND>(a, fabs(v));
 }
 
-// Joined over the block's 256 threads by a fixed tree; the result in every thread.
+// Joined over the block's 256 threads in a fixed order, the result in every thread: across a wavefront by exchanges, then its four.
 template <int KIND>
-__device__ inline double block_join(double v, double *lds /*[256]*/)
+__device__ inline double block_join(double v, double *lds /*[4]*/)
 {
-    const int tid = (int)threadIdx.x;
-    lds[tid] = v;
+#pragma unroll
+    for (int s = WAVE / 2; s > 0; s >>= 1) v = add_or_max<KIND>(v, __shfl_xor(v, s));
+    if (lane_id() == 0) lds[threadIdx.x / WAVE] = v;
     __syncthreads();
-    for (int s = 128; s > 0; s >>= 1) {
-        if (tid < s) lds[tid] = add_or_max<KIND>(lds[tid], lds[tid + s]);
-        __syncthreads();
-    }
-    const double r = lds[0];
-    __syncthreads();
-    return r;
+    return add_or_max<KIND>(add_or_max<KIND>(lds[0], lds[1]), add_or_max<KIND>(lds[2], lds[3]));
 }
 
 template <int KIND>
 __global__ __launch_bounds__(256) void grad_norm_k(GradMem m, int64_t tiles)
 {
-    __shared__ double lds[256];
+    __shared__ double lds[4];
     double sum[4] = {0.0, 0.0, 0.0, 0.0};
     for (int64_t t = blockIdx.x; t < tiles; t += gridDim.x) {
-        const GradDesc d = m.desc[m.tile_tensor[t]];
-        const int64_t beg = (t - d.first_tile) * GRAD_TILE, live = live_entries(d);
-        const int64_t end = beg + GRAD_TILE < live ? beg + GRAD_TILE : live;
-        if (end <= beg) continue;
+        Tile tile;
+        tile.ask(m, t);
         auto take = [&](const auto &v, auto *) {
             constexpr int V = (int)(sizeof(v.x) / sizeof(float));
 #pragma unroll
             for (int i = 0; i < V; ++i) sum[i % 4] = take_in<KIND>(sum[i % 4], v.x[i]);
         };
-        if (d.dtype == CSGS_F32) each_piece<float>(d, beg, end, take);
-        else each_piece<uint16_t>(d, beg, end, take);
+        if (tile.d.dtype == CSGS_F32) tile.each<float>(take);
+        else tile.each<uint16_t>(take);
     }
     const double own = add_or_max<KIND>(add_or_max<KIND>(sum[0], sum[1]), add_or_max<KIND>(sum[2], sum[3]));
     const double all = block_join<KIND>(own, lds);
@@ -176,7 +188,7 @@ __device__ inline double join_partials(const double *__restrict__ partial, int b
 
 __global__ __launch_bounds__(256) void grad_total_k(GradMem m, int blocks, int kind, double *__restrict__ total)
 {
-    __shared__ double lds[256];
+    __shared__ double lds[4];
     const double s = join_partials(m.partial, blocks, kind, lds);
     if (threadIdx.x == 0) *total = s;
 }
@@ -186,7 +198,11 @@ template <bool PAST>
 __global__ __launch_bounds__(256) void grad_scale_k(GradMem m, int64_t tiles, int blocks, int kind, const double *total, float max_norm, float *norm_out,
                                                     int32_t *status)
 {
-    __shared__ double lds[256];
+    __shared__ double lds[4];
+    // (from the last tile back: those may still be in the cache from the pass before; the first one's entries are on their way meanwhile)
+    int64_t t = tiles - 1 - blockIdx.x;
+    Tile tile;
+    tile.ask(m, t);
     const double s = total ? *total : join_partials(m.partial, blocks, kind, lds);
     const double norm = kind == CSGS_GRAD_L2 ? sqrt(s) : s;
     double coef = (double)max_norm / (norm + 1e-6);
@@ -195,21 +211,20 @@ __global__ __launch_bounds__(256) void grad_scale_k(GradMem m, int64_t tiles, in
         if (norm_out) *norm_out = (float)norm;
         if (status && !(norm <= 1.7976931348623157e308)) atomicOr(status, CSGS_ST_NONFINITE_GRAD);
     }
-    // (from the last tile back: those are still in the cache from the pass before)
-    for (int64_t t = tiles - 1 - blockIdx.x; t >= 0; t -= gridDim.x) {
-        const GradDesc d = m.desc[m.tile_tensor[t]];
-        if (!d.out || (coef == 1.0 && d.out == d.g)) continue;
-        const int64_t beg = (t - d.first_tile) * GRAD_TILE, live = live_entries(d);
-        const int64_t end = beg + GRAD_TILE < live ? beg + GRAD_TILE : live;
-        if (end <= beg) continue;
-        auto give = [&](auto v, auto *out) {
+    auto give = [&](auto v, auto *out) {
 #pragma unroll
-            for (float &x : v.x) x = (float)(coef * (double)x);
-            if constexpr (PAST) store_row_past_caches(out, v);
-            else store_row(out, v);
-        };
-        if (d.dtype == CSGS_F32) each_piece<float>(d, beg, end, give);
-        else each_piece<uint16_t>(d, beg, end, give);
+        for (float &x : v.x) x = (float)(coef * (double)x);
+        if constexpr (PAST) store_row_past_caches(out, v);
+        else store_row(out, v);
+    };
+    for (;;) {
+        if (tile.d.out && (coef != 1.0 || tile.d.out != tile.d.g)) {   // (NaN is not 1)
+            if (tile.d.dtype == CSGS_F32) tile.each<float>(give);
+            else tile.each<uint16_t>(give);
+        }
+        t -= gridDim.x;
+        if (t < 0) return;
+        tile.ask(m, t);
     }
 }
 
