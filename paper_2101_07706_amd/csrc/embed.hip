@@ -1,16 +1,28 @@
 // csgs_embed: rows of a learned table by id, scaled, and the table's gradient by sorted ids.
 //
-// Forward: out[t] = s T[i_t].  Gradient: dT[v] = s sum_{t : i_t = v} G[t].  The positions t are sorted by id (stable, least
-// significant digit first), so that the positions of a row lie side by side, in order; a row is then summed by one wavefront
-// and written once.
+// Forward: out[t] = s T[i_t].  Gradient: dT[v] = s sum_{t : i_t = v} G[t].  The positions t are sorted by id (stable), so that those of a row
+// lie side by side, in order; rows of G are then summed where they lie, in chunks of a fixed number of positions, in double, and
+// every row of the gradient is written once.  Nothing is added with atomics: two calls give the same bits.
+//
+// A lookup is bound by memory: the rows of T once, the output once.  So is the gradient of many wide rows (G once, the output once); of
+// few or narrow ones it is bound by the latency of its launches (3 to 4 us each) and of the loads in a row in them.  Three forms, by the
+// number of positions n (us for gradient rows of 100 floats, one launch / ranges / digits; hubs: half of the positions uniform over 2.4 M
+// rows, half log-uniform; zipf: log-uniform over 50 K; one: a single id):
+//     n = 300     hubs 9.7 / 19.1   zipf 8.9 / 19.2    one 12.6 / 17.3
+//     n = 2048    hubs 13.1 / 21.2 / 39   zipf 12.0 / 20.6 / 32   one 39 / 21.2 / 32
+//     n = 32768   hubs - / 30.8 / 53.6   zipf - / 27.6 / 42.2   one - / 42.7 / 42.7
+//     n = 98304   hubs - / 50.2 / 71.1   zipf - / 47.0 / 55.7   one - / 83.8 / 62.6
+//     n = 131072  hubs - / 58.6 / 77.9   zipf - / 72.4 / 59.6   one - / 104 / 70.1
 #include "common.hpp"
 #include "row_pieces.hpp"
 
 namespace csgs {
 
 // ---------------------------------------------------------------- lookup
-// G lanes take a row in pieces of V columns, and several rows at a time: the rows are as far apart as the ids say, so what counts is how many
+// G lanes take a row in pieces of V columns, and four rows at a time: the rows are as far apart as the ids say, so what counts is how many
 // are asked for before the first is needed.  The last piece of a width that V does not divide ends with the row and overlaps the one before.
+// (131 K rows of 100 bfloat16 values out of 2.4 M to floats 19.5 us, 4.0 TB/s of what has to move, a row lying across three lines of 128 bytes; a
+// value a lane and a row at a time 38.)
 template <typename TI, typename TO, int V, int G>
 __global__ __launch_bounds__(256) void embed_k(const TI *T, int64_t ld, int64_t rows, int32_t F, const int32_t *__restrict__ ids, int32_t n_cap,
                                                const int32_t *__restrict__ n_dev, float scale, TO *out, int64_t ldo)
@@ -45,7 +57,7 @@ __global__ __launch_bounds__(256) void embed_k(const TI *T, int64_t ld, int64_t 
 // ---------------------------------------------------------------- positions sorted by id
 // An entry is an id and its position, id << 32 | position.  A pass sorts by one digit of up to 8 bits.  At most SORT_TILES blocks
 // take consecutive tiles of the entries: the first kernel counts a tile's digits, the second one adds up what lies before its own
-// (the counts of all tiles, at most 64 K of them) and places its entries.  No block waits for another.
+// (the counts of all tiles, at most 64 K of them) and places its entries.  No block waits for another.  (1 M entries: 7 and 22 us a pass.)
 constexpr int SORT_TILES = 256, SORT_BLOCK = 256, SORT_WAVES = SORT_BLOCK / WAVE, DIGITS = 256;
 static_assert(DIGITS == SORT_BLOCK, "a thread per digit");
 constexpr int SORT_ITEMS = 8;                              // entries that a thread places at a time
@@ -475,12 +487,13 @@ __global__ __launch_bounds__(256) void rows_zero_k(ZeroRows z)
 // ---------------------------------------------------------------- positions sorted by id, in one launch
 // A block owns a range of ids, looks at all ids itself and lists those of its range in order of position; how many lie below the range
 // says where its list belongs among the sorted entries, so that no block waits for another.  Ranges hold about as many positions
-// each: every block sorts the same sample of the ids and takes its bounds from there.  An id that fills bounds by itself has a
+// each: every block selects its bounds from the same sample of the ids.  An id that fills bounds by itself has a
 // range of its own, which needs no sorting however many positions it holds; a list that outgrows LDS all the same (a sample that misses) is
-// sorted in memory.  Further blocks clear the gradient's rows meanwhile.
-constexpr int RANGES = 256, SAMPLE = 4 * WIDE, RANGE_CACHED = 32;
+// sorted in memory.  Further blocks clear the gradient's rows meanwhile.  Bound by the instructions that look at every id in every block (13 us for
+// 131 K) and by latency.  (us, 32 K positions: 13; of those 2 until the ids are there, 3 for the bounds, 2 for the lists, 1 to sort 120
+// entries.  Bounds by sorting 1024 samples took 6; lists sorted by digits 4; the ids kept in registers between counting and listing is level.)
+constexpr int RANGES = 256, SAMPLE = 4 * WIDE;
 constexpr uint32_t OWN_LIST = LDS_ENTRIES / WIDE_WAVES;   // entries of its range that a wavefront lists in LDS
-constexpr int64_t RANGE_CACHED_MAX = (int64_t)WIDE * RANGE_CACHED;
 // Block b's ids are [lo, lo + width): bounds are, of the sorted samples, the (r samples / RANGES)-th.  All threads call it.
 struct Range {
     uint32_t lo, width;
@@ -500,7 +513,6 @@ __device__ inline Range range_of(int b, const uint32_t (&sample)[SAMPLES], const
     if (lo > hi) lo = hi;
     return Range{lo, hi - lo};
 }
-template <bool CACHED>   // at most RANGE_CACHED_MAX positions: the ids stay in registers between counting and listing
 __global__ __launch_bounds__(WIDE) void sort_ranges_k(const int32_t *__restrict__ ids, int32_t n_cap, const int32_t *__restrict__ n_dev, uint32_t rows,
                                                       uint64_t *out, uint64_t *other, uint32_t *__restrict__ rank, uint32_t *__restrict__ distinct,
                                                       int32_t *__restrict__ n_valid, ZeroRows z)
@@ -551,24 +563,12 @@ __global__ __launch_bounds__(WIDE) void sort_ranges_k(const int32_t *__restrict_
         for (int u = 0; u < U; ++u)
             if (i0 + u * WAVE + lane >= w_end) id[u] = 0xFFFFFFFFu;
     };
-    uint32_t held[CACHED ? RANGE_CACHED / U : 1][U];
-    if constexpr (CACHED) {
-#pragma unroll
-        for (int q = 0; q < RANGE_CACHED / U; ++q)
-            if (q * U * WAVE < share) ask(w_beg + q * U * WAVE, held[q]);
-    }
     // f(ids, first position), over the wavefront's share
     auto each = [&](auto f) {
-        if constexpr (CACHED) {
-#pragma unroll
-            for (int q = 0; q < RANGE_CACHED / U; ++q)
-                if (q * U * WAVE < share) f(held[q], w_beg + q * U * WAVE);
-        } else {
-            for (int32_t i0 = w_beg; i0 < w_end; i0 += U * WAVE) {
-                uint32_t id[U];
-                ask(i0, id);
-                f(id, i0);
-            }
+        for (int32_t i0 = w_beg; i0 < w_end; i0 += U * WAVE) {
+            uint32_t id[U];
+            ask(i0, id);
+            f(id, i0);
         }
     };
     const Range range = range_of(b, sample, has, samples, rows, sel);
@@ -658,7 +658,7 @@ __global__ __launch_bounds__(WIDE) void sort_ranges_k(const int32_t *__restrict_
     }
     if (tid == 0) distinct[b] = alone ? 1u : base;
 }
-constexpr int64_t RANGES_MAX = 1 << 18;   // most positions of this form
+constexpr int64_t RANGES_MAX = 3 << 15;   // most positions of this form
 static_assert(RANGES_MAX <= 1 << 24 && RANGES <= 256, "a block and a rank in 32 bits");
 
 // ---------------------------------------------------------------- the different ids
@@ -783,7 +783,9 @@ __device__ inline uint32_t from_lane(uint32_t v, int from)
 // G lanes take a share of a chunk of sorted positions: the rows of G that they point to are added up in order, eight on their way at a time; a
 // table row all of whose positions lie in the share is written at once.  Parts of rows that go on across shares are joined in LDS, in order, and written
 // there as far as they lie in the chunk; parts of others go to `part`, slot 1 of a row that begins in the chunk and goes on, slot 0 of one that
-// began before it.  The work per chunk does not depend on how often an id occurs.
+// began before it.  The work per chunk does not depend on how often an id occurs.  Bound by memory.  (131 K rows of 250 floats 24 us, 5.4 TB/s; 65 K of
+// 512 bfloat16 values into 50 K rows of floats 21.  Parts left in memory by every share instead: 131 K positions of 100 values 18 and 20 us to join them,
+// 16 and 7 now.)
 template <typename TG, typename TD, int V, int G>
 __global__ __launch_bounds__(256) void chunk_sums_k(const TG *g, int64_t ldg, int32_t F, const uint64_t *__restrict__ entry,
                                                     int32_t n_cap, const int32_t *__restrict__ n_dev, uint32_t rows, int32_t share,
@@ -890,7 +892,8 @@ __global__ __launch_bounds__(256) void chunk_sums_k(const TG *g, int64_t ldg, in
 }
 
 // Table rows that go on across chunks: a wavefront per chunk looks whether one begins in it, and adds up its parts in order; one
-// of more than JOIN_LONG chunks is left to the whole block, whose groups of G lanes take consecutive shares of the parts.
+// of more than JOIN_LONG chunks is left to the whole block, whose groups of G lanes take consecutive shares of the parts.  Bound by the latency of
+// four dependent loads (4 to 8 us).
 constexpr int JOIN_WAVES = 16, JOIN_LONG = 16;
 template <typename TD, int V, int G>
 __global__ __launch_bounds__(JOIN_WAVES * WAVE) void chunk_join_k(int32_t F, Keys key, int32_t n_cap, const int32_t *__restrict__ n_dev, uint32_t rows,
@@ -975,11 +978,12 @@ __global__ __launch_bounds__(JOIN_WAVES * WAVE) void chunk_join_k(int32_t F, Key
 }
 
 // ---------------------------------------------------------------- few positions: everything in one launch
-// Ranges as above, but a block also adds up the rows of its range: all positions of an id are in one block, and so few in all that the
-// block which an often repeated id falls to is no slower for it.  Groups of G lanes take consecutive shares of the sorted list; a row within a share
+// Ranges as above, but a block also adds up the rows of its range: all positions of an id are in one block.  The block that an often repeated id falls
+// to reads its rows alone, at 25 GB/s or so, so that the rows must be few and not wide.  Groups of G lanes take consecutive shares of the sorted list; a row within a share
 // is written at once, parts of one that goes on across shares are joined in LDS.  The rank of a range's first id is the number of different ids
 // below it, which every block counts with a hash table.  Rows without positions are cleared in even shares of the table.
 constexpr int FEW = 2 * WIDE;
+constexpr int64_t FEW_VALUES = 1 << 18;   // most values of G: 1 MB of floats, 40 us for one compute unit if all of them belong to one id, half of that otherwise lost
 constexpr int FEW_TABLE = 2 * FEW, FEW_ROWS = 1 << 15;   // hash table; rows whose being met a block notes at a time
 template <typename TG, typename TD, int V, int G>
 __global__ __launch_bounds__(WIDE) void few_sums_k(const TG *g, int64_t ldg, int32_t F, const int32_t *__restrict__ ids, int32_t n_cap,
@@ -1102,8 +1106,8 @@ __global__ __launch_bounds__(WIDE) void few_sums_k(const TG *g, int64_t ldg, int
     __syncthreads();
     if (own == 0) return;
     auto row_of = [&](int i) { return o.rank ? base + local_rank[i] : key_of(e[i]); };
-    constexpr int U = 4;   // rows on their way, and fewest of a share
-    const int even = ((int)own + GROUPS - 1) / GROUPS, share = even < U ? U : even, groups = ((int)own + share - 1) / share, q = tid / G, sub = tid % G;
+    constexpr int U = 8, LEAST = 4;   // rows on their way; fewest of a share (they take no longer than one, and there are fewer shares to join)
+    const int even = ((int)own + GROUPS - 1) / GROUPS, share = even < LEAST ? LEAST : even, groups = ((int)own + share - 1) / share, q = tid / G, sub = tid % G;
     struct Share {
         int beg, end;
         bool open, goes_on, one;   // its first row began before it; its last one goes on after it; it holds one row
@@ -1132,8 +1136,11 @@ __global__ __launch_bounds__(WIDE) void few_sums_k(const TG *g, int64_t ldg, int
             bool open = s.open;
             for (int i0 = s.beg; i0 < s.end; i0 += U) {
                 RawPiece<TG, V> r[U];
+                uint64_t en[U + 1];
 #pragma unroll
-                for (int u = 0; u < U; ++u) r[u].load(g + (int64_t)(uint32_t)e[i0 + u < s.end ? i0 + u : s.end - 1] * ldg + pc.col);
+                for (int u = 0; u <= U; ++u) en[u] = e[i0 + u < s.end ? i0 + u : s.end - 1];
+#pragma unroll
+                for (int u = 0; u < U; ++u) r[u].load(g + (int64_t)(uint32_t)en[u] * ldg + pc.col);
 #pragma unroll
                 for (int u = 0; u < U; ++u) {
                     const int i = i0 + u;
@@ -1141,7 +1148,7 @@ __global__ __launch_bounds__(WIDE) void few_sums_k(const TG *g, int64_t ldg, int
 #pragma unroll
                         for (int j = 0; j < V; ++j) acc[j] += (double)r[u].value(j);
                         const bool last = i == s.end - 1;
-                        if (last || key_of(e[i + 1]) != key_of(e[i])) {
+                        if (last || key_of(en[u + 1]) != key_of(en[u])) {
                             if (open || (last && s.goes_on))
 #pragma unroll
                                 for (int j = 0; j < V; ++j) slot[open ? 0 : 1][q][sub * V + j] = acc[j];
@@ -1259,18 +1266,14 @@ static int embed_grad(const int32_t *ids, int64_t n, const int32_t *n_dev, const
     const ZeroRows z{d, uniq || accumulate ? 0 : rows, F * elt, ldd * elt};
     SumIn in{G, ldg, F, nullptr, (int32_t)n, n_dev, (uint32_t)rows, s.part};
     SumOut o{uniq ? s.rank : nullptr, nullptr, uniq, n_uniq, d, ldd, scale, accumulate};
-    if (n <= FEW) {
+    if (n <= FEW && n * F <= FEW_VALUES) {
         if (g_dtype == CSGS_F32) return d_dtype == CSGS_F32 ? embed_grad_few<float, float>(in, ids, z, o, st) : embed_grad_few<float, uint16_t>(in, ids, z, o, st);
         return d_dtype == CSGS_F32 ? embed_grad_few<uint16_t, float>(in, ids, z, o, st) : embed_grad_few<uint16_t, uint16_t>(in, ids, z, o, st);
     }
     if (n <= RANGES_MAX) {
         const dim3 grid(RANGES + (z.rows ? RANGES : 0)), block(WIDE);
-        if (n <= RANGE_CACHED_MAX)
-            CSGS_LAUNCH(K_EMBED_RANGES, sort_ranges_k<true>, grid, block, st, ids, (int32_t)n, n_dev, (uint32_t)rows, s.entry[0], s.entry[1], uniq ? s.rank : nullptr,
-                        s.heads, s.n_valid, z);
-        else
-            CSGS_LAUNCH(K_EMBED_RANGES, sort_ranges_k<false>, grid, block, st, ids, (int32_t)n, n_dev, (uint32_t)rows, s.entry[0], s.entry[1], uniq ? s.rank : nullptr,
-                        s.heads, s.n_valid, z);
+        CSGS_LAUNCH(K_EMBED_RANGES, sort_ranges_k, grid, block, st, ids, (int32_t)n, n_dev, (uint32_t)rows, s.entry[0], s.entry[1], uniq ? s.rank : nullptr, s.heads,
+                    s.n_valid, z);
         CSGS_LAUNCH_CHECK();
         in.entry = s.entry[0];
         in.n_dev = s.n_valid;
