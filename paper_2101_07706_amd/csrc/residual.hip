@@ -5,12 +5,19 @@
 // so with d = dL/dy as a whole = dy + the gradient through u's norm, n = N(h), a = a(gate):
 //     dx = beta d,   dgate = alpha d .* n .* a'(gate),   dn = alpha d .* a,   dh = the gradient through h's norm of dn,
 //     dpost_w = sum over rows of dn .* hat(h),  dpost_b = sum dn,  dpre_w = sum du .* hat(y),  dpre_b = sum du.
-// The gradient forms everything again from the forward's inputs: reading x and the row again costs the same bytes as reading y
-// and no statistics need be kept.  Both directions move a few bytes per operation: bound by memory.
+// The gradient forms everything again from the forward's inputs: reading x again costs the same bytes as reading y, and no statistics need
+// be kept.  Row sums, statistics and everything between are in fp32, one rounding per output.  Both directions move a few bytes per operation:
+// bound by memory where there are many rows (us and TB/s of what has to move; a large copy reaches 4.8 to 5.2: 131072 rows of 256 floats 126, 5.3; gradient
+// of 65536 rows of 1024, stream in floats, block in bfloat16, 279, 5.3; of 16384 rows of 2048 floats 205, 5.2; of 8192 rows of 4096 in bfloat16 180, 3.0),
+// by the latency of a row's loads and of four to six sums over it one after the other where there are few (256 rows of 64 3.1; gradient of 8192
+// rows of 256 18.4, of 1999 rows of 602 16.6, two launches each).
 #include "common.hpp"
 #include "row_pieces.hpp"
 
 namespace csgs {
+
+// Two forms: rows in registers (residual_rows_k), and rows walked over several times (residual_k), for fewer columns than a piece and more than the
+// registers of a block hold.
 
 struct ResidualArgs {
     int32_t M, F;
@@ -90,6 +97,7 @@ struct Row {
     __device__ float y(int32_t f) const { return a.beta * x(f) + (a.h ? a.alpha * gate(f).a * n(f) : 0.0f); }
 };
 
+// A block takes a row and reads it from memory or the caches each time it is needed (4096 rows of 8192 floats 371 us, rows in registers 144).
 template <typename TS, typename TB>
 __global__ __launch_bounds__(RES_BLOCK) void residual_k(ResidualArgs a, TS *y, int64_t ldy, TB *u, int64_t ldu)
 {
@@ -112,7 +120,9 @@ __global__ __launch_bounds__(RES_BLOCK) void residual_k(ResidualArgs a, TS *y, i
 // ---------------------------------------------------------------- rows in registers
 // G lanes take a row, N pieces of V columns each; what a lane holds of the vectors (weights, sums over rows) stays in registers
 // from row to row.  Rows start on any element.  RAGGED: V does not divide the width; the last piece then ends with the row and
-// overlaps the one before: the values that both hold are computed twice, alike, and count once in sums.
+// overlaps the one before: the values that both hold are computed twice, alike, and count once in sums.  All of a row's inputs are asked for
+// before any is widened: with a piece widened where it was loaded the branches waited for each other's loads (gradient of 65536 rows of 1024
+// in mixed types 438 us for 302).
 
 // Sum over the G lanes of a row, the same bits in each of them: every step adds two lanes' values that are each other's
 // counterparts, first in fours (quad_perm), then mirrored in eights and rows of 16, then rows and halves of the wavefront exchanged.
@@ -296,7 +306,8 @@ __global__ __launch_bounds__(row_block<G>()) void residual_rows_k(ResidualArgs a
     }
 }
 
-// Sums over rows: every block leaves one row of sums per vector, which a second kernel adds up.
+// Sums over rows: every block leaves one row of sums per vector, in fp32 over its share of the rows, which a second kernel adds up in double, in
+// order.
 enum { COL_POST_W = 0, COL_POST_B, COL_PRE_W, COL_PRE_B, COL_GATE, COL_KINDS };
 constexpr int COL_BLOCKS = 1024;   // most blocks
 __host__ inline int col_blocks(int32_t M) { return M < COL_BLOCKS ? M : COL_BLOCKS; }
@@ -519,7 +530,7 @@ __global__ __launch_bounds__(row_block<G>()) void residual_grad_rows_k(ResidualA
 struct ColOut {
     float *out[COL_KINDS];
 };
-// A block takes 64 columns of a vector; its wavefronts take the parts in turn.
+// A block takes 64 columns of a vector; its wavefronts take the parts in turn.  (512 parts of 256 columns 4 us, a launch's latency.)
 constexpr int COL_WAVES = 16;
 __global__ __launch_bounds__(COL_WAVES * WAVE) void col_sums_k(const float *__restrict__ part, int blocks, int32_t F, ColOut o)
 {
@@ -556,7 +567,10 @@ static int open_residual(const csgs_residual *r, ResidualArgs *a)
     return CSGS_OK;
 }
 
-// Calls f with the row's layout as constants: lanes, pieces a lane, and whether the width is no multiple of a piece.
+// Calls f with the row's layout as constants: lanes, pieces a lane, and whether the width is no multiple of a piece.  As few lanes as hold the row
+// in one piece, then up to three pieces a lane, then a block per row: with four pieces a lane the gradient takes 280 registers and a unit
+// holds one wavefront (us, gradient: 65536 rows of 1024, 64 lanes with four pieces 302, 256 with one 289; 1999 rows of 602, 64 with three 16.9, 256 with
+// one 21; 8192 rows of 4096 in bfloat16, 256 with four 217, 512 with two 180; 131072 rows of 16, 16 lanes, four of them busy, 32, 4 lanes 21).
 template <int V, typename F>
 static bool with_layout(int32_t width, F f)
 {

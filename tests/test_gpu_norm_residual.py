@@ -301,3 +301,31 @@ def test_on_another_stream_and_replayed(env):
         step(None)
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(got, [y, u, dx, dh] + vs)), f"replay {k}"
+
+
+def test_recorded_calls(env):
+    """Calls marshalled once and issued again see what the buffers hold then."""
+    csgs, dev = env
+    c = Case(csgs, dev, 60, 72, "mixed", act="silu", gate="row", count=50)
+    y, u = c.new(torch.float32), c.new(torch.bfloat16)
+    dx, dh, dw = c.new(torch.float32), c.new(torch.bfloat16), torch.empty(72, device=dev)
+    scratch = torch.empty(csgs.csgs_norm_residual_grad_scratch_bytes(60, 72), dtype=torch.uint8, device=dev)
+    ids, table, out = torch.arange(60, dtype=torch.int32, device=dev).flip(0).contiguous(), torch.randn(60, 72, device=dev), torch.empty(60, 72, device=dev)
+
+    def calls():
+        csgs.csgs_embed(table, ids, out, scale=2.0)
+        csgs.csgs_norm_residual(c.x, c.h, y, u, **c.args())
+        csgs.csgs_norm_residual_grad(c.x, c.h, c.dy, c.du, dx, dh, None, dw, None, None, None, scratch, **c.args())
+
+    with csgs.record() as plan:
+        calls()
+    for _ in range(2):
+        c.x.normal_()
+        table.normal_()
+        plan.run()
+        torch.cuda.synchronize()
+        got = [t.clone() for t in (out, y[:50], u[:50], dx[:50], dh[:50], dw)]
+        calls()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, (out, y[:50], u[:50], dx[:50], dh[:50], dw)))
+        assert torch.equal(out, 2.0 * table.flip(0))

@@ -134,7 +134,7 @@ def test_gradient_of_many_positions(env, n, rows, F, dist):
     check_grad(run_grad(csgs, dev, ids, G, rows, 1.0, torch.float32), ids, G, rows, 1.0)
 
 
-@pytest.mark.parametrize("n,rows", [(1 << 15, 1 << 24), (1 << 15, 1 << 17), (1 << 18, 1 << 24), (1 << 18, 1 << 17), (50_000, 1 << 20)])
+@pytest.mark.parametrize("n,rows", [(1 << 15, 1 << 24), (1 << 15, 1 << 17), (1 << 18, 1 << 24), (1 << 18, 1 << 17), (50_000, 1 << 20), (98_000, 1 << 18)])
 @pytest.mark.parametrize("sample", [1024, 4096])
 def test_ids_that_a_sample_misses(env, n, rows, sample):
     """Every (n / sample)-th position holds an id from all over the table, all the others one of a narrow range between two of those."""
@@ -149,7 +149,7 @@ def test_ids_that_a_sample_misses(env, n, rows, sample):
     check_grad(run_grad(csgs, dev, ids, G, rows, 1.0, torch.float32), ids, G, rows, 1.0)
 
 
-@pytest.mark.parametrize("n", [2048, 2049, 32768, 32769, 262_144, 262_145])
+@pytest.mark.parametrize("n", [2048, 2049, 32768, 32769, 98_304, 98_305, 262_144])
 @pytest.mark.parametrize("dist", ["steep", "half", "one", "none", "ascending"])
 def test_gradient_around_the_forms_of_the_sort(env, n, dist):
     csgs, dev = env
