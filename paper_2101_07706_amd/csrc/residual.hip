@@ -374,7 +374,7 @@ __global__ __launch_bounds__(RES_BLOCK) void residual_grad_k(ResidualArgs a, Res
             if (a.h) {
                 const Gate gt = row.gate(f);
                 const float t = a.alpha * v, dn = t * gt.a, hat = row.hat(f), dg = t * row.n(f) * gt.da;
-                const float dh = row.h_stats.r * (dn * (a.post_w ? a.post_w[f] : 1.0f) - p1 - hat * p2);
+                const float dh = a.post != CSGS_NORM_NONE ? row.h_stats.r * (dn * (a.post_w ? a.post_w[f] : 1.0f) - p1 - hat * p2) : dn;
                 if (g.want[COL_POST_W]) part(COL_POST_W, f) += dn * hat;
                 if (g.want[COL_POST_B]) part(COL_POST_B, f) += dn;
                 if (g.want[COL_GATE]) part(COL_GATE, f) += dg;
@@ -432,13 +432,18 @@ __global__ __launch_bounds__(row_block<G>()) void residual_grad_rows_k(ResidualA
         if (a.h) hs = stats_of<G>(h, c, inv_F, a.post, a.eps, lds, turn);
 #pragma unroll
         for (int i = 0; i < NV; ++i) h[i] = a.h ? (h[i] - hs.m) * hs.r : 0.0f;   // from here on hat(h)
+        constexpr int KEPT = N == 1 ? NV : 1;
+        Gate kept[KEPT];   // where there are registers for it
+        if (N == 1 && a.gate)
+#pragma unroll
+            for (int i = 0; i < KEPT; ++i) kept[i] = gate_of(gv[i], a.act);
         if (g.du) {
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
                 v[i] = a.x ? a.beta * v[i] : 0.0f;
                 if (a.h) {
                     const float n = h[i] * pw[i] + pb[i];
-                    v[i] += a.alpha * (a.gate ? gate_of(gv[i], a.act).a * n : n);
+                    v[i] += a.alpha * (a.gate ? (N == 1 ? kept[i % KEPT] : gate_of(gv[i], a.act)).a * n : n);
                 }
             }
             const Stats s = stats_of<G>(v, c, inv_F, a.pre, a.eps, lds, turn);
@@ -453,9 +458,13 @@ __global__ __launch_bounds__(row_block<G>()) void residual_grad_rows_k(ResidualA
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
                 d[i] += s.r * (du[i] * qw[i] - t[1] - v[i] * t[0]);
-                s_qw[i] += live ? du[i] * v[i] : 0.0f;
-                if constexpr (BIAS) s_qb[i] += live ? du[i] : 0.0f;
             }
+            if (live)
+#pragma unroll
+                for (int i = 0; i < NV; ++i) {
+                    s_qw[i] += du[i] * v[i];
+                    if constexpr (BIAS) s_qb[i] += du[i];
+                }
         }
         float t[2] = {0.0f, 0.0f};
         if (a.h) {
@@ -464,14 +473,19 @@ __global__ __launch_bounds__(row_block<G>()) void residual_grad_rows_k(ResidualA
             for (int i = 0; i < NV; ++i) {
                 const float e = a.alpha * d[i];
                 Gate gt{1.0f, 0.0f};
-                if (a.gate) gt = gate_of(gv[i], a.act);
+                if (a.gate) gt = N == 1 ? kept[i % KEPT] : gate_of(gv[i], a.act);
                 v[i] = e * gt.a;
                 du[i] = e * (h[i] * pw[i] + pb[i]) * gt.da;
-                s_pw[i] += live ? v[i] * h[i] : 0.0f;
-                if constexpr (BIAS) s_pb[i] += live ? v[i] : 0.0f;
-                if constexpr (GATE_ROW) s_g[i] += live ? du[i] : 0.0f;
-                v[i] *= pw[i];
             }
+            if (live)
+#pragma unroll
+                for (int i = 0; i < NV; ++i) {
+                    s_pw[i] += v[i] * h[i];
+                    if constexpr (BIAS) s_pb[i] += v[i];
+                    if constexpr (GATE_ROW) s_g[i] += du[i];
+                }
+#pragma unroll
+            for (int i = 0; i < NV; ++i) v[i] *= pw[i];
             if (a.post != CSGS_NORM_NONE) {
                 t[0] = c.sum([&](int i) { return v[i] * h[i]; });
                 t[1] = a.post == CSGS_NORM_LAYER ? c.sum([&](int i) { return v[i]; }) : 0.0f;
@@ -486,7 +500,7 @@ __global__ __launch_bounds__(row_block<G>()) void residual_grad_rows_k(ResidualA
             if (g.dgate && a.ldg) c.store((TB *)g.dgate + r * g.lddg, du);
             if (g.dh) {
 #pragma unroll
-                for (int i = 0; i < NV; ++i) v[i] = hs.r * (v[i] - t[1] - h[i] * t[0]);
+                for (int i = 0; i < NV; ++i) v[i] = a.post != CSGS_NORM_NONE ? hs.r * (v[i] - t[1] - h[i] * t[0]) : v[i];
                 c.store((TB *)g.dh + r * g.lddh, v);
             }
         }
@@ -616,8 +630,8 @@ template <typename TS, typename TB>
 static int launch_residual_grad(const ResidualArgs &a, const ResidualGrad &g, hipStream_t st)
 {
     int blocks = col_blocks(a.M);
-    const bool done = with_layout<4>(a.F, [&](auto lanes, auto pieces, auto ragged) {
-        constexpr int G = decltype(lanes)::value, N = decltype(pieces)::value, ROWS = row_block<G>() / G;
+    auto launch = [&](auto values, auto lanes, auto pieces, auto ragged) {
+        constexpr int V = decltype(values)::value, G = decltype(lanes)::value, N = decltype(pieces)::value, ROWS = row_block<G>() / G;
         constexpr bool R = decltype(ragged)::value;
         const int64_t need = ((int64_t)a.M + ROWS - 1) / ROWS;
         constexpr int MOST = grad_blocks<G, N>();
@@ -625,12 +639,28 @@ static int launch_residual_grad(const ResidualArgs &a, const ResidualGrad &g, hi
         blocks = (int)(need < MOST ? need : MOST);
         const dim3 grid((unsigned)blocks), block(row_block<G>());
         const bool bias = g.want[COL_POST_B] || g.want[COL_PRE_B], row = g.want[COL_GATE];
-        if (bias && row) CSGS_LAUNCH(K_RESIDUAL_GRAD, (residual_grad_rows_k<TS, TB, 4, G, N, R, true, true>), grid, block, st, a, g);
-        else if (bias) CSGS_LAUNCH(K_RESIDUAL_GRAD, (residual_grad_rows_k<TS, TB, 4, G, N, R, true, false>), grid, block, st, a, g);
-        else if (row) CSGS_LAUNCH(K_RESIDUAL_GRAD, (residual_grad_rows_k<TS, TB, 4, G, N, R, false, true>), grid, block, st, a, g);
-        else CSGS_LAUNCH(K_RESIDUAL_GRAD, (residual_grad_rows_k<TS, TB, 4, G, N, R, false, false>), grid, block, st, a, g);
-    });
-    if (!done) CSGS_LAUNCH(K_RESIDUAL_GRAD, (residual_grad_k<TS, TB>), dim3((unsigned)blocks), dim3(RES_BLOCK), st, a, g);
+        if (bias && row) CSGS_LAUNCH(K_RESIDUAL_GRAD, (residual_grad_rows_k<TS, TB, V, G, N, R, true, true>), grid, block, st, a, g);
+        else if (bias) CSGS_LAUNCH(K_RESIDUAL_GRAD, (residual_grad_rows_k<TS, TB, V, G, N, R, true, false>), grid, block, st, a, g);
+        else if (row) CSGS_LAUNCH(K_RESIDUAL_GRAD, (residual_grad_rows_k<TS, TB, V, G, N, R, false, true>), grid, block, st, a, g);
+        else CSGS_LAUNCH(K_RESIDUAL_GRAD, (residual_grad_rows_k<TS, TB, V, G, N, R, false, false>), grid, block, st, a, g);
+    };
+    using std::integral_constant;
+    // Rows of bfloat16 alone that 16 to 64 lanes hold in one piece of eight (us, pieces of four / eight: 131072 rows of 64 33.5 / 37.5, of 100 66 / 58, of
+    // 250 158 / 128; 65536 of 512 136 / 123; 32768 of 1000 160 / 171).
+    if constexpr (sizeof(TS) == 2) {
+        if (a.F > 64 && a.F <= 512) {
+            auto eight = [&](auto lanes) {
+                if (a.F % 8) launch(integral_constant<int, 8>{}, lanes, integral_constant<int, 1>{}, std::true_type{});
+                else launch(integral_constant<int, 8>{}, lanes, integral_constant<int, 1>{}, std::false_type{});
+            };
+            if (a.F <= 128) eight(integral_constant<int, 16>{});
+            else if (a.F <= 256) eight(integral_constant<int, 32>{});
+            else eight(integral_constant<int, 64>{});
+            return blocks;
+        }
+    }
+    if (!with_layout<4>(a.F, [&](auto lanes, auto pieces, auto ragged) { launch(integral_constant<int, 4>{}, lanes, pieces, ragged); }))
+        CSGS_LAUNCH(K_RESIDUAL_GRAD, (residual_grad_k<TS, TB>), dim3((unsigned)blocks), dim3(RES_BLOCK), st, a, g);
     return blocks;
 }
 

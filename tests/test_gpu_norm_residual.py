@@ -8,7 +8,7 @@ torch = pytest.importorskip("torch")
 import plain_operators as plain
 
 TYPES = {"f32": (torch.float32, torch.float32), "bf16": (torch.bfloat16, torch.bfloat16), "mixed": (torch.float32, torch.bfloat16)}
-SHAPES = [(1, 1), (1, 64), (3, 2), (5, 17), (256, 64), (77, 100), (300, 256), (130, 602), (41, 1024), (9, 1500), (65, 2047), (4, 4096), (3, 9001), (2, 40000)]
+SHAPES = [(1, 1), (1, 64), (3, 2), (5, 17), (256, 64), (77, 100), (300, 256), (130, 602), (23, 333), (40, 512), (41, 1024), (9, 1500), (65, 2047), (4, 4096), (3, 9001), (2, 40000)]
 
 
 @pytest.fixture(scope="module")
@@ -329,3 +329,13 @@ def test_recorded_calls(env):
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(got, (out, y[:50], u[:50], dx[:50], dh[:50], dw)))
         assert torch.equal(out, 2.0 * table.flip(0))
+
+
+@pytest.mark.parametrize("F", [3, 100, 9000])
+def test_without_a_norm_nothing_is_divided_by(env, F):
+    """No norm before the gate: the gradient of h does not depend on h, whatever it holds."""
+    csgs, dev = env
+    c = Case(csgs, dev, 9, F, "f32", post="none", pre="none", act="sigmoid", gate="row", du=False)
+    want = c.backward()["dh"].clone()
+    c.h[2, 1], c.h[3, 0], c.h[4] = float("inf"), float("nan"), float("-inf")
+    assert torch.equal(c.backward()["dh"], want)
