@@ -526,7 +526,7 @@ typedef struct csgs_residual {
 /* y [M x F] of x_dtype, leading dimension ldy, nullable; u [M x F] of h_dtype, ldu, nullable (pre = CSGS_NORM_NONE: must be
  * NULL); one of the two is needed.  An output may be an input of the same type at the same address with the same leading dimension (y = x,
  * u = h); other overlaps are not allowed.  A row depends on its own rows of x, h and gate alone.  fp32, one rounding per output.
- * Host errors: CSGS_EINVAL, CSGS_EUNSUPPORTED (types). */
+ * Host errors: CSGS_EINVAL, CSGS_EUNSUPPORTED (types, F above 2^30). */
 int csgs_norm_residual(const csgs_residual *r /*host*/, void *y, int64_t ldy, void *u, int64_t ldu, void *stream);
 
 /* Gradients of csgs_norm_residual from dy = dL/dy [M x F] of x_dtype (nullable: 0) and du = dL/du [M x F] of h_dtype

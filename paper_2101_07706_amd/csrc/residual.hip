@@ -8,7 +8,8 @@
 // The gradient forms everything again from the forward's inputs: reading x again costs the same bytes as reading y, and no statistics need
 // be kept.  Row sums, statistics and everything between are in fp32, one rounding per output.  Both directions move a few bytes per operation:
 // bound by memory where there are many rows (us and TB/s of what has to move; a large copy reaches 4.8 to 5.2: 131072 rows of 256 floats 126, 5.3; gradient
-// of 65536 rows of 1024, stream in floats, block in bfloat16, 279, 5.3; of 16384 rows of 2048 floats 205, 5.2; of 8192 rows of 4096 in bfloat16 180, 3.0),
+// of 65536 rows of 1024, stream in floats, block in bfloat16, 279, 5.3; of 16384 rows of 2048 floats 202, 5.3; of 8192 rows of 4096 in bfloat16 138, 3.9; of
+// 4096 rows of 8192 floats 269, 4.0),
 // by the latency of a row's loads and of four to six sums over it one after the other where there are few (256 rows of 64 3.1; gradient of 8192
 // rows of 256 18.4, of 1999 rows of 602 16.6, two launches each).
 #include "common.hpp"
@@ -97,7 +98,7 @@ struct Row {
     __device__ float y(int32_t f) const { return a.beta * x(f) + (a.h ? a.alpha * gate(f).a * n(f) : 0.0f); }
 };
 
-// A block takes a row and reads it from memory or the caches each time it is needed (4096 rows of 8192 floats 371 us, rows in registers 144).
+// A block takes a row and reads it from memory or the caches each time it is needed (4096 rows of 8192 floats 371 us, rows in registers 137).
 template <typename TS, typename TB>
 __global__ __launch_bounds__(RES_BLOCK) void residual_k(ResidualArgs a, TS *y, int64_t ldy, TB *u, int64_t ldu)
 {
@@ -312,9 +313,10 @@ enum { COL_POST_W = 0, COL_POST_B, COL_PRE_W, COL_PRE_B, COL_GATE, COL_KINDS };
 constexpr int COL_BLOCKS = 1024;   // most blocks
 __host__ inline int col_blocks(int32_t M) { return M < COL_BLOCKS ? M : COL_BLOCKS; }
 // Blocks of the gradient with rows in registers: about as many as the device holds at a time, by the registers that N pieces take (us, 256 / 512 /
-// 1024 / 1536 blocks: 8192 rows of 256, a piece a lane, 21.7 / 19.0 / 19.2 / 22.2; 1999 rows of 602, three pieces, 16.9 / 17.6 / 17.8 / 17.8).
+// 1024 / 1536 blocks: 8192 rows of 256, a piece a lane, 21.7 / 19.0 / 19.2 / 22.2; 1999 rows of 602, three pieces, 16.9 / 17.6 / 17.8 / 17.8; 256 / 512:
+// 8192 rows of 4096, 512 lanes, 194 / 205).
 template <int G, int N>
-constexpr int grad_blocks() { return (G > WAVE && N == 1) || G < 32 ? 1024 : (N >= 3 ? 256 : 512); }
+constexpr int grad_blocks() { return (G > WAVE && N == 1) || G < 32 ? 1024 : (G == 512 || (G == 64 && N >= 3) ? 256 : 512); }
 
 struct ResidualGrad {
     const void *dy, *du;
@@ -388,7 +390,7 @@ __global__ __launch_bounds__(RES_BLOCK) void residual_grad_k(ResidualArgs a, Res
 
 // The same with the row in registers.  BIAS: sums of post_b or pre_b are wanted; GATE_ROW: those of a gate for all rows.
 template <typename TS, typename TB, int V, int G, int N, bool RAGGED, bool BIAS, bool GATE_ROW>
-__global__ __launch_bounds__(row_block<G>()) void residual_grad_rows_k(ResidualArgs a, ResidualGrad g)
+__global__ __launch_bounds__(row_block<G>(), 2) void residual_grad_rows_k(ResidualArgs a, ResidualGrad g)
 {
     constexpr int NV = N * V, ROWS = row_block<G>() / G;
     __shared__ float lds[4 * row_block<G>() / WAVE];
@@ -397,10 +399,26 @@ __global__ __launch_bounds__(row_block<G>()) void residual_grad_rows_k(ResidualA
     const int32_t M = resolve_count(a.M, a.M_dev);
     const Cols<V, G, N, RAGGED> c{a.F, (int)threadIdx.x % G};
     const float inv_F = 1.0f / (float)a.F;
-    float pw[NV], pb[NV], qw[NV], gv[NV], s_pw[NV], s_pb[BIAS ? NV : 1], s_qw[NV], s_qb[BIAS ? NV : 1], s_g[GATE_ROW ? NV : 1];
-    c.load_or(pw, a.post_w, 1.0f);
-    c.load_or(pb, a.post_b, 0.0f);
-    c.load_or(qw, a.pre_w, 1.0f);
+    // (the vectors' weights: in registers, or of rows of many pieces in LDS, where each lane reads what it wrote: 24 to 48 registers fewer, of at most 256
+    // that let a block of 512 be there at all and two of 256.  8192 rows of 4096 in bfloat16 217 us, 141 so)
+    constexpr bool IN_LDS = G > WAVE && N >= 3;
+    __shared__ float held[IN_LDS ? 3 : 1][IN_LDS ? G * NV : 1];
+    float pw[IN_LDS ? 1 : NV], pb[IN_LDS ? 1 : NV], qw[IN_LDS ? 1 : NV], gv[NV], s_pw[NV], s_pb[BIAS ? NV : 1], s_qw[NV], s_qb[BIAS ? NV : 1], s_g[GATE_ROW ? NV : 1];
+    auto place = [&](int i) { return i / V * (G * V) + (int)threadIdx.x % G * V + i % V; };
+    auto keep = [&](auto &reg, int k, const float *row, float otherwise) {
+        if constexpr (IN_LDS) {
+            float t[NV];
+            c.load_or(t, row, otherwise);
+#pragma unroll
+            for (int i = 0; i < NV; ++i) held[k][place(i)] = t[i];
+        } else c.load_or(reg, row, otherwise);
+    };
+    keep(pw, 0, a.post_w, 1.0f);
+    keep(pb, 1, a.post_b, 0.0f);
+    keep(qw, 2, a.pre_w, 1.0f);
+    auto post_w = [&](int i) { if constexpr (IN_LDS) return held[0][place(i)]; else return pw[i]; };
+    auto post_b = [&](int i) { if constexpr (IN_LDS) return held[1][place(i)]; else return pb[i]; };
+    auto pre_w = [&](int i) { if constexpr (IN_LDS) return held[2][place(i)]; else return qw[i]; };
     c.load_or(gv, a.gate && !a.ldg ? (const float *)a.gate : nullptr, 0.0f);
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
@@ -442,7 +460,7 @@ __global__ __launch_bounds__(row_block<G>()) void residual_grad_rows_k(ResidualA
             for (int i = 0; i < NV; ++i) {
                 v[i] = a.x ? a.beta * v[i] : 0.0f;
                 if (a.h) {
-                    const float n = h[i] * pw[i] + pb[i];
+                    const float n = h[i] * post_w(i) + post_b(i);
                     v[i] += a.alpha * (a.gate ? (N == 1 ? kept[i % KEPT] : gate_of(gv[i], a.act)).a * n : n);
                 }
             }
@@ -450,14 +468,14 @@ __global__ __launch_bounds__(row_block<G>()) void residual_grad_rows_k(ResidualA
 #pragma unroll
             for (int i = 0; i < NV; ++i) v[i] = (v[i] - s.m) * s.r;              // hat(y)
             float t[2];
-            t[0] = c.sum([&](int i) { return du[i] * qw[i] * v[i]; });
-            t[1] = a.pre == CSGS_NORM_LAYER ? c.sum([&](int i) { return du[i] * qw[i]; }) : 0.0f;
+            t[0] = c.sum([&](int i) { return du[i] * pre_w(i) * v[i]; });
+            t[1] = a.pre == CSGS_NORM_LAYER ? c.sum([&](int i) { return du[i] * pre_w(i); }) : 0.0f;
             row_sums<G>(t, lds, turn);
             t[0] *= inv_F;
             t[1] *= inv_F;
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
-                d[i] += s.r * (du[i] * qw[i] - t[1] - v[i] * t[0]);
+                d[i] += s.r * (du[i] * pre_w(i) - t[1] - v[i] * t[0]);
             }
             if (live)
 #pragma unroll
@@ -475,7 +493,7 @@ __global__ __launch_bounds__(row_block<G>()) void residual_grad_rows_k(ResidualA
                 Gate gt{1.0f, 0.0f};
                 if (a.gate) gt = N == 1 ? kept[i % KEPT] : gate_of(gv[i], a.act);
                 v[i] = e * gt.a;
-                du[i] = e * (h[i] * pw[i] + pb[i]) * gt.da;
+                du[i] = e * (h[i] * post_w(i) + post_b(i)) * gt.da;
             }
             if (live)
 #pragma unroll
@@ -485,7 +503,7 @@ __global__ __launch_bounds__(row_block<G>()) void residual_grad_rows_k(ResidualA
                     if constexpr (GATE_ROW) s_g[i] += du[i];
                 }
 #pragma unroll
-            for (int i = 0; i < NV; ++i) v[i] *= pw[i];
+            for (int i = 0; i < NV; ++i) v[i] *= post_w(i);
             if (a.post != CSGS_NORM_NONE) {
                 t[0] = c.sum([&](int i) { return v[i] * h[i]; });
                 t[1] = a.post == CSGS_NORM_LAYER ? c.sum([&](int i) { return v[i]; }) : 0.0f;
@@ -573,7 +591,7 @@ static int open_residual(const csgs_residual *r, ResidualArgs *a)
         r->pre < CSGS_NORM_NONE || r->pre > CSGS_NORM_LAYER || r->gate_act < CSGS_GATE_LINEAR || r->gate_act > CSGS_GATE_SILU)
         return CSGS_EINVAL;
     const bool same = r->x_dtype == r->h_dtype && (r->x_dtype == CSGS_F32 || r->x_dtype == CSGS_BF16);
-    if (!same && !(r->x_dtype == CSGS_F32 && r->h_dtype == CSGS_BF16)) return CSGS_EUNSUPPORTED;
+    if ((!same && !(r->x_dtype == CSGS_F32 && r->h_dtype == CSGS_BF16)) || r->F > 1 << 30) return CSGS_EUNSUPPORTED;   // (a column and a block's step in 32 bits)
     *a = ResidualArgs{r->M, r->F, r->M_dev, r->x, r->h, r->gate, r->ldx, r->ldh, r->gate ? r->ldg : 0, r->post_w, r->post_b, r->pre_w, r->pre_b,
                       r->post, r->pre, r->gate_act, r->eps, r->alpha, r->beta};
     if (a->post == CSGS_NORM_NONE) a->post_w = a->post_b = nullptr;
@@ -582,10 +600,13 @@ static int open_residual(const csgs_residual *r, ResidualArgs *a)
 }
 
 // Calls f with the row's layout as constants: lanes, pieces a lane, and whether the width is no multiple of a piece.  As few lanes as hold the row
-// in one piece, then up to three pieces a lane, then a block per row: with four pieces a lane the gradient takes 280 registers and a unit
-// holds one wavefront (us, gradient: 65536 rows of 1024, 64 lanes with four pieces 302, 256 with one 289; 1999 rows of 602, 64 with three 16.9, 256 with
-// one 21; 8192 rows of 4096 in bfloat16, 256 with four 217, 512 with two 180; 131072 rows of 16, 16 lanes, four of them busy, 32, 4 lanes 21).
-template <int V, typename F>
+// in one piece, then up to three pieces a lane, then a block per row, of as few lanes: what counts there is how many rows a compute unit holds (us,
+// gradient: 65536 rows of 1024, 64 lanes with four pieces 302, 256 with one 289; 1999 rows of 602, 64 with three 16.9, 256 with one 21; 8192 rows of 2500
+// floats, 512 lanes with two 175, 256 with three 135; 8192 of 5000, 1024 with two 1021, spilling, 512 with three 283; 4096 of 8192, 1024 with two 569, 512
+// with four 269; 131072 rows of 16, 16 lanes, four of them busy, 32, 4 lanes 21).  FOUR: 256 lanes with four pieces rather than 512 with two, where
+// the registers suffice: the gradient with a block of bfloat16 and no bias (8192 rows of 4096 in bfloat16 138 for 175, with a bias 210 for 176; floats 245
+// for 221).
+template <int V, bool FOUR, typename F>
 static bool with_layout(int32_t width, F f)
 {
     if (width < V) return false;
@@ -606,15 +627,19 @@ static bool with_layout(int32_t width, F f)
     if (pieces <= 192) return go(integral_constant<int, 64>{}, integral_constant<int, 3>{});
     if (pieces <= 256) return go(integral_constant<int, 256>{}, integral_constant<int, 1>{});
     if (pieces <= 512) return go(integral_constant<int, 256>{}, integral_constant<int, 2>{});
+    if (pieces <= 768) return go(integral_constant<int, 256>{}, integral_constant<int, 3>{});
+    if constexpr (FOUR)
+        if (pieces <= 1024) return go(integral_constant<int, 256>{}, integral_constant<int, 4>{});
     if (pieces <= 1024) return go(integral_constant<int, 512>{}, integral_constant<int, 2>{});
-    if (pieces <= 2048) return go(integral_constant<int, 1024>{}, integral_constant<int, 2>{});
+    if (pieces <= 1536) return go(integral_constant<int, 512>{}, integral_constant<int, 3>{});
+    if (pieces <= 2048) return go(integral_constant<int, 512>{}, integral_constant<int, 4>{});
     return false;
 }
 
 template <typename TS, typename TB>
 static void launch_residual(const ResidualArgs &a, void *y, int64_t ldy, void *u, int64_t ldu, hipStream_t st)
 {
-    const bool done = with_layout<4>(a.F, [&](auto lanes, auto pieces, auto ragged) {
+    const bool done = with_layout<4, false>(a.F, [&](auto lanes, auto pieces, auto ragged) {
         constexpr int G = decltype(lanes)::value, N = decltype(pieces)::value;
         constexpr int ROWS = row_block<G>() / G;
         const int64_t need = ((int64_t)a.M + ROWS - 1) / ROWS;
@@ -630,6 +655,7 @@ template <typename TS, typename TB>
 static int launch_residual_grad(const ResidualArgs &a, const ResidualGrad &g, hipStream_t st)
 {
     int blocks = col_blocks(a.M);
+    const bool bias = g.want[COL_POST_B] || g.want[COL_PRE_B], row = g.want[COL_GATE];
     auto launch = [&](auto values, auto lanes, auto pieces, auto ragged) {
         constexpr int V = decltype(values)::value, G = decltype(lanes)::value, N = decltype(pieces)::value, ROWS = row_block<G>() / G;
         constexpr bool R = decltype(ragged)::value;
@@ -638,10 +664,12 @@ static int launch_residual_grad(const ResidualArgs &a, const ResidualGrad &g, hi
         static_assert(MOST <= COL_BLOCKS, "room for the sums");
         blocks = (int)(need < MOST ? need : MOST);
         const dim3 grid((unsigned)blocks), block(row_block<G>());
-        const bool bias = g.want[COL_POST_B] || g.want[COL_PRE_B], row = g.want[COL_GATE];
-        if (bias && row) CSGS_LAUNCH(K_RESIDUAL_GRAD, (residual_grad_rows_k<TS, TB, V, G, N, R, true, true>), grid, block, st, a, g);
-        else if (bias) CSGS_LAUNCH(K_RESIDUAL_GRAD, (residual_grad_rows_k<TS, TB, V, G, N, R, true, false>), grid, block, st, a, g);
-        else if (row) CSGS_LAUNCH(K_RESIDUAL_GRAD, (residual_grad_rows_k<TS, TB, V, G, N, R, false, true>), grid, block, st, a, g);
+        if constexpr (!(G == 256 && N == 4)) {
+            if (bias && row) CSGS_LAUNCH(K_RESIDUAL_GRAD, (residual_grad_rows_k<TS, TB, V, G, N, R, true, true>), grid, block, st, a, g);
+            else if (bias) CSGS_LAUNCH(K_RESIDUAL_GRAD, (residual_grad_rows_k<TS, TB, V, G, N, R, true, false>), grid, block, st, a, g);
+            if (bias) return;
+        }
+        if (row) CSGS_LAUNCH(K_RESIDUAL_GRAD, (residual_grad_rows_k<TS, TB, V, G, N, R, false, true>), grid, block, st, a, g);
         else CSGS_LAUNCH(K_RESIDUAL_GRAD, (residual_grad_rows_k<TS, TB, V, G, N, R, false, false>), grid, block, st, a, g);
     };
     using std::integral_constant;
@@ -659,7 +687,10 @@ static int launch_residual_grad(const ResidualArgs &a, const ResidualGrad &g, hi
             return blocks;
         }
     }
-    if (!with_layout<4>(a.F, [&](auto lanes, auto pieces, auto ragged) { launch(integral_constant<int, 4>{}, lanes, pieces, ragged); }))
+    auto four = [&](auto lanes, auto pieces, auto ragged) { launch(integral_constant<int, 4>{}, lanes, pieces, ragged); };
+    bool done = false;
+    if constexpr (sizeof(TB) == 2) done = !bias && with_layout<4, true>(a.F, four);
+    if (!done && !with_layout<4, false>(a.F, four))
         CSGS_LAUNCH(K_RESIDUAL_GRAD, (residual_grad_k<TS, TB>), dim3((unsigned)blocks), dim3(RES_BLOCK), st, a, g);
     return blocks;
 }

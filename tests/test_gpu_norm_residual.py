@@ -339,3 +339,17 @@ def test_without_a_norm_nothing_is_divided_by(env, F):
     want = c.backward()["dh"].clone()
     c.h[2, 1], c.h[3, 0], c.h[4] = float("inf"), float("nan"), float("-inf")
     assert torch.equal(c.backward()["dh"], want)
+
+
+@pytest.mark.parametrize("types", list(TYPES))
+@pytest.mark.parametrize("bias", [False, True])
+@pytest.mark.parametrize("gate", ["row", "full"])
+@pytest.mark.parametrize("F", [2049, 2052, 2999, 3508, 4095, 4100, 6001, 6148, 8190])
+def test_wide_rows(env, F, gate, bias, types):
+    Case(*env, 5, F, types, post="layer", pre="rms", act="silu", gate=gate, bias=bias).check()
+
+
+@pytest.mark.parametrize("types", list(TYPES))
+@pytest.mark.parametrize("F", [2500, 4096, 5000, 8192])
+def test_several_wide_rows_a_block(env, F, types):
+    Case(*env, 1100, F, types, post="rms", pre="layer", act="sigmoid", gate="full", count=1060).check()

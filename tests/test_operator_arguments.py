@@ -134,3 +134,11 @@ def test_binding_refuses_what_it_cannot_describe():
                 lambda: csgs.make_grad_list([ok], [torch.zeros(4, 5)]), lambda: csgs.make_grad_list([torch.zeros(5)], None, [ids[:1]])):
         with pytest.raises((AssertionError, TypeError)):
             bad()
+
+
+def test_norm_residual_wider_than_its_indices():
+    L = csgs.lib()
+    wide = (1 << 31) - 1
+    r = dict(F=wide - 100, ldx=wide, ldh=wide, ldg=wide)
+    assert L.csgs_norm_residual(C.byref(residual(**r)), P, wide, P, wide, Z) == csgs.EUNSUPPORTED
+    assert L.csgs_norm_residual_grad(C.byref(residual(**r)), P, wide, P, wide, P, wide, P, wide, P, wide, P, Z, Z, Z, P, 1 << 60, Z) == csgs.EUNSUPPORTED
