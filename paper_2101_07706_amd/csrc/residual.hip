@@ -150,7 +150,7 @@ __device__ inline float lanes_sum(float v)
     }
     return v;
 }
-// Sums of K values over a row's lanes; with G = 256 over the block, through LDS (turn: the two halves of `lds` in turn, so that one barrier a
+// Sums of K values over a row's lanes; with G above 64 over the block, through LDS (turn: the two halves of `lds` in turn, so that one barrier a
 // sum is enough).
 template <int G, int K>
 __device__ inline void row_sums(float (&v)[K], float *lds /*[2][G / WAVE][2]*/, int &turn)
@@ -172,9 +172,9 @@ __device__ inline void row_sums(float (&v)[K], float *lds /*[2][G / WAVE][2]*/, 
         }
     }
 }
-// Threads of a block: rows of up to 256 lanes share one.
+// Threads of a block: rows of up to 64 lanes share one.
 template <int G>
-constexpr int row_block() { return G > RES_BLOCK ? G : RES_BLOCK; }
+constexpr int row_block() { return G > WAVE ? G : RES_BLOCK; }
 
 // The columns that a lane holds: piece n begins at col(n); its first skip(n) values belong to the piece before.
 template <int V, int G, int N, bool RAGGED>
@@ -316,7 +316,7 @@ __host__ inline int col_blocks(int32_t M) { return M < COL_BLOCKS ? M : COL_BLOC
 // 1024 / 1536 blocks: 8192 rows of 256, a piece a lane, 21.7 / 19.0 / 19.2 / 22.2; 1999 rows of 602, three pieces, 16.9 / 17.6 / 17.8 / 17.8; 256 / 512:
 // 8192 rows of 4096, 512 lanes, 194 / 205).
 template <int G, int N>
-constexpr int grad_blocks() { return (G > WAVE && N == 1) || G < 32 ? 1024 : (G == 512 || (G == 64 && N >= 3) ? 256 : 512); }
+constexpr int grad_blocks() { return (G > WAVE && N == 1) || G == 128 || G < 32 ? 1024 : (G == 512 || (G == 64 && N >= 3) ? 256 : 512); }
 
 struct ResidualGrad {
     const void *dy, *du;
@@ -600,13 +600,15 @@ static int open_residual(const csgs_residual *r, ResidualArgs *a)
 }
 
 // Calls f with the row's layout as constants: lanes, pieces a lane, and whether the width is no multiple of a piece.  As few lanes as hold the row
-// in one piece, then up to three pieces a lane, then a block per row, of as few lanes: what counts there is how many rows a compute unit holds (us,
-// gradient: 65536 rows of 1024, 64 lanes with four pieces 302, 256 with one 289; 1999 rows of 602, 64 with three 16.9, 256 with one 21; 8192 rows of 2500
-// floats, 512 lanes with two 175, 256 with three 135; 8192 of 5000, 1024 with two 1021, spilling, 512 with three 283; 4096 of 8192, 1024 with two 569, 512
-// with four 269; 131072 rows of 16, 16 lanes, four of them busy, 32, 4 lanes 21).  FOUR: 256 lanes with four pieces rather than 512 with two, where
-// the registers suffice: the gradient with a block of bfloat16 and no bias (8192 rows of 4096 in bfloat16 138 for 175, with a bias 210 for 176; floats 245
-// for 221).
-template <int V, bool FOUR, typename F>
+// in one piece, then up to three pieces a lane, then a block per row, of as few lanes as that takes: what counts there is how many rows a compute unit
+// holds and how many lanes have nothing to do (us, gradient: 1999 rows of 602, 64 lanes with three pieces 16.9, 256 with one 21; 24000 rows of 1100 in
+// bfloat16, 256 lanes with two 207, 128 with three 146, floats 200 / 181; 8192 rows of 2500 floats, 512 with two 175, 256 with three 135; 8192 of 5000,
+// 1024 with two 1021, spilling, 512 with three 283; 4096 of 8192, 1024 with two 569, 512 with four 269; 131072 rows of 16, 16 lanes, four of them
+// busy, 32, 4 lanes 21).
+// ONE: 256 lanes with one piece rather than 128 with two, the gradient with a block of bfloat16 (65536 rows of 1024 in bfloat16 239 and 256, in floats
+// 457 and 413; forward 150 and 136, 274 and 266).  FOUR: 256 lanes with four pieces rather than 512 with two, where the registers suffice: the
+// gradient with a block of bfloat16 and no bias (8192 rows of 4096 in bfloat16 138 and 175, with a bias 210 and 176; floats 245 and 221).
+template <int V, bool ONE, bool FOUR, typename F>
 static bool with_layout(int32_t width, F f)
 {
     if (width < V) return false;
@@ -625,7 +627,10 @@ static bool with_layout(int32_t width, F f)
     if (pieces <= 64) return go(integral_constant<int, 64>{}, integral_constant<int, 1>{});
     if (pieces <= 128) return go(integral_constant<int, 64>{}, integral_constant<int, 2>{});
     if (pieces <= 192) return go(integral_constant<int, 64>{}, integral_constant<int, 3>{});
-    if (pieces <= 256) return go(integral_constant<int, 256>{}, integral_constant<int, 1>{});
+    if constexpr (ONE)
+        if (pieces <= 256) return go(integral_constant<int, 256>{}, integral_constant<int, 1>{});
+    if (pieces <= 256) return go(integral_constant<int, 128>{}, integral_constant<int, 2>{});
+    if (pieces <= 384) return go(integral_constant<int, 128>{}, integral_constant<int, 3>{});
     if (pieces <= 512) return go(integral_constant<int, 256>{}, integral_constant<int, 2>{});
     if (pieces <= 768) return go(integral_constant<int, 256>{}, integral_constant<int, 3>{});
     if constexpr (FOUR)
@@ -639,7 +644,7 @@ static bool with_layout(int32_t width, F f)
 template <typename TS, typename TB>
 static void launch_residual(const ResidualArgs &a, void *y, int64_t ldy, void *u, int64_t ldu, hipStream_t st)
 {
-    const bool done = with_layout<4, false>(a.F, [&](auto lanes, auto pieces, auto ragged) {
+    const bool done = with_layout<4, false, false>(a.F, [&](auto lanes, auto pieces, auto ragged) {
         constexpr int G = decltype(lanes)::value, N = decltype(pieces)::value;
         constexpr int ROWS = row_block<G>() / G;
         const int64_t need = ((int64_t)a.M + ROWS - 1) / ROWS;
@@ -689,8 +694,8 @@ static int launch_residual_grad(const ResidualArgs &a, const ResidualGrad &g, hi
     }
     auto four = [&](auto lanes, auto pieces, auto ragged) { launch(integral_constant<int, 4>{}, lanes, pieces, ragged); };
     bool done = false;
-    if constexpr (sizeof(TB) == 2) done = !bias && with_layout<4, true>(a.F, four);
-    if (!done && !with_layout<4, false>(a.F, four))
+    if constexpr (sizeof(TB) == 2) done = !bias && with_layout<4, true, true>(a.F, four);
+    if (!done && !with_layout<4, sizeof(TB) == 2, false>(a.F, four))
         CSGS_LAUNCH(K_RESIDUAL_GRAD, (residual_grad_k<TS, TB>), dim3((unsigned)blocks), dim3(RES_BLOCK), st, a, g);
     return blocks;
 }

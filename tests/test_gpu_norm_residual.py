@@ -353,3 +353,10 @@ def test_wide_rows(env, F, gate, bias, types):
 @pytest.mark.parametrize("F", [2500, 4096, 5000, 8192])
 def test_several_wide_rows_a_block(env, F, types):
     Case(*env, 1100, F, types, post="rms", pre="layer", act="sigmoid", gate="full", count=1060).check()
+
+
+@pytest.mark.parametrize("types", list(TYPES))
+@pytest.mark.parametrize("bias,gate", [(False, "full"), (True, "row")])
+@pytest.mark.parametrize("M,F", [(5, 769), (1100, 1000), (5, 1024), (5, 1025), (2100, 1300), (5, 1531), (5, 1536), (5, 1537)])
+def test_rows_of_two_wavefronts(env, M, F, bias, gate, types):
+    Case(*env, M, F, types, post="rms", pre="layer", act="silu", gate=gate, bias=bias).check()
