@@ -11,7 +11,7 @@
 // of 65536 rows of 1024, stream in floats, block in bfloat16, 279, 5.3; of 16384 rows of 2048 floats 202, 5.3; of 8192 rows of 4096 in bfloat16 138, 3.9; of
 // 4096 rows of 8192 floats 269, 4.0),
 // by the latency of a row's loads and of four to six sums over it one after the other where there are few (256 rows of 64 3.1; gradient of 8192
-// rows of 256 18.4, of 1999 rows of 602 16.6, two launches each).
+// rows of 256 17.4, of 1999 rows of 602 15.7, two launches each).
 #include "common.hpp"
 #include "row_pieces.hpp"
 
