@@ -626,10 +626,30 @@ def csgs_norm_residual_grad(x, h, dy, du, dx, dh, dgate, dpost_w, dpost_b, dpre_
           _f32(dpost_b, F), _f32(dpre_w, F), _f32(dpre_b, F), ptr, nbytes, _stream(stream))
 
 
+def _torch_stream(stream):
+    """The stream as torch knows it; None: the current one."""
+    if stream is None:
+        return torch.cuda.current_stream()
+    return stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(stream.cuda_stream)
+
+
+def _list_on(l, stream):
+    """A list as an argument of a call on `stream`.  Its buffer is no tensor that the caller holds: torch is told, once for every stream that it is used on, not to
+    hand the memory out again before what is enqueued there by the time the list is dropped has run."""
+    streams = getattr(l, "_streams", None)     # (a list that make_grad_list has not made brings memory of its own)
+    if streams is not None:
+        handle = _stream(stream)
+        if handle not in streams:
+            l._keep[0].record_stream(_torch_stream(stream))
+            streams.add(handle)
+    return C.byref(l)
+
+
 def make_grad_list(grads, outs=None, rows_dev=None, stream=None) -> GradList:
     """A list of gradients for csgs_grad_norm / _scale / _clip, described once in device memory.  outs: where the clipped gradients go (None: in
     place; entries may be None); rows_dev: per gradient, a device int32 with the number of rows that count, or None.
-    The list keeps the tensors; they must not be resized or freed by other means."""
+    The list keeps the tensors; they must not be resized or freed by other means.  It may be dropped while calls that use it are still enqueued: its own buffer
+    comes from the pool of `stream` and is given back when these are done, on whatever streams they are (the gradients are the caller's, as in every call)."""
     outs = grads if outs is None else outs
     rows_dev = [None] * len(grads) if rows_dev is None else rows_dev
     assert len(grads) > 0 and len(outs) == len(grads) and len(rows_dev) == len(grads)
@@ -647,27 +667,28 @@ def make_grad_list(grads, outs=None, rows_dev=None, stream=None) -> GradList:
     nbytes = int(lib().csgs_grad_list_bytes(ts, len(grads)))
     if nbytes == 0:
         raise CsgsError(EINVAL, "csgs_grad_list_bytes")
-    buf = torch.empty(nbytes // 8, dtype=torch.int64, device=grads[0].device)
+    with torch.cuda.stream(stream if stream is None else _torch_stream(stream)):     # (memory that this stream's earlier work may still use, and no other's)
+        buf = torch.empty(nbytes // 8, dtype=torch.int64, device=grads[0].device)
     l = GradList(buf.data_ptr(), nbytes, 0, 0, 0)
+    l._keep, l._streams = (buf, list(grads), list(outs), list(rows_dev)), {_stream(stream)}
     _call("csgs_grad_list_init", C.byref(l), ts, len(grads), _stream(stream))
-    l._keep = (buf, list(grads), list(outs), list(rows_dev))
     return l
 
 
 def csgs_grad_norm(l, kind, total, stream=None):
     """total: float64 tensor of one entry; receives the sum of squares, of absolute values, or the largest of these."""
     assert total.dtype == torch.float64
-    _call("csgs_grad_norm", C.byref(l), kind, _ptr(total), _stream(stream))
+    _call("csgs_grad_norm", _list_on(l, stream), kind, _ptr(total), _stream(stream))
 
 
 def csgs_grad_scale(l, kind, total, max_norm, norm=None, status=None, stream=None):
     assert total.dtype == torch.float64
-    _call("csgs_grad_scale", C.byref(l), kind, _ptr(total), max_norm, _f32(norm, 1), _i32(status), _stream(stream))
+    _call("csgs_grad_scale", _list_on(l, stream), kind, _ptr(total), max_norm, _f32(norm, 1), _i32(status), _stream(stream))
 
 
 def csgs_grad_clip(l, kind, max_norm, norm=None, status=None, stream=None):
     """out = min(1, max_norm / (total + 1e-6)) g over the list; norm receives the total before clipping."""
-    _call("csgs_grad_clip", C.byref(l), kind, max_norm, _f32(norm, 1), _i32(status), _stream(stream))
+    _call("csgs_grad_clip", _list_on(l, stream), kind, max_norm, _f32(norm, 1), _i32(status), _stream(stream))
 
 
 def csgs_profile_enable(on: bool):

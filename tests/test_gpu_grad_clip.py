@@ -213,3 +213,44 @@ def test_calls_on_a_recorded_plan(env):
     assert float(norm) == total
     plan.run()
     assert abs(float(norm) - total * 1e-3 / (total + 1e-6)) <= 1e-7
+
+
+@pytest.mark.parametrize("used_on", ["its own stream", "another"])
+def test_a_list_dropped_while_its_calls_are_enqueued(env, used_on):
+    """Made, used and dropped on side streams that are busy, while the current stream clears memory of the same size that was freed before and takes more of it
+    after.  (Descriptions that such work clears describe nothing: outputs then keep their NaN.)"""
+    csgs, dev = env
+    grads = make(LISTS["gaps"], dev, seed=6)
+    outs = [torch.full_like(g, float("nan")) for g in grads]
+    norm, total = torch.full((1,), -1.0, device=dev), total_of(grads, "l2")
+    long = [torch.empty(1 << 28, dtype=torch.float32, device=dev) for _ in range(3)]
+    words = csgs.make_grad_list(grads, outs)._keep[0].numel()
+    side, other = torch.cuda.Stream(), torch.cuda.Stream()
+    torch.cuda.synchronize()
+
+    def keep_busy(t):
+        for _ in range(20):      # 1 GB each
+            t.fill_(1.0)
+
+    freed = [torch.empty(words, dtype=torch.int64, device=dev) for _ in range(32)]
+    keep_busy(long[0])
+    for t in freed:
+        t.zero_()
+    del freed, t
+    with torch.cuda.stream(side):
+        keep_busy(long[1])
+    l = csgs.make_grad_list(grads, outs, stream=side)
+    last = side
+    if used_on == "another":
+        last = other
+        other.wait_stream(side)
+        with torch.cuda.stream(other):
+            keep_busy(long[2])
+    csgs.csgs_grad_clip(l, csgs.GRAD_L2, 0.5 * total, norm, stream=last)
+    del l
+    taken = [torch.zeros(words, dtype=torch.int64, device=dev) for _ in range(32)]
+    with torch.cuda.stream(side):
+        taken += [torch.zeros(words, dtype=torch.int64, device=dev) for _ in range(32)]
+    torch.cuda.synchronize()
+    assert abs(float(norm) - total) <= 2.0 ** -23 * total
+    check_clipped(grads, outs, total, float(torch.tensor(0.5 * total, dtype=torch.float32)))
