@@ -486,7 +486,7 @@ int csgs_embed(const void *T, int64_t ld, int64_t rows, int32_t F, int dtype, co
  *   uniq [n] out: the different ids inside [0, rows), ascending; *n_uniq of them; dR [n x F] of `d_dtype`, leading dimension
  *   ldd: row j is the gradient of row uniq[j].  Entries past *n_uniq are left untouched.
  * scratch: device, 256-byte aligned, csgs_embed_grad_scratch_bytes(n, rows, F) bytes (0 on bad input); nothing in it needs to
- *   be kept or cleared between calls.
+ *   be kept or cleared between calls.  The size does not fall as n, rows or F grow: a buffer for the largest call serves all.
  * Host errors: CSGS_EINVAL, CSGS_EWORKSPACE, CSGS_EUNSUPPORTED (dtype; n or rows above 2^31 - 1).
  */
 size_t csgs_embed_grad_scratch_bytes(int64_t n, int64_t rows, int32_t F);

@@ -86,6 +86,18 @@ struct EmbedScratch {
     double *part;                // [chunks][2][F] sums of rows that go on across chunks
     size_t bytes;
 };
+// Room for the parts of n positions, [chunks][2][F] doubles, and of fewer or narrower ones: a buffer for the largest call serves the smaller ones, though
+// these may have more chunks (a share doubles where there is enough to do).  F ceil(n / chunk) <= n F / chunk + F, and with the smallest lanes of all types
+//     a chunk is never shorter than 8 positions times 256 / lanes,
+//     one whose share is at its most never shorter than 128 positions,
+//     any other share c has n F < 2 c (2^20 + F), which leaves n F / chunk < (2^20 + F) lanes / 128 <= (2^20 + F) / 2.
+// Each bound grows with n and with F.
+__host__ inline size_t part_doubles(int64_t n, int32_t F)
+{
+    const int64_t shortest = n * F / (8 * SUM_BLOCK / sum_lanes(F, 4)), at_most = n * F / 128, other = ((1 << 20) + (int64_t)F) / 2;
+    const int64_t any = at_most > other ? at_most : other;
+    return 2 * (size_t)((shortest < any ? shortest : any) + F + 1);
+}
 __host__ inline EmbedScratch carve_embed(void *base, int64_t n, int32_t F)
 {
     EmbedScratch s;
@@ -100,8 +112,7 @@ __host__ inline EmbedScratch carve_embed(void *base, int64_t n, int32_t F)
     s.heads = (uint32_t *)take(sizeof(uint32_t) * SORT_TILES);
     s.n_valid = (int32_t *)take(4);
     s.rank = (uint32_t *)take((size_t)n * 4);
-    const int32_t chunk = share_of(n, F) * (SUM_BLOCK / sum_lanes(F, 4));   // (the smallest of all types)
-    s.part = (double *)take(sizeof(double) * 2 * (size_t)((n + chunk - 1) / chunk) * (size_t)F);
+    s.part = (double *)take(sizeof(double) * part_doubles(n, F));
     s.bytes = off;
     return s;
 }

@@ -283,3 +283,19 @@ def test_few_positions_of_a_long_table(env, rows, F, d_dtype):
         G = torch.randn(n, F, generator=torch.Generator().manual_seed(9)).to(dev)
         for extra in (0, 3):
             check_grad(run_grad(csgs, dev, ids, G, rows, 1.0, DTYPES[d_dtype], extra=extra), ids, G, rows, 1.0)
+
+
+@pytest.mark.parametrize("F,sized_for,n", [(1024, 32768, 32767), (1024, 16384, 16383), (512, 65536, 65535), (100, 200_000, 167_000), (256, 4096, 3000)])
+def test_scratch_sized_for_a_larger_call(env, F, sized_for, n):
+    """Exactly the bytes that the larger call asks for serve the smaller one, which stays within them."""
+    csgs, dev = env
+    rows = 300
+    nbytes = csgs.csgs_embed_grad_scratch_bytes(sized_for, rows, F)
+    raw = torch.full((nbytes + 4096,), 0xA5, dtype=torch.uint8, device=dev)
+    ids = make_ids(n, rows, "half", n)
+    G = torch.randn(n, F, generator=torch.Generator().manual_seed(3)).to(dev)
+    dT = torch.full((rows, F), float("nan"), device=dev)
+    csgs.csgs_embed_grad(ids.to(dev), G, dT, raw[:nbytes])
+    keys, want, mag = plain.embed_grad(ids, G.cpu(), rows, 1.0)
+    plain.check(dT.cpu()[torch.from_numpy(keys)], torch.from_numpy(want), torch.from_numpy(mag), 1e-2, "dense")
+    assert bool((raw[nbytes:] == 0xA5).all()), "wrote past the scratch"

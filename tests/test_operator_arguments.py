@@ -142,3 +142,35 @@ def test_norm_residual_wider_than_its_indices():
     r = dict(F=wide - 100, ldx=wide, ldh=wide, ldg=wide)
     assert L.csgs_norm_residual(C.byref(residual(**r)), P, wide, P, wide, Z) == csgs.EUNSUPPORTED
     assert L.csgs_norm_residual_grad(C.byref(residual(**r)), P, wide, P, wide, P, wide, P, wide, P, wide, P, Z, Z, Z, P, 1 << 60, Z) == csgs.EUNSUPPORTED
+
+
+def part_doubles_needed(n, F, bf16):
+    """What the sums of a call leave for the joins: two rows of F doubles a chunk (the library's share of a group, and lanes that take a row)."""
+    most = 16 if F <= 128 else 32 if F <= 256 else 64
+    share = 8
+    while share < most and n // (2 * share) * F >= 1 << 20:
+        share *= 2
+    V = 8 if bf16 else 4
+    lanes = 16 if F <= 16 * V else 32 if F <= 32 * V else 64
+    chunk = share * (256 // lanes)
+    return 2 * F * ((n + chunk - 1) // chunk)
+
+
+@pytest.mark.parametrize("F", [1, 3, 16, 33, 64, 65, 100, 128, 129, 256, 257, 512, 602, 1024, 5000, 1 << 20])
+def test_scratch_for_the_largest_table_gradient_serves_smaller_ones(F):
+    size = csgs.csgs_embed_grad_scratch_bytes
+    around = {1, 2, 7, 2048, 2049, 98_304, 98_305, 1 << 20, (1 << 31) - 1}
+    for share in (8, 16, 32):                   # where a share doubles
+        n = 2 * share * -(-(1 << 20) // F)
+        around |= {n - 1, n, n + 1, n // 2, 3 * n}
+    ns = sorted(n for n in around if 0 < n < 1 << 31)
+    sizes = [size(n, 1000, F) for n in ns]
+    assert all(a <= b for a, b in zip(sizes, sizes[1:])), list(zip(ns, sizes))
+    for n in ns:
+        assert size(n, 1, F) <= size(n, 1 << 30, F)
+        assert size(n, 1000, F) <= size(n, 1000, F + 1), n
+        for bf16 in (False, True):
+            assert size(n, 1000, F) >= n * 20 + 8 * part_doubles_needed(n, F, bf16), n
+    # and no more than the positions and the rows that are summed take
+    for n in ns:
+        assert size(n, 1000, F) <= 20 * n + (n + 64) * F * 4 + (1 << 20), n
