@@ -360,3 +360,59 @@ def test_several_wide_rows_a_block(env, F, types):
 @pytest.mark.parametrize("M,F", [(5, 769), (1100, 1000), (5, 1024), (5, 1025), (2100, 1300), (5, 1531), (5, 1536), (5, 1537)])
 def test_rows_of_two_wavefronts(env, M, F, bias, gate, types):
     Case(*env, M, F, types, post="rms", pre="layer", act="silu", gate=gate, bias=bias).check()
+
+
+@pytest.mark.parametrize("act", ["sigmoid", "silu"])
+@pytest.mark.parametrize("gate", ["row", "full"])
+@pytest.mark.parametrize("F", [3, 100, 1000, 6000])
+def test_gates_open_and_shut(env, F, gate, act):
+    """The gate itself and its derivative, to a number of roundings of their own size (y = a(g), dgate = a'(g) for h = dy = 1 without norms): an ulp each of the
+    exponential and the reciprocal, the operations between them, |g| / 20 for the constant that the exponential's argument is formed with."""
+    csgs, dev = env
+    special = torch.tensor([0.0, -0.0, 1e-30, -1e-30, 8.0, -8.0, 12.0, -12.0, 16.7, -16.7, 17.5, -17.5, 20.0, -20.0, 40.0, -40.0, 80.0, -80.0, 1e4, -1e4, 1e30, -1e30])
+    g = torch.randn(4096, generator=torch.Generator().manual_seed(F)) * 10
+    g[:2000] = torch.linspace(-80, 80, 2000)
+    g[2000:2000 + len(special)] = special
+    M = (len(g) + F - 1) // F
+    g = torch.cat([g, torch.zeros(M * F - len(g))]).view(M, F)
+    one, y, dg = torch.ones(1, F, device=dev), [], []
+    scratch = torch.empty(csgs.csgs_norm_residual_grad_scratch_bytes(M, F), dtype=torch.uint8, device=dev)
+    kw = dict(gate_act=csgs.GATE_SIGMOID if act == "sigmoid" else csgs.GATE_SILU, post=csgs.NORM_NONE, pre=csgs.NORM_NONE)
+    none = [None] * 4
+    if gate == "full":
+        one, gates = torch.ones(M, F, device=dev), [g.to(dev)]
+    else:
+        gates = [row.to(dev) for row in g]
+    for v in gates:
+        y.append(torch.empty_like(one))
+        dg.append(torch.empty_like(v))
+        csgs.csgs_norm_residual(None, one, y[-1], None, gate=v, **kw)
+        csgs.csgs_norm_residual_grad(None, one, one, None, None, None, dg[-1], *none, scratch, gate=v, **kw)
+    y, dg = torch.cat(y).double().cpu(), torch.cat([t.view(-1, F) for t in dg]).double().cpu()
+    g = g.double()
+    s, rest = 1 / (1 + torch.exp(-g)), 1 / (1 + torch.exp(g))
+    share = g.abs().clamp(max=100) / 20
+    if act == "sigmoid":
+        checks = [("gate", y, s, s, 8 + share), ("derivative", dg, s * rest, s * rest, 13 + share)]
+    else:
+        checks = [("gate", y, g * s, (g * s).abs(), 9 + share), ("derivative", dg, s * (1 + g * rest), s * (1 + g.abs() * rest), 18 + 2 * share)]
+    for what, got, want, mag, roundings_ in checks:
+        tol = roundings_ * 2.0 ** -24 * mag + 2e-36      # (below 2^-126, and up to |g| times that, nothing is left)
+        worst = ((got - want).abs() / tol)
+        at = int(worst.argmax())
+        assert float(worst.max()) <= 1.0, f"{what}: error {float(worst.max()):.2f} times its bound at g = {float(g.view(-1)[at])}"
+
+
+@pytest.mark.parametrize("F", [3, 100, 6000])
+def test_gates_that_are_not_finite(env, F):
+    csgs, dev = env
+    inf = float("inf")
+    g = torch.full((3, F), inf, device=dev)
+    g[1], g[2] = -inf, float("nan")
+    one, y, dg = torch.ones(3, F, device=dev), torch.empty(3, F, device=dev), torch.empty(3, F, device=dev)
+    scratch = torch.empty(csgs.csgs_norm_residual_grad_scratch_bytes(3, F), dtype=torch.uint8, device=dev)
+    kw = dict(gate=g, gate_act=csgs.GATE_SIGMOID, post=csgs.NORM_NONE, pre=csgs.NORM_NONE)
+    csgs.csgs_norm_residual(None, one, y, None, **kw)
+    csgs.csgs_norm_residual_grad(None, one, one, None, None, None, dg, None, None, None, None, scratch, **kw)
+    assert bool((y[0] == 1).all()) and bool((y[1] == 0).all()) and bool(torch.isnan(y[2]).all())
+    assert bool((dg[:2] == 0).all()) and bool(torch.isnan(dg[2]).all())
