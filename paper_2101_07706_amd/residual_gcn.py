@@ -32,7 +32,8 @@ from . import csgs, pipeline, synth
 
 class ResidualGCN:
     """Parameters, buffers and one training step.  The gradients of a step are left in .grads, the table's in .table_rows, .table_ids and
-    .table_count."""
+    .table_count; .norm and .status tell of the last clipping, .skipped how many steps were left out because their gradients were not finite (all on
+    the device)."""
 
     def __init__(self, dg, width, n_classes, n_layers, batch, samples, skew, adj_cap, seed=0, max_norm=1.0, lr=0.1, beta=0.5, gate_act=csgs.GATE_SIGMOID):
         dev = self.device = dg.device
@@ -67,7 +68,7 @@ class ResidualGCN:
         self.logits = torch.zeros(batch, n_classes, dtype=f32, device=dev)
         self.table_rows, self.table_ids = torch.zeros(total, D, dtype=f32, device=dev), torch.zeros(total, dtype=torch.int32, device=dev)
         self.table_count, self.row_place = torch.zeros(1, dtype=torch.int32, device=dev), torch.arange(total, dtype=torch.int32, device=dev)
-        self.norm, self.status = torch.zeros(1, dtype=f32, device=dev), torch.zeros(1, dtype=torch.int32, device=dev)
+        self.norm, self.status, self.skipped = torch.zeros(1, dtype=f32, device=dev), *(torch.zeros(1, dtype=torch.int32, device=dev) for _ in range(2))
         # scratch of the gradient calls; they follow each other on one stream
         nbytes = max([csgs.csgs_embed_grad_scratch_bytes(total, dg.n_nodes, D), csgs.csgs_aggregate_grad_scratch_bytes(samples, self.lbs[0].adj_col.numel()),
                       csgs.csgs_layer_gemm_grad_w_scratch_bytes(n_max, D, max(D, n_classes)), csgs.csgs_layer_gemm_grad_w_scratch_bytes(n_max, D, n_classes)]
@@ -124,13 +125,17 @@ class ResidualGCN:
         csgs.csgs_embed_grad_rows(self.ids, self.dX, self.dg.n_nodes, self.table_ids, self.table_count, self.table_rows, self.scratch, scale=self.scale)
 
     def clip(self):
+        self.status.zero_()      # (calls only set bits)
         csgs.csgs_grad_clip(self.list, csgs.GRAD_L2, self.max_norm, self.norm, self.status)
 
     def descend(self):
-        """A step of gradient descent on all parameters."""
+        """A step of gradient descent on all parameters.  Clipping makes NaN of gradients whose norm is not finite: such a step changes nothing.  Decided on the
+        device, from the status and not from the norm, which as a float may be infinite where the total is not."""
+        finite = (self.status & csgs.ST_NONFINITE_GRAD) == 0
+        self.skipped += ~finite
         for k, p in self.params.items():
-            p.sub_(self.grads[k], alpha=self.lr)
-        live = self.row_place < self.table_count
+            p.sub_(torch.where(finite, self.grads[k], 0.0), alpha=self.lr)
+        live = (self.row_place < self.table_count) & finite
         step = torch.where(live.unsqueeze(1), self.table_rows, torch.zeros(1, device=self.device))
         self.table.index_add_(0, torch.where(live, self.table_ids, 0).long(), step, alpha=-self.lr)
 
@@ -163,8 +168,10 @@ def main():
         torch.cuda.synchronize()
         t = time.perf_counter()
         loss = float(net.step(S0, labels, it))
-        print(f"step {it}: loss {loss:.4f}, gradient norm {float(net.norm):.4f}, rows of the table {int(net.table_count)}, {1e3 * (time.perf_counter() - t):.2f} ms", flush=True)
-    assert int(net.status) == 0 and all(int(lb.status) == 0 for lb in net.lbs), "a call reported an error"
+        ms = 1e3 * (time.perf_counter() - t)
+        print(f"step {it}: loss {loss:.4f}, gradient norm {float(net.norm):.4f}, rows of the table {int(net.table_count)}, {ms:.2f} ms"
+              + (", not taken" if int(net.status) else ""), flush=True)
+    assert int(net.skipped) == 0 and all(int(lb.status) == 0 for lb in net.lbs), "a call reported an error"
 
 
 if __name__ == "__main__":

@@ -124,3 +124,46 @@ def test_steps_repeat(env):
     for k in a[0].grads:
         assert torch.equal(a[0].grads[k], b[0].grads[k]), k
     assert torch.equal(a[0].table_rows, b[0].table_rows) and torch.equal(a[0].table_ids, b[0].table_ids) and torch.equal(a[0].norm, b[0].norm)
+
+
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), float("-inf")])
+def test_a_step_without_finite_gradients_changes_nothing(env, bad):
+    csgs, pipeline, residual_gcn = env
+    g, net, S0 = make(residual_gcn, pipeline, 48)
+    G = torch.randn(100, 5, device=S0.device) / 100
+
+    def step(G, it):
+        net.forward(S0, it)
+        net.backward(G)
+        net.clip()
+        net.descend()
+
+    weights = lambda: [net.table.clone()] + [v.clone() for v in net.params.values()]
+    step(G, 0)
+    before = weights()
+    wrong = G.clone()
+    wrong[7, 2] = bad
+    for it in (1, 2):
+        step(wrong, it)
+        assert int(net.status) == csgs.ST_NONFINITE_GRAD and int(net.skipped) == it
+        assert all(torch.equal(a.view(torch.int32), b.view(torch.int32)) for a, b in zip(before, weights()))
+    # the next one is an ordinary step again
+    step(G, 3)
+    after = weights()
+    assert int(net.status) == 0 and int(net.skipped) == 2
+    assert all(bool(torch.isfinite(t).all()) for t in after) and not any(torch.equal(a, b) for a, b in zip(before, after))
+
+
+def test_a_norm_past_a_float_is_not_a_bad_step(env):
+    """Gradients of finite numbers are clipped and taken, also where their norm is no float."""
+    csgs, pipeline, residual_gcn = env
+    g, net, S0 = make(residual_gcn, pipeline, 48)
+    net.forward(S0, 0)
+    net.backward(torch.zeros(100, 5, device=S0.device))
+    net.grads["w_out"].fill_(3e38)
+    before = net.params["w_out"].clone()
+    net.clip()
+    assert float(net.norm) == math.inf and int(net.status) == 0
+    net.descend()
+    moved = before - net.params["w_out"]
+    assert int(net.skipped) == 0 and bool((moved > 0).all()) and abs(float((moved / net.lr).double().norm()) - net.max_norm) < 1e-3
