@@ -215,7 +215,7 @@ __global__ __launch_bounds__(256) void grad_scale_k(GradMem m, int64_t tiles, in
     }
     auto give = [&](auto v, auto *out) {
 #pragma unroll
-        for (float &x : v.x) x = (float)(coef * (double)x);
+        for (float &x : v.x) x = float_to_store<std::remove_pointer_t<decltype(out)>>(coef * (double)x);
         if constexpr (PAST) store_row_past_caches(out, v);
         else store_row(out, v);
     };

@@ -754,14 +754,14 @@ __device__ inline void write_sum(const SumOut &o, uint32_t row, const Piece1<V> 
     if (pc.skip == 0) {
         if (o.accumulate) v = load_row<TD, V>(d);
 #pragma unroll
-        for (int i = 0; i < V; ++i) v.x[i] = (float)(acc[i] * (double)o.scale + (double)v.x[i]);
+        for (int i = 0; i < V; ++i) v.x[i] = float_to_store<TD>(acc[i] * (double)o.scale + (double)v.x[i]);
         store_row<TD, V>(d, v);
     } else {
 #pragma unroll
         for (int i = 0; i < V; ++i)
             if (i >= pc.skip) {
                 const float old = o.accumulate ? load_row<TD, 1>(d + i).x[0] : 0.0f;
-                store_row<TD, 1>(d + i, Vec<1>{{(float)(acc[i] * (double)o.scale + (double)old)}});
+                store_row<TD, 1>(d + i, Vec<1>{{float_to_store<TD>(acc[i] * (double)o.scale + (double)old)}});
             }
     }
 }

@@ -117,6 +117,13 @@ struct RawPiece {
 
 // The same the other way: a row's values to memory, bfloat16 by rounding to nearest even (NaN stays NaN).
 __device__ inline uint32_t bf16_bits(float x) { return (uint32_t)__builtin_bit_cast(uint16_t, (__bf16)x); }
+// A double as the float that store_row is given for it, rounded once: for bfloat16 to one of its numbers, which store_row then keeps as it is.
+template <typename T>
+__device__ inline float float_to_store(double d)
+{
+    if constexpr (sizeof(T) == 4) return (float)d;
+    return (float)(__bf16)d;
+}
 template <typename T, int V>
 __device__ inline void store_row(T *p, const Vec<V> &v)
 {
