@@ -254,3 +254,44 @@ def test_a_list_dropped_while_its_calls_are_enqueued(env, used_on):
     torch.cuda.synchronize()
     assert abs(float(norm) - total) <= 2.0 ** -23 * total
     check_clipped(grads, outs, total, float(torch.tensor(0.5 * total, dtype=torch.float32)))
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_rows_with_gaps_longer_than_a_tile(env, dtype, kind):
+    """A tile of a tensor with gaps between its rows that lies in two of them, or in the middle of one."""
+    csgs, dev = env
+    grads, outs = [], []
+    for rows, cols, gap in ((5, 20_000, 3), (3, 8193, 1), (2, 30_001, 8), (40, 8192, 5), (9, 4097, 7)):
+        g = torch.full((rows, cols + gap), float("nan"), dtype=dtype, device=dev)[:, :cols]
+        g.copy_(torch.randn(rows, cols, generator=torch.Generator().manual_seed(cols)) * 0.1)
+        grads.append(g)
+        outs.append(torch.full((rows, cols + gap + 1), -5.0, dtype=dtype, device=dev)[:, :cols])
+    total = total_of(grads, kind)
+    norm = torch.zeros(1, device=dev)
+    csgs.csgs_grad_clip(csgs.make_grad_list(grads, outs), kind_of(csgs, kind), 0.5 * total, norm)
+    assert abs(float(norm) - total) <= 2.0 ** -23 * total
+    check_clipped(grads, outs, total, float(torch.tensor(0.5 * total, dtype=torch.float32)))
+    for o in outs:                      # nothing between the rows
+        whole = o.as_strided((o.shape[0] - 1, o.stride(0)), (o.stride(0), 1))
+        assert bool((whole[:, o.shape[1]:] == -5.0).all())
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("in_place", [False, True])
+def test_lists_longer_than_the_caches(env, dtype, in_place):
+    """More than 2^26 entries, whose outputs go past the caches: whole pieces, what is left of one, tensors off any alignment, rows with gaps."""
+    csgs, dev = env
+    g = torch.Generator(device=dev).manual_seed(3)
+    mk = lambda *s: torch.randn(*s, generator=g, device=dev).mul_(0.01).to(dtype)
+    grads = [mk((1 << 26) + 5), mk(8195)[1:], mk(3, 701)[:, :700], mk(1)]
+    grads.append(grads[0].new_empty(50_003)[3:].copy_(mk(50_000)))
+    before = [t.clone() for t in grads]
+    outs = grads if in_place else [torch.full_like(t, float("nan")) for t in grads]
+    total, norm = total_of(before, "l2"), torch.zeros(1, device=dev)
+    l = csgs.make_grad_list(grads, outs)
+    csgs.csgs_grad_clip(l, csgs.GRAD_L2, 0.3 * total, norm)
+    assert abs(float(norm) - total) <= 2.0 ** -23 * total
+    check_clipped(before, outs, total, float(torch.tensor(0.3 * total, dtype=torch.float32)))
+    if not in_place:
+        assert all(torch.equal(a, b) for a, b in zip(before, grads))

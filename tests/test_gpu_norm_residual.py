@@ -416,3 +416,53 @@ def test_gates_that_are_not_finite(env, F):
     csgs.csgs_norm_residual_grad(None, one, one, None, None, None, dg, None, None, None, None, scratch, **kw)
     assert bool((y[0] == 1).all()) and bool((y[1] == 0).all()) and bool(torch.isnan(y[2]).all())
     assert bool((dg[:2] == 0).all()) and bool(torch.isnan(dg[2]).all())
+
+
+# rows of fewer columns than a piece and of more than a block's registers hold are walked over in memory
+WALKED = [1, 2, 3, 8193, 9000]
+
+
+@pytest.mark.parametrize("types", list(TYPES))
+@pytest.mark.parametrize("M,count", [(40, 0), (40, 1), (40, 39), (40, 400), (40, -5), (1100, 1060)])
+def test_walked_rows_up_to_a_device_count(env, M, count, types):
+    for F in (3, 9000) if M < 1000 else (2, 8193):
+        Case(*env, M, F, types, post="layer", pre="rms", act="silu", gate="row" if M < 1000 else "full", count=count).check()
+
+
+@pytest.mark.parametrize("types", ["f32", "bf16"])
+@pytest.mark.parametrize("F", WALKED)
+def test_walked_rows_in_place(env, F, types):
+    csgs, dev = env
+    for gate in ("full", "row"):
+        c = Case(csgs, dev, 50, F, types, post="layer", pre="rms", act="silu", gate=gate)
+        y, u = c.forward()
+        o = c.backward()
+        h, x = c.h.clone(), c.x.clone()
+        csgs.csgs_norm_residual(x, h, x, h, **c.args())
+        assert torch.equal(x, y) and torch.equal(h, u)
+        for onto in ("du", "h"):             # where the gradient of h goes
+            dy, du, h, kw = c.dy.clone(), c.du.clone(), c.h.clone(), c.args()
+            kw["gate"] = c.gate.clone()
+            dh = du if onto == "du" else h
+            scratch = torch.empty(csgs.csgs_norm_residual_grad_scratch_bytes(50, F), dtype=torch.uint8, device=dev)
+            vec = [torch.empty(F, device=dev) for _ in range(4)]
+            dgate = kw["gate"] if gate == "full" else torch.empty(F, device=dev)
+            csgs.csgs_norm_residual_grad(c.x, h, dy, du, dy, dh, dgate, *vec, scratch, **kw)
+            assert torch.equal(dy, o["dx"]) and torch.equal(dh, o["dh"]) and torch.equal(dgate, o["dgate"])
+            for v, k in zip(vec, ("dpost_w", "dpost_b", "dpre_w", "dpre_b")):
+                assert torch.equal(v, o[k]), k
+
+
+@pytest.mark.parametrize("F", [3, 9000])
+@pytest.mark.parametrize("x,h,dy,du", [(True, False, True, True), (False, True, True, True), (True, True, True, False), (True, True, False, True), (True, False, False, True),
+                                       (False, True, False, True)])
+def test_absent_parts_of_walked_rows(env, F, x, h, dy, du):
+    for types in ("f32", "mixed"):
+        Case(*env, 19, F, types, post="layer", pre="layer", act="sigmoid", gate="full" if h else "none", x=x, h=h, dy=dy, du=du).check()
+
+
+@pytest.mark.parametrize("post,pre", [("none", "rms"), ("none", "layer"), ("rms", "none"), ("layer", "none"), ("none", "none")])
+@pytest.mark.parametrize("F", [3, 8193])
+def test_walked_rows_without_a_norm(env, F, post, pre):
+    for gate in ("none", "row", "full"):
+        Case(*env, 9, F, "mixed", post=post, pre=pre, act="sigmoid", gate=gate, bias=F == 3, weights=F != 3).check()

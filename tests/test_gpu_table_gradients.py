@@ -299,3 +299,29 @@ def test_scratch_sized_for_a_larger_call(env, F, sized_for, n):
     keys, want, mag = plain.embed_grad(ids, G.cpu(), rows, 1.0)
     plain.check(dT.cpu()[torch.from_numpy(keys)], torch.from_numpy(want), torch.from_numpy(mag), 1e-2, "dense")
     assert bool((raw[nbytes:] == 0xA5).all()), "wrote past the scratch"
+
+
+@pytest.mark.parametrize("g_dtype,d_dtype,extra", [("f32", "f32", 0), ("bf16", "bf16", 3), ("f32", "bf16", 1), ("bf16", "f32", 5)])
+@pytest.mark.parametrize("count", [0, 1, 65_536, 98_304, 131_071, 200_000, -7])
+def test_many_positions_up_to_a_device_count(env, count, g_dtype, d_dtype, extra):
+    """The sort by digits with a count of its own, ids outside the table among those that count, and rows that start anywhere."""
+    csgs, dev = env
+    n, rows, F = 131_072, 3000, 9
+    ids = make_ids(n, rows, "steep", 11)
+    m = max(0, min(count, n))
+    G = strided(n, F, extra, DTYPES[g_dtype], dev)
+    G.copy_(torch.randn(n, F, generator=torch.Generator().manual_seed(12)))
+    G[m:] = float("inf")
+    G[((ids < 0) | (ids >= rows)).to(dev)] = float("nan")
+    out = run_grad(csgs, dev, ids, G, rows, 1.3, DTYPES[d_dtype], n_dev=torch.tensor([count], dtype=torch.int32, device=dev), extra=extra)
+    check_grad(out, ids, G, rows, 1.3, m)
+
+
+@pytest.mark.parametrize("g_dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n,F,rows,dist", [(131_072, 300, 900, "steep"), (262_144, 160, 40, "half"), (131_072, 600, 700, "steep"), (98_304, 1000, 300, "half"), (131_072, 520, 131_072, "uniform")])
+def test_long_shares(env, n, F, rows, dist, g_dtype):
+    """Groups whose share of a chunk is 32 positions (the first two) and 64, of many positions of wide rows."""
+    csgs, dev = env
+    ids = make_ids(n, rows, dist, n + F)
+    G = torch.randn(n, F, generator=torch.Generator().manual_seed(13)).to(DTYPES[g_dtype]).to(dev)
+    check_grad(run_grad(csgs, dev, ids, G, rows, 1.0, torch.float32), ids, G, rows, 1.0)
