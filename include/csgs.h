@@ -465,7 +465,7 @@ int csgs_aggregate_grad(const int32_t *adj_rowptr, const int32_t *adj_col, const
  * rows looks them up once more):
  *     out[t, 0..F) = scale * T[ids[t], 0..F)     for t < n; a row of zeros where ids[t] is outside [0, rows)
  * T [rows x F] of `dtype`, out [n x F] of `out_dtype` (CSGS_F32 or CSGS_BF16 each), leading dimensions ld and ldo in
- * elements; rows start on any element.  Computed in fp32, one rounding.  n up to 2^31 - 1; n_dev as everywhere (rows of out
+ * elements; rows start on any element.  The product is a float; a bfloat16 output is rounded from that.  n up to 2^31 - 1; n_dev as everywhere (rows of out
  * past the device count are left untouched).
  * Host errors: CSGS_EINVAL, CSGS_EUNSUPPORTED.
  */
@@ -584,7 +584,8 @@ int csgs_grad_list_init(csgs_grad_list *l /*host*/, const csgs_grad_tensor *t /*
  * fixed order; a NaN anywhere makes each of them NaN.  The halves of csgs_grad_clip, for gradients that lie on several GPUs:
  * totals are added (CSGS_GRAD_MAX: their maximum taken) between the two calls. */
 int csgs_grad_norm(const csgs_grad_list *l /*host*/, int kind, double *total, void *stream);
-/* out = c g for every tensor with an out, from such a total.  norm (device float, nullable) receives the norm.  Where c = 1, tensors
+/* out = c g for every tensor with an out, from such a total.  norm (device float, nullable) receives the norm (infinite also where a
+ * finite total is past a float's range: it is *status that tells of the total).  Where c = 1, tensors
  * that are their own output are not written.  A total that is NaN or infinite gives c = NaN or 0 by the formula and sets CSGS_ST_NONFINITE_GRAD in
  * *status (nullable): a caller that then skips its step keeps its weights.
  * Host errors: CSGS_EINVAL (also max_norm <= 0 or NaN; +infinity: nothing is clipped). */

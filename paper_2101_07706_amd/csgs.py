@@ -649,7 +649,8 @@ def make_grad_list(grads, outs=None, rows_dev=None, stream=None) -> GradList:
     """A list of gradients for csgs_grad_norm / _scale / _clip, described once in device memory.  outs: where the clipped gradients go (None: in
     place; entries may be None); rows_dev: per gradient, a device int32 with the number of rows that count, or None.
     The list keeps the tensors; they must not be resized or freed by other means.  It may be dropped while calls that use it are still enqueued: its own buffer
-    comes from the pool of `stream` and is given back when these are done, on whatever streams they are (the gradients are the caller's, as in every call)."""
+    comes from the pool of `stream` and is given back when these are done, on whatever streams they are (the gradients are the caller's, as in every call).  A
+    plan keeps the list; one that was captured into a graph has to be kept as long as the graph is replayed."""
     outs = grads if outs is None else outs
     rows_dev = [None] * len(grads) if rows_dev is None else rows_dev
     assert len(grads) > 0 and len(outs) == len(grads) and len(rows_dev) == len(grads)

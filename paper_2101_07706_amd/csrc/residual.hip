@@ -7,11 +7,11 @@
 //     dpost_w = sum over rows of dn .* hat(h),  dpost_b = sum dn,  dpre_w = sum du .* hat(y),  dpre_b = sum du.
 // The gradient forms everything again from the forward's inputs: reading x again costs the same bytes as reading y, and no statistics need
 // be kept.  Row sums, statistics and everything between are in fp32, one rounding per output.  Both directions move a few bytes per operation:
-// bound by memory where there are many rows (us and TB/s of what has to move; a large copy reaches 4.8 to 5.2: 131072 rows of 256 floats 126, 5.3; gradient
-// of 65536 rows of 1024, stream in floats, block in bfloat16, 279, 5.3; of 16384 rows of 2048 floats 202, 5.3; of 8192 rows of 4096 in bfloat16 138, 3.9; of
-// 4096 rows of 8192 floats 269, 4.0),
+// bound by memory where there are many rows (us and TB/s of what has to move; a large copy reaches 4.8 to 5.2: 131072 rows of 256 floats 129, 5.2; gradient
+// of 65536 rows of 1024, stream in floats, block in bfloat16, 290, 5.1; of 16384 rows of 2048 floats 201, 5.3; of 8192 rows of 4096 in bfloat16 143, 3.8; of
+// 4096 rows of 8192 floats 282, 3.8),
 // by the latency of a row's loads and of four to six sums over it one after the other where there are few (256 rows of 64 3.1; gradient of 8192
-// rows of 256 17.4, of 1999 rows of 602 15.7, two launches each).
+// rows of 256 17.9, of 1999 rows of 602 15.9, two launches each).  Times that stand beside a choice below are those it was made by; the present gates take 1.4 % more.
 #include "common.hpp"
 #include "row_pieces.hpp"
 
