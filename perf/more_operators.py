@@ -227,8 +227,8 @@ def prepare(case, seed):
     if op == "adamw":
         es = s["entries"]
         s["clip"] = csgs.make_grad_list([e["g"] for e in es], [None] * len(es), [e["n"] for e in es])
-        s["list"] = csgs.make_adamw_list([csgs.adamw_entry(e["p"], e["g"], e["m"], e["v"], m_exp=e["m_exp"], v_exp=e["v_exp"], copy=e["copy"],
-                                                           ids=e["ids"], n_dev=e["n"], weight_decay=e["decay"]) for e in es])
+        s["list"] = csgs.make_adamw_list([csgs.adamw_entry(e["p"], e["g"], e["m"], e["v"], m_exp=e["m_exp"], v_exp=e["v_exp"],
+                                                           copy=None if e["copy"] is e["p"] else e["copy"], ids=e["ids"], n_dev=e["n"], weight_decay=e["decay"]) for e in es])
         for e in es:
             if e["m_exp"] is not None:
                 e["m_out"], e["v_out"] = _empty(*e["m"].shape), _empty(*e["v"].shape)
