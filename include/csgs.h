@@ -594,6 +594,85 @@ int csgs_grad_scale(const csgs_grad_list *l /*host*/, int kind, const double *to
 /* Both: csgs_grad_norm then csgs_grad_scale, without the total passing through the caller's memory. */
 int csgs_grad_clip(const csgs_grad_list *l /*host*/, int kind, float max_norm, float *norm, int32_t *status, void *stream);
 
+/*
+ * One step of AdamW over all tensors of a network:
+ *     g' = c g          c = min(1, max_norm / (total + 1e-6)), or 1 where nothing is clipped
+ *     m  = beta1 m + (1 - beta1) g'          v = beta2 v + (1 - beta2) g'^2
+ *     p  = p - lr (m / (1 - beta1^t) / (sqrt(v / (1 - beta2^t)) + eps) + weight_decay p)          t = 1, 2, ... the step
+ * in one pass over p, g, m and v.  g', m and v are formed in double and rounded to float once, the rest in float; p (and copy) are rounded
+ * once.  p is formed from m and v before these are rounded to 8 bits.
+ *
+ * The tensors are described once, as those of csgs_grad_list.  A tensor may be a table of which the gradient holds rows alone
+ * (csgs_embed_grad_rows): with ids, row j of g belongs to row ids[j] of p, and the rows that no id names are left untouched,
+ * their states among them.  ids have to ascend strictly; ids outside [0, rows) are passed over; a row whose id does not ascend is left
+ * untouched and sets CSGS_ST_BAD_NODE_ID.
+ *
+ * States in 8 bits.  A row's entries are cut into blocks of CSGS_STATE_BLOCK (the last one may be shorter); a block keeps one byte,
+ * the exponent field E of its largest value's float (0: the block is zero; 255: the block holds a value that is not finite, all of it reads
+ * back as NaN), and a byte for each entry:
+ *   m   sign, 4 bits of exponent and 3 of mantissa (the code c stands for e4m3(c) 2^(E - 134)), rounded to nearest even;
+ *   v   5 bits of exponent and 3 of mantissa: code 0 is 0, code c >= 1 is (1 + f / 8) 2^(k - 31 + E - 127) with 8 k + f = c + 1, so that
+ *       255 is 2 and 1 is 1.25 / 2^31 of the block's power of two; rounded to nearest even, what is not zero never to zero.
+ * All zero is a valid start for states of either kind.
+ */
+enum { CSGS_STATE_F32 = 0, CSGS_STATE_8BIT = 1 };
+enum { CSGS_STATE_FIRST = 0, CSGS_STATE_SECOND = 1 };
+#define CSGS_STATE_BLOCK 256
+
+typedef struct csgs_adamw_tensor {
+    void *p;                  /* [rows x cols] of p_dtype, leading dimension ldp */
+    void *copy;               /* nullable: [rows x cols] bfloat16, leading dimension ldcopy: receives p (for products in bfloat16) */
+    const void *g;            /* [n x cols] of g_dtype, leading dimension ldg */
+    void *m, *v;              /* [rows x cols], rows side by side: floats, or bytes for CSGS_STATE_8BIT */
+    uint8_t *m_exp, *v_exp;   /* CSGS_STATE_8BIT: [rows x ceil(cols / CSGS_STATE_BLOCK)], rows side by side; else NULL */
+    const int32_t *ids;       /* nullable: [n]; NULL: n = rows */
+    const int32_t *n_dev;     /* nullable: min(max(*n_dev, 0), n) rows of g count, the others change nothing */
+    int64_t rows, cols, n, ldp, ldcopy, ldg;
+    int32_t p_dtype, g_dtype; /* CSGS_F32 or CSGS_BF16 each */
+    int32_t state;            /* CSGS_STATE_* */
+    float weight_decay, lr_scale; /* the tensor's own; lr_scale multiplies lr */
+    int32_t reserved;
+} csgs_adamw_tensor;
+
+typedef struct csgs_adamw_list {
+    void *base;               /* device buffer, 256-byte aligned */
+    size_t bytes;
+    /* owned by the library: */
+    int64_t tiles;
+    int32_t n, ready;
+} csgs_adamw_list;
+
+typedef struct csgs_adamw_args {
+    double beta1, beta2, eps; /* betas in [0, 1), eps >= 0 */
+    float lr;
+    float max_norm;           /* +infinity: nothing is clipped */
+    const float *lr_dev;      /* nullable: *lr_dev times lr (a schedule under graph replay) */
+    int32_t *step;            /* device: steps taken so far; the call adds 1 when its step is taken */
+    const csgs_grad_list *clip; /* nullable, host: the gradients whose norm counts (their out entries are not used) */
+    const double *total;      /* nullable, device: that norm's total, of csgs_grad_norm, added over GPUs; at most one of clip and total */
+    int32_t kind;             /* CSGS_GRAD_*, for clip and total */
+    int32_t reserved;
+    float *norm;              /* nullable, device: receives the norm (needs clip or total) */
+    int32_t *status;          /* nullable, device */
+} csgs_adamw_args;
+
+/* Bytes of device memory for a list of these tensors; 0 on bad input (n outside [1, 2^20], a tensor that csgs_adamw_list_init
+ * would refuse). */
+size_t csgs_adamw_list_bytes(const csgs_adamw_tensor *t /*host*/, int32_t n);
+/* Writes the descriptions of the n tensors into l->base (kernels that carry them as arguments).  No two may share a parameter.
+ * Host errors: CSGS_EINVAL, CSGS_EWORKSPACE, CSGS_EUNSUPPORTED (dtype, state, more than 2^40 entries, ids of more than 2^31 - 1 rows). */
+int csgs_adamw_list_init(csgs_adamw_list *l /*host*/, const csgs_adamw_tensor *t /*host*/, int32_t n, void *stream);
+/* The step.  Two launches with clip, one without.  Where clip or total is given and the total is NaN or infinite, nothing is changed, *step
+ * neither, and CSGS_ST_NONFINITE_GRAD is set.  Calls that share a list must be ordered on one stream.
+ * Host errors: CSGS_EINVAL. */
+int csgs_adamw(const csgs_adamw_list *l /*host*/, const csgs_adamw_args *a /*host*/, void *stream);
+
+/* States in 8 bits, as values and back (checkpoints; a change of the kind): codes [rows x cols] with exps as above, `which` CSGS_STATE_FIRST (m)
+ * or CSGS_STATE_SECOND (v; negative values and NaN in it read as: the former 0, the latter NaN), values [rows x cols] float with leading dimension ld.
+ * Host errors: CSGS_EINVAL, CSGS_EUNSUPPORTED (more than 2^40 entries). */
+int csgs_state_read(const uint8_t *codes, const uint8_t *exps, int which, int64_t rows, int64_t cols, float *values, int64_t ld, void *stream);
+int csgs_state_write(const float *values, int64_t ld, int which, int64_t rows, int64_t cols, uint8_t *codes, uint8_t *exps, void *stream);
+
 /* Static string for a CSGS_E* code. */
 const char *csgs_strerror(int code);
 

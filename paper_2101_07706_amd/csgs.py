@@ -23,6 +23,7 @@ F32, BF16 = 0, 1
 NORM_NONE, NORM_RMS, NORM_LAYER = 0, 1, 2
 GATE_LINEAR, GATE_SIGMOID, GATE_SILU = 0, 1, 2
 GRAD_L2, GRAD_L1, GRAD_MAX = 0, 1, 2
+STATE_F32, STATE_8BIT, STATE_FIRST, STATE_SECOND, STATE_BLOCK = 0, 1, 0, 1, 256
 
 EXPORTS = ["csgs_workspace_bytes", "csgs_workspace_clean_bytes", "csgs_workspace_init", "csgs_workspace_wait_limit", "csgs_fixed_point", "csgs_build_probs", "csgs_build_probs_auto",
            "csgs_sample_layer", "csgs_draw_nodes", "csgs_sampled_adjacency", "csgs_remote_count", "csgs_aggregate", "csgs_gather_rows",
@@ -30,7 +31,7 @@ EXPORTS = ["csgs_workspace_bytes", "csgs_workspace_clean_bytes", "csgs_workspace
            "csgs_aggregate_grad_scratch_bytes", "csgs_aggregate_grad", "csgs_strerror",
            "csgs_embed", "csgs_embed_grad_scratch_bytes", "csgs_embed_grad", "csgs_embed_grad_rows", "csgs_norm_residual",
            "csgs_norm_residual_grad_scratch_bytes", "csgs_norm_residual_grad", "csgs_grad_list_bytes", "csgs_grad_list_init", "csgs_grad_norm",
-           "csgs_grad_scale", "csgs_grad_clip",
+           "csgs_grad_scale", "csgs_grad_clip", "csgs_adamw_list_bytes", "csgs_adamw_list_init", "csgs_adamw", "csgs_state_read", "csgs_state_write",
            "csgs_profile_enable", "csgs_profile_kernel_count", "csgs_profile_kernel_name", "csgs_profile_collect", "csgs_profile_samples",
            "csgs_calib_copy", "csgs_calib_atomics", "csgs_calib_mfma_f64", "csgs_calib_lookups"]
 
@@ -95,6 +96,26 @@ class GradList(C.Structure):
     _fields_ = [("base", C.c_void_p), ("bytes", C.c_size_t), ("tiles", C.c_int64), ("n", C.c_int32), ("ready", C.c_int32)]
 
 
+class AdamwTensor(C.Structure):
+    """csgs_adamw_tensor: one parameter of a list."""
+    _fields_ = [("p", C.c_void_p), ("copy", C.c_void_p), ("g", C.c_void_p), ("m", C.c_void_p), ("v", C.c_void_p), ("m_exp", C.c_void_p), ("v_exp", C.c_void_p),
+                ("ids", C.c_void_p), ("n_dev", C.c_void_p), ("rows", C.c_int64), ("cols", C.c_int64), ("n", C.c_int64), ("ldp", C.c_int64), ("ldcopy", C.c_int64),
+                ("ldg", C.c_int64), ("p_dtype", C.c_int32), ("g_dtype", C.c_int32), ("state", C.c_int32), ("weight_decay", C.c_float), ("lr_scale", C.c_float),
+                ("reserved", C.c_int32)]
+
+
+class AdamwList(C.Structure):
+    """csgs_adamw_list: host descriptor of a prepared list of parameters."""
+    _fields_ = [("base", C.c_void_p), ("bytes", C.c_size_t), ("tiles", C.c_int64), ("n", C.c_int32), ("ready", C.c_int32)]
+
+
+class AdamwArgs(C.Structure):
+    """csgs_adamw_args: what a step takes beside the list."""
+    _fields_ = [("beta1", C.c_double), ("beta2", C.c_double), ("eps", C.c_double), ("lr", C.c_float), ("max_norm", C.c_float), ("lr_dev", C.c_void_p),
+                ("step", C.c_void_p), ("clip", C.POINTER(GradList)), ("total", C.c_void_p), ("kind", C.c_int32), ("reserved", C.c_int32), ("norm", C.c_void_p),
+                ("status", C.c_void_p)]
+
+
 _lib = None
 
 
@@ -156,6 +177,12 @@ def lib():
         L.csgs_grad_norm.argtypes = [C.POINTER(GradList), C.c_int, vp, vp]
         L.csgs_grad_scale.argtypes = [C.POINTER(GradList), C.c_int, vp, f32, vp, vp, vp]
         L.csgs_grad_clip.argtypes = [C.POINTER(GradList), C.c_int, f32, vp, vp, vp]
+        L.csgs_adamw_list_bytes.restype = sz
+        L.csgs_adamw_list_bytes.argtypes = [C.POINTER(AdamwTensor), i32]
+        L.csgs_adamw_list_init.argtypes = [C.POINTER(AdamwList), C.POINTER(AdamwTensor), i32, vp]
+        L.csgs_adamw.argtypes = [C.POINTER(AdamwList), C.POINTER(AdamwArgs), vp]
+        L.csgs_state_read.argtypes = [vp, vp, C.c_int, i64, i64, vp, i64, vp]
+        L.csgs_state_write.argtypes = [vp, i64, C.c_int, i64, i64, vp, vp, vp]
         L.csgs_strerror.restype = C.c_char_p
         L.csgs_strerror.argtypes = [C.c_int]
         L.csgs_calib_copy.argtypes = [vp, vp, sz, vp]
@@ -645,6 +672,17 @@ def _list_on(l, stream):
     return C.byref(l)
 
 
+def _list_buffer(nbytes, device, stream):
+    """Memory that this stream's earlier work may still use, and no other's."""
+    with torch.cuda.stream(stream if stream is None else _torch_stream(stream)):
+        return torch.empty(nbytes // 8, dtype=torch.int64, device=device)
+
+
+def _as_matrix(t):
+    """A tensor as rows x cols."""
+    return t if t.dim() == 2 else t.reshape(1, -1) if t.is_contiguous() else t.unsqueeze(0)
+
+
 def make_grad_list(grads, outs=None, rows_dev=None, stream=None) -> GradList:
     """A list of gradients for csgs_grad_norm / _scale / _clip, described once in device memory.  outs: where the clipped gradients go (None: in
     place; entries may be None); rows_dev: per gradient, a device int32 with the number of rows that count, or None.
@@ -655,10 +693,7 @@ def make_grad_list(grads, outs=None, rows_dev=None, stream=None) -> GradList:
     rows_dev = [None] * len(grads) if rows_dev is None else rows_dev
     assert len(grads) > 0 and len(outs) == len(grads) and len(rows_dev) == len(grads)
     assert _recording is None, "a list is made once, not by a recorded call"
-
-    def matrix(t):   # as rows x cols
-        return t if t.dim() == 2 else t.reshape(1, -1) if t.is_contiguous() else t.unsqueeze(0)
-
+    matrix = _as_matrix
     ts = (GradTensor * len(grads))()
     for i, (g, o, n) in enumerate(zip(grads, outs, rows_dev)):
         assert o is None or (o.shape == g.shape and o.dtype == g.dtype)
@@ -668,8 +703,7 @@ def make_grad_list(grads, outs=None, rows_dev=None, stream=None) -> GradList:
     nbytes = int(lib().csgs_grad_list_bytes(ts, len(grads)))
     if nbytes == 0:
         raise CsgsError(EINVAL, "csgs_grad_list_bytes")
-    with torch.cuda.stream(stream if stream is None else _torch_stream(stream)):     # (memory that this stream's earlier work may still use, and no other's)
-        buf = torch.empty(nbytes // 8, dtype=torch.int64, device=grads[0].device)
+    buf = _list_buffer(nbytes, grads[0].device, stream)
     l = GradList(buf.data_ptr(), nbytes, 0, 0, 0)
     l._keep, l._streams = (buf, list(grads), list(outs), list(rows_dev)), {_stream(stream)}
     _call("csgs_grad_list_init", C.byref(l), ts, len(grads), _stream(stream))
@@ -690,6 +724,95 @@ def csgs_grad_scale(l, kind, total, max_norm, norm=None, status=None, stream=Non
 def csgs_grad_clip(l, kind, max_norm, norm=None, status=None, stream=None):
     """out = min(1, max_norm / (total + 1e-6)) g over the list; norm receives the total before clipping."""
     _call("csgs_grad_clip", _list_on(l, stream), kind, max_norm, _f32(norm, 1), _i32(status), _stream(stream))
+
+
+def adamw_states(p, bits=32):
+    """States of a new parameter, all zero, for adamw_entry: dict of m and v, for bits=8 also of m_exp and v_exp."""
+    assert bits in (8, 32)
+    rows, cols = _as_matrix(p).shape
+    if bits == 32:
+        return {k: torch.zeros(rows, cols, dtype=torch.float32, device=p.device) for k in ("m", "v")}
+    blocks = (cols + STATE_BLOCK - 1) // STATE_BLOCK
+    return {k: torch.zeros(rows, blocks if "exp" in k else cols, dtype=torch.uint8, device=p.device) for k in ("m", "v", "m_exp", "v_exp")}
+
+
+def adamw_entry(p, g, m, v, m_exp=None, v_exp=None, copy=None, ids=None, n_dev=None, weight_decay=0.0, lr_scale=1.0):
+    """A parameter for make_adamw_list: p with its gradient g, states m and v (float32, or uint8 with exponents m_exp and v_exp: adamw_states), a bfloat16
+    copy of p, for a table whose gradient holds rows alone their ids (strictly ascending), a device int32 with the number of rows of g that count."""
+    mp, mg = _as_matrix(p), _as_matrix(g)
+    rows, cols = mp.shape
+    n = mg.shape[0]
+    assert mg.shape[1] == cols and (ids is not None or n == rows), "a gradient like its parameter, or rows of it with their ids"
+    assert ids is None or (p.dim() == 2 and ids.numel() >= n), "an id for every row of the gradient"
+    assert n_dev is None or g.dim() == 2, "rows are those of a matrix"
+    small = m.dtype is torch.uint8
+    for t in (m, v):
+        assert t.dtype is (torch.uint8 if small else torch.float32) and t.numel() == rows * cols and t.is_contiguous(), "states like the parameter, contiguous"
+    blocks = (cols + STATE_BLOCK - 1) // STATE_BLOCK
+    assert (m_exp is None) == (v_exp is None) == (not small), "exponents for states in 8 bits"
+    for t in (m_exp, v_exp):
+        assert t is None or (t.dtype is torch.uint8 and t.numel() == rows * blocks and t.is_contiguous()), f"uint8, {blocks} a row, contiguous"
+    ldcopy = 0
+    if copy is not None:
+        assert copy.dtype is torch.bfloat16 and copy.shape == p.shape, "a bfloat16 copy of the parameter's shape"
+        ldcopy = _ld(_as_matrix(copy), cols)
+    e = AdamwTensor(_ptr(p), _ptr(copy), _ptr(g), _ptr(m), _ptr(v), _ptr(m_exp), _ptr(v_exp), _i32(ids), _i32(n_dev), rows, cols, n, _ld(mp, cols), ldcopy,
+                    _ld(mg, cols), _elem(p), _elem(g), STATE_8BIT if small else STATE_F32, weight_decay, lr_scale, 0)
+    e._keep = (p, g, m, v, m_exp, v_exp, copy, ids, n_dev)
+    return e
+
+
+def make_adamw_list(entries, stream=None) -> AdamwList:
+    """A list of parameters (adamw_entry) for csgs_adamw, described once in device memory.  The list keeps their tensors, and is kept and dropped as those of
+    make_grad_list are."""
+    assert len(entries) > 0
+    assert _recording is None, "a list is made once, not by a recorded call"
+    written = [e._keep[k].data_ptr() for e in entries for k in (0, 2, 3)]
+    assert len(set(written)) == len(written), "a parameter and its states belong to one entry"
+    ts = (AdamwTensor * len(entries))(*entries)
+    nbytes = int(lib().csgs_adamw_list_bytes(ts, len(entries)))
+    if nbytes == 0:
+        raise CsgsError(EINVAL, "csgs_adamw_list_bytes")
+    buf = _list_buffer(nbytes, entries[0]._keep[0].device, stream)
+    l = AdamwList(buf.data_ptr(), nbytes, 0, 0, 0)
+    l._keep, l._streams = (buf, [e._keep for e in entries]), {_stream(stream)}
+    _call("csgs_adamw_list_init", C.byref(l), ts, len(entries), _stream(stream))
+    return l
+
+
+def csgs_adamw(l, lr, step, beta1=0.9, beta2=0.999, eps=1e-8, clip=None, total=None, kind=GRAD_L2, max_norm=float("inf"), lr_dev=None, norm=None, status=None,
+               stream=None):
+    """One step over a list of make_adamw_list.  step: device int32, the steps taken so far.  clip: a list of make_grad_list whose norm bounds the gradients by
+    max_norm (or total: a float64 of csgs_grad_norm); gradients whose norm is not finite change nothing.  lr_dev: a float32 that multiplies lr."""
+    assert total is None or total.dtype == torch.float64
+    assert step.dtype is torch.int32 and step.numel() == 1
+    grads = None
+    if clip is not None:
+        _list_on(clip, stream)
+        grads = C.pointer(clip)
+    a = AdamwArgs(beta1, beta2, eps, lr, max_norm, _f32(lr_dev, 1), step.data_ptr(), grads, _ptr(total), kind, 0, _f32(norm, 1), _i32(status))
+    _call("csgs_adamw", _list_on(l, stream), C.byref(a), _stream(stream))
+
+
+def _state_shape(codes, exps):
+    rows, cols = _as_matrix(codes).shape
+    blocks = (cols + STATE_BLOCK - 1) // STATE_BLOCK
+    assert codes.dtype is torch.uint8 and exps.dtype is torch.uint8 and codes.is_contiguous() and exps.is_contiguous() and exps.numel() == rows * blocks
+    return rows, cols
+
+
+def csgs_state_read(codes, exps, which, values, stream=None):
+    """The values (float32) of states in 8 bits; which: STATE_FIRST (m) or STATE_SECOND (v)."""
+    rows, cols = _state_shape(codes, exps)
+    vp, ld = _mat(_as_matrix(values), (rows, cols), torch.float32)
+    _call("csgs_state_read", codes.data_ptr(), exps.data_ptr(), which, rows, cols, vp, ld, _stream(stream))
+
+
+def csgs_state_write(values, which, codes, exps, stream=None):
+    """States in 8 bits from their values (float32)."""
+    rows, cols = _state_shape(codes, exps)
+    vp, ld = _mat(_as_matrix(values), (rows, cols), torch.float32)
+    _call("csgs_state_write", vp, ld, which, rows, cols, codes.data_ptr(), exps.data_ptr(), _stream(stream))
 
 
 def csgs_profile_enable(on: bool):

@@ -9,39 +9,10 @@
 // and a chain of four loads (tile, description, row count, entries) where they are short (13 tensors of 3.0 M entries 5 and 7 us).
 #include <math.h>
 #include "common.hpp"
+#include "grad_list.hpp"
 #include "row_pieces.hpp"
 
 namespace csgs {
-
-constexpr int64_t GRAD_TILE = 8192;
-constexpr int GRAD_BLOCKS = 2048;      // most blocks of either kernel
-constexpr int64_t GRAD_ENTRIES = 1ll << 40;
-
-// A tensor as the kernels see it.  flat: its rows lie side by side, in g and in out.
-struct GradDesc {
-    const void *g;
-    void *out;
-    const int32_t *rows_dev;
-    int64_t rows, cols, ldg, ldo, first_tile;
-    int32_t dtype, flat;
-};
-struct GradMem {
-    double *partial;      // [GRAD_BLOCKS]
-    GradDesc *desc;       // [n]
-    int32_t *tile_tensor; // [tiles]
-    size_t bytes;
-};
-__host__ __device__ inline GradMem carve_grads(void *base, int32_t n, int64_t tiles)
-{
-    GradMem m;
-    size_t off = align_up(sizeof(double) * GRAD_BLOCKS, 256);
-    m.partial = (double *)base;
-    m.desc = (GradDesc *)((char *)base + off);
-    off = align_up(off + sizeof(GradDesc) * (size_t)n, 256);
-    m.tile_tensor = (int32_t *)((char *)base + off);
-    m.bytes = align_up(off + sizeof(int32_t) * (size_t)tiles, 256);
-    return m;
-}
 
 constexpr int DESC_PER_LAUNCH = 32;
 struct DescBatch {
@@ -125,30 +96,12 @@ struct Tile {
     }
 };
 
-// The sum, or the larger one with NaN above everything.
-template <int KIND>
-__device__ inline double add_or_max(double a, double b)
-{
-    if (KIND != CSGS_GRAD_MAX) return a + b;
-    return !(a >= b) && !(a != a) ? b : a;
-}
 template <int KIND>
 __device__ inline double take_in(double a, float x)
 {
     const double v = (double)x;
     if (KIND == CSGS_GRAD_L2) return fma(v, v, a);   // (a float's square is exact in double)
     return add_or_max<KIND>(a, fabs(v));
-}
-
-// Joined over the block's 256 threads in a fixed order, the result in every thread: across a wavefront by exchanges, then its four.
-template <int KIND>
-__device__ inline double block_join(double v, double *lds /*[4]*/)
-{
-#pragma unroll
-    for (int s = WAVE / 2; s > 0; s >>= 1) v = add_or_max<KIND>(v, __shfl_xor(v, s));
-    if (lane_id() == 0) lds[threadIdx.x / WAVE] = v;
-    __syncthreads();
-    return add_or_max<KIND>(add_or_max<KIND>(lds[0], lds[1]), add_or_max<KIND>(lds[2], lds[3]));
 }
 
 template <int KIND>
@@ -170,22 +123,6 @@ __global__ __launch_bounds__(256) void grad_norm_k(GradMem m, int64_t tiles)
     const double own = add_or_max<KIND>(add_or_max<KIND>(sum[0], sum[1]), add_or_max<KIND>(sum[2], sum[3]));
     const double all = block_join<KIND>(own, lds);
     if (threadIdx.x == 0) m.partial[blockIdx.x] = all;
-}
-
-template <int KIND>
-__device__ inline double join_partials(const double *__restrict__ partial, int blocks, double *lds)
-{
-    double p[GRAD_BLOCKS / 256], s = 0.0;
-#pragma unroll
-    for (int k = 0; k < GRAD_BLOCKS / 256; ++k) p[k] = k * 256 + (int)threadIdx.x < blocks ? partial[k * 256 + (int)threadIdx.x] : 0.0;
-#pragma unroll
-    for (int k = 0; k < GRAD_BLOCKS / 256; ++k) s = add_or_max<KIND>(s, p[k]);
-    return block_join<KIND>(s, lds);
-}
-// (kind: the same for all threads)
-__device__ inline double join_partials(const double *__restrict__ partial, int blocks, int kind, double *lds)
-{
-    return kind == CSGS_GRAD_MAX ? join_partials<CSGS_GRAD_MAX>(partial, blocks, lds) : join_partials<CSGS_GRAD_L2>(partial, blocks, lds);
 }
 
 __global__ __launch_bounds__(256) void grad_total_k(GradMem m, int blocks, int kind, double *__restrict__ total)
@@ -249,12 +186,6 @@ static int describe(const csgs_grad_tensor &t, int64_t *tiles, GradDesc *d)
     return *tiles > GRAD_ENTRIES / GRAD_TILE ? CSGS_EUNSUPPORTED : CSGS_OK;
 }
 
-static int grad_blocks(int64_t tiles) { return (int)(tiles < GRAD_BLOCKS ? tiles : GRAD_BLOCKS); }
-static bool list_ok(const csgs_grad_list *l, int kind)
-{
-    return l && l->base && l->ready && l->n > 0 && l->tiles > 0 && kind >= CSGS_GRAD_L2 && kind <= CSGS_GRAD_MAX;
-}
-
 // Entries from which outputs go past the caches: 256 MB of floats, the memory-side cache (us, through / past: 245 M floats 534 / 517).
 constexpr int64_t PAST_TILES = (1ll << 26) / GRAD_TILE;
 static int launch_scale(const csgs_grad_list *l, int kind, const double *total, float max_norm, float *norm, int32_t *status, hipStream_t st)
@@ -268,7 +199,7 @@ static int launch_scale(const csgs_grad_list *l, int kind, const double *total, 
     CSGS_LAUNCH_CHECK();
     return CSGS_OK;
 }
-static int launch_norm(const csgs_grad_list *l, int kind, hipStream_t st)
+int launch_grad_norm(const csgs_grad_list *l, int kind, hipStream_t st)
 {
     const GradMem m = carve_grads(l->base, l->n, l->tiles);
     const dim3 grid((unsigned)grad_blocks(l->tiles)), block(256);
@@ -325,7 +256,7 @@ extern "C" int csgs_grad_list_init(csgs_grad_list *l, const csgs_grad_tensor *t,
 extern "C" int csgs_grad_norm(const csgs_grad_list *l, int kind, double *total, void *stream)
 {
     if (!list_ok(l, kind) || !total) return CSGS_EINVAL;
-    const int rc = launch_norm(l, kind, (hipStream_t)stream);
+    const int rc = launch_grad_norm(l, kind, (hipStream_t)stream);
     if (rc != CSGS_OK) return rc;
     CSGS_LAUNCH(K_GRAD_TOTAL, grad_total_k, dim3(1), dim3(256), (hipStream_t)stream, carve_grads(l->base, l->n, l->tiles), grad_blocks(l->tiles), kind, total);
     CSGS_LAUNCH_CHECK();
@@ -341,6 +272,6 @@ extern "C" int csgs_grad_scale(const csgs_grad_list *l, int kind, const double *
 extern "C" int csgs_grad_clip(const csgs_grad_list *l, int kind, float max_norm, float *norm, int32_t *status, void *stream)
 {
     if (!list_ok(l, kind) || !(max_norm > 0.0f)) return CSGS_EINVAL;
-    const int rc = launch_norm(l, kind, (hipStream_t)stream);
+    const int rc = launch_grad_norm(l, kind, (hipStream_t)stream);
     return rc != CSGS_OK ? rc : launch_scale(l, kind, nullptr, max_norm, norm, status, (hipStream_t)stream);
 }

@@ -27,7 +27,8 @@ static const char *const kNames[K_COUNT] = {"row_prefix", "scan_edges", "cand_pa
                                             "adjT_count", "adjT_prefix", "adjT_fill", "adjT_order", "aggregate_grad", "fill_zero", "copy", "atomics", "mfma_f64", "lookups", "layer_forward",
                                             "layer_gemm_digits", "gemm_grad_z_digits",
                                             "embed", "embed_count", "embed_place", "embed_heads", "embed_zero", "embed_few", "embed_ranges", "embed_sum", "embed_join", "residual", "residual_grad",
-                                            "col_sums", "grad_list", "grad_norm", "grad_total", "grad_scale"};
+                                            "col_sums", "grad_list", "grad_norm", "grad_total", "grad_scale",
+                                            "adamw_list", "adamw", "state_read", "state_write"};
 
 bool next_pair(int kid, hipEvent_t *start, hipEvent_t *stop)
 {
