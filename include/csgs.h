@@ -595,6 +595,74 @@ int csgs_grad_scale(const csgs_grad_list *l /*host*/, int kind, const double *to
 int csgs_grad_clip(const csgs_grad_list *l /*host*/, int kind, float max_norm, float *norm, int32_t *status, void *stream);
 
 /*
+ * Products of a feed-forward block on the rows of a layer, in bfloat16 or float, on the matrix cores with sums in float (the products of the sampled
+ * layers themselves, in double, are csgs_layer_gemm).
+ *
+ * csgs_linear: a product with its epilogue,
+ *     y = alpha act(a w + bias) + beta r
+ * with a [M x K], w [K x N] of `dtype`, bias [N] float, r and y [M x N] of `y_dtype`, all row-major, rows starting on any element.
+ * act: the identity, max(z, 0), the logistic function s(z), z s(z), or z Phi(z) with the normal distribution's Phi.  One rounding per output.
+ * y may be r (same address and leading dimension); other overlaps are not allowed.  A row of y depends on its own rows of a and r alone.
+ * With M_dev only rows below the device count are computed and written; a's rows past it may be read, whatever they hold.
+ * Host errors: CSGS_EINVAL, CSGS_EUNSUPPORTED (types).
+ */
+enum { CSGS_ACT_NONE = 0, CSGS_ACT_RELU = 1, CSGS_ACT_SIGMOID = 2, CSGS_ACT_SILU = 3, CSGS_ACT_GELU = 4 };
+
+typedef struct csgs_linear_args {
+    int32_t M, K, N;            /* rows (capacity if M_dev is given), width, outputs */
+    int32_t act;                /* CSGS_ACT_* */
+    const int32_t *M_dev;       /* nullable */
+    const void *a, *w;          /* [M x K], [K x N] of dtype */
+    const float *bias;          /* [N], nullable: 0 */
+    const void *r;              /* [M x N] of y_dtype, nullable: 0 */
+    int64_t lda, ldw, ldr;      /* leading dimensions in elements */
+    int32_t dtype, y_dtype;     /* both CSGS_F32, both CSGS_BF16, or dtype CSGS_BF16 with y_dtype CSGS_F32 */
+    float alpha, beta;
+} csgs_linear_args;
+
+int csgs_linear(const csgs_linear_args *p /*host*/, void *y, int64_t ldy, void *stream);
+
+/* Gradients of csgs_linear from dy = dL/dy [M x N] of y_dtype; `p` as in the forward call (nothing has to be kept from it but its inputs).  With
+ * t = alpha dy .* act'(a w + bias):
+ *     da = t w^T [M x K], dw = a^T t [K x N] of dtype, dbias = column sums of t [N] float, dr = beta dy [M x N] of y_dtype
+ * each nullable, not all of them.  Rows of a and dy past the device count add nothing, whatever they hold; those rows of da and dr are left untouched.
+ * For dtype CSGS_BF16, t is rounded to bfloat16 between the products, dbias is summed from t before that.  Sums over rows are split into parts that
+ * are added in a fixed order: two calls on the same input give the same bits.  dr may be dy (same leading dimension); other overlaps are not allowed.
+ * scratch: device, 256-byte aligned, csgs_linear_grad_scratch_bytes(M, K, N, dtype) bytes (0 on bad input); nothing in it needs to be kept or
+ * cleared between calls.  The size does not fall as M, K or N grow.
+ * Host errors: CSGS_EINVAL (also: dbias or dr without the input it belongs to), CSGS_EWORKSPACE, CSGS_EUNSUPPORTED. */
+size_t csgs_linear_grad_scratch_bytes(int32_t M, int32_t K, int32_t N, int dtype);
+int csgs_linear_grad(const csgs_linear_args *p /*host*/, const void *dy, int64_t lddy, void *da, int64_t ldda, void *dw, int64_t lddw, float *dbias, void *dr,
+                     int64_t lddr, void *scratch, size_t scratch_bytes, void *stream);
+
+/*
+ * csgs_gated: the first half of a gated feed-forward block, both projections, the activation and the product in one kernel,
+ *     h = act(x wg + bg) .* (x wu + bu)
+ * with x [M x K], wg and wu [K x N], h [M x N] of `dtype`, bg and bu [N] float.  (wg and wu may be the halves of one matrix.)  The block's second product is
+ * csgs_linear with the residual as r.  Roundings, device counts and overlaps as csgs_linear.
+ * Host errors: CSGS_EINVAL, CSGS_EUNSUPPORTED.
+ */
+typedef struct csgs_gated_args {
+    int32_t M, K, N, act;
+    const int32_t *M_dev;       /* nullable */
+    const void *x, *wg, *wu;
+    const float *bg, *bu;       /* nullable: 0 */
+    int64_t ldx, ldwg, ldwu;
+    int32_t dtype;              /* CSGS_F32 or CSGS_BF16 */
+    int32_t reserved;
+} csgs_gated_args;
+
+int csgs_gated(const csgs_gated_args *p /*host*/, void *h, int64_t ldh, void *stream);
+
+/* Gradients of csgs_gated from dh = dL/dh [M x N] of dtype; `p` as in the forward call.  With g = x wg + bg, u = x wu + bu, formed again,
+ *     tg = dh .* u .* act'(g), tu = dh .* act(g):
+ *     dx = tg wg^T + tu wu^T [M x K], dwg = x^T tg, dwu = x^T tu [K x N] of dtype, dbg and dbu [N] float: column sums of tg and tu
+ * each nullable, not all of them.  Everything else as csgs_linear_grad (CSGS_EINVAL also for dbg without bg, dbu without bu). */
+size_t csgs_gated_grad_scratch_bytes(int32_t M, int32_t K, int32_t N, int dtype);
+int csgs_gated_grad(const csgs_gated_args *p /*host*/, const void *dh, int64_t lddh, void *dx, int64_t lddx, void *dwg, int64_t lddwg, void *dwu, int64_t lddwu,
+                    float *dbg, float *dbu, void *scratch, size_t scratch_bytes, void *stream);
+
+/*
  * One step of AdamW over all tensors of a network:
  *     g' = c g          c = min(1, max_norm / (total + 1e-6)), or 1 where nothing is clipped
  *     m  = beta1 m + (1 - beta1) g'          v = beta2 v + (1 - beta2) g'^2

@@ -23,6 +23,7 @@ F32, BF16 = 0, 1
 NORM_NONE, NORM_RMS, NORM_LAYER = 0, 1, 2
 GATE_LINEAR, GATE_SIGMOID, GATE_SILU = 0, 1, 2
 GRAD_L2, GRAD_L1, GRAD_MAX = 0, 1, 2
+ACT_NONE, ACT_RELU, ACT_SIGMOID, ACT_SILU, ACT_GELU = 0, 1, 2, 3, 4
 STATE_F32, STATE_8BIT, STATE_FIRST, STATE_SECOND, STATE_BLOCK = 0, 1, 0, 1, 256
 
 EXPORTS = ["csgs_workspace_bytes", "csgs_workspace_clean_bytes", "csgs_workspace_init", "csgs_workspace_wait_limit", "csgs_fixed_point", "csgs_build_probs", "csgs_build_probs_auto",
@@ -32,6 +33,7 @@ EXPORTS = ["csgs_workspace_bytes", "csgs_workspace_clean_bytes", "csgs_workspace
            "csgs_embed", "csgs_embed_grad_scratch_bytes", "csgs_embed_grad", "csgs_embed_grad_rows", "csgs_norm_residual",
            "csgs_norm_residual_grad_scratch_bytes", "csgs_norm_residual_grad", "csgs_grad_list_bytes", "csgs_grad_list_init", "csgs_grad_norm",
            "csgs_grad_scale", "csgs_grad_clip", "csgs_adamw_list_bytes", "csgs_adamw_list_init", "csgs_adamw", "csgs_state_read", "csgs_state_write",
+           "csgs_linear", "csgs_linear_grad_scratch_bytes", "csgs_linear_grad", "csgs_gated", "csgs_gated_grad_scratch_bytes", "csgs_gated_grad",
            "csgs_profile_enable", "csgs_profile_kernel_count", "csgs_profile_kernel_name", "csgs_profile_collect", "csgs_profile_samples",
            "csgs_calib_copy", "csgs_calib_atomics", "csgs_calib_mfma_f64", "csgs_calib_lookups"]
 
@@ -94,6 +96,20 @@ class GradTensor(C.Structure):
 class GradList(C.Structure):
     """csgs_grad_list: host descriptor of a prepared list of gradients."""
     _fields_ = [("base", C.c_void_p), ("bytes", C.c_size_t), ("tiles", C.c_int64), ("n", C.c_int32), ("ready", C.c_int32)]
+
+
+class LinearArgs(C.Structure):
+    """csgs_linear_args: host struct of the inputs of csgs_linear and its gradient."""
+    _fields_ = [("M", C.c_int32), ("K", C.c_int32), ("N", C.c_int32), ("act", C.c_int32), ("M_dev", C.c_void_p), ("a", C.c_void_p), ("w", C.c_void_p),
+                ("bias", C.c_void_p), ("r", C.c_void_p), ("lda", C.c_int64), ("ldw", C.c_int64), ("ldr", C.c_int64), ("dtype", C.c_int32), ("y_dtype", C.c_int32),
+                ("alpha", C.c_float), ("beta", C.c_float)]
+
+
+class GatedArgs(C.Structure):
+    """csgs_gated_args: host struct of the inputs of csgs_gated and its gradient."""
+    _fields_ = [("M", C.c_int32), ("K", C.c_int32), ("N", C.c_int32), ("act", C.c_int32), ("M_dev", C.c_void_p), ("x", C.c_void_p), ("wg", C.c_void_p),
+                ("wu", C.c_void_p), ("bg", C.c_void_p), ("bu", C.c_void_p), ("ldx", C.c_int64), ("ldwg", C.c_int64), ("ldwu", C.c_int64), ("dtype", C.c_int32),
+                ("reserved", C.c_int32)]
 
 
 class AdamwTensor(C.Structure):
@@ -183,6 +199,14 @@ def lib():
         L.csgs_adamw.argtypes = [C.POINTER(AdamwList), C.POINTER(AdamwArgs), vp]
         L.csgs_state_read.argtypes = [vp, vp, C.c_int, i64, i64, vp, i64, vp]
         L.csgs_state_write.argtypes = [vp, i64, C.c_int, i64, i64, vp, vp, vp]
+        L.csgs_linear.argtypes = [vp, vp, i64, vp]
+        L.csgs_linear_grad_scratch_bytes.restype = sz
+        L.csgs_linear_grad_scratch_bytes.argtypes = [i32, i32, i32, C.c_int]
+        L.csgs_linear_grad.argtypes = [vp, vp, i64, vp, i64, vp, i64, vp, vp, i64, vp, sz, vp]
+        L.csgs_gated.argtypes = [vp, vp, i64, vp]
+        L.csgs_gated_grad_scratch_bytes.restype = sz
+        L.csgs_gated_grad_scratch_bytes.argtypes = [i32, i32, i32, C.c_int]
+        L.csgs_gated_grad.argtypes = [vp, vp, i64, vp, i64, vp, i64, vp, i64, vp, vp, vp, sz, vp]
         L.csgs_strerror.restype = C.c_char_p
         L.csgs_strerror.argtypes = [C.c_int]
         L.csgs_calib_copy.argtypes = [vp, vp, sz, vp]
@@ -724,6 +748,67 @@ def csgs_grad_scale(l, kind, total, max_norm, norm=None, status=None, stream=Non
 def csgs_grad_clip(l, kind, max_norm, norm=None, status=None, stream=None):
     """out = min(1, max_norm / (total + 1e-6)) g over the list; norm receives the total before clipping."""
     _call("csgs_grad_clip", _list_on(l, stream), kind, max_norm, _f32(norm, 1), _i32(status), _stream(stream))
+
+
+_linear_layout, _gated_layout = struct.Struct("<iiiiQQQQQqqqiiff"), struct.Struct("<iiiiQQQQQQqqqii")     # csgs_linear_args, csgs_gated_args
+
+
+def _linear(a, w, y, bias, r, act, alpha, beta, M_dev):
+    """csgs_linear_args and the shape of y; y: a tensor of the output's type."""
+    M, K = a.shape
+    N = w.shape[1]
+    ap, lda = _mat(a, (M, K), a.dtype)
+    wp, ldw = _mat(w, (K, N), a.dtype)
+    rp, ldr = _mat(r, (M, N), y.dtype)
+    args = _linear_layout.pack(M, K, N, act, _i32(M_dev) or 0, ap, wp, _f32(bias, N) or 0, rp or 0, lda, ldw, ldr, _elem(a), _elem(y), alpha, beta)
+    return args, (M, K, N)
+
+
+def csgs_linear(a, w, y, bias=None, r=None, act=ACT_NONE, alpha=1.0, beta=1.0, M_dev=None, stream=None):
+    """y = alpha act(a w + bias) + beta r.  a and w float32 or bfloat16, bias float32, r and y of their type or, for bfloat16, float32."""
+    args, (M, K, N) = _linear(a, w, y, bias, r, act, alpha, beta, M_dev)
+    _call("csgs_linear", args, *_mat(y, (M, N), y.dtype), _stream(stream))
+
+
+def csgs_linear_grad_scratch_bytes(M, K, N, dtype) -> int:
+    """dtype: F32 or BF16, of a and w."""
+    return int(lib().csgs_linear_grad_scratch_bytes(M, K, N, dtype))
+
+
+def csgs_linear_grad(a, w, dy, da, dw, dbias, dr, scratch, bias=None, act=ACT_NONE, alpha=1.0, beta=1.0, M_dev=None, stream=None):
+    """Gradients of csgs_linear from dy; outputs may be None.  scratch: a tensor of at least csgs_linear_grad_scratch_bytes(M, K, N, dtype) bytes."""
+    args, (M, K, N) = _linear(a, w, dy, bias, dr, act, alpha, beta, M_dev)      # (of r only that there is one counts)
+    ptr, nbytes = _scratch(scratch)
+    _call("csgs_linear_grad", args, *_mat(dy, (M, N), dy.dtype), *_mat(da, (M, K), a.dtype), *_mat(dw, (K, N), a.dtype), _f32(dbias, N), *_mat(dr, (M, N), dy.dtype),
+          ptr, nbytes, _stream(stream))
+
+
+def _gated(x, wg, wu, bg, bu, act, M_dev):
+    M, K = x.shape
+    N = wg.shape[1]
+    xp, ldx = _mat(x, (M, K), x.dtype)
+    gp, ldwg = _mat(wg, (K, N), x.dtype)
+    up, ldwu = _mat(wu, (K, N), x.dtype)
+    return _gated_layout.pack(M, K, N, act, _i32(M_dev) or 0, xp, gp, up, _f32(bg, N) or 0, _f32(bu, N) or 0, ldx, ldwg, ldwu, _elem(x), 0), (M, K, N)
+
+
+def csgs_gated(x, wg, wu, h, bg=None, bu=None, act=ACT_SILU, M_dev=None, stream=None):
+    """h = act(x wg + bg) .* (x wu + bu); x, wg, wu and h float32 or bfloat16, the same for all, bg and bu float32."""
+    args, (M, K, N) = _gated(x, wg, wu, bg, bu, act, M_dev)
+    _call("csgs_gated", args, *_mat(h, (M, N), x.dtype), _stream(stream))
+
+
+def csgs_gated_grad_scratch_bytes(M, K, N, dtype) -> int:
+    """dtype: F32 or BF16, of x, wg and wu."""
+    return int(lib().csgs_gated_grad_scratch_bytes(M, K, N, dtype))
+
+
+def csgs_gated_grad(x, wg, wu, dh, dx, dwg, dwu, dbg, dbu, scratch, bg=None, bu=None, act=ACT_SILU, M_dev=None, stream=None):
+    """Gradients of csgs_gated from dh; outputs may be None.  scratch: a tensor of at least csgs_gated_grad_scratch_bytes(M, K, N, dtype) bytes."""
+    args, (M, K, N) = _gated(x, wg, wu, bg, bu, act, M_dev)
+    ptr, nbytes = _scratch(scratch)
+    _call("csgs_gated_grad", args, *_mat(dh, (M, N), x.dtype), *_mat(dx, (M, K), x.dtype), *_mat(dwg, (K, N), x.dtype), *_mat(dwu, (K, N), x.dtype), _f32(dbg, N),
+          _f32(dbu, N), ptr, nbytes, _stream(stream))
 
 
 def adamw_states(p, bits=32):

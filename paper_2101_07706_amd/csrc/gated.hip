@@ -1,0 +1,225 @@
+// csgs_gated: h = act(x wg + bg) .* (x wu + bu), and its gradient.  One tile of x serves both products.
+#include "products.hpp"
+
+namespace csgs {
+
+struct GatedArgs {
+    Operand x, w[2];
+    int32_t M, K, N, act;
+    const int32_t *M_dev;
+    const float *b[2];
+    const void *dh;
+    int64_t lddh, ldh, ldt;
+    void *h, *t[2];
+    float *columns[2];           // nullable: a row of column sums for each wavefront's rows
+    int64_t tiles_m, tiles_n;
+};
+
+// GRAD = false: h.  GRAD = true: tg and tu as operands of the gradients' products, and their column sums.
+template <typename T, int BM, int BN, int WM, int WN, bool GRAD>
+__global__ __launch_bounds__(WM *WN *WAVE) void gated_k(GatedArgs p)
+{
+    using Tile = MatrixTile<T, BM, BN, WM, WN, false, true, 2>;
+    __shared__ __attribute__((aligned(128))) char lds[Tile::LDS_BYTES];
+    int64_t tm, tn;
+    tile_place(blockIdx.x, p.tiles_m, p.tiles_n, &tm, &tn);
+    const int64_t m0 = tm * BM, n0 = tn * BN, rows = live_rows(p.M, p.M_dev);
+    const bool columns = GRAD && (p.columns[0] || p.columns[1]);
+    if (m0 >= rows && !columns) return;
+    Tile tile;
+    tile.clear();
+    if (m0 < rows) tile.accumulate(lds, p.x, p.w, m0, rows, n0, p.N, 0, p.K);
+    float sums[2][4] = {};
+    tile.each([&](int m, int n, const float(&v)[2][4], int which) {
+        const int64_t row = m0 + m, col = n0 + n, rest = p.N - col;
+        const int count = rest >= 4 ? 4 : rest > 0 ? (int)rest : 0;
+        float t[2][4] = {};
+        if (row < rows && count) {
+            float x[4], h[4];
+            if constexpr (GRAD) load_some((const T *)p.dh + row * p.lddh + col, count, x);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float g = v[0][i] + (p.b[0] && i < count ? p.b[0][col + i] : 0.0f), u = v[1][i] + (p.b[1] && i < count ? p.b[1][col + i] : 0.0f);
+                const Activation a = activate(g, p.act);
+                if constexpr (!GRAD) {
+                    h[i] = a.a * u;
+                } else if (i < count) {
+                    t[0][i] = x[i] * u * a.da;
+                    t[1][i] = x[i] * a.a;
+                }
+            }
+            if constexpr (!GRAD) {
+                store_some((T *)p.h + row * p.ldh + col, count, h);
+            } else {
+                store_some((T *)p.t[0] + row * p.ldt + col, count, t[0]);
+                store_some((T *)p.t[1] + row * p.ldt + col, count, t[1]);
+            }
+        }
+        if (columns) {
+            const int64_t part = tm * WM + (int)threadIdx.x / WAVE / WN;
+#pragma unroll
+            for (int b = 0; b < 2; ++b)
+                if (p.columns[b])
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        sums[b][i] = which == 0 ? t[b][i] : sums[b][i] + t[b][i];
+                        if (which == Tile::TM - 1) {
+                            const float s = sum_of_32(sums[b][i]);
+                            if (((int)threadIdx.x & 31) == 0 && i < count) p.columns[b][part * p.N + col + i] = s;
+                        }
+                    }
+        }
+    });
+}
+
+template <typename T, int BM, int BN, int WM, int WN, bool GRAD>
+static int launch_shape(GatedArgs p, int64_t *parts, hipStream_t st)
+{
+    p.tiles_m = ((int64_t)p.M + BM - 1) / BM;
+    p.tiles_n = ((int64_t)p.N + BN - 1) / BN;
+    *parts = p.tiles_m * WM;
+    if (p.tiles_m * p.tiles_n > 1 << 30) return CSGS_EUNSUPPORTED;
+    CSGS_LAUNCH(K_GATED, (gated_k<T, BM, BN, WM, WN, GRAD>), dim3((unsigned)(p.tiles_m * p.tiles_n)), dim3(WM * WN * WAVE), st, p);
+    CSGS_LAUNCH_CHECK();
+    return CSGS_OK;
+}
+template <bool GRAD>
+static int launch_gated(const GatedArgs &p, int dtype, int64_t *parts, hipStream_t st)
+{
+    const bool large = (((int64_t)p.M + 127) / 128) * (((int64_t)p.N + 63) / 64) >= 256;
+    if (dtype == CSGS_F32) return large ? launch_shape<float, 128, 64, 2, 2, GRAD>(p, parts, st) : launch_shape<float, 64, 64, 2, 2, GRAD>(p, parts, st);
+    return large ? launch_shape<uint16_t, 128, 64, 2, 2, GRAD>(p, parts, st) : launch_shape<uint16_t, 64, 64, 2, 2, GRAD>(p, parts, st);
+}
+
+static int check(const csgs_gated_args *p, GatedArgs *a)
+{
+    if (!p || p->M <= 0 || p->K <= 0 || p->N <= 0 || !p->x || !p->wg || !p->wu || p->ldx < p->K || p->ldwg < p->N || p->ldwu < p->N) return CSGS_EINVAL;
+    if (p->act < CSGS_ACT_NONE || p->act > CSGS_ACT_GELU) return CSGS_EINVAL;
+    if (p->dtype != CSGS_F32 && p->dtype != CSGS_BF16) return CSGS_EUNSUPPORTED;
+    *a = GatedArgs{};
+    a->x = Operand{p->x, p->ldx};
+    a->w[0] = Operand{p->wg, p->ldwg};
+    a->w[1] = Operand{p->wu, p->ldwu};
+    a->M = p->M;
+    a->K = p->K;
+    a->N = p->N;
+    a->act = p->act;
+    a->M_dev = p->M_dev;
+    a->b[0] = p->bg;
+    a->b[1] = p->bu;
+    return CSGS_OK;
+}
+
+struct GatedScratch {
+    void *t[2];
+    float *columns[2], *parts;
+    size_t bytes;
+};
+static GatedScratch carve_gated(void *base, int32_t M, int32_t K, int32_t N, int dtype)
+{
+    GatedScratch s;
+    size_t off = 0;
+    for (int i = 0; i < 2; ++i) {
+        s.t[i] = (char *)base + off;
+        off = align_up(off + (size_t)M * (size_t)N * (dtype == CSGS_F32 ? 4 : 2), 256);
+    }
+    for (int i = 0; i < 2; ++i) {
+        s.columns[i] = (float *)((char *)base + off);
+        off = align_up(off + (size_t)column_parts(M) * (size_t)N * 4, 256);
+    }
+    s.parts = (float *)((char *)base + off);
+    const int64_t dx = out_product_floats(M, K, N, 1), dw = out_product_floats(K, N, M, 2);
+    s.bytes = align_up(off + (size_t)(dx > dw ? dx : dw) * 4, 256);
+    return s;
+}
+
+}  // namespace csgs
+
+using namespace csgs;
+
+extern "C" int csgs_gated(const csgs_gated_args *p, void *h, int64_t ldh, void *stream)
+{
+    GatedArgs a;
+    const int rc = check(p, &a);
+    if (rc != CSGS_OK) return rc;
+    if (!h || ldh < p->N || h == p->x || h == p->wg || h == p->wu) return CSGS_EINVAL;
+    a.h = h;
+    a.ldh = ldh;
+    int64_t parts;
+    return launch_gated<false>(a, p->dtype, &parts, (hipStream_t)stream);
+}
+
+extern "C" size_t csgs_gated_grad_scratch_bytes(int32_t M, int32_t K, int32_t N, int dtype)
+{
+    if (M <= 0 || K <= 0 || N <= 0 || (dtype != CSGS_F32 && dtype != CSGS_BF16)) return 0;
+    return carve_gated(nullptr, M, K, N, dtype).bytes;
+}
+
+extern "C" int csgs_gated_grad(const csgs_gated_args *p, const void *dh, int64_t lddh, void *dx, int64_t lddx, void *dwg, int64_t lddwg, void *dwu, int64_t lddwu,
+                               float *dbg, float *dbu, void *scratch, size_t scratch_bytes, void *stream)
+{
+    GatedArgs a;
+    int rc = check(p, &a);
+    if (rc != CSGS_OK) return rc;
+    if (!dh || lddh < p->N || (dx && lddx < p->K) || (dwg && lddwg < p->N) || (dwu && lddwu < p->N)) return CSGS_EINVAL;
+    if ((!dx && !dwg && !dwu && !dbg && !dbu) || (dbg && !p->bg) || (dbu && !p->bu) || dx == dh || dwg == dh || dwu == dh) return CSGS_EINVAL;
+    if (!scratch || ((uintptr_t)scratch & 255)) return CSGS_EINVAL;
+    const GatedScratch s = carve_gated(scratch, p->M, p->K, p->N, p->dtype);
+    if (scratch_bytes < s.bytes) return CSGS_EWORKSPACE;
+    hipStream_t st = (hipStream_t)stream;
+    a.dh = dh;
+    a.lddh = lddh;
+    a.ldt = p->N;
+    a.t[0] = s.t[0];
+    a.t[1] = s.t[1];
+    a.columns[0] = dbg ? s.columns[0] : nullptr;
+    a.columns[1] = dbu ? s.columns[1] : nullptr;
+    int64_t parts;
+    rc = launch_gated<true>(a, p->dtype, &parts, st);
+    if (rc != CSGS_OK) return rc;
+    if (dx) {
+        OutProduct o{};
+        for (int i = 0; i < 2; ++i) {
+            o.a[i] = Operand{s.t[i], p->N};
+            o.b[i] = a.w[i];
+        }
+        o.pairs = 2;
+        o.outs = 1;
+        o.out[0] = dx;
+        o.ldo[0] = lddx;
+        o.rows = p->M;
+        o.cols = p->K;
+        o.red = p->N;
+        o.rows_dev = p->M_dev;
+        o.scale = 1.0f;
+        o.across = false;
+        rc = launch_out_product(o, p->dtype, s.parts, st);
+        if (rc != CSGS_OK) return rc;
+    }
+    if (dwg || dwu) {
+        OutProduct o{};
+        o.a[0] = a.x;
+        void *out[2] = {dwg, dwu};
+        const int64_t ld[2] = {lddwg, lddwu};
+        for (int i = 0; i < 2; ++i)
+            if (out[i]) {
+                o.b[o.outs] = Operand{s.t[i], p->N};
+                o.out[o.outs] = out[i];
+                o.ldo[o.outs++] = ld[i];
+            }
+        o.pairs = 1;
+        o.rows = p->K;
+        o.cols = p->N;
+        o.red = p->M;
+        o.red_dev = p->M_dev;
+        o.scale = 1.0f;
+        o.across = true;
+        rc = launch_out_product(o, p->dtype, s.parts, st);
+        if (rc != CSGS_OK) return rc;
+    }
+    if (dbg) {
+        rc = launch_join_columns(s.columns[0], parts, p->N, dbg, st);
+        if (rc != CSGS_OK) return rc;
+    }
+    return dbu ? launch_join_columns(s.columns[1], parts, p->N, dbu, st) : CSGS_OK;
+}

@@ -1,0 +1,277 @@
+// csgs_linear: y = alpha act(a w + bias) + beta r, and its gradient.
+#include "products.hpp"
+
+namespace csgs {
+
+struct LinearArgs {
+    Operand a, w;
+    int32_t M, K, N, act;
+    const int32_t *M_dev;
+    const float *bias;
+    const void *r, *dy;
+    int64_t ldr, lddy, ldy, lddr, ldt;
+    float alpha, beta;
+    void *y, *dr, *t;
+    float *columns;              // nullable: a row of column sums for each wavefront's rows
+    int64_t tiles_m, tiles_n;
+};
+
+// GRAD = false: y.  GRAD = true: t = alpha dy act'(a w + bias) as an operand of the gradients' products, its column sums, dr = beta dy.
+template <typename T, typename TY, int BM, int BN, int WM, int WN, bool GRAD>
+__global__ __launch_bounds__(WM *WN *WAVE) void linear_k(LinearArgs p)
+{
+    using Tile = MatrixTile<T, BM, BN, WM, WN, false, true, 1>;
+    __shared__ __attribute__((aligned(128))) char lds[Tile::LDS_BYTES];
+    int64_t tm, tn;
+    tile_place(blockIdx.x, p.tiles_m, p.tiles_n, &tm, &tn);
+    const int64_t m0 = tm * BM, n0 = tn * BN, rows = live_rows(p.M, p.M_dev);
+    if (m0 >= rows && !(GRAD && p.columns)) return;
+    Tile tile;
+    tile.clear();
+    if (m0 < rows) tile.accumulate(lds, p.a, &p.w, m0, rows, n0, p.N, 0, p.K);
+    float sums[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    tile.each([&](int m, int n, const float(&v)[1][4], int which) {
+        const int64_t row = m0 + m, col = n0 + n, rest = p.N - col;
+        const int count = rest >= 4 ? 4 : rest > 0 ? (int)rest : 0;
+        float z[4], x[4], t[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+        if (row < rows && count) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) z[i] = v[0][i] + (p.bias && i < count ? p.bias[col + i] : 0.0f);
+            if constexpr (!GRAD) {
+                if (p.r) load_some((const TY *)p.r + row * p.ldr + col, count, x);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    z[i] = p.alpha * activate(z[i], p.act).a;
+                    if (p.r) z[i] += p.beta * x[i];
+                }
+                store_some((TY *)p.y + row * p.ldy + col, count, z);
+            } else {
+                load_some((const TY *)p.dy + row * p.lddy + col, count, x);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) t[i] = i < count ? p.alpha * x[i] * activate(z[i], p.act).da : 0.0f;
+                store_some((T *)p.t + row * p.ldt + col, count, t);
+                if (p.dr) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) x[i] *= p.beta;
+                    store_some((TY *)p.dr + row * p.lddr + col, count, x);
+                }
+            }
+        }
+        if constexpr (GRAD) {
+            if (p.columns) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) sums[i] = which == 0 ? t[i] : sums[i] + t[i];
+                if (which == Tile::TM - 1) {
+                    const int64_t part = tm * WM + (int)threadIdx.x / WAVE / WN;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const float s = sum_of_32(sums[i]);
+                        if (((int)threadIdx.x & 31) == 0 && i < count) p.columns[part * p.N + col + i] = s;
+                    }
+                }
+            }
+        }
+    });
+}
+
+// Without an activation t is dy but for a factor.  A pass over dy: t in the operands' type, dr, column sums of alpha dy (a block's 64 rows at a time).
+constexpr int DY_ROWS = 64;
+template <typename T, typename TY>
+__global__ __launch_bounds__(256) void linear_dy_k(LinearArgs p)
+{
+    __shared__ float lds[4][64][4];
+    const int lane = (int)threadIdx.x & 63, group = (int)threadIdx.x >> 6;
+    const int64_t rows = live_rows(p.M, p.M_dev), part = blockIdx.x / p.tiles_n, col = ((int64_t)(blockIdx.x % p.tiles_n) * 64 + lane) * 4, rest = p.N - col;
+    const int count = rest >= 4 ? 4 : rest > 0 ? (int)rest : 0;
+    float sums[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    if (count)
+        for (int64_t row = part * DY_ROWS + group, k = 0; k < DY_ROWS / 4 && row < rows; row += 4, ++k) {
+            float x[4], t[4];
+            load_some((const TY *)p.dy + row * p.lddy + col, count, x);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                t[i] = p.alpha * x[i];
+                sums[i] += t[i];
+                x[i] *= p.beta;
+            }
+            if (p.t) store_some((T *)p.t + row * p.ldt + col, count, t);
+            if (p.dr) store_some((TY *)p.dr + row * p.lddr + col, count, x);
+        }
+    if (!p.columns) return;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) lds[group][lane][i] = sums[i];
+    __syncthreads();
+    if (group == 0)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (i < count) p.columns[part * p.N + col + i] = (lds[0][lane][i] + lds[1][lane][i]) + (lds[2][lane][i] + lds[3][lane][i]);
+}
+
+template <typename T, typename TY, int BM, int BN, int WM, int WN, bool GRAD>
+static int launch_shape(LinearArgs p, int64_t *parts, hipStream_t st)
+{
+    p.tiles_m = ((int64_t)p.M + BM - 1) / BM;
+    p.tiles_n = ((int64_t)p.N + BN - 1) / BN;
+    *parts = p.tiles_m * WM;
+    if (p.tiles_m * p.tiles_n > 1 << 30) return CSGS_EUNSUPPORTED;
+    CSGS_LAUNCH(K_LINEAR, (linear_k<T, TY, BM, BN, WM, WN, GRAD>), dim3((unsigned)(p.tiles_m * p.tiles_n)), dim3(WM * WN * WAVE), st, p);
+    CSGS_LAUNCH_CHECK();
+    return CSGS_OK;
+}
+template <typename T, typename TY, bool GRAD>
+static int launch_types(const LinearArgs &p, int64_t *parts, hipStream_t st)
+{
+    if ((((int64_t)p.M + 127) / 128) * (((int64_t)p.N + 127) / 128) >= 256) return launch_shape<T, TY, 128, 128, 2, 2, GRAD>(p, parts, st);
+    return launch_shape<T, TY, 64, 64, 2, 2, GRAD>(p, parts, st);
+}
+template <bool GRAD>
+static int launch_linear(const LinearArgs &p, int dtype, int y_dtype, int64_t *parts, hipStream_t st)
+{
+    if (dtype == CSGS_F32) return launch_types<float, float, GRAD>(p, parts, st);
+    if (y_dtype == CSGS_F32) return launch_types<uint16_t, float, GRAD>(p, parts, st);
+    return launch_types<uint16_t, uint16_t, GRAD>(p, parts, st);
+}
+static int launch_dy(LinearArgs p, int dtype, int y_dtype, int64_t *parts, hipStream_t st)
+{
+    *parts = ((int64_t)p.M + DY_ROWS - 1) / DY_ROWS;
+    p.tiles_n = ((int64_t)p.N + 255) / 256;
+    if (*parts * p.tiles_n > 1 << 30) return CSGS_EUNSUPPORTED;
+    const dim3 grid((unsigned)(*parts * p.tiles_n)), block(256);
+    if (dtype == CSGS_F32) CSGS_LAUNCH(K_LINEAR_DY, (linear_dy_k<float, float>), grid, block, st, p);
+    else if (y_dtype == CSGS_F32) CSGS_LAUNCH(K_LINEAR_DY, (linear_dy_k<uint16_t, float>), grid, block, st, p);
+    else CSGS_LAUNCH(K_LINEAR_DY, (linear_dy_k<uint16_t, uint16_t>), grid, block, st, p);
+    CSGS_LAUNCH_CHECK();
+    return CSGS_OK;
+}
+
+static int check(const csgs_linear_args *p, LinearArgs *a)
+{
+    if (!p || p->M <= 0 || p->K <= 0 || p->N <= 0 || !p->a || !p->w || p->lda < p->K || p->ldw < p->N || (p->r && p->ldr < p->N)) return CSGS_EINVAL;
+    if (p->act < CSGS_ACT_NONE || p->act > CSGS_ACT_GELU) return CSGS_EINVAL;
+    const bool same = p->dtype == p->y_dtype && (p->dtype == CSGS_F32 || p->dtype == CSGS_BF16);
+    if (!same && !(p->dtype == CSGS_BF16 && p->y_dtype == CSGS_F32)) return CSGS_EUNSUPPORTED;
+    *a = LinearArgs{};
+    a->a = Operand{p->a, p->lda};
+    a->w = Operand{p->w, p->ldw};
+    a->M = p->M;
+    a->K = p->K;
+    a->N = p->N;
+    a->act = p->act;
+    a->M_dev = p->M_dev;
+    a->bias = p->bias;
+    a->r = p->r;
+    a->ldr = p->ldr;
+    a->alpha = p->alpha;
+    a->beta = p->beta;
+    return CSGS_OK;
+}
+
+// Scratch of the gradient: t, rows of column sums, parts of the products.
+struct LinearScratch {
+    void *t;
+    float *columns, *parts;
+    size_t bytes;
+};
+static LinearScratch carve_linear(void *base, int32_t M, int32_t K, int32_t N, int dtype)
+{
+    LinearScratch s;
+    size_t off = align_up((size_t)M * (size_t)N * (dtype == CSGS_F32 ? 4 : 2), 256);
+    s.t = base;
+    s.columns = (float *)((char *)base + off);
+    off = align_up(off + (size_t)column_parts(M) * (size_t)N * 4, 256);
+    s.parts = (float *)((char *)base + off);
+    const int64_t da = out_product_floats(M, K, N, 1), dw = out_product_floats(K, N, M, 1);
+    s.bytes = align_up(off + (size_t)(da > dw ? da : dw) * 4, 256);
+    return s;
+}
+
+}  // namespace csgs
+
+using namespace csgs;
+
+extern "C" int csgs_linear(const csgs_linear_args *p, void *y, int64_t ldy, void *stream)
+{
+    LinearArgs a;
+    const int rc = check(p, &a);
+    if (rc != CSGS_OK) return rc;
+    if (!y || ldy < p->N || (y == p->r && ldy != p->ldr) || y == p->a || y == p->w) return CSGS_EINVAL;
+    a.y = y;
+    a.ldy = ldy;
+    int64_t parts;
+    return launch_linear<false>(a, p->dtype, p->y_dtype, &parts, (hipStream_t)stream);
+}
+
+extern "C" size_t csgs_linear_grad_scratch_bytes(int32_t M, int32_t K, int32_t N, int dtype)
+{
+    if (M <= 0 || K <= 0 || N <= 0 || (dtype != CSGS_F32 && dtype != CSGS_BF16)) return 0;
+    return carve_linear(nullptr, M, K, N, dtype).bytes;
+}
+
+extern "C" int csgs_linear_grad(const csgs_linear_args *p, const void *dy, int64_t lddy, void *da, int64_t ldda, void *dw, int64_t lddw, float *dbias, void *dr,
+                                int64_t lddr, void *scratch, size_t scratch_bytes, void *stream)
+{
+    LinearArgs a;
+    int rc = check(p, &a);
+    if (rc != CSGS_OK) return rc;
+    if (!dy || lddy < p->N || (da && ldda < p->K) || (dw && lddw < p->N) || (dr && lddr < p->N) || (!da && !dw && !dbias && !dr)) return CSGS_EINVAL;
+    if ((dbias && !p->bias) || (dr && !p->r) || (dr == dy && lddr != lddy) || da == dy || dw == dy) return CSGS_EINVAL;
+    if (!scratch || ((uintptr_t)scratch & 255)) return CSGS_EINVAL;
+    const LinearScratch s = carve_linear(scratch, p->M, p->K, p->N, p->dtype);
+    if (scratch_bytes < s.bytes) return CSGS_EWORKSPACE;
+    hipStream_t st = (hipStream_t)stream;
+    a.dy = dy;
+    a.lddy = lddy;
+    a.dr = dr;
+    a.lddr = lddr;
+    a.ldt = p->N;
+    a.columns = dbias ? s.columns : nullptr;
+    int64_t parts = 0;
+    Operand t{s.t, p->N};
+    float scale = 1.0f;
+    const bool plain = p->act == CSGS_ACT_NONE, direct = plain && p->dtype == p->y_dtype;
+    if (direct) {                   // (t is dy itself, its factor that of the products)
+        t = Operand{dy, lddy};
+        scale = p->alpha;
+    } else if (!plain || da || dw || dbias || dr) {
+        a.t = plain && !da && !dw ? nullptr : s.t;
+        rc = plain ? launch_dy(a, p->dtype, p->y_dtype, &parts, st) : launch_linear<true>(a, p->dtype, p->y_dtype, &parts, st);
+        if (rc != CSGS_OK) return rc;
+    }
+    if (da) {
+        OutProduct o{};
+        o.a[0] = t;
+        o.b[0] = a.w;
+        o.pairs = o.outs = 1;
+        o.out[0] = da;
+        o.ldo[0] = ldda;
+        o.rows = p->M;
+        o.cols = p->K;
+        o.red = p->N;
+        o.rows_dev = p->M_dev;
+        o.scale = scale;
+        o.across = false;
+        rc = launch_out_product(o, p->dtype, s.parts, st);
+        if (rc != CSGS_OK) return rc;
+    }
+    if (dw) {
+        OutProduct o{};
+        o.a[0] = a.a;
+        o.b[0] = t;
+        o.pairs = o.outs = 1;
+        o.out[0] = dw;
+        o.ldo[0] = lddw;
+        o.rows = p->K;
+        o.cols = p->N;
+        o.red = p->M;
+        o.red_dev = p->M_dev;
+        o.scale = scale;
+        o.across = true;
+        rc = launch_out_product(o, p->dtype, s.parts, st);
+        if (rc != CSGS_OK) return rc;
+    }
+    if (direct && (dbias || dr)) {   // (after the products: dr may be dy)
+        rc = launch_dy(a, p->dtype, p->y_dtype, &parts, st);
+        if (rc != CSGS_OK) return rc;
+    }
+    return dbias ? launch_join_columns(s.columns, parts, p->N, dbias, st) : CSGS_OK;
+}

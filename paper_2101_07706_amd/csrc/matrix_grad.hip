@@ -1,0 +1,167 @@
+// Products of the gradients: da = t w^T (both operands with the reduction side by side) and dw = a^T t (both with the outer index side by side).
+#include "products.hpp"
+
+namespace csgs {
+
+struct OutArgs {
+    Operand a[2], b[2];
+    void *out[2];
+    int64_t ldo[2];
+    int64_t rows, cols, red, part_len;
+    const int32_t *rows_dev, *red_dev;
+    int32_t pairs, parts, outs;
+    float scale;
+    float *part;
+    int64_t tiles_m, tiles_n;
+};
+
+template <typename T, int BM, int BN, int WM, int WN, bool ACROSS>
+__global__ __launch_bounds__(WM *WN *WAVE) void out_product_k(OutArgs p)
+{
+    using Tile = MatrixTile<T, BM, BN, WM, WN, ACROSS, ACROSS, 1>;
+    __shared__ __attribute__((aligned(128))) char lds[Tile::LDS_BYTES];
+    int64_t tm, tn;
+    tile_place(blockIdx.x, p.tiles_m, p.tiles_n, &tm, &tn);
+    const int64_t m0 = tm * BM, n0 = tn * BN;
+    const int64_t rows = p.rows_dev ? live_rows((int32_t)p.rows, p.rows_dev) : p.rows, red = p.red_dev ? live_rows((int32_t)p.red, p.red_dev) : p.red;
+    if (m0 >= rows) return;
+    const int which = (int)blockIdx.z;
+    const int64_t k0 = (int64_t)blockIdx.y * p.part_len, end = k0 + p.part_len, k1 = end < red ? end : red;
+    Tile tile;
+    tile.clear();
+    for (int i = 0; i < p.pairs; ++i) tile.accumulate(lds, p.a[i], &p.b[p.outs > 1 ? which : i], m0, rows, n0, p.cols, k0, k1);
+    float *part = p.part ? p.part + ((int64_t)which * p.parts + blockIdx.y) * p.rows * p.cols : nullptr;
+    tile.each([&](int m, int n, const float(&v)[1][4], int) {
+        const int64_t row = m0 + m, col = n0 + n, rest = p.cols - col;
+        if (row >= rows || rest <= 0) return;
+        const int count = rest < 4 ? (int)rest : 4;
+        if (part) {
+            store_some(part + row * p.cols + col, count, v[0]);
+        } else {
+            float x[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x[i] = p.scale * v[0][i];
+            store_some((T *)p.out[which] + row * p.ldo[which] + col, count, x);
+        }
+    });
+}
+
+// out = scale * the sum of the parts, in double in their order.
+template <typename T>
+__global__ __launch_bounds__(256) void join_parts_k(const float *__restrict__ part, int32_t parts, int64_t rows, int64_t cols, const int32_t *rows_dev, float scale,
+                                                    OutArgs p)
+{
+    const int which = (int)blockIdx.y;
+    const int64_t live = rows_dev ? live_rows((int32_t)rows, rows_dev) : rows, quads = (cols + 3) / 4, n = live * quads, stride = rows * cols;
+    const float *from = part + (int64_t)which * parts * stride;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
+        const int64_t row = i / quads, col = (i - row * quads) * 4, rest = cols - col;
+        const int count = rest < 4 ? (int)rest : 4;
+        double s[4] = {0.0, 0.0, 0.0, 0.0};
+        for (int32_t k = 0; k < parts; ++k) {
+            float x[4];
+            load_some(from + k * stride + row * cols + col, count, x);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s[e] += (double)x[e];
+        }
+        float x[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[e] = float_to_store<T>((double)scale * s[e]);
+        store_some((T *)p.out[which] + row * p.ldo[which] + col, count, x);
+    }
+}
+
+constexpr int JOIN_ROWS = 16;
+__global__ __launch_bounds__(64 * JOIN_ROWS) void join_columns_k(const float *__restrict__ part, int64_t parts, int32_t n, float *__restrict__ out)
+{
+    __shared__ double lds[JOIN_ROWS][64];
+    const int lane = (int)threadIdx.x & 63, group = (int)threadIdx.x >> 6;
+    const int64_t col = (int64_t)blockIdx.x * 64 + lane;
+    double s = 0.0;
+    if (col < n)
+        for (int64_t p = group; p < parts; p += JOIN_ROWS) s += (double)part[p * n + col];
+    lds[group][lane] = s;
+    __syncthreads();
+    if (group == 0 && col < n) {
+        for (int g = 1; g < JOIN_ROWS; ++g) s += lds[g][lane];
+        out[col] = (float)s;
+    }
+}
+
+int launch_join_columns(const float *part, int64_t parts, int32_t n, float *out, hipStream_t st)
+{
+    CSGS_LAUNCH(K_JOIN_COLUMNS, join_columns_k, dim3((unsigned)((n + 63) / 64)), dim3(64 * JOIN_ROWS), st, part, parts, n, out);
+    CSGS_LAUNCH_CHECK();
+    return CSGS_OK;
+}
+
+// Parts of a sum: as many as fill the device, each of at least PART_MIN terms, for at most PART_FLOATS floats beside one part.
+constexpr int64_t PART_MIN = 512, PART_FLOATS = 16ll << 20;
+int64_t out_product_floats(int64_t rows, int64_t cols, int64_t red, int outs)
+{
+    const int64_t one = rows * cols * outs, most = (red + PART_MIN - 1) / PART_MIN;
+    return most > 1 + PART_FLOATS / one ? one + PART_FLOATS : most * one;
+}
+static int64_t parts_of(int64_t rows, int64_t cols, int64_t red, int outs, int64_t blocks)
+{
+    const int64_t one = rows * cols * outs, most = (red + PART_MIN - 1) / PART_MIN, room = 1 + PART_FLOATS / one;
+    int64_t parts = (512 + blocks - 1) / blocks;
+    if (parts > most) parts = most;
+    if (parts > room) parts = room;
+    return parts < 1 ? 1 : parts;
+}
+
+template <typename T, int BM, int BN, int WM, int WN, bool ACROSS>
+static int launch_shape(const OutProduct &p, float *parts, hipStream_t st)
+{
+    OutArgs a{};
+    for (int i = 0; i < 2; ++i) {
+        a.a[i] = p.a[i];
+        a.b[i] = p.b[i];
+        a.out[i] = p.out[i];
+        a.ldo[i] = p.ldo[i];
+    }
+    a.rows = p.rows;
+    a.cols = p.cols;
+    a.red = p.red;
+    a.rows_dev = p.rows_dev;
+    a.red_dev = p.red_dev;
+    a.pairs = p.pairs;
+    a.outs = p.outs;
+    a.scale = p.scale;
+    a.tiles_m = (p.rows + BM - 1) / BM;
+    a.tiles_n = (p.cols + BN - 1) / BN;
+    const int64_t blocks = a.tiles_m * a.tiles_n;
+    if (blocks > 1 << 30) return CSGS_EUNSUPPORTED;
+    constexpr int64_t BK = Element<T>::BK;
+    int64_t n = parts_of(p.rows, p.cols, p.red, p.outs, blocks * p.outs);
+    a.part_len = ((p.red + n - 1) / n + BK - 1) / BK * BK;
+    n = (p.red + a.part_len - 1) / a.part_len;
+    a.parts = (int32_t)n;
+    a.part = n > 1 ? parts : nullptr;
+    CSGS_LAUNCH(K_OUT_PRODUCT, (out_product_k<T, BM, BN, WM, WN, ACROSS>), dim3((unsigned)blocks, (unsigned)n, (unsigned)p.outs), dim3(WM * WN * WAVE), st, a);
+    CSGS_LAUNCH_CHECK();
+    if (n > 1) {
+        const int64_t quads = p.rows * ((p.cols + 3) / 4), need = (quads + 255) / 256;
+        CSGS_LAUNCH(K_JOIN_PARTS, join_parts_k<T>, dim3((unsigned)(need < 2048 ? need : 2048), (unsigned)p.outs), dim3(256), st, parts, a.parts, p.rows, p.cols, p.rows_dev,
+                    p.scale, a);
+        CSGS_LAUNCH_CHECK();
+    }
+    return CSGS_OK;
+}
+
+template <typename T, bool ACROSS>
+static int launch_sides(const OutProduct &p, float *parts, hipStream_t st)
+{
+    const int64_t blocks = ((p.rows + 127) / 128) * ((p.cols + 127) / 128) * p.outs;
+    if (blocks * ((p.red + PART_MIN - 1) / PART_MIN) >= 256) return launch_shape<T, 128, 128, 2, 2, ACROSS>(p, parts, st);
+    return launch_shape<T, 64, 64, 2, 2, ACROSS>(p, parts, st);
+}
+
+int launch_out_product(const OutProduct &p, int dtype, float *parts, hipStream_t st)
+{
+    if (dtype == CSGS_F32) return p.across ? launch_sides<float, true>(p, parts, st) : launch_sides<float, false>(p, parts, st);
+    return p.across ? launch_sides<uint16_t, true>(p, parts, st) : launch_sides<uint16_t, false>(p, parts, st);
+}
+
+}  // namespace csgs

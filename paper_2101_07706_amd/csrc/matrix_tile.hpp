@@ -1,0 +1,246 @@
+// A block's tile of a product C [m x n] = A B on the matrix cores, for operands in bfloat16 or float whose rows start on any element.
+//
+// An operand is seen as outer index times reduction index k.  It lies in memory either with k side by side (ACROSS = false) or with the outer
+// index side by side (ACROSS = true); a tile is copied to LDS as it lies, in pieces of 16 bytes:
+//   k side by side      [outer][128 bytes of k]: a lane's part of a row is one 16-byte read.  Eight rows that are read together would meet in
+//                       the same banks: piece g of row r is kept at place g ^ (r / 2 % 8).
+//   outer side by side  [k][outer]: bfloat16 is turned by the LDS's transposing read (ds_read_b64_tr_b16: 16 lanes read 4 rows of k by 16
+//                       columns, each gets its column's 4 values); floats are read one by one.  32-byte segment s of row k at s ^ f(k), so that the four
+//                       rows of a read and those of its neighbours lie in different banks.
+// Products: v_mfma_f32_32x32x16_bf16 and v_mfma_f32_32x32x2_f32, sums in float.  The B operand is given to the instruction as its rows, so that a
+// lane ends up with four neighbouring columns of a row of C.
+#pragma once
+#include "common.hpp"
+#include "row_pieces.hpp"
+
+namespace csgs {
+
+#define CSGS_LDS __attribute__((address_space(3)))
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+
+// An operand: element (o, k) at p[o * ld + k], or p[k * ld + o] where the outer index lies side by side.
+struct Operand {
+    const void *p;
+    int64_t ld;
+};
+
+constexpr int TILE_ROW = 128;     // bytes of k in a row of a tile
+
+template <typename T>
+struct Element;
+template <>
+struct Element<uint16_t> {
+    static constexpr int BK = TILE_ROW / 2, PIECE = 8;
+};
+template <>
+struct Element<float> {
+    static constexpr int BK = TILE_ROW / 4, PIECE = 4;
+};
+
+// Which 32-byte segment of a row of k holds segment s (R outer entries of bfloat16 a row).
+template <int R>
+__device__ inline int across_turn(int k)
+{
+    if constexpr (R * 2 >= 256) return 2 * (k & 3) | ((k >> 3) & 1);
+    return 2 * ((k >> 1) & 1) | ((k >> 3) & 1);
+}
+
+// R outer entries by BK of an operand: copied to LDS by NT threads, read from there by wavefronts.
+template <typename T, int R, bool ACROSS, int NT>
+struct TileSide {
+    static constexpr int BK = Element<T>::BK, PIECE = Element<T>::PIECE;
+    static constexpr int BYTES = R * TILE_ROW;
+    static constexpr int PIECES = R * (TILE_ROW / 16) / NT;     // a thread's
+    static_assert(R * (TILE_ROW / 16) % NT == 0 && PIECES >= 1, "whole pieces for every thread");
+    static constexpr int ROW_PIECES = ACROSS ? R / PIECE : TILE_ROW / 16;
+
+    // The first element of the piece that belongs to place `id` of the tile.
+    static __device__ inline void piece(int id, int *o, int *k)
+    {
+        const int row = id / ROW_PIECES, place = id % ROW_PIECES;
+        if constexpr (!ACROSS) {
+            *o = row;
+            *k = (place ^ ((row >> 1) & 7)) * PIECE;
+        } else {
+            *k = row;
+            if constexpr (sizeof(T) == 2) *o = (((((place >> 1) ^ across_turn<R>(row)) << 1) | (place & 1))) * PIECE;
+            else *o = place * PIECE;
+        }
+    }
+
+    // Pieces by way of registers: anything outside the operand is zero.
+    u32x4 held[PIECES];
+    __device__ void ask(const Operand &op, int64_t o0, int64_t outer, int64_t k0, int64_t red)
+    {
+        const T *base = (const T *)op.p;
+#pragma unroll
+        for (int i = 0; i < PIECES; ++i) {
+            int po, pk;
+            piece((int)threadIdx.x + i * NT, &po, &pk);
+            const int64_t o = o0 + po, k = k0 + pk;
+            const int64_t at = ACROSS ? k * op.ld + o : o * op.ld + k;
+            const int64_t rest = ACROSS ? (k < red ? outer - o : 0) : (o < outer ? red - k : 0);
+            if (rest >= PIECE) {
+                held[i] = load_global<u32x4, (int)sizeof(T)>(base + at);
+            } else {
+                uint32_t w[4] = {0, 0, 0, 0};
+#pragma unroll
+                for (int e = 0; e < PIECE; ++e)
+                    if (e < rest) {
+                        if constexpr (sizeof(T) == 4) w[e] = load_global<uint32_t>(base + at + e);
+                        else w[e / 2] |= (uint32_t)load_global<uint16_t>(base + at + e) << (16 * (e & 1));
+                    }
+                held[i] = u32x4{w[0], w[1], w[2], w[3]};
+            }
+        }
+    }
+    __device__ void put(char *lds) const
+    {
+#pragma unroll
+        for (int i = 0; i < PIECES; ++i) *(u32x4 *)(lds + ((int)threadIdx.x + i * NT) * 16) = held[i];
+    }
+
+    // What a lane gives the matrix cores for the 32 outer entries from `first` on, of k from 16 * step (bfloat16) or 8 * step (floats) on.
+    static __device__ inline bf16x8 fragment(const char *lds, int first, int step, int lane)
+    {
+        static_assert(sizeof(T) == 2, "bfloat16");
+        if constexpr (!ACROSS) {
+            const int row = first + (lane & 31), g = 2 * step + (lane >> 5);
+            return *(const bf16x8 *)(lds + row * TILE_ROW + ((g ^ ((row >> 1) & 7)) << 4));
+        } else {
+            const int i = lane & 15, k = step * 16 + 8 * (lane >> 5) + (i >> 2);
+            const int segment = first / 16 + ((lane >> 4) & 1);
+            typedef short s16x8 __attribute__((ext_vector_type(8)));
+            s16x4 part[2];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int kk = k + 4 * h;
+                const char *at = lds + kk * (R * 2) + ((segment ^ across_turn<R>(kk)) << 5) + (i & 3) * 8;
+                part[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((CSGS_LDS s16x4 *)(CSGS_LDS void *)at);
+            }
+            const s16x8 both = {part[0].x, part[0].y, part[0].z, part[0].w, part[1].x, part[1].y, part[1].z, part[1].w};
+            return __builtin_bit_cast(bf16x8, both);
+        }
+    }
+    static __device__ inline f32x4 fragment_f32(const char *lds, int first, int step, int lane)
+    {
+        static_assert(sizeof(T) == 4, "floats");
+        if constexpr (!ACROSS) {
+            const int row = first + (lane & 31), g = 2 * step + (lane >> 5);
+            return *(const f32x4 *)(lds + row * TILE_ROW + ((g ^ ((row >> 1) & 7)) << 4));
+        } else {
+            const float *at = (const float *)lds + (step * 8 + 4 * (lane >> 5)) * R + first + (lane & 31);
+            return f32x4{at[0], at[R], at[2 * R], at[3 * R]};
+        }
+    }
+};
+
+// The tile: BM rows and, of each of NB matrices B, BN columns; WM x WN wavefronts.
+template <typename T, int BM, int BN, int WM, int WN, bool A_ACROSS, bool B_ACROSS, int NB>
+struct MatrixTile {
+    static constexpr int NT = WM * WN * WAVE, BK = Element<T>::BK;
+    static constexpr int TM = BM / WM / 32, TN = BN / WN / 32;     // 32 x 32 tiles of a wavefront
+    static_assert(TM >= 1 && TN >= 1 && TM * 32 * WM == BM && TN * 32 * WN == BN, "whole tiles");
+    using SideA = TileSide<T, BM, A_ACROSS, NT>;
+    using SideB = TileSide<T, BN, B_ACROSS, NT>;
+    static constexpr int LDS_BYTES = SideA::BYTES + NB * SideB::BYTES;
+
+    f32x16 acc[NB][TN][TM];
+
+    __device__ void clear()
+    {
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+            for (int n = 0; n < TN; ++n)
+#pragma unroll
+                for (int m = 0; m < TM; ++m)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) acc[b][n][m][r] = 0.0f;
+    }
+
+    __device__ void multiply(const char *lds)
+    {
+        const int lane = (int)threadIdx.x & (WAVE - 1), wave = (int)threadIdx.x / WAVE;
+        const int m0 = wave / WN * (TM * 32), n0 = wave % WN * (TN * 32);
+#pragma unroll
+        for (int step = 0; step < 4; ++step) {
+            if constexpr (sizeof(T) == 2) {
+                bf16x8 a[TM];
+#pragma unroll
+                for (int m = 0; m < TM; ++m) a[m] = SideA::fragment(lds, m0 + 32 * m, step, lane);
+#pragma unroll
+                for (int b = 0; b < NB; ++b)
+#pragma unroll
+                    for (int n = 0; n < TN; ++n) {
+                        const bf16x8 f = SideB::fragment(lds + SideA::BYTES + b * SideB::BYTES, n0 + 32 * n, step, lane);
+#pragma unroll
+                        for (int m = 0; m < TM; ++m) acc[b][n][m] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f, a[m], acc[b][n][m], 0, 0, 0);
+                    }
+            } else {
+                f32x4 a[TM];
+#pragma unroll
+                for (int m = 0; m < TM; ++m) a[m] = SideA::fragment_f32(lds, m0 + 32 * m, step, lane);
+#pragma unroll
+                for (int b = 0; b < NB; ++b)
+#pragma unroll
+                    for (int n = 0; n < TN; ++n) {
+                        const f32x4 f = SideB::fragment_f32(lds + SideA::BYTES + b * SideB::BYTES, n0 + 32 * n, step, lane);
+#pragma unroll
+                        for (int j = 0; j < 4; ++j)
+#pragma unroll
+                            for (int m = 0; m < TM; ++m) acc[b][n][m] = __builtin_amdgcn_mfma_f32_32x32x2f32(f[j], a[m][j], acc[b][n][m], 0, 0, 0);
+                    }
+            }
+        }
+    }
+
+    // Adds the products over k in [k0, k1): rows from m0 on of `rows`, columns from n0 on of `cols`.  One buffer in LDS: the next pieces are on their way
+    // while this one's products are formed.
+    __device__ void accumulate(char *lds, const Operand &a, const Operand *b, int64_t m0, int64_t rows, int64_t n0, int64_t cols, int64_t k0, int64_t k1)
+    {
+        SideA sa;
+        SideB sb[NB];
+        auto ask = [&](int64_t k) {
+            sa.ask(a, m0, rows, k, k1);
+#pragma unroll
+            for (int i = 0; i < NB; ++i) sb[i].ask(b[i], n0, cols, k, k1);
+        };
+        if (k0 >= k1) return;
+        ask(k0);
+        for (int64_t k = k0; k < k1; k += BK) {
+            __syncthreads();       // (the buffer's last readers are done)
+            sa.put(lds);
+#pragma unroll
+            for (int i = 0; i < NB; ++i) sb[i].put(lds + SideA::BYTES + i * SideB::BYTES);
+            __syncthreads();
+            if (k + BK < k1) ask(k + BK);
+            multiply(lds);
+        }
+    }
+
+    // f(row in the tile, first of four columns in it, the values of the NB matrices, which tile of the wavefront's): every lane's sums.
+    template <typename F>
+    __device__ void each(F f)
+    {
+        const int lane = (int)threadIdx.x & (WAVE - 1), wave = (int)threadIdx.x / WAVE;
+        const int m0 = wave / WN * (TM * 32) + (lane & 31), n0 = wave % WN * (TN * 32) + 4 * (lane >> 5);
+#pragma unroll
+        for (int n = 0; n < TN; ++n)
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+#pragma unroll
+                for (int m = 0; m < TM; ++m) {
+                    float v[NB][4];
+#pragma unroll
+                    for (int b = 0; b < NB; ++b)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) v[b][i] = acc[b][n][m][4 * q + i];
+                    f(m0 + 32 * m, n0 + 32 * n + 8 * q, v, m);
+                }
+    }
+};
+
+}  // namespace csgs

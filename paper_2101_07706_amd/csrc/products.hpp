@@ -1,0 +1,77 @@
+// Kernels of the feed-forward block's products: what they share (linear.hip, gated.hip, matrix_grad.hip).
+#pragma once
+#include "matrix_tile.hpp"
+
+namespace csgs {
+
+// act(z) and its derivative.  s(z) as the gates of the residual (residual.hip): e = exp(-z) with what the exponent's rounding loses put back, s = 1 / (1 + e), 1 - s = e s: both
+// keep their relative precision.  Phi(z) = erfc(-z / sqrt 2) / 2, without a difference.
+struct Activation {
+    float a, da;
+};
+__device__ inline Activation activate(float z, int32_t act)
+{
+    if (act == CSGS_ACT_NONE) return Activation{z, 1.0f};
+    if (act == CSGS_ACT_RELU) return Activation{z < 0.0f ? 0.0f : z, z > 0.0f ? 1.0f : 0.0f};     // (NaN stays)
+    if (act == CSGS_ACT_GELU) {
+        const float phi = 0.5f * erfcf(z * -0.707106781f);
+        return Activation{z * phi, phi + z * (0.398942280f * expf(-0.5f * z * z))};
+    }
+    const float t = z * -1.44269504f;
+    const float e = __builtin_amdgcn_exp2f(t) * fminf(1.0f + fmaf(t, -0.693147181f, -z), 2.0f);
+    const float s = __builtin_amdgcn_rcpf(1.0f + e), rest = fminf(e * s, 1.0f);
+    if (act == CSGS_ACT_SIGMOID) return Activation{s, s * rest};
+    return Activation{z * s, s * (1.0f + z * rest)};
+}
+
+__device__ inline int32_t live_rows(int32_t M, const int32_t *M_dev)
+{
+    if (!M_dev) return M;
+    const int32_t n = *M_dev;
+    return n < 0 ? 0 : n < M ? n : M;
+}
+
+// Block -> tile.  Blocks are handed to the eight dies in turn: each die takes tiles that follow each other, in bands of TILE_BAND tile rows, column by column, so
+// that what its cache holds of both operands is used by its next blocks.
+constexpr int TILE_BAND = 8, DIES = 8;
+__device__ inline void tile_place(int64_t b, int64_t tiles_m, int64_t tiles_n, int64_t *tm, int64_t *tn)
+{
+    const int64_t all = tiles_m * tiles_n, each = all / DIES, more = all % DIES, die = b % DIES, turn = b / DIES;
+    const int64_t t = die * each + (die < more ? die : more) + turn;
+    const int64_t band = t / (TILE_BAND * tiles_n), first = band * TILE_BAND;
+    const int64_t high = tiles_m - first < TILE_BAND ? tiles_m - first : TILE_BAND, in = t - first * tiles_n;
+    *tm = first + in % high;
+    *tn = in / high;
+}
+
+// Column sums over the rows of a wavefront's tile: v summed over its 32 lanes, in a fixed order.
+__device__ inline float sum_of_32(float v)
+{
+#pragma unroll
+    for (int s = 1; s < 32; s <<= 1) v += __shfl_xor(v, s);
+    return v;
+}
+
+// ---------------------------------------------------------------- host side, matrix_grad.hip
+// Sums over rows that blocks left as parts [parts x n], joined in double in their order.
+int launch_join_columns(const float *part, int64_t parts, int32_t n, float *out, hipStream_t st);
+
+// C = scale * (A B^T summed over the pairs of operands): what the gradients have of products.
+struct OutProduct {
+    Operand a[2], b[2];
+    int32_t pairs;            // 1, or 2: a[0] b[0] + a[1] b[1]
+    int32_t outs;             // 1, or 2: out[i] = a[0] b[i]
+    void *out[2];
+    int64_t ldo[2];
+    int64_t rows, cols, red;
+    const int32_t *rows_dev, *red_dev;   // nullable
+    float scale;
+    bool across;              // both operands lie with their outer index side by side, or both with the reduction
+};
+// Floats of memory for parts of such a product; does not fall as the sizes grow.
+int64_t out_product_floats(int64_t rows, int64_t cols, int64_t red, int outs);
+int launch_out_product(const OutProduct &p, int dtype, float *parts, hipStream_t st);
+
+// Rows of the scratch for column sums: a wavefront leaves one for at least 32 rows.
+inline int64_t column_parts(int32_t M) { return ((int64_t)M + 31) / 32 + 8; }
+}  // namespace csgs

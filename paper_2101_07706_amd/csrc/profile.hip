@@ -28,7 +28,7 @@ static const char *const kNames[K_COUNT] = {"row_prefix", "scan_edges", "cand_pa
                                             "layer_gemm_digits", "gemm_grad_z_digits",
                                             "embed", "embed_count", "embed_place", "embed_heads", "embed_zero", "embed_few", "embed_ranges", "embed_sum", "embed_join", "residual", "residual_grad",
                                             "col_sums", "grad_list", "grad_norm", "grad_total", "grad_scale",
-                                            "adamw_list", "adamw", "state_read", "state_write"};
+                                            "adamw_list", "adamw", "state_read", "state_write", "linear", "linear_dy", "gated", "out_product", "join_parts", "join_columns"};
 
 bool next_pair(int kid, hipEvent_t *start, hipEvent_t *stop)
 {

@@ -11,7 +11,8 @@ enum Kid {
     K_AGGREGATE, K_GEMM, K_GATHER_ROWS, K_GEMM_DZ, K_GEMM_DW, K_GEMM_DW_REDUCE, K_ADJT_COUNT, K_ADJT_PREFIX, K_ADJT_FILL, K_ADJT_ORDER,
     K_AGGREGATE_GRAD, K_FILL_ZERO, K_COPY, K_ATOMICS, K_MFMA_F64, K_LOOKUPS, K_LAYER_FORWARD, K_GEMM_DIGITS, K_GEMM_DZ_DIGITS,
     K_EMBED, K_EMBED_COUNT, K_EMBED_PLACE, K_EMBED_HEADS, K_EMBED_ZERO, K_EMBED_FEW, K_EMBED_RANGES, K_EMBED_SUM, K_EMBED_JOIN, K_RESIDUAL, K_RESIDUAL_GRAD, K_COL_SUMS, K_GRAD_LIST, K_GRAD_NORM,
-    K_GRAD_TOTAL, K_GRAD_SCALE, K_ADAMW_LIST, K_ADAMW, K_STATE_READ, K_STATE_WRITE, K_COUNT
+    K_GRAD_TOTAL, K_GRAD_SCALE, K_ADAMW_LIST, K_ADAMW, K_STATE_READ, K_STATE_WRITE, K_LINEAR, K_LINEAR_DY, K_GATED, K_OUT_PRODUCT,
+    K_JOIN_PARTS, K_JOIN_COLUMNS, K_COUNT
 };
 
 extern bool g_enabled;

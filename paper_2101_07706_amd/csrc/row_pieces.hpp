@@ -158,4 +158,28 @@ __device__ inline void store_row_past_caches(T *p, const Vec<V> &v)
         store_past_caches(p, u32x4{two(0), two(2), two(4), two(6)});
     }
 }
+// Up to four values at p: n of them.
+template <typename T>
+__device__ inline void load_some(const T *p, int n, float (&x)[4])
+{
+    if (n >= 4) {
+        const Vec<4> v = load_row<T, 4>(p);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] = v.x[i];
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = i < n ? load_row<T, 1>(p + i).x[0] : 0.0f;
+}
+template <typename T>
+__device__ inline void store_some(T *p, int n, const float (&x)[4])
+{
+    if (n >= 4) {
+        store_row<T, 4>(p, Vec<4>{{x[0], x[1], x[2], x[3]}});
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        if (i < n) store_row<T, 1>(p + i, Vec<1>{{x[i]}});
+}
 }  // namespace csgs

@@ -115,3 +115,123 @@ def test_plain_codes():
         assert torch.equal(plain.decode(codes, exps, second_state).float(), x) or second_state
         back = plain.decode(codes, exps, second_state)
         assert float((back - x.double()).abs().max()) <= 2.0 ** -16 * top
+
+
+def linear(**kw):
+    p = dict(M=4, K=6, N=5, act=0, M_dev=0, a=4096, w=8192, bias=12288, r=16384, lda=6, ldw=5, ldr=5, dtype=0, y_dtype=0, alpha=1.0, beta=1.0)
+    p.update(kw)
+    return csgs.LinearArgs(*[p[k] for k, _ in csgs.LinearArgs._fields_])
+
+
+def gated(**kw):
+    p = dict(M=4, K=6, N=5, act=3, M_dev=0, x=4096, wg=8192, wu=12288, bg=16384, bu=16384, ldx=6, ldwg=5, ldwu=5, dtype=0, reserved=0)
+    p.update(kw)
+    return csgs.GatedArgs(*[p[k] for k, _ in csgs.GatedArgs._fields_])
+
+
+def test_product_struct_layouts_match_the_header():
+    assert C.sizeof(csgs.LinearArgs) == 96 and csgs.LinearArgs.lda.offset == 56 and csgs.LinearArgs.alpha.offset == 88
+    assert C.sizeof(csgs.GatedArgs) == 96 and csgs.GatedArgs.ldx.offset == 64 and csgs.GatedArgs.dtype.offset == 88
+    assert csgs._linear_layout.size == 96 and csgs._gated_layout.size == 96
+
+
+BAD_LINEAR = [(dict(M=0), "EINVAL"), (dict(K=0), "EINVAL"), (dict(N=-1), "EINVAL"), (dict(a=0), "EINVAL"), (dict(w=0), "EINVAL"), (dict(lda=5), "EINVAL"), (dict(ldw=4), "EINVAL"),
+              (dict(ldr=4), "EINVAL"), (dict(act=5), "EINVAL"), (dict(act=-1), "EINVAL"), (dict(dtype=0, y_dtype=1), "EUNSUPPORTED"), (dict(dtype=2, y_dtype=2), "EUNSUPPORTED")]
+BAD_GATED = [(dict(M=0), "EINVAL"), (dict(K=-2), "EINVAL"), (dict(N=0), "EINVAL"), (dict(x=0), "EINVAL"), (dict(wg=0), "EINVAL"), (dict(wu=0), "EINVAL"), (dict(ldx=5), "EINVAL"),
+             (dict(ldwg=4), "EINVAL"), (dict(ldwu=4), "EINVAL"), (dict(act=5), "EINVAL"), (dict(act=-1), "EINVAL"), (dict(dtype=2), "EUNSUPPORTED")]
+ptr = C.c_void_p
+
+
+def test_linear():
+    L = csgs.lib()
+
+    def call(p, y=ptr(1 << 20), ldy=5):
+        return L.csgs_linear(C.byref(p), y, ldy, Z)
+    assert L.csgs_linear(None, P, 5, Z) == csgs.EINVAL
+    for bad, code in BAD_LINEAR:
+        assert call(linear(**bad)) == getattr(csgs, code), bad
+    for bad in (dict(y=Z), dict(ldy=4), dict(y=ptr(4096)), dict(y=ptr(8192)), dict(y=ptr(16384), ldy=6)):
+        assert call(linear(), **bad) == csgs.EINVAL, bad
+
+
+def test_linear_gradient():
+    L = csgs.lib()
+    need = csgs.csgs_linear_grad_scratch_bytes(4, 6, 5, csgs.F32)
+    full = dict(dy=ptr(1 << 20), lddy=5, da=ptr(2 << 20), ldda=6, dw=ptr(3 << 20), lddw=5, db=ptr(4 << 20), dr=ptr(5 << 20), lddr=5, scratch=ptr(6 << 20), nbytes=need)
+
+    def call(p, **kw):
+        a = {**full, **kw}
+        return L.csgs_linear_grad(None if p is None else C.byref(p), a["dy"], a["lddy"], a["da"], a["ldda"], a["dw"], a["lddw"], a["db"], a["dr"], a["lddr"], a["scratch"], a["nbytes"], Z)
+    assert call(None) == csgs.EINVAL
+    for bad, code in BAD_LINEAR:
+        assert call(linear(**bad)) == getattr(csgs, code), bad
+    for bad in (dict(dy=Z), dict(lddy=4), dict(ldda=5), dict(lddw=4), dict(lddr=4), dict(da=Z, dw=Z, db=Z, dr=Z), dict(dr=ptr(1 << 20), lddr=6), dict(da=ptr(1 << 20)),
+                dict(dw=ptr(1 << 20)), dict(scratch=Z), dict(scratch=ptr(4224))):
+        assert call(linear(), **bad) == csgs.EINVAL, bad
+    assert call(linear(bias=0)) == csgs.EINVAL and call(linear(r=0)) == csgs.EINVAL
+    assert call(linear(), nbytes=need - 1) == csgs.EWORKSPACE
+
+
+def test_gated():
+    L = csgs.lib()
+
+    def call(p, h=ptr(1 << 20), ldh=5):
+        return L.csgs_gated(C.byref(p), h, ldh, Z)
+    assert L.csgs_gated(None, P, 5, Z) == csgs.EINVAL
+    for bad, code in BAD_GATED:
+        assert call(gated(**bad)) == getattr(csgs, code), bad
+    for bad in (dict(h=Z), dict(ldh=4), dict(h=ptr(4096)), dict(h=ptr(8192)), dict(h=ptr(12288))):
+        assert call(gated(), **bad) == csgs.EINVAL, bad
+
+
+def test_gated_gradient():
+    L = csgs.lib()
+    need = csgs.csgs_gated_grad_scratch_bytes(4, 6, 5, csgs.F32)
+    full = dict(dh=ptr(1 << 20), lddh=5, dx=ptr(2 << 20), lddx=6, dwg=ptr(3 << 20), lddwg=5, dwu=ptr(4 << 20), lddwu=5, dbg=ptr(5 << 20), dbu=ptr(6 << 20), scratch=ptr(7 << 20), nbytes=need)
+
+    def call(p, **kw):
+        a = {**full, **kw}
+        return L.csgs_gated_grad(None if p is None else C.byref(p), a["dh"], a["lddh"], a["dx"], a["lddx"], a["dwg"], a["lddwg"], a["dwu"], a["lddwu"], a["dbg"], a["dbu"], a["scratch"],
+                                 a["nbytes"], Z)
+    assert call(None) == csgs.EINVAL
+    for bad, code in BAD_GATED:
+        assert call(gated(**bad)) == getattr(csgs, code), bad
+    for bad in (dict(dh=Z), dict(lddh=4), dict(lddx=5), dict(lddwg=4), dict(lddwu=4), dict(dx=Z, dwg=Z, dwu=Z, dbg=Z, dbu=Z), dict(dx=ptr(1 << 20)), dict(dwg=ptr(1 << 20)),
+                dict(dwu=ptr(1 << 20)), dict(scratch=Z), dict(scratch=ptr(4224))):
+        assert call(gated(), **bad) == csgs.EINVAL, bad
+    assert call(gated(bg=0)) == csgs.EINVAL and call(gated(bu=0)) == csgs.EINVAL
+    assert call(gated(), nbytes=need - 1) == csgs.EWORKSPACE
+
+
+@pytest.mark.parametrize("size", [csgs.csgs_linear_grad_scratch_bytes, csgs.csgs_gated_grad_scratch_bytes])
+def test_scratch_for_the_largest_product_serves_smaller_ones(size):
+    assert size(0, 1, 1, 0) == 0 and size(1, 0, 1, 0) == 0 and size(1, 1, 0, 0) == 0 and size(1, 1, 1, 2) == 0 and size(-1, 1, 1, 0) == 0
+    Ms, Ks, Ns = [1, 2, 63, 64, 65, 511, 512, 513, 8192, 8193, 65_536, 131_072, 1 << 24], [1, 7, 64, 512, 513, 1024, 4096, 1 << 20], [1, 5, 64, 512, 513, 1111, 4096, 1 << 20]
+    for dtype in (csgs.F32, csgs.BF16):
+        for M in Ms:
+            for K in Ks:
+                row = [size(M, K, N, dtype) for N in Ns]
+                assert all(0 < a <= b for a, b in zip(row, row[1:]))
+        for M in Ms:
+            for N in Ns:
+                row = [size(M, K, N, dtype) for K in Ks]
+                assert all(a <= b for a, b in zip(row, row[1:]))
+        for K in Ks:
+            for N in Ns:
+                row = [size(M, K, N, dtype) for M in Ms]
+                assert all(a <= b for a, b in zip(row, row[1:]))
+
+
+def test_binding_refuses_products_that_it_cannot_describe():
+    a, w, y, b = torch.zeros(4, 6), torch.zeros(6, 5), torch.zeros(4, 5), torch.zeros(5)
+    s = torch.zeros(64)
+    for bad in (lambda: csgs.csgs_linear(a.half(), w.half(), y), lambda: csgs.csgs_linear(a, w.bfloat16(), y), lambda: csgs.csgs_linear(a, torch.zeros(7, 5), y),
+                lambda: csgs.csgs_linear(a, w, torch.zeros(4, 6)), lambda: csgs.csgs_linear(a, w, y, bias=torch.zeros(6)), lambda: csgs.csgs_linear(a, w, y, bias=b.double()),
+                lambda: csgs.csgs_linear(a, w, y, r=y.bfloat16()), lambda: csgs.csgs_linear(a, w, y, r=torch.zeros(3, 5)), lambda: csgs.csgs_linear(a.t().contiguous().t(), w, y),
+                lambda: csgs.csgs_linear(a, w, y, M_dev=torch.zeros(1)), lambda: csgs.csgs_linear_grad(a, w, y, torch.zeros(4, 5), None, None, None, s),
+                lambda: csgs.csgs_linear_grad(a, w, y, None, w.bfloat16(), None, None, s), lambda: csgs.csgs_linear_grad(a, w, y, None, w, torch.zeros(4), None, s),
+                lambda: csgs.csgs_linear_grad(a, w, y, None, w, None, None, torch.zeros(8, 8)[:, :4]), lambda: csgs.csgs_gated(a, w, torch.zeros(6, 4), y),
+                lambda: csgs.csgs_gated(a, w, w, y.bfloat16()), lambda: csgs.csgs_gated(a, w, w, y, bg=torch.zeros(4)), lambda: csgs.csgs_gated(a.double(), w.double(), w.double(), y),
+                lambda: csgs.csgs_gated_grad(a, w, w, y, None, w, torch.zeros(5, 6), None, None, s), lambda: csgs.csgs_gated_grad(a, w, w, torch.zeros(4, 6), a, w, w, None, None, s)):
+        with pytest.raises((AssertionError, TypeError)):
+            bad()
