@@ -1,5 +1,6 @@
 // csgs_gated: h = act(x wg + bg) .* (x wu + bu), and its gradient.  One tile of x serves both products.
 #include "products.hpp"
+#include "direct_tile.hpp"
 
 namespace csgs {
 
@@ -16,10 +17,10 @@ struct GatedArgs {
 };
 
 // GRAD = false: h.  GRAD = true: tg and tu as operands of the gradients' products, and their column sums.
-template <typename T, int BM, int BN, int WM, int WN, bool GRAD>
-__global__ __launch_bounds__(WM *WN *WAVE) void gated_k(GatedArgs p)
+template <class Tile, typename T, bool GRAD>
+__global__ __launch_bounds__(Tile::NT) void gated_k(GatedArgs p)
 {
-    using Tile = MatrixTile<T, BM, BN, WM, WN, false, true, 2>;
+    constexpr int BM = Tile::ROWS, BN = Tile::COLS, WM = Tile::WAVES_M, WN = Tile::WAVES_N;
     __shared__ __attribute__((aligned(128))) char lds[Tile::LDS_BYTES];
     int64_t tm, tn;
     tile_place(blockIdx.x, p.tiles_m, p.tiles_n, &tm, &tn);
@@ -28,67 +29,84 @@ __global__ __launch_bounds__(WM *WN *WAVE) void gated_k(GatedArgs p)
     if (m0 >= rows && !columns) return;
     Tile tile;
     tile.clear();
-    if (m0 < rows) tile.accumulate(lds, p.x, p.w, m0, rows, n0, p.N, 0, p.K);
+    if (m0 < rows) tile.accumulate(lds, p.x, p.w, m0, rows, n0, p.N, 0, p.K, stagger(tm, tn));
     float sums[2][4] = {};
-    tile.each([&](int m, int n, const float(&v)[2][4], int which) {
-        const int64_t row = m0 + m, col = n0 + n, rest = p.N - col;
-        const int count = rest >= 4 ? 4 : rest > 0 ? (int)rest : 0;
-        float t[2][4] = {};
-        if (row < rows && count) {
-            float x[4], h[4];
-            if constexpr (GRAD) load_some((const T *)p.dh + row * p.lddh + col, count, x);
+    const auto count_of = [&](int64_t row, int64_t col) CSGS_INLINE { return row >= rows || col >= p.N ? 0 : p.N - col >= 4 ? 4 : (int)(p.N - col); };
+    const auto ask = [&](int m, int n) CSGS_INLINE {
+        if constexpr (GRAD) {
+            Quad<T> x;
+            x.load((const T *)p.dh + (m0 + m) * p.lddh + n0 + n, count_of(m0 + m, n0 + n));
+            return x;
+        } else {
+            return Nothing{};
+        }
+    };
+    with_activation(p.act, [&](auto act) CSGS_INLINE {
+        constexpr int ACT = decltype(act)::value;
+        tile.each(lds, ask, [&](int m, int n, const float(&v)[2][4], const auto &held) CSGS_INLINE {
+            const int64_t row = m0 + m, col = n0 + n;
+            const int count = count_of(row, col);
+            if (!count) return;
+            float t[2][4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const float g = v[0][i] + (p.b[0] && i < count ? p.b[0][col + i] : 0.0f), u = v[1][i] + (p.b[1] && i < count ? p.b[1][col + i] : 0.0f);
-                const Activation a = activate(g, p.act);
+                const Activation a = activate<ACT>(g);
                 if constexpr (!GRAD) {
-                    h[i] = a.a * u;
-                } else if (i < count) {
-                    t[0][i] = x[i] * u * a.da;
-                    t[1][i] = x[i] * a.a;
+                    t[0][i] = a.a * u;
+                } else {
+                    t[0][i] = i < count ? held.value(i) * u * a.da : 0.0f;
+                    t[1][i] = i < count ? held.value(i) * a.a : 0.0f;
+                    sums[0][i] += t[0][i];
+                    sums[1][i] += t[1][i];
                 }
             }
             if constexpr (!GRAD) {
-                store_some((T *)p.h + row * p.ldh + col, count, h);
+                store_some((T *)p.h + row * p.ldh + col, count, t[0]);
             } else {
                 store_some((T *)p.t[0] + row * p.ldt + col, count, t[0]);
                 store_some((T *)p.t[1] + row * p.ldt + col, count, t[1]);
             }
-        }
-        if (columns) {
-            const int64_t part = tm * WM + (int)threadIdx.x / WAVE / WN;
-#pragma unroll
-            for (int b = 0; b < 2; ++b)
-                if (p.columns[b])
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        sums[b][i] = which == 0 ? t[b][i] : sums[b][i] + t[b][i];
-                        if (which == Tile::TM - 1) {
-                            const float s = sum_of_32(sums[b][i]);
-                            if (((int)threadIdx.x & 31) == 0 && i < count) p.columns[b][part * p.N + col + i] = s;
-                        }
-                    }
-        }
+        });
     });
+    if constexpr (GRAD)
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+            if (p.columns[b])
+                Tile::columns(sums[b], [&](int n, const float(&s)[4]) CSGS_INLINE {
+                    const int64_t col = n0 + n, rest = p.N - col;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        if (i < rest) p.columns[b][(tm * WM + (int)threadIdx.x / WAVE / WN) * p.N + col + i] = s[i];
+                });
 }
 
-template <typename T, int BM, int BN, int WM, int WN, bool GRAD>
+template <class Tile, typename T, bool GRAD>
 static int launch_shape(GatedArgs p, int64_t *parts, hipStream_t st)
 {
+    constexpr int BM = Tile::ROWS, BN = Tile::COLS, WM = Tile::WAVES_M;
     p.tiles_m = ((int64_t)p.M + BM - 1) / BM;
     p.tiles_n = ((int64_t)p.N + BN - 1) / BN;
     *parts = p.tiles_m * WM;
     if (p.tiles_m * p.tiles_n > 1 << 30) return CSGS_EUNSUPPORTED;
-    CSGS_LAUNCH(K_GATED, (gated_k<T, BM, BN, WM, WN, GRAD>), dim3((unsigned)(p.tiles_m * p.tiles_n)), dim3(WM * WN * WAVE), st, p);
+    CSGS_LAUNCH(K_GATED, (gated_k<Tile, T, GRAD>), dim3((unsigned)(p.tiles_m * p.tiles_n)), dim3(Tile::NT), st, p);
     CSGS_LAUNCH_CHECK();
     return CSGS_OK;
+}
+template <typename T, bool GRAD>
+static int launch_types(const GatedArgs &p, int64_t *parts, hipStream_t st)
+{
+    const auto tiles = [&](int64_t m, int64_t n) { return (p.M + m - 1) / m * ((p.N + n - 1) / n); };
+    if constexpr (sizeof(T) == 2)
+        if (tiles(256, 128) >= 200 && direct_operand(p.x, false, p.M, p.K, 256) && direct_operand(p.w[0], true, p.N, p.K, 128) && direct_operand(p.w[1], true, p.N, p.K, 128))
+            return launch_shape<DirectTile<256, 128, 2, 2, false, true, 2>, T, GRAD>(p, parts, st);
+    if (tiles(128, 64) >= 256) return launch_shape<MatrixTile<T, 128, 64, 2, 2, false, true, 2>, T, GRAD>(p, parts, st);
+    return launch_shape<MatrixTile<T, 64, 64, 2, 2, false, true, 2>, T, GRAD>(p, parts, st);
 }
 template <bool GRAD>
 static int launch_gated(const GatedArgs &p, int dtype, int64_t *parts, hipStream_t st)
 {
-    const bool large = (((int64_t)p.M + 127) / 128) * (((int64_t)p.N + 63) / 64) >= 256;
-    if (dtype == CSGS_F32) return large ? launch_shape<float, 128, 64, 2, 2, GRAD>(p, parts, st) : launch_shape<float, 64, 64, 2, 2, GRAD>(p, parts, st);
-    return large ? launch_shape<uint16_t, 128, 64, 2, 2, GRAD>(p, parts, st) : launch_shape<uint16_t, 64, 64, 2, 2, GRAD>(p, parts, st);
+    return dtype == CSGS_F32 ? launch_types<float, GRAD>(p, parts, st) : launch_types<uint16_t, GRAD>(p, parts, st);
 }
 
 static int check(const csgs_gated_args *p, GatedArgs *a)

@@ -1,5 +1,6 @@
 // csgs_linear: y = alpha act(a w + bias) + beta r, and its gradient.
 #include "products.hpp"
+#include "direct_tile.hpp"
 
 namespace csgs {
 
@@ -17,10 +18,10 @@ struct LinearArgs {
 };
 
 // GRAD = false: y.  GRAD = true: t = alpha dy act'(a w + bias) as an operand of the gradients' products, its column sums, dr = beta dy.
-template <typename T, typename TY, int BM, int BN, int WM, int WN, bool GRAD>
-__global__ __launch_bounds__(WM *WN *WAVE) void linear_k(LinearArgs p)
+template <class Tile, typename T, typename TY, bool GRAD>
+__global__ __launch_bounds__(Tile::NT) void linear_k(LinearArgs p)
 {
-    using Tile = MatrixTile<T, BM, BN, WM, WN, false, true, 1>;
+    constexpr int BM = Tile::ROWS, BN = Tile::COLS, WM = Tile::WAVES_M, WN = Tile::WAVES_N;
     __shared__ __attribute__((aligned(128))) char lds[Tile::LDS_BYTES];
     int64_t tm, tn;
     tile_place(blockIdx.x, p.tiles_m, p.tiles_n, &tm, &tn);
@@ -28,50 +29,53 @@ __global__ __launch_bounds__(WM *WN *WAVE) void linear_k(LinearArgs p)
     if (m0 >= rows && !(GRAD && p.columns)) return;
     Tile tile;
     tile.clear();
-    if (m0 < rows) tile.accumulate(lds, p.a, &p.w, m0, rows, n0, p.N, 0, p.K);
+    if (m0 < rows) tile.accumulate(lds, p.a, &p.w, m0, rows, n0, p.N, 0, p.K, stagger(tm, tn));
     float sums[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-    tile.each([&](int m, int n, const float(&v)[1][4], int which) {
-        const int64_t row = m0 + m, col = n0 + n, rest = p.N - col;
-        const int count = rest >= 4 ? 4 : rest > 0 ? (int)rest : 0;
-        float z[4], x[4], t[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-        if (row < rows && count) {
+    const auto count_of = [&](int64_t row, int64_t col) CSGS_INLINE { return row >= rows || col >= p.N ? 0 : p.N - col >= 4 ? 4 : (int)(p.N - col); };
+    const TY *beside = (const TY *)(GRAD ? p.dy : p.r);
+    const int64_t ld = GRAD ? p.lddy : p.ldr;
+    const auto ask = [&](int m, int n) CSGS_INLINE {
+        Quad<TY> x;
+        const int count = beside ? count_of(m0 + m, n0 + n) : 0;
+        x.load(beside + (m0 + m) * ld + n0 + n, count);
+        return x;
+    };
+    with_activation(p.act, [&](auto act) CSGS_INLINE {
+        constexpr int ACT = decltype(act)::value;
+        tile.each(lds, ask, [&](int m, int n, const float(&v)[1][4], const Quad<TY> &held) CSGS_INLINE {
+            const int64_t row = m0 + m, col = n0 + n;
+            const int count = count_of(row, col);
+            if (!count) return;
+            float z[4], x[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) z[i] = v[0][i] + (p.bias && i < count ? p.bias[col + i] : 0.0f);
             if constexpr (!GRAD) {
-                if (p.r) load_some((const TY *)p.r + row * p.ldr + col, count, x);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    z[i] = p.alpha * activate(z[i], p.act).a;
-                    if (p.r) z[i] += p.beta * x[i];
+                    z[i] = p.alpha * activate<ACT>(z[i]).a;
+                    if (p.r) z[i] += p.beta * held.value(i);
                 }
                 store_some((TY *)p.y + row * p.ldy + col, count, z);
             } else {
-                load_some((const TY *)p.dy + row * p.lddy + col, count, x);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) t[i] = i < count ? p.alpha * x[i] * activate(z[i], p.act).da : 0.0f;
-                store_some((T *)p.t + row * p.ldt + col, count, t);
-                if (p.dr) {
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) x[i] *= p.beta;
-                    store_some((TY *)p.dr + row * p.lddr + col, count, x);
+                for (int i = 0; i < 4; ++i) {
+                    x[i] = held.value(i);
+                    z[i] = i < count ? p.alpha * x[i] * activate<ACT>(z[i]).da : 0.0f;
+                    sums[i] += z[i];
+                    x[i] *= p.beta;
                 }
+                if (p.t) store_some((T *)p.t + row * p.ldt + col, count, z);
+                if (p.dr) store_some((TY *)p.dr + row * p.lddr + col, count, x);
             }
-        }
-        if constexpr (GRAD) {
-            if (p.columns) {
-#pragma unroll
-                for (int i = 0; i < 4; ++i) sums[i] = which == 0 ? t[i] : sums[i] + t[i];
-                if (which == Tile::TM - 1) {
-                    const int64_t part = tm * WM + (int)threadIdx.x / WAVE / WN;
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const float s = sum_of_32(sums[i]);
-                        if (((int)threadIdx.x & 31) == 0 && i < count) p.columns[part * p.N + col + i] = s;
-                    }
-                }
-            }
-        }
+        });
     });
+    if (GRAD && p.columns)
+        Tile::columns(sums, [&](int n, const float(&s)[4]) CSGS_INLINE {
+            const int64_t col = n0 + n, rest = p.N - col;
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (i < rest) p.columns[(tm * WM + (int)threadIdx.x / WAVE / WN) * p.N + col + i] = s[i];
+        });
 }
 
 // Without an activation t is dy but for a factor.  A pass over dy: t in the operands' type, dr, column sums of alpha dy (a block's 64 rows at a time).
@@ -107,22 +111,27 @@ __global__ __launch_bounds__(256) void linear_dy_k(LinearArgs p)
             if (i < count) p.columns[part * p.N + col + i] = (lds[0][lane][i] + lds[1][lane][i]) + (lds[2][lane][i] + lds[3][lane][i]);
 }
 
-template <typename T, typename TY, int BM, int BN, int WM, int WN, bool GRAD>
+template <class Tile, typename T, typename TY, bool GRAD>
 static int launch_shape(LinearArgs p, int64_t *parts, hipStream_t st)
 {
+    constexpr int BM = Tile::ROWS, BN = Tile::COLS, WM = Tile::WAVES_M;
     p.tiles_m = ((int64_t)p.M + BM - 1) / BM;
     p.tiles_n = ((int64_t)p.N + BN - 1) / BN;
     *parts = p.tiles_m * WM;
     if (p.tiles_m * p.tiles_n > 1 << 30) return CSGS_EUNSUPPORTED;
-    CSGS_LAUNCH(K_LINEAR, (linear_k<T, TY, BM, BN, WM, WN, GRAD>), dim3((unsigned)(p.tiles_m * p.tiles_n)), dim3(WM * WN * WAVE), st, p);
+    CSGS_LAUNCH(K_LINEAR, (linear_k<Tile, T, TY, GRAD>), dim3((unsigned)(p.tiles_m * p.tiles_n)), dim3(Tile::NT), st, p);
     CSGS_LAUNCH_CHECK();
     return CSGS_OK;
 }
 template <typename T, typename TY, bool GRAD>
 static int launch_types(const LinearArgs &p, int64_t *parts, hipStream_t st)
 {
-    if ((((int64_t)p.M + 127) / 128) * (((int64_t)p.N + 127) / 128) >= 256) return launch_shape<T, TY, 128, 128, 2, 2, GRAD>(p, parts, st);
-    return launch_shape<T, TY, 64, 64, 2, 2, GRAD>(p, parts, st);
+    const auto tiles = [&](int64_t m, int64_t n) { return (p.M + m - 1) / m * ((p.N + n - 1) / n); };
+    if constexpr (sizeof(T) == 2)
+        if (tiles(256, 256) >= 200 && direct_operand(p.a, false, p.M, p.K, 256) && direct_operand(p.w, true, p.N, p.K, 256))
+            return launch_shape<DirectTile<256, 256, 2, 2, false, true, 1>, T, TY, GRAD>(p, parts, st);
+    if (tiles(128, 128) >= 256) return launch_shape<MatrixTile<T, 128, 128, 2, 2, false, true, 1>, T, TY, GRAD>(p, parts, st);
+    return launch_shape<MatrixTile<T, 64, 64, 2, 2, false, true, 1>, T, TY, GRAD>(p, parts, st);
 }
 template <bool GRAD>
 static int launch_linear(const LinearArgs &p, int dtype, int y_dtype, int64_t *parts, hipStream_t st)

@@ -1,5 +1,6 @@
 // Products of the gradients: da = t w^T (both operands with the reduction side by side) and dw = a^T t (both with the outer index side by side).
 #include "products.hpp"
+#include "direct_tile.hpp"
 
 namespace csgs {
 
@@ -15,10 +16,10 @@ struct OutArgs {
     int64_t tiles_m, tiles_n;
 };
 
-template <typename T, int BM, int BN, int WM, int WN, bool ACROSS>
-__global__ __launch_bounds__(WM *WN *WAVE) void out_product_k(OutArgs p)
+template <class Tile, typename T>
+__global__ __launch_bounds__(Tile::NT) void out_product_k(OutArgs p)
 {
-    using Tile = MatrixTile<T, BM, BN, WM, WN, ACROSS, ACROSS, 1>;
+    constexpr int BM = Tile::ROWS, BN = Tile::COLS;
     __shared__ __attribute__((aligned(128))) char lds[Tile::LDS_BYTES];
     int64_t tm, tn;
     tile_place(blockIdx.x, p.tiles_m, p.tiles_n, &tm, &tn);
@@ -29,9 +30,9 @@ __global__ __launch_bounds__(WM *WN *WAVE) void out_product_k(OutArgs p)
     const int64_t k0 = (int64_t)blockIdx.y * p.part_len, end = k0 + p.part_len, k1 = end < red ? end : red;
     Tile tile;
     tile.clear();
-    for (int i = 0; i < p.pairs; ++i) tile.accumulate(lds, p.a[i], &p.b[p.outs > 1 ? which : i], m0, rows, n0, p.cols, k0, k1);
+    for (int i = 0; i < p.pairs; ++i) tile.accumulate(lds, p.a[i], &p.b[p.outs > 1 ? which : i], m0, rows, n0, p.cols, k0, k1, stagger(tm, tn));
     float *part = p.part ? p.part + ((int64_t)which * p.parts + blockIdx.y) * p.rows * p.cols : nullptr;
-    tile.each([&](int m, int n, const float(&v)[1][4], int) {
+    tile.each(lds, [](int, int) { return Nothing{}; }, [&](int m, int n, const float(&v)[1][4], Nothing) CSGS_INLINE {
         const int64_t row = m0 + m, col = n0 + n, rest = p.cols - col;
         if (row >= rows || rest <= 0) return;
         const int count = rest < 4 ? (int)rest : 4;
@@ -111,9 +112,10 @@ static int64_t parts_of(int64_t rows, int64_t cols, int64_t red, int outs, int64
     return parts < 1 ? 1 : parts;
 }
 
-template <typename T, int BM, int BN, int WM, int WN, bool ACROSS>
+template <class Tile, typename T>
 static int launch_shape(const OutProduct &p, float *parts, hipStream_t st)
 {
+    constexpr int BM = Tile::ROWS, BN = Tile::COLS;
     OutArgs a{};
     for (int i = 0; i < 2; ++i) {
         a.a[i] = p.a[i];
@@ -139,7 +141,7 @@ static int launch_shape(const OutProduct &p, float *parts, hipStream_t st)
     n = (p.red + a.part_len - 1) / a.part_len;
     a.parts = (int32_t)n;
     a.part = n > 1 ? parts : nullptr;
-    CSGS_LAUNCH(K_OUT_PRODUCT, (out_product_k<T, BM, BN, WM, WN, ACROSS>), dim3((unsigned)blocks, (unsigned)n, (unsigned)p.outs), dim3(WM * WN * WAVE), st, a);
+    CSGS_LAUNCH(K_OUT_PRODUCT, (out_product_k<Tile, T>), dim3((unsigned)blocks, (unsigned)n, (unsigned)p.outs), dim3(Tile::NT), st, a);
     CSGS_LAUNCH_CHECK();
     if (n > 1) {
         const int64_t quads = p.rows * ((p.cols + 3) / 4), need = (quads + 255) / 256;
@@ -153,9 +155,18 @@ static int launch_shape(const OutProduct &p, float *parts, hipStream_t st)
 template <typename T, bool ACROSS>
 static int launch_sides(const OutProduct &p, float *parts, hipStream_t st)
 {
-    const int64_t blocks = ((p.rows + 127) / 128) * ((p.cols + 127) / 128) * p.outs;
-    if (blocks * ((p.red + PART_MIN - 1) / PART_MIN) >= 256) return launch_shape<T, 128, 128, 2, 2, ACROSS>(p, parts, st);
-    return launch_shape<T, 64, 64, 2, 2, ACROSS>(p, parts, st);
+    const int64_t most = (p.red + PART_MIN - 1) / PART_MIN;
+    const auto tiles = [&](int64_t m, int64_t n) { return (p.rows + m - 1) / m * ((p.cols + n - 1) / n) * p.outs; };
+    if constexpr (sizeof(T) == 2) {
+        bool direct = tiles(256, 256) * most >= 200;
+        for (int i = 0; direct && i < 2; ++i) {
+            if (i < p.pairs) direct = direct_operand(p.a[i], ACROSS, p.rows, p.red, 256);
+            if (direct && (i < p.pairs || i < p.outs)) direct = direct_operand(p.b[i], ACROSS, p.cols, p.red, 256);
+        }
+        if (direct) return launch_shape<DirectTile<256, 256, 2, 2, ACROSS, ACROSS, 1>, T>(p, parts, st);
+    }
+    if (tiles(128, 128) * most >= 256) return launch_shape<MatrixTile<T, 128, 128, 2, 2, ACROSS, ACROSS, 1>, T>(p, parts, st);
+    return launch_shape<MatrixTile<T, 64, 64, 2, 2, ACROSS, ACROSS, 1>, T>(p, parts, st);
 }
 
 int launch_out_product(const OutProduct &p, int dtype, float *parts, hipStream_t st)

@@ -16,9 +16,20 @@
 namespace csgs {
 
 #define CSGS_LDS __attribute__((address_space(3)))
+#define CSGS_INLINE __attribute__((always_inline))     // (of a lambda: what it captures stays in registers)
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
+
+// f(0), f(1) .. f(N - 1) with the numbers as constants: an array that is indexed so is registers from the first pass of the compiler on, however large what surrounds it.
+template <int N, typename F>
+__device__ CSGS_INLINE inline void each_of(F f)
+{
+    if constexpr (N > 0) {
+        each_of<N - 1>(f);
+        f(std::integral_constant<int, N - 1>());
+    }
+}
 
 // An operand: element (o, k) at p[o * ld + k], or p[k * ld + o] where the outer index lies side by side.
 struct Operand {
@@ -72,7 +83,7 @@ struct TileSide {
 
     // Pieces by way of registers: anything outside the operand is zero.
     u32x4 held[PIECES];
-    __device__ void ask(const Operand &op, int64_t o0, int64_t outer, int64_t k0, int64_t red)
+    __device__ CSGS_INLINE void ask(const Operand &op, int64_t o0, int64_t outer, int64_t k0, int64_t red)
     {
         const T *base = (const T *)op.p;
 #pragma unroll
@@ -96,14 +107,14 @@ struct TileSide {
             }
         }
     }
-    __device__ void put(char *lds) const
+    __device__ CSGS_INLINE void put(char *lds) const
     {
 #pragma unroll
         for (int i = 0; i < PIECES; ++i) *(u32x4 *)(lds + ((int)threadIdx.x + i * NT) * 16) = held[i];
     }
 
     // What a lane gives the matrix cores for the 32 outer entries from `first` on, of k from 16 * step (bfloat16) or 8 * step (floats) on.
-    static __device__ inline bf16x8 fragment(const char *lds, int first, int step, int lane)
+    static __device__ CSGS_INLINE inline bf16x8 fragment(const char *lds, int first, int step, int lane)
     {
         static_assert(sizeof(T) == 2, "bfloat16");
         if constexpr (!ACROSS) {
@@ -124,7 +135,7 @@ struct TileSide {
             return __builtin_bit_cast(bf16x8, both);
         }
     }
-    static __device__ inline f32x4 fragment_f32(const char *lds, int first, int step, int lane)
+    static __device__ CSGS_INLINE inline f32x4 fragment_f32(const char *lds, int first, int step, int lane)
     {
         static_assert(sizeof(T) == 4, "floats");
         if constexpr (!ACROSS) {
@@ -140,66 +151,54 @@ struct TileSide {
 // The tile: BM rows and, of each of NB matrices B, BN columns; WM x WN wavefronts.
 template <typename T, int BM, int BN, int WM, int WN, bool A_ACROSS, bool B_ACROSS, int NB>
 struct MatrixTile {
-    static constexpr int NT = WM * WN * WAVE, BK = Element<T>::BK;
+    static constexpr int ROWS = BM, COLS = BN, WAVES_M = WM, WAVES_N = WN, NT = WM * WN * WAVE, BK = Element<T>::BK;
     static constexpr int TM = BM / WM / 32, TN = BN / WN / 32;     // 32 x 32 tiles of a wavefront
     static_assert(TM >= 1 && TN >= 1 && TM * 32 * WM == BM && TN * 32 * WN == BN, "whole tiles");
     using SideA = TileSide<T, BM, A_ACROSS, NT>;
     using SideB = TileSide<T, BN, B_ACROSS, NT>;
-    static constexpr int LDS_BYTES = SideA::BYTES + NB * SideB::BYTES;
+    // sums on their way out: 32 rows of a wavefront, rows 16 bytes further apart than they are long (lanes that write one below the other would meet in a bank)
+    static constexpr int ROW_LANES = TN * 8, PITCH = TN * 32 + 4, STRIP = NB * 32 * PITCH * 4;
+    static constexpr int TILE_BYTES = SideA::BYTES + NB * SideB::BYTES, OUT_BYTES = WM * WN * STRIP;
+    static constexpr int LDS_BYTES = TILE_BYTES > OUT_BYTES ? TILE_BYTES : OUT_BYTES;
 
     f32x16 acc[NB][TN][TM];
 
-    __device__ void clear()
+    __device__ CSGS_INLINE void clear()
     {
-#pragma unroll
-        for (int b = 0; b < NB; ++b)
-#pragma unroll
-            for (int n = 0; n < TN; ++n)
-#pragma unroll
-                for (int m = 0; m < TM; ++m)
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) acc[b][n][m][r] = 0.0f;
+        each_of<NB * TN * TM>([&](auto i) CSGS_INLINE { acc[i / (TN * TM)][i / TM % TN][i % TM] = f32x16{}; });
     }
 
-    __device__ void multiply(const char *lds)
+    __device__ CSGS_INLINE void multiply(const char *lds)
     {
         const int lane = (int)threadIdx.x & (WAVE - 1), wave = (int)threadIdx.x / WAVE;
         const int m0 = wave / WN * (TM * 32), n0 = wave % WN * (TN * 32);
-#pragma unroll
-        for (int step = 0; step < 4; ++step) {
+        each_of<4>([&](auto step) CSGS_INLINE {
             if constexpr (sizeof(T) == 2) {
                 bf16x8 a[TM];
-#pragma unroll
-                for (int m = 0; m < TM; ++m) a[m] = SideA::fragment(lds, m0 + 32 * m, step, lane);
-#pragma unroll
-                for (int b = 0; b < NB; ++b)
-#pragma unroll
-                    for (int n = 0; n < TN; ++n) {
-                        const bf16x8 f = SideB::fragment(lds + SideA::BYTES + b * SideB::BYTES, n0 + 32 * n, step, lane);
-#pragma unroll
-                        for (int m = 0; m < TM; ++m) acc[b][n][m] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f, a[m], acc[b][n][m], 0, 0, 0);
-                    }
+                each_of<TM>([&](auto m) CSGS_INLINE { a[m] = SideA::fragment(lds, m0 + 32 * m, step, lane); });
+                each_of<NB * TN>([&](auto i) CSGS_INLINE {
+                    constexpr int b = i / TN, n = i % TN;
+                    const bf16x8 f = SideB::fragment(lds + SideA::BYTES + b * SideB::BYTES, n0 + 32 * n, step, lane);
+                    each_of<TM>([&](auto m) CSGS_INLINE { acc[b][n][m] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f, a[m], acc[b][n][m], 0, 0, 0); });
+                });
             } else {
                 f32x4 a[TM];
-#pragma unroll
-                for (int m = 0; m < TM; ++m) a[m] = SideA::fragment_f32(lds, m0 + 32 * m, step, lane);
-#pragma unroll
-                for (int b = 0; b < NB; ++b)
-#pragma unroll
-                    for (int n = 0; n < TN; ++n) {
-                        const f32x4 f = SideB::fragment_f32(lds + SideA::BYTES + b * SideB::BYTES, n0 + 32 * n, step, lane);
-#pragma unroll
-                        for (int j = 0; j < 4; ++j)
-#pragma unroll
-                            for (int m = 0; m < TM; ++m) acc[b][n][m] = __builtin_amdgcn_mfma_f32_32x32x2f32(f[j], a[m][j], acc[b][n][m], 0, 0, 0);
-                    }
+                each_of<TM>([&](auto m) CSGS_INLINE { a[m] = SideA::fragment_f32(lds, m0 + 32 * m, step, lane); });
+                each_of<NB * TN>([&](auto i) CSGS_INLINE {
+                    constexpr int b = i / TN, n = i % TN;
+                    const f32x4 f = SideB::fragment_f32(lds + SideA::BYTES + b * SideB::BYTES, n0 + 32 * n, step, lane);
+                    each_of<4 * TM>([&](auto j) CSGS_INLINE {
+                        constexpr int k = j / TM, m = j % TM;
+                        acc[b][n][m] = __builtin_amdgcn_mfma_f32_32x32x2f32(f[k], a[m][k], acc[b][n][m], 0, 0, 0);
+                    });
+                });
             }
-        }
+        });
     }
 
     // Adds the products over k in [k0, k1): rows from m0 on of `rows`, columns from n0 on of `cols`.  One buffer in LDS: the next pieces are on their way
     // while this one's products are formed.
-    __device__ void accumulate(char *lds, const Operand &a, const Operand *b, int64_t m0, int64_t rows, int64_t n0, int64_t cols, int64_t k0, int64_t k1)
+    __device__ CSGS_INLINE void accumulate(char *lds, const Operand &a, const Operand *b, int64_t m0, int64_t rows, int64_t n0, int64_t cols, int64_t k0, int64_t k1, int32_t)
     {
         SideA sa;
         SideB sb[NB];
@@ -221,25 +220,62 @@ struct MatrixTile {
         }
     }
 
-    // f(row in the tile, first of four columns in it, the values of the NB matrices, which tile of the wavefront's): every lane's sums.
-    template <typename F>
-    __device__ void each(F f)
+    // give(row in the tile, first of four columns in it, the values of the NB matrices, what ask(row, column) has answered) for all of the tile.  A wavefront's sums go through
+    // LDS, 32 rows at a time, so that its lanes take whole rows of what is read and written beside them; a lane's columns are the same in every call.  What is asked for
+    // is asked for together, a group of rows ahead of where it is needed: few wavefronts are here to wait for it.
+    template <typename Ask, typename Give>
+    __device__ CSGS_INLINE void each(char *lds, Ask ask, Give give) const
     {
         const int lane = (int)threadIdx.x & (WAVE - 1), wave = (int)threadIdx.x / WAVE;
-        const int m0 = wave / WN * (TM * 32) + (lane & 31), n0 = wave % WN * (TN * 32) + 4 * (lane >> 5);
-#pragma unroll
-        for (int n = 0; n < TN; ++n)
-#pragma unroll
-            for (int q = 0; q < 4; ++q)
-#pragma unroll
-                for (int m = 0; m < TM; ++m) {
+        const int m0 = wave / WN * (TM * 32) + lane / ROW_LANES, n0 = wave % WN * (TN * 32) + lane % ROW_LANES * 4;
+        float *strip = (float *)lds + wave * (STRIP / 4);
+        const float *mine = strip + lane / ROW_LANES * PITCH + lane % ROW_LANES * 4;
+        constexpr int STEP = WAVE / ROW_LANES, GROUP = 16 / STEP;      // two groups of rows of a strip
+        using Held = decltype(ask(0, 0));
+        Held held[2][GROUP];
+        __syncthreads();           // (the tiles' readers are done)
+        each_of<GROUP>([&](auto i) CSGS_INLINE { held[0][i] = ask(m0 + i * STEP, n0); });
+#pragma unroll 1
+        for (int m = 0; m < TM; ++m) {
+            // (a branch for each of them: registers have no index)
+            each_of<TM>([&](auto k) CSGS_INLINE {
+                if (k == m)
+                    each_of<NB * TN * 4>([&](auto i) CSGS_INLINE {
+                        constexpr int b = i / (TN * 4), n = i / 4 % TN, q = i % 4;
+                        const f32x16 &x = acc[b][n][k];
+                        *(f32x4 *)(strip + (b * 32 + (lane & 31)) * PITCH + 32 * n + 8 * q + 4 * (lane >> 5)) = f32x4{x[4 * q], x[4 * q + 1], x[4 * q + 2], x[4 * q + 3]};
+                    });
+            });
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+            each_of<2>([&](auto g) CSGS_INLINE {
+                const int next = 32 * m + 16 * (g + 1);
+                if (next < 32 * TM) each_of<GROUP>([&](auto i) CSGS_INLINE { held[g ^ 1][i] = ask(m0 + next + i * STEP, n0); });
+                each_of<GROUP>([&](auto i) CSGS_INLINE {
                     float v[NB][4];
 #pragma unroll
-                    for (int b = 0; b < NB; ++b)
+                    for (int b = 0; b < NB; ++b) {
+                        const f32x4 x = *(const f32x4 *)(mine + (b * 32 + 16 * g + i * STEP) * PITCH);
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) v[b][i] = acc[b][n][m][4 * q + i];
-                    f(m0 + 32 * m, n0 + 32 * n + 8 * q, v, m);
-                }
+                        for (int e = 0; e < 4; ++e) v[b][e] = x[e];
+                    }
+                    give(m0 + 32 * m + 16 * g + i * STEP, n0, v, held[g][i]);
+                });
+            });
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+        }
+    }
+    // What the lanes of a wavefront hold for their columns, added up in a fixed order; f(first of four columns, sums) in one lane of each.
+    template <typename F>
+    static __device__ CSGS_INLINE void columns(float (&s)[4], F f)
+    {
+        const int lane = (int)threadIdx.x & (WAVE - 1), wave = (int)threadIdx.x / WAVE;
+#pragma unroll
+        for (int d = ROW_LANES; d < WAVE; d <<= 1)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) s[i] += __shfl_xor(s[i], d);
+        if (lane < ROW_LANES) f(wave % WN * (TN * 32) + lane * 4, s);
     }
 };
 

@@ -9,20 +9,53 @@ namespace csgs {
 struct Activation {
     float a, da;
 };
-__device__ inline Activation activate(float z, int32_t act)
+template <int ACT>
+__device__ CSGS_INLINE inline Activation activate(float z)
 {
-    if (act == CSGS_ACT_NONE) return Activation{z, 1.0f};
-    if (act == CSGS_ACT_RELU) return Activation{z < 0.0f ? 0.0f : z, z > 0.0f ? 1.0f : 0.0f};     // (NaN stays)
-    if (act == CSGS_ACT_GELU) {
+    if constexpr (ACT == CSGS_ACT_NONE) return Activation{z, 1.0f};
+    if constexpr (ACT == CSGS_ACT_RELU) return Activation{z < 0.0f ? 0.0f : z, z > 0.0f ? 1.0f : 0.0f};     // (NaN stays)
+    if constexpr (ACT == CSGS_ACT_GELU) {
         const float phi = 0.5f * erfcf(z * -0.707106781f);
         return Activation{z * phi, phi + z * (0.398942280f * expf(-0.5f * z * z))};
     }
     const float t = z * -1.44269504f;
     const float e = __builtin_amdgcn_exp2f(t) * fminf(1.0f + fmaf(t, -0.693147181f, -z), 2.0f);
     const float s = __builtin_amdgcn_rcpf(1.0f + e), rest = fminf(e * s, 1.0f);
-    if (act == CSGS_ACT_SIGMOID) return Activation{s, s * rest};
+    if constexpr (ACT == CSGS_ACT_SIGMOID) return Activation{s, s * rest};
     return Activation{z * s, s * (1.0f + z * rest)};
 }
+// f with the activation as a constant: chosen once a block, not once an entry.
+template <typename F>
+__device__ CSGS_INLINE inline void with_activation(int32_t act, F f)
+{
+    if (act == CSGS_ACT_NONE) f(std::integral_constant<int, CSGS_ACT_NONE>());
+    else if (act == CSGS_ACT_RELU) f(std::integral_constant<int, CSGS_ACT_RELU>());
+    else if (act == CSGS_ACT_SIGMOID) f(std::integral_constant<int, CSGS_ACT_SIGMOID>());
+    else if (act == CSGS_ACT_SILU) f(std::integral_constant<int, CSGS_ACT_SILU>());
+    else f(std::integral_constant<int, CSGS_ACT_GELU>());
+}
+// Four values of a row as they lie in memory, or what there is of them.
+template <typename T>
+struct Quad {
+    RawPiece<T, 4> raw;
+    __device__ void load(const T *p, int n)
+    {
+        if (n >= 4) {
+            raw.load(p);
+            return;
+        }
+#pragma unroll
+        for (int w = 0; w < RawPiece<T, 4>::WORDS; ++w) raw.w[w] = 0;
+#pragma unroll
+        for (int i = 0; i < 3; ++i)
+            if (i < n) {
+                if constexpr (sizeof(T) == 4) raw.w[i] = load_global<uint32_t>(p + i);
+                else raw.w[i / 2] |= (uint32_t)load_global<uint16_t>(p + i) << (16 * (i & 1));
+            }
+    }
+    __device__ float value(int i) const { return raw.value(i); }
+};
+struct Nothing {};
 
 __device__ inline int32_t live_rows(int32_t M, const int32_t *M_dev)
 {
@@ -44,13 +77,7 @@ __device__ inline void tile_place(int64_t b, int64_t tiles_m, int64_t tiles_n, i
     *tn = in / high;
 }
 
-// Column sums over the rows of a wavefront's tile: v summed over its 32 lanes, in a fixed order.
-__device__ inline float sum_of_32(float v)
-{
-#pragma unroll
-    for (int s = 1; s < 32; s <<= 1) v += __shfl_xor(v, s);
-    return v;
-}
+__device__ inline int32_t stagger(int64_t tm, int64_t tn) { return 2 * (int32_t)(tm & 7); }
 
 // ---------------------------------------------------------------- host side, matrix_grad.hip
 // Sums over rows that blocks left as parts [parts x n], joined in double in their order.
