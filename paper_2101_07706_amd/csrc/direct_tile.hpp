@@ -1,5 +1,5 @@
 // A block's tile of a product of bfloat16 operands whose pieces of 16 bytes start on multiples of 4 bytes: copied from memory to LDS without passing through
-// registers (buffer_load ... lds), into two buffers in turn.
+// registers (buffer_load ... lds), into two or three buffers in turn.
 //
 // The tile's layout in LDS is that of matrix_tile.hpp.  The copy writes a wavefront's 64 pieces side by side, so a lane asks for the piece that belongs to
 // its place.  What lies outside of an operand is asked for outside of the buffer's bounds and arrives as zero: rows past the end by the bounds themselves, k past the
@@ -21,16 +21,21 @@ __device__ inline void copy_to_lds(i32x4 buffer, uint32_t offset, uint32_t base,
 {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"(lds), "v"(offset), "s"(buffer), "s"(base) : "memory");
 }
-// Every copy of this wavefront has arrived and every fragment is in registers; then the same of the block.
-__device__ inline void wait_and_meet() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+// All but the last `LEFT` copies of this wavefront have arrived (they arrive in order) and every fragment is in registers; then the same of the block.
+template <int LEFT>
+__device__ inline void wait_and_meet()
+{
+    static_assert(LEFT < 64, "the counter's range");
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(LEFT) : "memory");
+}
 __device__ inline uint32_t lds_offset(const void *p) { return (uint32_t)(uintptr_t)(CSGS_LDS const void *)p; }
 __device__ inline int32_t one_for_all(int32_t x) { return __builtin_amdgcn_readfirstlane(x); }
 
 constexpr uint32_t NOWHERE = 0x7FFFFFF0u;     // an offset outside of every buffer
 
-template <int R, bool ACROSS, int NT>
+template <int R, bool ACROSS, int NT, int ROWB>
 struct DirectSide {
-    using Layout = TileSide<uint16_t, R, ACROSS, NT>;
+    using Layout = TileSide<uint16_t, R, ACROSS, NT, ROWB>;
     static constexpr int PIECES = Layout::PIECES, BK = Layout::BK;
     // pieces of a thread lie NT places apart: this many rows of the tile.  Rows 16 apart are turned alike
     static constexpr int ROWS = NT / Layout::ROW_PIECES, TURNS = ROWS % 16 == 0 ? 1 : 2;
@@ -74,18 +79,19 @@ struct DirectSide {
     }
 };
 
-template <int BM, int BN, int WM, int WN, bool A_ACROSS, bool B_ACROSS, int NB>
-struct DirectTile : MatrixTile<uint16_t, BM, BN, WM, WN, A_ACROSS, B_ACROSS, NB> {
-    using Base = MatrixTile<uint16_t, BM, BN, WM, WN, A_ACROSS, B_ACROSS, NB>;
+template <int BM, int BN, int WM, int WN, bool A_ACROSS, bool B_ACROSS, int NB, int ROWB, int BUFFERS>
+struct DirectTile : MatrixTile<uint16_t, BM, BN, WM, WN, A_ACROSS, B_ACROSS, NB, ROWB> {
+    using Base = MatrixTile<uint16_t, BM, BN, WM, WN, A_ACROSS, B_ACROSS, NB, ROWB>;
     using Base::acc;
     using Base::NT;
     using Base::TM;
     using Base::TN;
     using LayoutA = typename Base::SideA;
     using LayoutB = typename Base::SideB;
-    static constexpr int BUFFER = Base::TILE_BYTES, LDS_BYTES = 2 * BUFFER > Base::OUT_BYTES ? 2 * BUFFER : Base::OUT_BYTES, BK = Base::BK;
-    using SideA = DirectSide<BM, A_ACROSS, NT>;
-    using SideB = DirectSide<BN, B_ACROSS, NT>;
+    static constexpr int BUFFER = Base::TILE_BYTES, LDS_BYTES = BUFFERS * BUFFER > Base::OUT_BYTES ? BUFFERS * BUFFER : Base::OUT_BYTES, BK = Base::BK;
+    static constexpr int STEPS = Base::STEPS;
+    using SideA = DirectSide<BM, A_ACROSS, NT, ROWB>;
+    using SideB = DirectSide<BN, B_ACROSS, NT, ROWB>;
 
     static constexpr int PRODUCTS = NB * TN * TM, READS = NB * TN + TM;
     struct Fragments {
@@ -114,7 +120,7 @@ struct DirectTile : MatrixTile<uint16_t, BM, BN, WM, WN, A_ACROSS, B_ACROSS, NB>
         });
     }
 
-    __device__ CSGS_INLINE void accumulate(char *lds, const Operand &a, const Operand *b, int64_t m0, int64_t rows, int64_t n0, int64_t cols, int64_t k0, int64_t k1, int32_t ahead)
+    __device__ CSGS_INLINE void accumulate(char *lds, const Operand &a, const Operand *b, int64_t m0, int64_t rows, int64_t n0, int64_t cols, int64_t k0, int64_t k1)
     {
         if (k0 >= k1) return;
         const int lane = (int)threadIdx.x & (WAVE - 1), wave = (int)threadIdx.x / WAVE;
@@ -127,50 +133,41 @@ struct DirectTile : MatrixTile<uint16_t, BM, BN, WM, WN, A_ACROSS, B_ACROSS, NB>
         const uint32_t first = lds_offset(lds);
         // one of the pieces that a thread copies of a chunk
         constexpr int COPIES = SideA::PIECES + NB * SideB::PIECES;
-        auto copy = [&](int i, int64_t k, int buffer) {
-            const uint32_t to = first + buffer * BUFFER;
+        auto copy = [&](int i, int64_t k, uint32_t to) CSGS_INLINE {
             if (i < SideA::PIECES) sa.copy(i, k, k1, to);
             else sb[(i - SideA::PIECES) / SideB::PIECES].copy((i - SideA::PIECES) % SideB::PIECES, k, k1, to + LayoutA::BYTES + (i - SideA::PIECES) / SideB::PIECES * LayoutB::BYTES);
         };
         const int32_t chunks = (int32_t)((k1 - k0 + BK - 1) / BK);
-        int64_t k = k0 + ahead % chunks * (int64_t)BK;       // of the next chunk to be copied
-        auto advance = [&](int32_t copied) {
+        int64_t k = k0;                 // of the next chunk to be copied; past the last one: zeros
+        wait_and_meet<0>();             // (the buffers' readers of an earlier call are done)
+        each_of<BUFFERS>([&](auto n) CSGS_INLINE {
+            each_of<COPIES>([&](auto i) CSGS_INLINE { copy(i, k, first + n * BUFFER); });
             k += BK;
-            if (k >= k1) k = k0;
-            if (copied >= chunks) k = k1;                     // nothing is left: zeros
-        };
-        wait_and_meet();                // (the buffers' readers of an earlier call are done)
-#pragma unroll
-        for (int i = 0; i < COPIES; ++i) copy(i, k, 0);
-        advance(1);
-        wait_and_meet();
-#pragma unroll
-        for (int i = 0; i < COPIES; ++i) copy(i, k, 1);
-        advance(2);
+        });
+        wait_and_meet<(BUFFERS - 1) * COPIES>();
         Fragments f[2];
-#pragma unroll
-        for (int i = 0; i < READS; ++i) read(f[0], i, lds, 0, wm, wn, lane);
-        int buffer = 0;
+        each_of<READS>([&](auto i) CSGS_INLINE { read(f[0], i, lds, 0, wm, wn, lane); });
+        int32_t here = 0;               // the buffer's place in LDS
         for (int32_t c = 0; c < chunks; ++c) {
-            const char *here = lds + buffer * BUFFER;
-            each_of<3>([&](auto step) CSGS_INLINE {
+            each_of<STEPS - 1>([&](auto step) CSGS_INLINE {
                 products(f[step & 1], [&](int i) CSGS_INLINE {
-                    if (i < READS) read(f[(step & 1) ^ 1], i, here, step + 1, wm, wn, lane);
+                    if (i < READS) read(f[(step & 1) ^ 1], i, lds + here, step + 1, wm, wn, lane);
                 });
             });
-            wait_and_meet();
+            wait_and_meet<(BUFFERS - 2) * COPIES>();
             // (behind the last chunks: zeros, and fragments that no product takes)
-            const char *next = lds + (buffer ^ 1) * BUFFER;
-            products(f[1], [&](int i) CSGS_INLINE {
-                if (i < READS) read(f[0], i, next, 0, wm, wn, lane);
+            const int32_t next = here + BUFFER < BUFFERS * BUFFER ? here + BUFFER : 0;
+            products(f[(STEPS - 1) & 1], [&](int i) CSGS_INLINE {
+                if (i < READS) read(f[STEPS & 1], i, lds + next, 0, wm, wn, lane);
 #pragma unroll
-                for (int j = i * COPIES / PRODUCTS; j < (i + 1) * COPIES / PRODUCTS; ++j) copy(j, k, buffer);
+                for (int j = i * COPIES / PRODUCTS; j < (i + 1) * COPIES / PRODUCTS; ++j) copy(j, k, first + here);
             });
-            advance(c + 3);
-            buffer ^= 1;
+            k += BK;
+            here = next;
         }
-        wait_and_meet();
+        wait_and_meet<0>();
     }
+    static_assert(STEPS % 2 == 0 && READS <= PRODUCTS, "fragments in turn, all asked for beside a step's products");
 };
 
 // Whether an operand's tiles can be copied so: outer by red entries, at most `tile` of the former in one tile.

@@ -29,13 +29,18 @@ __global__ __launch_bounds__(Tile::NT) void gated_k(GatedArgs p)
     if (m0 >= rows && !columns) return;
     Tile tile;
     tile.clear();
-    if (m0 < rows) tile.accumulate(lds, p.x, p.w, m0, rows, n0, p.N, 0, p.K, stagger(tm, tn));
+    if (m0 < rows) tile.accumulate(lds, p.x, p.w, m0, rows, n0, p.N, 0, p.K);
     float sums[2][4] = {};
-    const auto count_of = [&](int64_t row, int64_t col) CSGS_INLINE { return row >= rows || col >= p.N ? 0 : p.N - col >= 4 ? 4 : (int)(p.N - col); };
+    // (this lane's columns and what is left of them; rows of the tile that count)
+    const int mine = Tile::my_column(), left = (int)(p.N - n0 < BN ? p.N - n0 : BN) - mine, count = left < 0 ? 0 : left < 4 ? left : 4;
+    const int high = m0 < rows ? (int)(rows - m0 < BM ? rows - m0 : BM) : 0;
+    float bias[2][4];
+#pragma unroll
+    for (int b = 0; b < 2; ++b) load_bias(p.b[b] + n0 + mine, p.b[b] ? count : 0, bias[b]);
     const auto ask = [&](int m, int n) CSGS_INLINE {
         if constexpr (GRAD) {
             Quad<T> x;
-            x.load((const T *)p.dh + (m0 + m) * p.lddh + n0 + n, count_of(m0 + m, n0 + n));
+            x.load((const T *)p.dh + (m0 + m) * p.lddh + n0 + n, m < high ? count : 0);
             return x;
         } else {
             return Nothing{};
@@ -44,13 +49,12 @@ __global__ __launch_bounds__(Tile::NT) void gated_k(GatedArgs p)
     with_activation(p.act, [&](auto act) CSGS_INLINE {
         constexpr int ACT = decltype(act)::value;
         tile.each(lds, ask, [&](int m, int n, const float(&v)[2][4], const auto &held) CSGS_INLINE {
+            if (m >= high || count == 0) return;
             const int64_t row = m0 + m, col = n0 + n;
-            const int count = count_of(row, col);
-            if (!count) return;
             float t[2][4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const float g = v[0][i] + (p.b[0] && i < count ? p.b[0][col + i] : 0.0f), u = v[1][i] + (p.b[1] && i < count ? p.b[1][col + i] : 0.0f);
+                const float g = v[0][i] + bias[0][i], u = v[1][i] + bias[1][i];
                 const Activation a = activate<ACT>(g);
                 if constexpr (!GRAD) {
                     t[0][i] = a.a * u;
@@ -99,7 +103,7 @@ static int launch_types(const GatedArgs &p, int64_t *parts, hipStream_t st)
     const auto tiles = [&](int64_t m, int64_t n) { return (p.M + m - 1) / m * ((p.N + n - 1) / n); };
     if constexpr (sizeof(T) == 2)
         if (tiles(256, 128) >= 200 && direct_operand(p.x, false, p.M, p.K, 256) && direct_operand(p.w[0], true, p.N, p.K, 128) && direct_operand(p.w[1], true, p.N, p.K, 128))
-            return launch_shape<DirectTile<256, 128, 2, 2, false, true, 2>, T, GRAD>(p, parts, st);
+            return launch_shape<DirectTile<256, 128, 2, 4, false, true, 2, 128, 2>, T, GRAD>(p, parts, st);
     if (tiles(128, 64) >= 256) return launch_shape<MatrixTile<T, 128, 64, 2, 2, false, true, 2>, T, GRAD>(p, parts, st);
     return launch_shape<MatrixTile<T, 64, 64, 2, 2, false, true, 2>, T, GRAD>(p, parts, st);
 }

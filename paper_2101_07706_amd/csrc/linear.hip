@@ -29,26 +29,29 @@ __global__ __launch_bounds__(Tile::NT) void linear_k(LinearArgs p)
     if (m0 >= rows && !(GRAD && p.columns)) return;
     Tile tile;
     tile.clear();
-    if (m0 < rows) tile.accumulate(lds, p.a, &p.w, m0, rows, n0, p.N, 0, p.K, stagger(tm, tn));
+    if (m0 < rows) tile.accumulate(lds, p.a, &p.w, m0, rows, n0, p.N, 0, p.K);
     float sums[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-    const auto count_of = [&](int64_t row, int64_t col) CSGS_INLINE { return row >= rows || col >= p.N ? 0 : p.N - col >= 4 ? 4 : (int)(p.N - col); };
+    // (this lane's columns and what is left of them; rows of the tile that count)
+    const int mine = Tile::my_column(), left = (int)(p.N - n0 < BN ? p.N - n0 : BN) - mine, count = left < 0 ? 0 : left < 4 ? left : 4;
+    const int high = m0 < rows ? (int)(rows - m0 < BM ? rows - m0 : BM) : 0;
     const TY *beside = (const TY *)(GRAD ? p.dy : p.r);
     const int64_t ld = GRAD ? p.lddy : p.ldr;
+    if (beside) beside += m0 * ld + n0;
+    float bias[4];
+    load_bias(p.bias + n0 + mine, p.bias ? count : 0, bias);
     const auto ask = [&](int m, int n) CSGS_INLINE {
         Quad<TY> x;
-        const int count = beside ? count_of(m0 + m, n0 + n) : 0;
-        x.load(beside + (m0 + m) * ld + n0 + n, count);
+        x.load(beside + m * ld + n, beside && m < high ? count : 0);
         return x;
     };
     with_activation(p.act, [&](auto act) CSGS_INLINE {
         constexpr int ACT = decltype(act)::value;
         tile.each(lds, ask, [&](int m, int n, const float(&v)[1][4], const Quad<TY> &held) CSGS_INLINE {
+            if (m >= high || count == 0) return;
             const int64_t row = m0 + m, col = n0 + n;
-            const int count = count_of(row, col);
-            if (!count) return;
             float z[4], x[4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) z[i] = v[0][i] + (p.bias && i < count ? p.bias[col + i] : 0.0f);
+            for (int i = 0; i < 4; ++i) z[i] = v[0][i] + bias[i];
             if constexpr (!GRAD) {
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
@@ -129,7 +132,7 @@ static int launch_types(const LinearArgs &p, int64_t *parts, hipStream_t st)
     const auto tiles = [&](int64_t m, int64_t n) { return (p.M + m - 1) / m * ((p.N + n - 1) / n); };
     if constexpr (sizeof(T) == 2)
         if (tiles(256, 256) >= 200 && direct_operand(p.a, false, p.M, p.K, 256) && direct_operand(p.w, true, p.N, p.K, 256))
-            return launch_shape<DirectTile<256, 256, 2, 2, false, true, 1>, T, TY, GRAD>(p, parts, st);
+            return launch_shape<DirectTile<256, 256, 2, 4, false, true, 1, 128, 2>, T, TY, GRAD>(p, parts, st);
     if (tiles(128, 128) >= 256) return launch_shape<MatrixTile<T, 128, 128, 2, 2, false, true, 1>, T, TY, GRAD>(p, parts, st);
     return launch_shape<MatrixTile<T, 64, 64, 2, 2, false, true, 1>, T, TY, GRAD>(p, parts, st);
 }

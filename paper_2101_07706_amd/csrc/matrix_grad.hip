@@ -30,21 +30,22 @@ __global__ __launch_bounds__(Tile::NT) void out_product_k(OutArgs p)
     const int64_t k0 = (int64_t)blockIdx.y * p.part_len, end = k0 + p.part_len, k1 = end < red ? end : red;
     Tile tile;
     tile.clear();
-    for (int i = 0; i < p.pairs; ++i) tile.accumulate(lds, p.a[i], &p.b[p.outs > 1 ? which : i], m0, rows, n0, p.cols, k0, k1, stagger(tm, tn));
+    for (int i = 0; i < p.pairs; ++i) tile.accumulate(lds, p.a[i], &p.b[p.outs > 1 ? which : i], m0, rows, n0, p.cols, k0, k1);
     float *part = p.part ? p.part + ((int64_t)which * p.parts + blockIdx.y) * p.rows * p.cols : nullptr;
-    tile.each(lds, [](int, int) { return Nothing{}; }, [&](int m, int n, const float(&v)[1][4], Nothing) CSGS_INLINE {
-        const int64_t row = m0 + m, col = n0 + n, rest = p.cols - col;
-        if (row >= rows || rest <= 0) return;
-        const int count = rest < 4 ? (int)rest : 4;
-        if (part) {
-            store_some(part + row * p.cols + col, count, v[0]);
-        } else {
+    const int mine = Tile::my_column(), left = (int)(p.cols - n0 < BN ? p.cols - n0 : BN) - mine, count = left < 0 ? 0 : left < 4 ? left : 4;
+    const int high = (int)(rows - m0 < BM ? rows - m0 : BM);
+    const auto none = [](int, int) CSGS_INLINE { return Nothing{}; };
+    if (part)
+        tile.each(lds, none, [&](int m, int n, const float(&v)[1][4], Nothing) CSGS_INLINE {
+            if (m < high && count) store_some(part + (m0 + m) * p.cols + n0 + n, count, v[0]);
+        });
+    else
+        tile.each(lds, none, [&](int m, int n, const float(&v)[1][4], Nothing) CSGS_INLINE {
             float x[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) x[i] = p.scale * v[0][i];
-            store_some((T *)p.out[which] + row * p.ldo[which] + col, count, x);
-        }
-    });
+            if (m < high && count) store_some((T *)p.out[which] + (m0 + m) * p.ldo[which] + n0 + n, count, x);
+        });
 }
 
 // out = scale * the sum of the parts, in double in their order.
@@ -135,7 +136,7 @@ static int launch_shape(const OutProduct &p, float *parts, hipStream_t st)
     a.tiles_n = (p.cols + BN - 1) / BN;
     const int64_t blocks = a.tiles_m * a.tiles_n;
     if (blocks > 1 << 30) return CSGS_EUNSUPPORTED;
-    constexpr int64_t BK = Element<T>::BK;
+    constexpr int64_t BK = Tile::BK;
     int64_t n = parts_of(p.rows, p.cols, p.red, p.outs, blocks * p.outs);
     a.part_len = ((p.red + n - 1) / n + BK - 1) / BK * BK;
     n = (p.red + a.part_len - 1) / a.part_len;
@@ -163,7 +164,7 @@ static int launch_sides(const OutProduct &p, float *parts, hipStream_t st)
             if (i < p.pairs) direct = direct_operand(p.a[i], ACROSS, p.rows, p.red, 256);
             if (direct && (i < p.pairs || i < p.outs)) direct = direct_operand(p.b[i], ACROSS, p.cols, p.red, 256);
         }
-        if (direct) return launch_shape<DirectTile<256, 256, 2, 2, ACROSS, ACROSS, 1>, T>(p, parts, st);
+        if (direct) return launch_shape<DirectTile<256, 256, 2, 4, ACROSS, ACROSS, 1, 128, 2>, T>(p, parts, st);
     }
     if (tiles(128, 128) * most >= 256) return launch_shape<MatrixTile<T, 128, 128, 2, 2, ACROSS, ACROSS, 1>, T>(p, parts, st);
     return launch_shape<MatrixTile<T, 64, 64, 2, 2, ACROSS, ACROSS, 1>, T>(p, parts, st);

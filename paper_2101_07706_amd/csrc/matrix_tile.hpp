@@ -2,8 +2,8 @@
 //
 // An operand is seen as outer index times reduction index k.  It lies in memory either with k side by side (ACROSS = false) or with the outer
 // index side by side (ACROSS = true); a tile is copied to LDS as it lies, in pieces of 16 bytes:
-//   k side by side      [outer][128 bytes of k]: a lane's part of a row is one 16-byte read.  Eight rows that are read together would meet in
-//                       the same banks: piece g of row r is kept at place g ^ (r / 2 % 8).
+//   k side by side      [outer][128 or 64 bytes of k]: a lane's part of a row is one 16-byte read.  Rows that are read together would meet in
+//                       the same banks: the pieces of a row are kept in an order that its number turns.
 //   outer side by side  [k][outer]: bfloat16 is turned by the LDS's transposing read (ds_read_b64_tr_b16: 16 lanes read 4 rows of k by 16
 //                       columns, each gets its column's 4 values); floats are read one by one.  32-byte segment s of row k at s ^ f(k), so that the four
 //                       rows of a read and those of its neighbours lie in different banks.
@@ -37,18 +37,6 @@ struct Operand {
     int64_t ld;
 };
 
-constexpr int TILE_ROW = 128;     // bytes of k in a row of a tile
-
-template <typename T>
-struct Element;
-template <>
-struct Element<uint16_t> {
-    static constexpr int BK = TILE_ROW / 2, PIECE = 8;
-};
-template <>
-struct Element<float> {
-    static constexpr int BK = TILE_ROW / 4, PIECE = 4;
-};
 
 // Which 32-byte segment of a row of k holds segment s (R outer entries of bfloat16 a row).
 template <int R>
@@ -58,14 +46,22 @@ __device__ inline int across_turn(int k)
     return 2 * ((k >> 1) & 1) | ((k >> 3) & 1);
 }
 
-// R outer entries by BK of an operand: copied to LDS by NT threads, read from there by wavefronts.
-template <typename T, int R, bool ACROSS, int NT>
+// Where piece 0 of row r is kept among the pieces of its row (rows of ROWB bytes): rows that share banks differ.
+template <int ROWB>
+__device__ inline int along_turn(int row)
+{
+    static_assert(ROWB == 128 || ROWB == 64, "rows of 128 or 64 bytes");
+    return ROWB == 128 ? (row >> 1) & 7 : (row >> 2) & 3;
+}
+
+// R outer entries by BK of an operand, ROWB bytes of k: copied to LDS by NT threads, read from there by wavefronts.
+template <typename T, int R, bool ACROSS, int NT, int ROWB>
 struct TileSide {
-    static constexpr int BK = Element<T>::BK, PIECE = Element<T>::PIECE;
-    static constexpr int BYTES = R * TILE_ROW;
-    static constexpr int PIECES = R * (TILE_ROW / 16) / NT;     // a thread's
-    static_assert(R * (TILE_ROW / 16) % NT == 0 && PIECES >= 1, "whole pieces for every thread");
-    static constexpr int ROW_PIECES = ACROSS ? R / PIECE : TILE_ROW / 16;
+    static constexpr int BK = ROWB / (int)sizeof(T), PIECE = 16 / (int)sizeof(T);
+    static constexpr int BYTES = R * ROWB;
+    static constexpr int PIECES = R * (ROWB / 16) / NT;     // a thread's
+    static_assert(R * (ROWB / 16) % NT == 0 && PIECES >= 1, "whole pieces for every thread");
+    static constexpr int ROW_PIECES = ACROSS ? R / PIECE : ROWB / 16;
 
     // The first element of the piece that belongs to place `id` of the tile.
     static __device__ inline void piece(int id, int *o, int *k)
@@ -73,7 +69,7 @@ struct TileSide {
         const int row = id / ROW_PIECES, place = id % ROW_PIECES;
         if constexpr (!ACROSS) {
             *o = row;
-            *k = (place ^ ((row >> 1) & 7)) * PIECE;
+            *k = (place ^ along_turn<ROWB>(row)) * PIECE;
         } else {
             *k = row;
             if constexpr (sizeof(T) == 2) *o = (((((place >> 1) ^ across_turn<R>(row)) << 1) | (place & 1))) * PIECE;
@@ -119,7 +115,7 @@ struct TileSide {
         static_assert(sizeof(T) == 2, "bfloat16");
         if constexpr (!ACROSS) {
             const int row = first + (lane & 31), g = 2 * step + (lane >> 5);
-            return *(const bf16x8 *)(lds + row * TILE_ROW + ((g ^ ((row >> 1) & 7)) << 4));
+            return *(const bf16x8 *)(lds + row * ROWB + ((g ^ along_turn<ROWB>(row)) << 4));
         } else {
             const int i = lane & 15, k = step * 16 + 8 * (lane >> 5) + (i >> 2);
             const int segment = first / 16 + ((lane >> 4) & 1);
@@ -140,7 +136,7 @@ struct TileSide {
         static_assert(sizeof(T) == 4, "floats");
         if constexpr (!ACROSS) {
             const int row = first + (lane & 31), g = 2 * step + (lane >> 5);
-            return *(const f32x4 *)(lds + row * TILE_ROW + ((g ^ ((row >> 1) & 7)) << 4));
+            return *(const f32x4 *)(lds + row * ROWB + ((g ^ along_turn<ROWB>(row)) << 4));
         } else {
             const float *at = (const float *)lds + (step * 8 + 4 * (lane >> 5)) * R + first + (lane & 31);
             return f32x4{at[0], at[R], at[2 * R], at[3 * R]};
@@ -149,13 +145,13 @@ struct TileSide {
 };
 
 // The tile: BM rows and, of each of NB matrices B, BN columns; WM x WN wavefronts.
-template <typename T, int BM, int BN, int WM, int WN, bool A_ACROSS, bool B_ACROSS, int NB>
+template <typename T, int BM, int BN, int WM, int WN, bool A_ACROSS, bool B_ACROSS, int NB, int ROWB = 128>
 struct MatrixTile {
-    static constexpr int ROWS = BM, COLS = BN, WAVES_M = WM, WAVES_N = WN, NT = WM * WN * WAVE, BK = Element<T>::BK;
+    static constexpr int ROWS = BM, COLS = BN, WAVES_M = WM, WAVES_N = WN, NT = WM * WN * WAVE, BK = ROWB / (int)sizeof(T), STEPS = ROWB / 32;
     static constexpr int TM = BM / WM / 32, TN = BN / WN / 32;     // 32 x 32 tiles of a wavefront
     static_assert(TM >= 1 && TN >= 1 && TM * 32 * WM == BM && TN * 32 * WN == BN, "whole tiles");
-    using SideA = TileSide<T, BM, A_ACROSS, NT>;
-    using SideB = TileSide<T, BN, B_ACROSS, NT>;
+    using SideA = TileSide<T, BM, A_ACROSS, NT, ROWB>;
+    using SideB = TileSide<T, BN, B_ACROSS, NT, ROWB>;
     // sums on their way out: 32 rows of a wavefront, rows 16 bytes further apart than they are long (lanes that write one below the other would meet in a bank)
     static constexpr int ROW_LANES = TN * 8, PITCH = TN * 32 + 4, STRIP = NB * 32 * PITCH * 4;
     static constexpr int TILE_BYTES = SideA::BYTES + NB * SideB::BYTES, OUT_BYTES = WM * WN * STRIP;
@@ -172,7 +168,7 @@ struct MatrixTile {
     {
         const int lane = (int)threadIdx.x & (WAVE - 1), wave = (int)threadIdx.x / WAVE;
         const int m0 = wave / WN * (TM * 32), n0 = wave % WN * (TN * 32);
-        each_of<4>([&](auto step) CSGS_INLINE {
+        each_of<STEPS>([&](auto step) CSGS_INLINE {
             if constexpr (sizeof(T) == 2) {
                 bf16x8 a[TM];
                 each_of<TM>([&](auto m) CSGS_INLINE { a[m] = SideA::fragment(lds, m0 + 32 * m, step, lane); });
@@ -198,7 +194,7 @@ struct MatrixTile {
 
     // Adds the products over k in [k0, k1): rows from m0 on of `rows`, columns from n0 on of `cols`.  One buffer in LDS: the next pieces are on their way
     // while this one's products are formed.
-    __device__ CSGS_INLINE void accumulate(char *lds, const Operand &a, const Operand *b, int64_t m0, int64_t rows, int64_t n0, int64_t cols, int64_t k0, int64_t k1, int32_t)
+    __device__ CSGS_INLINE void accumulate(char *lds, const Operand &a, const Operand *b, int64_t m0, int64_t rows, int64_t n0, int64_t cols, int64_t k0, int64_t k1)
     {
         SideA sa;
         SideB sb[NB];
@@ -227,7 +223,7 @@ struct MatrixTile {
     __device__ CSGS_INLINE void each(char *lds, Ask ask, Give give) const
     {
         const int lane = (int)threadIdx.x & (WAVE - 1), wave = (int)threadIdx.x / WAVE;
-        const int m0 = wave / WN * (TM * 32) + lane / ROW_LANES, n0 = wave % WN * (TN * 32) + lane % ROW_LANES * 4;
+        const int m0 = wave / WN * (TM * 32) + lane / ROW_LANES, n0 = my_column();
         float *strip = (float *)lds + wave * (STRIP / 4);
         const float *mine = strip + lane / ROW_LANES * PITCH + lane % ROW_LANES * 4;
         constexpr int STEP = WAVE / ROW_LANES, GROUP = 16 / STEP;      // two groups of rows of a strip
@@ -237,14 +233,16 @@ struct MatrixTile {
         each_of<GROUP>([&](auto i) CSGS_INLINE { held[0][i] = ask(m0 + i * STEP, n0); });
 #pragma unroll 1
         for (int m = 0; m < TM; ++m) {
-            // (a branch for each of them: registers have no index)
+            // (a branch for each of them: registers have no index.  The empty statement differs from branch to branch, so that they are not made one, of an index, again)
             each_of<TM>([&](auto k) CSGS_INLINE {
-                if (k == m)
+                if (k == m) {
                     each_of<NB * TN * 4>([&](auto i) CSGS_INLINE {
                         constexpr int b = i / (TN * 4), n = i / 4 % TN, q = i % 4;
-                        const f32x16 &x = acc[b][n][k];
+                        const f32x16 x = acc[b][n][k];
                         *(f32x4 *)(strip + (b * 32 + (lane & 31)) * PITCH + 32 * n + 8 * q + 4 * (lane >> 5)) = f32x4{x[4 * q], x[4 * q + 1], x[4 * q + 2], x[4 * q + 3]};
                     });
+                    asm volatile("; rows %0" ::"n"(32 * decltype(k)::value));
+                }
             });
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
             __builtin_amdgcn_wave_barrier();
@@ -266,16 +264,22 @@ struct MatrixTile {
             __builtin_amdgcn_wave_barrier();
         }
     }
+    // The first of the four columns of the tile that this lane is given.
+    static __device__ inline int my_column()
+    {
+        const int lane = (int)threadIdx.x & (WAVE - 1), wave = (int)threadIdx.x / WAVE;
+        return wave % WN * (TN * 32) + lane % ROW_LANES * 4;
+    }
     // What the lanes of a wavefront hold for their columns, added up in a fixed order; f(first of four columns, sums) in one lane of each.
     template <typename F>
     static __device__ CSGS_INLINE void columns(float (&s)[4], F f)
     {
-        const int lane = (int)threadIdx.x & (WAVE - 1), wave = (int)threadIdx.x / WAVE;
+        const int lane = (int)threadIdx.x & (WAVE - 1);
 #pragma unroll
         for (int d = ROW_LANES; d < WAVE; d <<= 1)
 #pragma unroll
             for (int i = 0; i < 4; ++i) s[i] += __shfl_xor(s[i], d);
-        if (lane < ROW_LANES) f(wave % WN * (TN * 32) + lane * 4, s);
+        if (lane < ROW_LANES) f(my_column(), s);
     }
 };
 

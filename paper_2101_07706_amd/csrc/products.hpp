@@ -56,6 +56,13 @@ struct Quad {
     __device__ float value(int i) const { return raw.value(i); }
 };
 struct Nothing {};
+// Four entries of a vector from `col` on, zeros where there is none.
+__device__ inline void load_bias(const float *b, int count, float (&x)[4])
+{
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = 0.0f;
+    if (b && count > 0) load_some(b, count, x);
+}
 
 __device__ inline int32_t live_rows(int32_t M, const int32_t *M_dev)
 {
@@ -66,7 +73,7 @@ __device__ inline int32_t live_rows(int32_t M, const int32_t *M_dev)
 
 // Block -> tile.  Blocks are handed to the eight dies in turn: each die takes tiles that follow each other, in bands of TILE_BAND tile rows, column by column, so
 // that what its cache holds of both operands is used by its next blocks.
-constexpr int TILE_BAND = 8, DIES = 8;
+constexpr int TILE_BAND = 4, DIES = 8;
 __device__ inline void tile_place(int64_t b, int64_t tiles_m, int64_t tiles_n, int64_t *tm, int64_t *tn)
 {
     const int64_t all = tiles_m * tiles_n, each = all / DIES, more = all % DIES, die = b % DIES, turn = b / DIES;
@@ -76,8 +83,6 @@ __device__ inline void tile_place(int64_t b, int64_t tiles_m, int64_t tiles_n, i
     *tm = first + in % high;
     *tn = in / high;
 }
-
-__device__ inline int32_t stagger(int64_t tm, int64_t tn) { return 2 * (int32_t)(tm & 7); }
 
 // ---------------------------------------------------------------- host side, matrix_grad.hip
 // Sums over rows that blocks left as parts [parts x n], joined in double in their order.
