@@ -16,8 +16,8 @@
 
 namespace csgs {
 
-constexpr int ADAM_U = 4;              // segments of a thread in one tile, all asked for before the first is worked on
-constexpr int ADAM_BLOCKS = 2048;
+constexpr int ADAM_U = 2;              // segments of a thread in one tile, all asked for before the first is worked on
+constexpr int ADAM_BLOCKS = 1024;      // what the device holds at once (us, 51 M entries with 8-bit states: 1024 473, 2048 475, 8192 485)
 constexpr int64_t ADAM_ENTRIES = 1ll << 40;
 
 struct AdamDesc {
@@ -30,8 +30,10 @@ struct AdamDesc {
     int32_t p_dtype, g_dtype, state, lane_bits;
     float weight_decay, lr_scale;
 };
+// Blocks that are done are counted in DONE_GROUPS places, and full groups in one more: additions to one place follow each other at 45 ns.
+constexpr int DONE_GROUPS = 64, DONE_STEP = 16;
 struct AdamMem {
-    uint32_t *done;       // blocks of the running call that are done; 0 between calls
+    uint32_t *done;       // [DONE_GROUPS + 1], DONE_STEP apart: 0 between calls
     AdamDesc *desc;       // [n]
     int32_t *tile_tensor; // [tiles]
     size_t bytes;
@@ -39,7 +41,7 @@ struct AdamMem {
 __host__ __device__ inline AdamMem carve_adamw(void *base, int32_t n, int64_t tiles)
 {
     AdamMem m;
-    size_t off = 256;
+    size_t off = align_up(sizeof(uint32_t) * DONE_STEP * (DONE_GROUPS + 1), 256);
     m.done = (uint32_t *)base;
     m.desc = (AdamDesc *)((char *)base + off);
     off = align_up(off + sizeof(AdamDesc) * (size_t)n, 256);
@@ -58,8 +60,8 @@ __global__ __launch_bounds__(256) void adamw_list_k(AdamBatch b, int32_t first, 
     const int k = (int)blockIdx.x;
     if (threadIdx.x == 0) {
         m.desc[first + k] = b.d[k];
-        if (first + k == 0) *m.done = 0;
     }
+    if (first + k == 0 && threadIdx.x <= DONE_GROUPS) m.done[threadIdx.x * DONE_STEP] = 0;
     for (int64_t t = b.d[k].first_tile + threadIdx.x; t < b.end_tile[k]; t += blockDim.x) m.tile_tensor[t] = first + k;
 }
 
@@ -265,7 +267,7 @@ __device__ inline void adam_tile(const AdamDesc &d, int64_t tile, const AdamNow 
     }
 }
 
-__global__ __launch_bounds__(256) void adamw_k(AdamMem m, int64_t tiles, AdamArgs a)
+__global__ __launch_bounds__(256, 4) void adamw_k(AdamMem m, int64_t tiles, AdamArgs a)
 {
     __shared__ double lds[4];
     AdamNow now;
@@ -286,14 +288,14 @@ __global__ __launch_bounds__(256) void adamw_k(AdamMem m, int64_t tiles, AdamArg
         }
     }
     // (the counter is advanced by the block that ends last: every block has read it by then)
-    const int32_t before = *a.step;
+    const int32_t before = __builtin_amdgcn_readfirstlane(*a.step);
     const double t = (double)(before < 0 ? 0 : before) + 1.0;
     now.inv_first = (float)(-1.0 / expm1(t * a.log_beta1));
     now.inv_root = (float)(1.0 / sqrt(-expm1(t * a.log_beta2)));
     now.lr = a.lr_dev ? a.lr * *a.lr_dev : a.lr;
     if (take)
         for (int64_t k = blockIdx.x; k < tiles; k += gridDim.x) {
-            const AdamDesc &d = m.desc[m.tile_tensor[k]];
+            const AdamDesc d = m.desc[__builtin_amdgcn_readfirstlane(m.tile_tensor[k])];      // (its own copy: what is stored cannot change it)
             const int64_t tile = k - d.first_tile;
             if (d.state == CSGS_STATE_8BIT) {
                 if (d.p_dtype == CSGS_F32) {
@@ -314,11 +316,16 @@ __global__ __launch_bounds__(256) void adamw_k(AdamMem m, int64_t tiles, AdamArg
             }
         }
     if (threadIdx.x == 0) {
-        const uint32_t k = __hip_atomic_fetch_add(m.done, 1u, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT);
-        if (k + 1 == gridDim.x) {
-            *m.done = 0;
+        const uint32_t blocks = gridDim.x, group = blockIdx.x % DONE_GROUPS, groups = blocks < DONE_GROUPS ? blocks : DONE_GROUPS;
+        const auto last_of = [&](uint32_t place, uint32_t n) {
+            uint32_t *at = m.done + place * DONE_STEP;
+            // (relaxed: nothing that the blocks have written is handed on, and the counter was read long before; a release would write back a die's cache)
+            if (__hip_atomic_fetch_add(at, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) + 1 != n) return false;
+            *at = 0;
+            return true;
+        };
+        if (last_of(group, (blocks - group + DONE_GROUPS - 1) / DONE_GROUPS) && last_of(DONE_GROUPS, groups))
             if (take && before < 0x7FFFFFFF) *a.step = (before < 0 ? 0 : before) + 1;
-        }
     }
 }
 
