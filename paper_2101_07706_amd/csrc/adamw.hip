@@ -89,25 +89,34 @@ __device__ inline uint32_t encode_second(const float (&x)[4], int32_t E)
     }
     return w;
 }
+// (a block that holds a value that is not finite: all of it times NaN)
+__device__ inline float block_scale(int32_t E, int32_t of) { return E == 255 ? __uint_as_float(0x7FC00000u) : ldexpf(1.0f, E - of); }
 __device__ inline void decode_first(uint32_t w, int32_t E, float (&x)[4])
 {
-    const float bad = E == 255 ? __uint_as_float(0x7FC00000u) : 0.0f;
+    const float scale = block_scale(E, 134);
     const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, true);
-    x[0] = ldexpf(lo[0], E - 134) + bad;
-    x[1] = ldexpf(lo[1], E - 134) + bad;
-    x[2] = ldexpf(hi[0], E - 134) + bad;
-    x[3] = ldexpf(hi[1], E - 134) + bad;
+    x[0] = lo[0] * scale;
+    x[1] = lo[1] * scale;
+    x[2] = hi[0] * scale;
+    x[3] = hi[1] * scale;
 }
 __device__ inline void decode_second(uint32_t w, int32_t E, float (&x)[4])
 {
-    const float bad = E == 255 ? __uint_as_float(0x7FC00000u) : 0.0f;
+    const float scale = block_scale(E, 127);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const uint32_t c = (w >> (8 * i)) & 255u;
-        x[i] = (c ? ldexpf(__uint_as_float((c + 769u) << 20), E - 127) : 0.0f) + bad;
+        x[i] = (c ? __uint_as_float((c + 769u) << 20) : 0.0f) * scale;
     }
 }
-// Exponent fields of the largest of the lanes' values, of two kinds at once, over the 1 << bits lanes of a segment.
+// Exponent fields of the largest of the lanes' values, of two kinds at once, over the 1 << bits lanes of a segment (the same in all of them).  Lane exchanges in
+// the vector unit within four lanes, eight and a row of sixteen, by way of the LDS beyond.
+typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+template <int CTRL>
+__device__ inline u16x2 larger_of_lanes(u16x2 e)
+{
+    return __builtin_elementwise_max(e, __builtin_bit_cast(u16x2, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, e), CTRL, 15, 15, true)));
+}
 __device__ inline void block_exponents(const float (&m)[4], const float (&v)[4], int bits, int32_t *Em, int32_t *Ev)
 {
     uint32_t a = 0, b = 0;
@@ -117,12 +126,12 @@ __device__ inline void block_exponents(const float (&m)[4], const float (&v)[4],
         a = x > a ? x : a;
         b = y > b ? y : b;
     }
-    typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
     u16x2 e = {(uint16_t)(a >> 23), (uint16_t)(b >> 23)};
-    for (int s = 0; s < bits; ++s) {
-        const u16x2 o = __builtin_bit_cast(u16x2, __shfl_xor(__builtin_bit_cast(int, e), 1 << s));
-        e = __builtin_elementwise_max(e, o);
-    }
+    if (bits > 0) e = larger_of_lanes<0xB1>(e);       // lanes 1 0 3 2
+    if (bits > 1) e = larger_of_lanes<0x4E>(e);       // lanes 2 3 0 1
+    if (bits > 2) e = larger_of_lanes<0x141>(e);      // eight lanes the other way round
+    if (bits > 3) e = larger_of_lanes<0x140>(e);      // sixteen
+    for (int s = 4; s < bits; ++s) e = __builtin_elementwise_max(e, __builtin_bit_cast(u16x2, __shfl_xor(__builtin_bit_cast(int, e), 1 << s)));
     *Em = e.x;
     *Ev = e.y;
 }
@@ -130,7 +139,8 @@ __device__ inline void block_exponents(const float (&m)[4], const float (&v)[4],
 // ---------------------------------------------------------------- the step
 struct AdamArgs {
     double beta1, beta2, log_beta1, log_beta2;
-    float lr, eps, max_norm;
+    double eps;
+    float lr, max_norm;
     int32_t kind, blocks;         // blocks: of clip_partial
     const float *lr_dev;
     int32_t *step;
@@ -138,10 +148,18 @@ struct AdamArgs {
     float *norm;
     int32_t *status;
 };
+// With f = 1 - beta1^t and r = sqrt(1 - beta2^t):  m / f / (sqrt(v) / r + eps) = m (r / f) / (sqrt(v) + eps r).
 struct AdamNow {
-    double c, beta1, beta2;
-    float lr, eps, inv_first, inv_root;   // 1 / (1 - beta1^t), 1 / sqrt(1 - beta2^t)
+    double beta1, beta2, add1, add2;      // (1 - beta1) c, (1 - beta2) c^2
+    float lr, eps, gain;                  // eps r, r / f
 };
+// The hardware's root is within an ulp, for what is not below its range.
+__device__ inline float root_of(float v)
+{
+    const bool small = v < 1.26217745e-29f;       // 2^-96
+    const float r = __builtin_amdgcn_sqrtf(small ? v * 1.84467441e19f : v);
+    return small ? r * 2.32830644e-10f : r;
+}
 
 __device__ inline uint32_t load_codes(const uint8_t *p, int n)
 {
@@ -238,10 +256,10 @@ __device__ inline void adam_tile(const AdamDesc &d, int64_t tile, const AdamNow 
                 m[u][i] = v[u][i] = 0.0f;
                 continue;
             }
-            const double gc = now.c * (double)g[u][i];
-            m[u][i] = (float)(now.beta1 * (double)m[u][i] + (1.0 - now.beta1) * gc);
-            v[u][i] = (float)(now.beta2 * (double)v[u][i] + (1.0 - now.beta2) * (gc * gc));
-            const float step = m[u][i] * now.inv_first / (sqrtf(v[u][i]) * now.inv_root + now.eps);
+            const double x = (double)g[u][i];      // (its square is exact)
+            m[u][i] = (float)fma(now.beta1, (double)m[u][i], now.add1 * x);
+            v[u][i] = (float)fma(now.beta2, (double)v[u][i], now.add2 * (x * x));
+            const float step = m[u][i] * now.gain * __builtin_amdgcn_rcpf(root_of(v[u][i]) + now.eps);
             p[u][i] -= lr * (step + d.weight_decay * p[u][i]);
         }
         if constexpr (SMALL) {
@@ -271,16 +289,13 @@ __global__ __launch_bounds__(256, 4) void adamw_k(AdamMem m, int64_t tiles, Adam
 {
     __shared__ double lds[4];
     AdamNow now;
-    now.c = 1.0;
-    now.beta1 = a.beta1;
-    now.beta2 = a.beta2;
-    now.eps = a.eps;
+    double c = 1.0;
     bool take = true;
     if (a.clip_partial || a.total) {
         const double s = a.total ? *a.total : join_partials(a.clip_partial, a.blocks, a.kind, lds);
         const double norm = a.kind == CSGS_GRAD_L2 ? sqrt(s) : s;
-        now.c = (double)a.max_norm / (norm + 1e-6);
-        if (!(now.c < 1.0)) now.c = 1.0;
+        c = (double)a.max_norm / (norm + 1e-6);
+        if (!(c < 1.0)) c = 1.0;
         take = norm <= 1.7976931348623157e308;
         if (blockIdx.x == 0 && threadIdx.x == 0) {
             if (a.norm) *a.norm = (float)norm;
@@ -290,8 +305,13 @@ __global__ __launch_bounds__(256, 4) void adamw_k(AdamMem m, int64_t tiles, Adam
     // (the counter is advanced by the block that ends last: every block has read it by then)
     const int32_t before = __builtin_amdgcn_readfirstlane(*a.step);
     const double t = (double)(before < 0 ? 0 : before) + 1.0;
-    now.inv_first = (float)(-1.0 / expm1(t * a.log_beta1));
-    now.inv_root = (float)(1.0 / sqrt(-expm1(t * a.log_beta2)));
+    const double r = sqrt(-expm1(t * a.log_beta2));
+    now.beta1 = a.beta1;
+    now.beta2 = a.beta2;
+    now.add1 = (1.0 - a.beta1) * c;
+    now.add2 = (1.0 - a.beta2) * c * c;
+    now.gain = (float)(-r / expm1(t * a.log_beta1));
+    now.eps = (float)(a.eps * r);
     now.lr = a.lr_dev ? a.lr * *a.lr_dev : a.lr;
     if (take)
         for (int64_t k = blockIdx.x; k < tiles; k += gridDim.x) {
@@ -477,7 +497,7 @@ extern "C" int csgs_adamw(const csgs_adamw_list *l, const csgs_adamw_args *a, vo
     k.log_beta1 = log(a->beta1);      // (of 0: -infinity, whose power is 0 for every step)
     k.log_beta2 = log(a->beta2);
     k.lr = a->lr;
-    k.eps = (float)a->eps;
+    k.eps = a->eps;
     k.max_norm = a->max_norm;
     k.kind = a->kind;
     k.lr_dev = a->lr_dev;
