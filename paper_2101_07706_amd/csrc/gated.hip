@@ -1,6 +1,7 @@
 // csgs_gated: h = act(x wg + bg) .* (x wu + bu), and its gradient.  One tile of x serves both products.
 #include "products.hpp"
 #include "direct_tile.hpp"
+#include "split_tile.hpp"
 
 namespace csgs {
 
@@ -18,7 +19,7 @@ struct GatedArgs {
 
 // GRAD = false: h.  GRAD = true: tg and tu as operands of the gradients' products, and their column sums.
 template <class Tile, typename T, bool GRAD>
-__global__ __launch_bounds__(Tile::NT) void gated_k(GatedArgs p)
+__global__ __launch_bounds__(Tile::NT, Tile::WAVES) void gated_k(GatedArgs p)
 {
     constexpr int BM = Tile::ROWS, BN = Tile::COLS, WM = Tile::WAVES_M, WN = Tile::WAVES_N;
     __shared__ __attribute__((aligned(128))) char lds[Tile::LDS_BYTES];
@@ -28,8 +29,9 @@ __global__ __launch_bounds__(Tile::NT) void gated_k(GatedArgs p)
     const bool columns = GRAD && (p.columns[0] || p.columns[1]);
     if (m0 >= rows && !columns) return;
     Tile tile;
-    tile.clear();
-    if (m0 < rows) tile.accumulate(lds, p.x, p.w, m0, rows, n0, p.N, 0, p.K);
+    form_sums(tile, [&](auto &t) CSGS_INLINE {
+        if (m0 < rows) t.accumulate(lds, p.x, p.w, m0, rows, n0, p.N, 0, p.K);
+    });
     float sums[2][4] = {};
     // (this lane's columns and what is left of them; rows of the tile that count)
     const int mine = Tile::my_column(), left = (int)(p.N - n0 < BN ? p.N - n0 : BN) - mine, count = left < 0 ? 0 : left < 4 ? left : 4;
@@ -104,8 +106,8 @@ static int launch_types(const GatedArgs &p, int64_t *parts, hipStream_t st)
     if constexpr (sizeof(T) == 2)
         if (tiles(256, 128) >= 200 && direct_operand(p.x, false, p.M, p.K, 256) && direct_operand(p.w[0], true, p.N, p.K, 128) && direct_operand(p.w[1], true, p.N, p.K, 128))
             return launch_shape<DirectTile<256, 128, 2, 4, false, true, 2, 128, 2>, T, GRAD>(p, parts, st);
-    if (tiles(128, 64) >= 256) return launch_shape<MatrixTile<T, 128, 64, 2, 2, false, true, 2>, T, GRAD>(p, parts, st);
-    return launch_shape<MatrixTile<T, 64, 64, 2, 2, false, true, 2>, T, GRAD>(p, parts, st);
+    if (tiles(128, 64) >= 256) return launch_shape<AnyTile<T, 128, 64, 2, 2, false, true, 2>, T, GRAD>(p, parts, st);
+    return launch_shape<AnyTile<T, 64, 64, 2, 2, false, true, 2>, T, GRAD>(p, parts, st);
 }
 template <bool GRAD>
 static int launch_gated(const GatedArgs &p, int dtype, int64_t *parts, hipStream_t st)

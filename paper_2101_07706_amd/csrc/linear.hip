@@ -1,6 +1,7 @@
 // csgs_linear: y = alpha act(a w + bias) + beta r, and its gradient.
 #include "products.hpp"
 #include "direct_tile.hpp"
+#include "split_tile.hpp"
 
 namespace csgs {
 
@@ -19,7 +20,7 @@ struct LinearArgs {
 
 // GRAD = false: y.  GRAD = true: t = alpha dy act'(a w + bias) as an operand of the gradients' products, its column sums, dr = beta dy.
 template <class Tile, typename T, typename TY, bool GRAD>
-__global__ __launch_bounds__(Tile::NT) void linear_k(LinearArgs p)
+__global__ __launch_bounds__(Tile::NT, Tile::WAVES) void linear_k(LinearArgs p)
 {
     constexpr int BM = Tile::ROWS, BN = Tile::COLS, WM = Tile::WAVES_M, WN = Tile::WAVES_N;
     __shared__ __attribute__((aligned(128))) char lds[Tile::LDS_BYTES];
@@ -28,8 +29,9 @@ __global__ __launch_bounds__(Tile::NT) void linear_k(LinearArgs p)
     const int64_t m0 = tm * BM, n0 = tn * BN, rows = live_rows(p.M, p.M_dev);
     if (m0 >= rows && !(GRAD && p.columns)) return;
     Tile tile;
-    tile.clear();
-    if (m0 < rows) tile.accumulate(lds, p.a, &p.w, m0, rows, n0, p.N, 0, p.K);
+    form_sums(tile, [&](auto &t) CSGS_INLINE {
+        if (m0 < rows) t.accumulate(lds, p.a, &p.w, m0, rows, n0, p.N, 0, p.K);
+    });
     float sums[4] = {0.0f, 0.0f, 0.0f, 0.0f};
     // (this lane's columns and what is left of them; rows of the tile that count)
     const int mine = Tile::my_column(), left = (int)(p.N - n0 < BN ? p.N - n0 : BN) - mine, count = left < 0 ? 0 : left < 4 ? left : 4;
@@ -133,8 +135,8 @@ static int launch_types(const LinearArgs &p, int64_t *parts, hipStream_t st)
     if constexpr (sizeof(T) == 2)
         if (tiles(256, 256) >= 200 && direct_operand(p.a, false, p.M, p.K, 256) && direct_operand(p.w, true, p.N, p.K, 256))
             return launch_shape<DirectTile<256, 256, 2, 4, false, true, 1, 128, 2>, T, TY, GRAD>(p, parts, st);
-    if (tiles(128, 128) >= 256) return launch_shape<MatrixTile<T, 128, 128, 2, 2, false, true, 1>, T, TY, GRAD>(p, parts, st);
-    return launch_shape<MatrixTile<T, 64, 64, 2, 2, false, true, 1>, T, TY, GRAD>(p, parts, st);
+    if (tiles(128, 128) >= 256) return launch_shape<AnyTile<T, 128, 128, 2, 2, false, true, 1>, T, TY, GRAD>(p, parts, st);
+    return launch_shape<AnyTile<T, 64, 64, 2, 2, false, true, 1>, T, TY, GRAD>(p, parts, st);
 }
 template <bool GRAD>
 static int launch_linear(const LinearArgs &p, int dtype, int y_dtype, int64_t *parts, hipStream_t st)

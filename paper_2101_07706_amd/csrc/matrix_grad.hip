@@ -1,6 +1,7 @@
 // Products of the gradients: da = t w^T (both operands with the reduction side by side) and dw = a^T t (both with the outer index side by side).
 #include "products.hpp"
 #include "direct_tile.hpp"
+#include "split_tile.hpp"
 
 namespace csgs {
 
@@ -17,7 +18,7 @@ struct OutArgs {
 };
 
 template <class Tile, typename T>
-__global__ __launch_bounds__(Tile::NT) void out_product_k(OutArgs p)
+__global__ __launch_bounds__(Tile::NT, Tile::WAVES) void out_product_k(OutArgs p)
 {
     constexpr int BM = Tile::ROWS, BN = Tile::COLS;
     __shared__ __attribute__((aligned(128))) char lds[Tile::LDS_BYTES];
@@ -29,8 +30,9 @@ __global__ __launch_bounds__(Tile::NT) void out_product_k(OutArgs p)
     const int which = (int)blockIdx.z;
     const int64_t k0 = (int64_t)blockIdx.y * p.part_len, end = k0 + p.part_len, k1 = end < red ? end : red;
     Tile tile;
-    tile.clear();
-    for (int i = 0; i < p.pairs; ++i) tile.accumulate(lds, p.a[i], &p.b[p.outs > 1 ? which : i], m0, rows, n0, p.cols, k0, k1);
+    form_sums(tile, [&](auto &t) CSGS_INLINE {
+        for (int i = 0; i < p.pairs; ++i) t.accumulate(lds, p.a[i], &p.b[p.outs > 1 ? which : i], m0, rows, n0, p.cols, k0, k1);
+    });
     float *part = p.part ? p.part + ((int64_t)which * p.parts + blockIdx.y) * p.rows * p.cols : nullptr;
     const int mine = Tile::my_column(), left = (int)(p.cols - n0 < BN ? p.cols - n0 : BN) - mine, count = left < 0 ? 0 : left < 4 ? left : 4;
     const int high = (int)(rows - m0 < BM ? rows - m0 : BM);
@@ -166,8 +168,8 @@ static int launch_sides(const OutProduct &p, float *parts, hipStream_t st)
         }
         if (direct) return launch_shape<DirectTile<256, 256, 2, 4, ACROSS, ACROSS, 1, 128, 2>, T>(p, parts, st);
     }
-    if (tiles(128, 128) * most >= 256) return launch_shape<MatrixTile<T, 128, 128, 2, 2, ACROSS, ACROSS, 1>, T>(p, parts, st);
-    return launch_shape<MatrixTile<T, 64, 64, 2, 2, ACROSS, ACROSS, 1>, T>(p, parts, st);
+    if (tiles(128, 128) * most >= 256) return launch_shape<AnyTile<T, 128, 128, 2, 2, ACROSS, ACROSS, 1>, T>(p, parts, st);
+    return launch_shape<AnyTile<T, 64, 64, 2, 2, ACROSS, ACROSS, 1>, T>(p, parts, st);
 }
 
 int launch_out_product(const OutProduct &p, int dtype, float *parts, hipStream_t st)

@@ -157,6 +157,8 @@ struct MatrixTile {
     static constexpr int TILE_BYTES = SideA::BYTES + NB * SideB::BYTES, OUT_BYTES = WM * WN * STRIP;
     static constexpr int LDS_BYTES = TILE_BYTES > OUT_BYTES ? TILE_BYTES : OUT_BYTES;
 
+    static constexpr int WAVES = 2;       // wavefronts that a SIMD is to hold
+
     f32x16 acc[NB][TN][TM];
 
     __device__ CSGS_INLINE void clear()
@@ -215,6 +217,11 @@ struct MatrixTile {
             multiply(lds);
         }
     }
+
+    // Whether sums have to be formed again: never here.
+    __device__ CSGS_INLINE bool settle() { return false; }
+    template <typename F>
+    __device__ CSGS_INLINE void again(F) {}
 
     // give(row in the tile, first of four columns in it, the values of the NB matrices, what ask(row, column) has answered) for all of the tile.  A wavefront's sums go through
     // LDS, 32 rows at a time, so that its lanes take whole rows of what is read and written beside them; a lane's columns are the same in every call.  What is asked for

@@ -84,6 +84,15 @@ __device__ inline void tile_place(int64_t b, int64_t tiles_m, int64_t tiles_n, i
     *tn = in / high;
 }
 
+// A tile's sums, by `sum(tile)` from zero on: once more where the tile asks for it.
+template <class Tile, typename F>
+__device__ CSGS_INLINE inline void form_sums(Tile &tile, F sum)
+{
+    tile.clear();
+    sum(tile);
+    if (tile.settle()) tile.again(sum);
+}
+
 // ---------------------------------------------------------------- host side, matrix_grad.hip
 // Sums over rows that blocks left as parts [parts x n], joined in double in their order.
 int launch_join_columns(const float *part, int64_t parts, int32_t n, float *out, hipStream_t st);

@@ -1,0 +1,159 @@
+// A block's tile of a product of floats, on the bfloat16 matrix cores.
+//
+// A float is the sum of three bfloat16 numbers, exactly: its upper 16 bits h, the upper 16 bits m of x - h, and l = x - h - m, of which 8 bits are left.  Of the nine products of
+// two such sums the six with weights down to 2^-16 are formed,
+//     a b = ah bh + (ah bm + am bh) + (ah bl + am bm + al bh) + rest,     |rest| < 2^-23 |a b|, 2^-25 |a b| on average
+// (each by the matrix cores without a rounding, summed in float): a product costs six times 32 cycles a step of 16 k instead of 8 times 64 on the float cores.  ah bh has sums of its own,
+// the others share one set, which is added at the end: the large sums are rounded once for 16 k.  (Products down to 2^-149 keep what floats keep: the matrix cores take and
+// give numbers below 2^-126.)
+//
+// x - h is NaN where x is not finite.  Sums that are not finite are formed again, by the float cores: those give what the inputs do.
+#pragma once
+#include "matrix_tile.hpp"
+
+namespace csgs {
+
+template <int R, bool ACROSS, int NT>
+struct SplitSide {
+    using Layout = TileSide<uint16_t, R, ACROSS, NT, 64>;        // of each of the three planes
+    static constexpr int PIECES = Layout::PIECES, BYTES = 3 * Layout::BYTES;
+
+    float held[PIECES][8];
+    __device__ CSGS_INLINE void ask(const Operand &op, int64_t o0, int64_t outer, int64_t k0, int64_t red)
+    {
+        const float *base = (const float *)op.p;
+#pragma unroll
+        for (int i = 0; i < PIECES; ++i) {
+            int po, pk;
+            Layout::piece((int)threadIdx.x + i * NT, &po, &pk);
+            const int64_t o = o0 + po, k = k0 + pk;
+            const int64_t rest = ACROSS ? (k < red ? outer - o : 0) : (o < outer ? red - k : 0);
+            const float *from = base + (ACROSS ? k * op.ld + o : o * op.ld + k);
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                float x[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+                const int64_t n = rest - 4 * h;
+                if (n > 0) load_some(from + 4 * h, n < 4 ? (int)n : 4, x);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) held[i][4 * h + e] = x[e];
+            }
+        }
+    }
+    __device__ CSGS_INLINE void put(char *lds) const
+    {
+#pragma unroll
+        for (int i = 0; i < PIECES; ++i) {
+            u32x4 plane[3];
+#pragma unroll
+            for (int e = 0; e < 8; e += 2) {
+                uint32_t part[2][3];
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    const float x = held[i][e + j], r = x - __uint_as_float(__float_as_uint(x) & 0xFFFF0000u);
+                    part[j][0] = __float_as_uint(x);
+                    part[j][1] = __float_as_uint(r);
+                    part[j][2] = __float_as_uint(r - __uint_as_float(__float_as_uint(r) & 0xFFFF0000u));
+                }
+#pragma unroll
+                for (int q = 0; q < 3; ++q) plane[q][e / 2] = __builtin_amdgcn_perm(part[1][q], part[0][q], 0x07060302u);      // (the upper halves)
+            }
+#pragma unroll
+            for (int q = 0; q < 3; ++q) *(u32x4 *)(lds + q * Layout::BYTES + ((int)threadIdx.x + i * NT) * 16) = plane[q];
+        }
+    }
+};
+
+template <int BM, int BN, int WM, int WN, bool A_ACROSS, bool B_ACROSS, int NB>
+struct SplitTile : MatrixTile<float, BM, BN, WM, WN, A_ACROSS, B_ACROSS, NB> {
+    using Base = MatrixTile<float, BM, BN, WM, WN, A_ACROSS, B_ACROSS, NB>;
+    using Base::acc;
+    using Base::NT;
+    using Base::TM;
+    using Base::TN;
+    using SideA = SplitSide<BM, A_ACROSS, NT>;
+    using SideB = SplitSide<BN, B_ACROSS, NT>;
+    static constexpr int BK = 32, STEPS = 2, WAVES = 2;
+    static constexpr int SPLIT_BYTES = SideA::BYTES + NB * SideB::BYTES, LDS_BYTES = SPLIT_BYTES > Base::LDS_BYTES ? SPLIT_BYTES : Base::LDS_BYTES;
+
+    Base second;      // sums of the smaller products; then, where they are asked for, of the float cores
+
+    __device__ CSGS_INLINE void clear()
+    {
+        Base::clear();
+        second.clear();
+    }
+    __device__ CSGS_INLINE void multiply(const char *lds)
+    {
+        const int lane = (int)threadIdx.x & (WAVE - 1), wave = (int)threadIdx.x / WAVE;
+        const int m0 = wave / WN * (TM * 32), n0 = wave % WN * (TN * 32);
+        each_of<STEPS>([&](auto step) CSGS_INLINE {
+            bf16x8 a[3][TM];
+            each_of<3 * TM>([&](auto i) CSGS_INLINE { a[i / TM][i % TM] = SideA::Layout::fragment(lds + i / TM * SideA::Layout::BYTES, m0 + 32 * (i % TM), step, lane); });
+            each_of<NB * TN>([&](auto j) CSGS_INLINE {
+                constexpr int b = j / TN, n = j % TN;
+                bf16x8 f[3];
+                each_of<3>([&](auto q) CSGS_INLINE {
+                    f[q] = SideB::Layout::fragment(lds + SideA::BYTES + b * SideB::BYTES + q * SideB::Layout::BYTES, n0 + 32 * n, step, lane);
+                });
+                // (small products first)
+                each_of<6 * TM>([&](auto i) CSGS_INLINE {
+                    constexpr int which = i / TM, m = i % TM;
+                    constexpr int pa[6] = {2, 1, 0, 1, 0, 0}, pb[6] = {0, 1, 2, 0, 1, 0};
+                    f32x16 &sum = which == 5 ? acc[b][n][m] : second.acc[b][n][m];
+                    sum = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f[pb[which]], a[pa[which]][m], sum, 0, 0, 0);
+                });
+            });
+        });
+    }
+    __device__ CSGS_INLINE void accumulate(char *lds, const Operand &a, const Operand *b, int64_t m0, int64_t rows, int64_t n0, int64_t cols, int64_t k0, int64_t k1)
+    {
+        SideA sa;
+        SideB sb[NB];
+        const auto ask = [&](int64_t k) CSGS_INLINE {
+            sa.ask(a, m0, rows, k, k1);
+            each_of<NB>([&](auto i) CSGS_INLINE { sb[i].ask(b[i], n0, cols, k, k1); });
+        };
+        if (k0 >= k1) return;
+        ask(k0);
+        for (int64_t k = k0; k < k1; k += BK) {
+            __syncthreads();       // (the buffer's last readers are done)
+            sa.put(lds);
+            each_of<NB>([&](auto i) CSGS_INLINE { sb[i].put(lds + SideA::BYTES + i * SideB::BYTES); });
+            __syncthreads();
+            if (k + BK < k1) ask(k + BK);
+            multiply(lds);
+        }
+    }
+    static __device__ CSGS_INLINE bool finite(float x) { return fabsf(x) <= 3.4028234e38f; }
+    // The sums as a whole; whether one of the block's is not finite.
+    __device__ CSGS_INLINE bool settle()
+    {
+        bool bad = false;
+        each_of<NB * TN * TM>([&](auto i) CSGS_INLINE {
+            f32x16 &x = acc[i / (TN * TM)][i / TM % TN][i % TM];
+            x += second.acc[i / (TN * TM)][i / TM % TN][i % TM];
+#pragma unroll
+            for (int r = 0; r < 16; ++r) bad |= !finite(x[r]);
+        });
+        return __syncthreads_or(bad);
+    }
+    // Sums that are not finite are those of the float cores (the others stay: a row's sums do not depend on other rows).
+    template <typename F>
+    __device__ CSGS_INLINE void again(F sum)
+    {
+        second.clear();
+        sum(second);
+        each_of<NB * TN * TM>([&](auto i) CSGS_INLINE {
+            f32x16 &x = acc[i / (TN * TM)][i / TM % TN][i % TM];
+            const f32x16 y = second.acc[i / (TN * TM)][i / TM % TN][i % TM];
+#pragma unroll
+            for (int r = 0; r < 16; ++r) x[r] = finite(x[r]) ? x[r] : y[r];
+        });
+    }
+};
+
+// The tile for operands that start anywhere.
+template <typename T, int BM, int BN, int WM, int WN, bool A_ACROSS, bool B_ACROSS, int NB>
+using AnyTile = std::conditional_t<sizeof(T) == 4, SplitTile<BM, BN, WM, WN, A_ACROSS, B_ACROSS, NB>, MatrixTile<T, BM, BN, WM, WN, A_ACROSS, B_ACROSS, NB>>;
+
+}  // namespace csgs
