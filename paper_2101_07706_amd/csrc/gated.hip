@@ -19,7 +19,7 @@ struct GatedArgs {
 
 // GRAD = false: h.  GRAD = true: tg and tu as operands of the gradients' products, and their column sums.
 template <class Tile, typename T, bool GRAD>
-__global__ __launch_bounds__(Tile::NT, Tile::WAVES) void gated_k(GatedArgs p)
+__global__ __launch_bounds__(Tile::THREADS, Tile::WAVES) void gated_k(GatedArgs p)
 {
     constexpr int BM = Tile::ROWS, BN = Tile::COLS, WM = Tile::WAVES_M, WN = Tile::WAVES_N;
     __shared__ __attribute__((aligned(128))) char lds[Tile::LDS_BYTES];
@@ -29,7 +29,7 @@ __global__ __launch_bounds__(Tile::NT, Tile::WAVES) void gated_k(GatedArgs p)
     const bool columns = GRAD && (p.columns[0] || p.columns[1]);
     if (m0 >= rows && !columns) return;
     Tile tile;
-    form_sums(tile, [&](auto &t) CSGS_INLINE {
+    form_sums(tile, lds, [&](auto &t) CSGS_INLINE {
         if (m0 < rows) t.accumulate(lds, p.x, p.w, m0, rows, n0, p.N, 0, p.K);
     });
     float sums[2][4] = {};
@@ -83,7 +83,7 @@ __global__ __launch_bounds__(Tile::NT, Tile::WAVES) void gated_k(GatedArgs p)
                     const int64_t col = n0 + n, rest = p.N - col;
 #pragma unroll
                     for (int i = 0; i < 4; ++i)
-                        if (i < rest) p.columns[b][(tm * WM + (int)threadIdx.x / WAVE / WN) * p.N + col + i] = s[i];
+                        if (i < rest) p.columns[b][(tm * WM + Tile::my_wave() / WN) * p.N + col + i] = s[i];
                 });
 }
 
@@ -95,7 +95,7 @@ static int launch_shape(GatedArgs p, int64_t *parts, hipStream_t st)
     p.tiles_n = ((int64_t)p.N + BN - 1) / BN;
     *parts = p.tiles_m * WM;
     if (p.tiles_m * p.tiles_n > 1 << 30) return CSGS_EUNSUPPORTED;
-    CSGS_LAUNCH(K_GATED, (gated_k<Tile, T, GRAD>), dim3((unsigned)(p.tiles_m * p.tiles_n)), dim3(Tile::NT), st, p);
+    CSGS_LAUNCH(K_GATED, (gated_k<Tile, T, GRAD>), dim3((unsigned)(p.tiles_m * p.tiles_n)), dim3(Tile::THREADS), st, p);
     CSGS_LAUNCH_CHECK();
     return CSGS_OK;
 }
@@ -107,6 +107,8 @@ static int launch_types(const GatedArgs &p, int64_t *parts, hipStream_t st)
         if (tiles(256, 128) >= 200 && direct_operand(p.x, false, p.M, p.K, 256) && direct_operand(p.w[0], true, p.N, p.K, 128) && direct_operand(p.w[1], true, p.N, p.K, 128))
             return launch_shape<DirectTile<256, 128, 2, 4, false, true, 2, 128, 2>, T, GRAD>(p, parts, st);
     if (tiles(128, 64) >= 256) return launch_shape<AnyTile<T, 128, 64, 2, 2, false, true, 2>, T, GRAD>(p, parts, st);
+    if (p.K >= 256 && p.M <= 32) return launch_shape<AnyTile<T, 32, 64, 1, 2, false, true, 2, sizeof(T) == 4 ? 4 : 8>, T, GRAD>(p, parts, st);
+    if (p.K >= 256 && tiles(64, 64) <= 256) return launch_shape<AnyTile<T, 64, 64, 2, 2, false, true, 2, sizeof(T) == 4 ? 2 : 4>, T, GRAD>(p, parts, st);
     return launch_shape<AnyTile<T, 64, 64, 2, 2, false, true, 2>, T, GRAD>(p, parts, st);
 }
 template <bool GRAD>

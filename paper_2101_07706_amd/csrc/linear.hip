@@ -20,7 +20,7 @@ struct LinearArgs {
 
 // GRAD = false: y.  GRAD = true: t = alpha dy act'(a w + bias) as an operand of the gradients' products, its column sums, dr = beta dy.
 template <class Tile, typename T, typename TY, bool GRAD>
-__global__ __launch_bounds__(Tile::NT, Tile::WAVES) void linear_k(LinearArgs p)
+__global__ __launch_bounds__(Tile::THREADS, Tile::WAVES) void linear_k(LinearArgs p)
 {
     constexpr int BM = Tile::ROWS, BN = Tile::COLS, WM = Tile::WAVES_M, WN = Tile::WAVES_N;
     __shared__ __attribute__((aligned(128))) char lds[Tile::LDS_BYTES];
@@ -29,7 +29,7 @@ __global__ __launch_bounds__(Tile::NT, Tile::WAVES) void linear_k(LinearArgs p)
     const int64_t m0 = tm * BM, n0 = tn * BN, rows = live_rows(p.M, p.M_dev);
     if (m0 >= rows && !(GRAD && p.columns)) return;
     Tile tile;
-    form_sums(tile, [&](auto &t) CSGS_INLINE {
+    form_sums(tile, lds, [&](auto &t) CSGS_INLINE {
         if (m0 < rows) t.accumulate(lds, p.a, &p.w, m0, rows, n0, p.N, 0, p.K);
     });
     float sums[4] = {0.0f, 0.0f, 0.0f, 0.0f};
@@ -79,7 +79,7 @@ __global__ __launch_bounds__(Tile::NT, Tile::WAVES) void linear_k(LinearArgs p)
             const int64_t col = n0 + n, rest = p.N - col;
 #pragma unroll
             for (int i = 0; i < 4; ++i)
-                if (i < rest) p.columns[(tm * WM + (int)threadIdx.x / WAVE / WN) * p.N + col + i] = s[i];
+                if (i < rest) p.columns[(tm * WM + Tile::my_wave() / WN) * p.N + col + i] = s[i];
         });
 }
 
@@ -124,7 +124,7 @@ static int launch_shape(LinearArgs p, int64_t *parts, hipStream_t st)
     p.tiles_n = ((int64_t)p.N + BN - 1) / BN;
     *parts = p.tiles_m * WM;
     if (p.tiles_m * p.tiles_n > 1 << 30) return CSGS_EUNSUPPORTED;
-    CSGS_LAUNCH(K_LINEAR, (linear_k<Tile, T, TY, GRAD>), dim3((unsigned)(p.tiles_m * p.tiles_n)), dim3(Tile::NT), st, p);
+    CSGS_LAUNCH(K_LINEAR, (linear_k<Tile, T, TY, GRAD>), dim3((unsigned)(p.tiles_m * p.tiles_n)), dim3(Tile::THREADS), st, p);
     CSGS_LAUNCH_CHECK();
     return CSGS_OK;
 }
@@ -136,6 +136,8 @@ static int launch_types(const LinearArgs &p, int64_t *parts, hipStream_t st)
         if (tiles(256, 256) >= 200 && direct_operand(p.a, false, p.M, p.K, 256) && direct_operand(p.w, true, p.N, p.K, 256))
             return launch_shape<DirectTile<256, 256, 2, 4, false, true, 1, 128, 2>, T, TY, GRAD>(p, parts, st);
     if (tiles(128, 128) >= 256) return launch_shape<AnyTile<T, 128, 128, 2, 2, false, true, 1>, T, TY, GRAD>(p, parts, st);
+    if (p.K >= 256 && p.M <= 32) return launch_shape<AnyTile<T, 32, 64, 1, 2, false, true, 1, 8>, T, TY, GRAD>(p, parts, st);
+    if (p.K >= 256 && tiles(64, 64) <= 256) return launch_shape<AnyTile<T, 64, 64, 2, 2, false, true, 1, 4>, T, TY, GRAD>(p, parts, st);
     return launch_shape<AnyTile<T, 64, 64, 2, 2, false, true, 1>, T, TY, GRAD>(p, parts, st);
 }
 template <bool GRAD>

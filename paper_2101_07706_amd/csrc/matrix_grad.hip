@@ -18,7 +18,7 @@ struct OutArgs {
 };
 
 template <class Tile, typename T>
-__global__ __launch_bounds__(Tile::NT, Tile::WAVES) void out_product_k(OutArgs p)
+__global__ __launch_bounds__(Tile::THREADS, Tile::WAVES) void out_product_k(OutArgs p)
 {
     constexpr int BM = Tile::ROWS, BN = Tile::COLS;
     __shared__ __attribute__((aligned(128))) char lds[Tile::LDS_BYTES];
@@ -30,7 +30,7 @@ __global__ __launch_bounds__(Tile::NT, Tile::WAVES) void out_product_k(OutArgs p
     const int which = (int)blockIdx.z;
     const int64_t k0 = (int64_t)blockIdx.y * p.part_len, end = k0 + p.part_len, k1 = end < red ? end : red;
     Tile tile;
-    form_sums(tile, [&](auto &t) CSGS_INLINE {
+    form_sums(tile, lds, [&](auto &t) CSGS_INLINE {
         for (int i = 0; i < p.pairs; ++i) t.accumulate(lds, p.a[i], &p.b[p.outs > 1 ? which : i], m0, rows, n0, p.cols, k0, k1);
     });
     float *part = p.part ? p.part + ((int64_t)which * p.parts + blockIdx.y) * p.rows * p.cols : nullptr;
@@ -144,7 +144,7 @@ static int launch_shape(const OutProduct &p, float *parts, hipStream_t st)
     n = (p.red + a.part_len - 1) / a.part_len;
     a.parts = (int32_t)n;
     a.part = n > 1 ? parts : nullptr;
-    CSGS_LAUNCH(K_OUT_PRODUCT, (out_product_k<Tile, T>), dim3((unsigned)blocks, (unsigned)n, (unsigned)p.outs), dim3(Tile::NT), st, a);
+    CSGS_LAUNCH(K_OUT_PRODUCT, (out_product_k<Tile, T>), dim3((unsigned)blocks, (unsigned)n, (unsigned)p.outs), dim3(Tile::THREADS), st, a);
     CSGS_LAUNCH_CHECK();
     if (n > 1) {
         const int64_t quads = p.rows * ((p.cols + 3) / 4), need = (quads + 255) / 256;

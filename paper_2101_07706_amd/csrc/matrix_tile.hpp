@@ -79,13 +79,13 @@ struct TileSide {
 
     // Pieces by way of registers: anything outside the operand is zero.
     u32x4 held[PIECES];
-    __device__ CSGS_INLINE void ask(const Operand &op, int64_t o0, int64_t outer, int64_t k0, int64_t red)
+    __device__ CSGS_INLINE void ask(int tid, const Operand &op, int64_t o0, int64_t outer, int64_t k0, int64_t red)
     {
         const T *base = (const T *)op.p;
 #pragma unroll
         for (int i = 0; i < PIECES; ++i) {
             int po, pk;
-            piece((int)threadIdx.x + i * NT, &po, &pk);
+            piece(tid + i * NT, &po, &pk);
             const int64_t o = o0 + po, k = k0 + pk;
             const int64_t at = ACROSS ? k * op.ld + o : o * op.ld + k;
             const int64_t rest = ACROSS ? (k < red ? outer - o : 0) : (o < outer ? red - k : 0);
@@ -103,10 +103,10 @@ struct TileSide {
             }
         }
     }
-    __device__ CSGS_INLINE void put(char *lds) const
+    __device__ CSGS_INLINE void put(int tid, char *lds) const
     {
 #pragma unroll
-        for (int i = 0; i < PIECES; ++i) *(u32x4 *)(lds + ((int)threadIdx.x + i * NT) * 16) = held[i];
+        for (int i = 0; i < PIECES; ++i) *(u32x4 *)(lds + (tid + i * NT) * 16) = held[i];
     }
 
     // What a lane gives the matrix cores for the 32 outer entries from `first` on, of k from 16 * step (bfloat16) or 8 * step (floats) on.
@@ -144,10 +144,11 @@ struct TileSide {
     }
 };
 
-// The tile: BM rows and, of each of NB matrices B, BN columns; WM x WN wavefronts.
-template <typename T, int BM, int BN, int WM, int WN, bool A_ACROSS, bool B_ACROSS, int NB, int ROWB = 128>
+// The tile: BM rows and, of each of NB matrices B, BN columns; WM x WN wavefronts, KG times: where there are few tiles of long sums, KG groups of wavefronts take
+// the chunks of k in turn, and the first one adds up what they have, in their order, and gives it out.
+template <typename T, int BM, int BN, int WM, int WN, bool A_ACROSS, bool B_ACROSS, int NB, int ROWB = 128, int KG = 1>
 struct MatrixTile {
-    static constexpr int ROWS = BM, COLS = BN, WAVES_M = WM, WAVES_N = WN, NT = WM * WN * WAVE, BK = ROWB / (int)sizeof(T), STEPS = ROWB / 32;
+    static constexpr int ROWS = BM, COLS = BN, WAVES_M = WM, WAVES_N = WN, NT = WM * WN * WAVE, THREADS = NT * KG, BK = ROWB / (int)sizeof(T), STEPS = ROWB / 32;
     static constexpr int TM = BM / WM / 32, TN = BN / WN / 32;     // 32 x 32 tiles of a wavefront
     static_assert(TM >= 1 && TN >= 1 && TM * 32 * WM == BM && TN * 32 * WN == BN, "whole tiles");
     using SideA = TileSide<T, BM, A_ACROSS, NT, ROWB>;
@@ -155,9 +156,16 @@ struct MatrixTile {
     // sums on their way out: 32 rows of a wavefront, rows 16 bytes further apart than they are long (lanes that write one below the other would meet in a bank)
     static constexpr int ROW_LANES = TN * 8, PITCH = TN * 32 + 4, STRIP = NB * 32 * PITCH * 4;
     static constexpr int TILE_BYTES = SideA::BYTES + NB * SideB::BYTES, OUT_BYTES = WM * WN * STRIP;
-    static constexpr int LDS_BYTES = TILE_BYTES > OUT_BYTES ? TILE_BYTES : OUT_BYTES;
+    static constexpr int SUMS = NB * TN * TM * 16, JOIN_BYTES = (KG - 1) * SUMS * NT * 4;
+    static constexpr int larger(int a, int b) { return a > b ? a : b; }
+    static constexpr int LDS_BYTES = larger(KG * TILE_BYTES, larger(OUT_BYTES, JOIN_BYTES));
 
-    static constexpr int WAVES = 2;       // wavefronts that a SIMD is to hold
+    // This thread in its group, and the group.
+    static __device__ inline int my_id() { return KG == 1 ? (int)threadIdx.x : (int)threadIdx.x % NT; }
+    static __device__ inline int my_group() { return KG == 1 ? 0 : __builtin_amdgcn_readfirstlane((int)threadIdx.x / NT); }
+    static __device__ inline int my_wave() { return my_id() / WAVE; }
+
+    static constexpr int WAVES = THREADS > 512 ? THREADS / 256 : 2;       // wavefronts that a SIMD is to hold
 
     f32x16 acc[NB][TN][TM];
 
@@ -168,7 +176,7 @@ struct MatrixTile {
 
     __device__ CSGS_INLINE void multiply(const char *lds)
     {
-        const int lane = (int)threadIdx.x & (WAVE - 1), wave = (int)threadIdx.x / WAVE;
+        const int lane = (int)threadIdx.x & (WAVE - 1), wave = my_wave();
         const int m0 = wave / WN * (TM * 32), n0 = wave % WN * (TN * 32);
         each_of<STEPS>([&](auto step) CSGS_INLINE {
             if constexpr (sizeof(T) == 2) {
@@ -200,28 +208,53 @@ struct MatrixTile {
     {
         SideA sa;
         SideB sb[NB];
-        auto ask = [&](int64_t k) {
-            sa.ask(a, m0, rows, k, k1);
-#pragma unroll
-            for (int i = 0; i < NB; ++i) sb[i].ask(b[i], n0, cols, k, k1);
+        const int tid = my_id(), group = my_group();
+        const auto ask = [&](int64_t k) CSGS_INLINE {
+            sa.ask(tid, a, m0, rows, k, k1);
+            each_of<NB>([&](auto i) CSGS_INLINE { sb[i].ask(tid, b[i], n0, cols, k, k1); });
         };
         if (k0 >= k1) return;
-        ask(k0);
-        for (int64_t k = k0; k < k1; k += BK) {
+        char *mine = lds + group * TILE_BYTES;
+        const int64_t first = k0 + group * BK;
+        ask(first);
+        // (all groups go round equally often: k past the end is zeros)
+        for (int64_t k = k0; k < k1; k += KG * BK) {
             __syncthreads();       // (the buffer's last readers are done)
-            sa.put(lds);
-#pragma unroll
-            for (int i = 0; i < NB; ++i) sb[i].put(lds + SideA::BYTES + i * SideB::BYTES);
+            sa.put(tid, mine);
+            each_of<NB>([&](auto i) CSGS_INLINE { sb[i].put(tid, mine + SideA::BYTES + i * SideB::BYTES); });
             __syncthreads();
-            if (k + BK < k1) ask(k + BK);
-            multiply(lds);
+            if (k + KG * BK < k1) ask(k + (KG + group) * BK);
+            multiply(mine);
+        }
+    }
+    // The groups' sums, in the first one.
+    __device__ CSGS_INLINE void join(char *lds)
+    {
+        if constexpr (KG > 1) {
+            float *at = (float *)lds + my_id();
+            const int group = my_group();
+            __syncthreads();
+            if (group > 0)
+                each_of<SUMS>([&](auto i) CSGS_INLINE { at[((group - 1) * SUMS + i) * NT] = acc[i / 16 / (TN * TM)][i / 16 / TM % TN][i / 16 % TM][i % 16]; });
+            __syncthreads();
+            if (group == 0)
+                each_of<SUMS>([&](auto i) CSGS_INLINE {
+                    float x = acc[i / 16 / (TN * TM)][i / 16 / TM % TN][i / 16 % TM][i % 16];
+#pragma unroll
+                    for (int g = 0; g < KG - 1; ++g) x += at[(g * SUMS + i) * NT];
+                    acc[i / 16 / (TN * TM)][i / 16 / TM % TN][i / 16 % TM][i % 16] = x;
+                });
         }
     }
 
     // Whether sums have to be formed again: never here.
-    __device__ CSGS_INLINE bool settle() { return false; }
+    __device__ CSGS_INLINE bool settle(char *lds)
+    {
+        join(lds);
+        return false;
+    }
     template <typename F>
-    __device__ CSGS_INLINE void again(F) {}
+    __device__ CSGS_INLINE void again(char *, F) {}
 
     // give(row in the tile, first of four columns in it, the values of the NB matrices, what ask(row, column) has answered) for all of the tile.  A wavefront's sums go through
     // LDS, 32 rows at a time, so that its lanes take whole rows of what is read and written beside them; a lane's columns are the same in every call.  What is asked for
@@ -229,7 +262,7 @@ struct MatrixTile {
     template <typename Ask, typename Give>
     __device__ CSGS_INLINE void each(char *lds, Ask ask, Give give) const
     {
-        const int lane = (int)threadIdx.x & (WAVE - 1), wave = (int)threadIdx.x / WAVE;
+        const int lane = (int)threadIdx.x & (WAVE - 1), wave = my_wave();
         const int m0 = wave / WN * (TM * 32) + lane / ROW_LANES, n0 = my_column();
         float *strip = (float *)lds + wave * (STRIP / 4);
         const float *mine = strip + lane / ROW_LANES * PITCH + lane % ROW_LANES * 4;
@@ -237,6 +270,7 @@ struct MatrixTile {
         using Held = decltype(ask(0, 0));
         Held held[2][GROUP];
         __syncthreads();           // (the tiles' readers are done)
+        if (my_group() > 0) return;
         each_of<GROUP>([&](auto i) CSGS_INLINE { held[0][i] = ask(m0 + i * STEP, n0); });
 #pragma unroll 1
         for (int m = 0; m < TM; ++m) {
@@ -274,7 +308,7 @@ struct MatrixTile {
     // The first of the four columns of the tile that this lane is given.
     static __device__ inline int my_column()
     {
-        const int lane = (int)threadIdx.x & (WAVE - 1), wave = (int)threadIdx.x / WAVE;
+        const int lane = (int)threadIdx.x & (WAVE - 1), wave = my_wave();
         return wave % WN * (TN * 32) + lane % ROW_LANES * 4;
     }
     // What the lanes of a wavefront hold for their columns, added up in a fixed order; f(first of four columns, sums) in one lane of each.
@@ -282,6 +316,7 @@ struct MatrixTile {
     static __device__ CSGS_INLINE void columns(float (&s)[4], F f)
     {
         const int lane = (int)threadIdx.x & (WAVE - 1);
+        if (my_group() > 0) return;
 #pragma unroll
         for (int d = ROW_LANES; d < WAVE; d <<= 1)
 #pragma unroll

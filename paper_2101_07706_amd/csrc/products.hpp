@@ -86,11 +86,11 @@ __device__ inline void tile_place(int64_t b, int64_t tiles_m, int64_t tiles_n, i
 
 // A tile's sums, by `sum(tile)` from zero on: once more where the tile asks for it.
 template <class Tile, typename F>
-__device__ CSGS_INLINE inline void form_sums(Tile &tile, F sum)
+__device__ CSGS_INLINE inline void form_sums(Tile &tile, char *lds, F sum)
 {
     tile.clear();
     sum(tile);
-    if (tile.settle()) tile.again(sum);
+    if (tile.settle(lds)) tile.again(lds, sum);
 }
 
 // ---------------------------------------------------------------- host side, matrix_grad.hip

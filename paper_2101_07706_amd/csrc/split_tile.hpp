@@ -19,13 +19,13 @@ struct SplitSide {
     static constexpr int PIECES = Layout::PIECES, BYTES = 3 * Layout::BYTES;
 
     float held[PIECES][8];
-    __device__ CSGS_INLINE void ask(const Operand &op, int64_t o0, int64_t outer, int64_t k0, int64_t red)
+    __device__ CSGS_INLINE void ask(int tid, const Operand &op, int64_t o0, int64_t outer, int64_t k0, int64_t red)
     {
         const float *base = (const float *)op.p;
 #pragma unroll
         for (int i = 0; i < PIECES; ++i) {
             int po, pk;
-            Layout::piece((int)threadIdx.x + i * NT, &po, &pk);
+            Layout::piece(tid + i * NT, &po, &pk);
             const int64_t o = o0 + po, k = k0 + pk;
             const int64_t rest = ACROSS ? (k < red ? outer - o : 0) : (o < outer ? red - k : 0);
             const float *from = base + (ACROSS ? k * op.ld + o : o * op.ld + k);
@@ -39,7 +39,7 @@ struct SplitSide {
             }
         }
     }
-    __device__ CSGS_INLINE void put(char *lds) const
+    __device__ CSGS_INLINE void put(int tid, char *lds) const
     {
 #pragma unroll
         for (int i = 0; i < PIECES; ++i) {
@@ -58,22 +58,22 @@ struct SplitSide {
                 for (int q = 0; q < 3; ++q) plane[q][e / 2] = __builtin_amdgcn_perm(part[1][q], part[0][q], 0x07060302u);      // (the upper halves)
             }
 #pragma unroll
-            for (int q = 0; q < 3; ++q) *(u32x4 *)(lds + q * Layout::BYTES + ((int)threadIdx.x + i * NT) * 16) = plane[q];
+            for (int q = 0; q < 3; ++q) *(u32x4 *)(lds + q * Layout::BYTES + (tid + i * NT) * 16) = plane[q];
         }
     }
 };
 
-template <int BM, int BN, int WM, int WN, bool A_ACROSS, bool B_ACROSS, int NB>
-struct SplitTile : MatrixTile<float, BM, BN, WM, WN, A_ACROSS, B_ACROSS, NB> {
-    using Base = MatrixTile<float, BM, BN, WM, WN, A_ACROSS, B_ACROSS, NB>;
+template <int BM, int BN, int WM, int WN, bool A_ACROSS, bool B_ACROSS, int NB, int KG>
+struct SplitTile : MatrixTile<float, BM, BN, WM, WN, A_ACROSS, B_ACROSS, NB, 128, KG> {
+    using Base = MatrixTile<float, BM, BN, WM, WN, A_ACROSS, B_ACROSS, NB, 128, KG>;
     using Base::acc;
     using Base::NT;
     using Base::TM;
     using Base::TN;
     using SideA = SplitSide<BM, A_ACROSS, NT>;
     using SideB = SplitSide<BN, B_ACROSS, NT>;
-    static constexpr int BK = 32, STEPS = 2, WAVES = 2;
-    static constexpr int SPLIT_BYTES = SideA::BYTES + NB * SideB::BYTES, LDS_BYTES = SPLIT_BYTES > Base::LDS_BYTES ? SPLIT_BYTES : Base::LDS_BYTES;
+    static constexpr int BK = 32, STEPS = 2;
+    static constexpr int SPLIT_BYTES = SideA::BYTES + NB * SideB::BYTES, LDS_BYTES = Base::larger(KG * SPLIT_BYTES, Base::LDS_BYTES);
 
     Base second;      // sums of the smaller products; then, where they are asked for, of the float cores
 
@@ -84,7 +84,7 @@ struct SplitTile : MatrixTile<float, BM, BN, WM, WN, A_ACROSS, B_ACROSS, NB> {
     }
     __device__ CSGS_INLINE void multiply(const char *lds)
     {
-        const int lane = (int)threadIdx.x & (WAVE - 1), wave = (int)threadIdx.x / WAVE;
+        const int lane = (int)threadIdx.x & (WAVE - 1), wave = Base::my_wave();
         const int m0 = wave / WN * (TM * 32), n0 = wave % WN * (TN * 32);
         each_of<STEPS>([&](auto step) CSGS_INLINE {
             bf16x8 a[3][TM];
@@ -109,29 +109,32 @@ struct SplitTile : MatrixTile<float, BM, BN, WM, WN, A_ACROSS, B_ACROSS, NB> {
     {
         SideA sa;
         SideB sb[NB];
+        const int tid = Base::my_id(), group = Base::my_group();
         const auto ask = [&](int64_t k) CSGS_INLINE {
-            sa.ask(a, m0, rows, k, k1);
-            each_of<NB>([&](auto i) CSGS_INLINE { sb[i].ask(b[i], n0, cols, k, k1); });
+            sa.ask(tid, a, m0, rows, k, k1);
+            each_of<NB>([&](auto i) CSGS_INLINE { sb[i].ask(tid, b[i], n0, cols, k, k1); });
         };
         if (k0 >= k1) return;
-        ask(k0);
-        for (int64_t k = k0; k < k1; k += BK) {
+        char *mine = lds + group * SPLIT_BYTES;
+        ask(k0 + group * BK);
+        for (int64_t k = k0; k < k1; k += KG * BK) {
             __syncthreads();       // (the buffer's last readers are done)
-            sa.put(lds);
-            each_of<NB>([&](auto i) CSGS_INLINE { sb[i].put(lds + SideA::BYTES + i * SideB::BYTES); });
+            sa.put(tid, mine);
+            each_of<NB>([&](auto i) CSGS_INLINE { sb[i].put(tid, mine + SideA::BYTES + i * SideB::BYTES); });
             __syncthreads();
-            if (k + BK < k1) ask(k + BK);
-            multiply(lds);
+            if (k + KG * BK < k1) ask(k + (KG + group) * BK);
+            multiply(mine);
         }
     }
     static __device__ CSGS_INLINE bool finite(float x) { return fabsf(x) <= 3.4028234e38f; }
     // The sums as a whole; whether one of the block's is not finite.
-    __device__ CSGS_INLINE bool settle()
+    __device__ CSGS_INLINE bool settle(char *lds)
     {
         bool bad = false;
+        each_of<NB * TN * TM>([&](auto i) CSGS_INLINE { acc[i / (TN * TM)][i / TM % TN][i % TM] += second.acc[i / (TN * TM)][i / TM % TN][i % TM]; });
+        Base::join(lds);
         each_of<NB * TN * TM>([&](auto i) CSGS_INLINE {
-            f32x16 &x = acc[i / (TN * TM)][i / TM % TN][i % TM];
-            x += second.acc[i / (TN * TM)][i / TM % TN][i % TM];
+            const f32x16 &x = acc[i / (TN * TM)][i / TM % TN][i % TM];
 #pragma unroll
             for (int r = 0; r < 16; ++r) bad |= !finite(x[r]);
         });
@@ -139,10 +142,11 @@ struct SplitTile : MatrixTile<float, BM, BN, WM, WN, A_ACROSS, B_ACROSS, NB> {
     }
     // Sums that are not finite are those of the float cores (the others stay: a row's sums do not depend on other rows).
     template <typename F>
-    __device__ CSGS_INLINE void again(F sum)
+    __device__ CSGS_INLINE void again(char *lds, F sum)
     {
         second.clear();
         sum(second);
+        second.join(lds);
         each_of<NB * TN * TM>([&](auto i) CSGS_INLINE {
             f32x16 &x = acc[i / (TN * TM)][i / TM % TN][i % TM];
             const f32x16 y = second.acc[i / (TN * TM)][i / TM % TN][i % TM];
@@ -153,7 +157,7 @@ struct SplitTile : MatrixTile<float, BM, BN, WM, WN, A_ACROSS, B_ACROSS, NB> {
 };
 
 // The tile for operands that start anywhere.
-template <typename T, int BM, int BN, int WM, int WN, bool A_ACROSS, bool B_ACROSS, int NB>
-using AnyTile = std::conditional_t<sizeof(T) == 4, SplitTile<BM, BN, WM, WN, A_ACROSS, B_ACROSS, NB>, MatrixTile<T, BM, BN, WM, WN, A_ACROSS, B_ACROSS, NB>>;
+template <typename T, int BM, int BN, int WM, int WN, bool A_ACROSS, bool B_ACROSS, int NB, int KG = 1>
+using AnyTile = std::conditional_t<sizeof(T) == 4, SplitTile<BM, BN, WM, WN, A_ACROSS, B_ACROSS, NB, KG>, MatrixTile<T, BM, BN, WM, WN, A_ACROSS, B_ACROSS, NB, 128, KG>>;
 
 }  // namespace csgs
