@@ -10,11 +10,18 @@ once more:
     u_l = N(beta x_l + a(gate_l) .* N(h_l))     gate, residual and the norms around them      csgs_norm_residual
     logits = u_0 W_out
 
+With ffn = F the layer's product is a gated feed-forward block on the aggregated rows instead,
+
+    z_l = P~_l relu(u_{l+1}),  h_l = (silu(z_l Wg_l) .* (z_l Wu_l)) Wd_l + b_l      csgs_aggregate, csgs_gated, csgs_linear
+
+and with optimizer = "adamw" the step is csgs_adamw, which takes the clipping factor in: with weight decay on the matrices, the rows of the table that were looked
+up alone, and states in 32 bits or, but for vectors, in 8 (state_bits).
+
 The gradients go the same way back; a node that is in several layers' sets receives the sum of its rows' gradients
 (csgs_embed_grad_rows), and what all gradients together measure is clipped (csgs_grad_clip) before the step.  No call waits for the device:
 the numbers of sampled nodes stay there.
 
-  python -m paper_2101_07706_amd.residual_gcn [--config tiny] [--steps 20]
+  python -m paper_2101_07706_amd.residual_gcn [--config tiny] [--steps 20] [--ffn 0] [--optimizer sgd|adamw] [--state-bits 32|8]
 
 trains on made-up labels: which part of the local id range a node is in.
 """
@@ -35,7 +42,9 @@ class ResidualGCN:
     .table_count; .norm and .status tell of the last clipping, .skipped how many steps were left out because their gradients were not finite (all on
     the device)."""
 
-    def __init__(self, dg, width, n_classes, n_layers, batch, samples, skew, adj_cap, seed=0, max_norm=1.0, lr=0.1, beta=0.5, gate_act=csgs.GATE_SIGMOID):
+    def __init__(self, dg, width, n_classes, n_layers, batch, samples, skew, adj_cap, seed=0, max_norm=1.0, lr=0.1, beta=0.5, gate_act=csgs.GATE_SIGMOID, ffn=0,
+                 optimizer="sgd", state_bits=32, weight_decay=0.01):
+        assert optimizer in ("sgd", "adamw")
         dev = self.device = dg.device
         self.dg, self.width, self.L, self.batch, self.B, self.skew, self.seed = dg, width, n_layers, batch, samples, skew, seed
         self.max_norm, self.lr, self.beta, self.gate_act, self.scale = max_norm, lr, beta, gate_act, math.sqrt(width)
@@ -44,8 +53,13 @@ class ResidualGCN:
         randn = lambda *shape, std: (torch.randn(*shape, generator=g) * std).to(dev)
         self.table = randn(dg.n_nodes, D, std=1.0 / math.sqrt(D))
         self.params = {"w_out": randn(D, n_classes, std=1.0 / math.sqrt(D)), "bottom.pre_w": torch.ones(D, device=dev), "bottom.pre_b": torch.zeros(D, device=dev)}
+        self.ffn, self.optimizer = ffn, optimizer
         for l in range(L):
-            self.params[f"{l}.w"] = randn(D, D, std=1.0 / math.sqrt(D))
+            if ffn:
+                self.params[f"{l}.wg"], self.params[f"{l}.wu"] = randn(D, ffn, std=1.0 / math.sqrt(D)), randn(D, ffn, std=1.0 / math.sqrt(D))
+                self.params[f"{l}.wd"], self.params[f"{l}.bd"] = randn(ffn, D, std=1.0 / math.sqrt(ffn)), torch.zeros(D, device=dev)
+            else:
+                self.params[f"{l}.w"] = randn(D, D, std=1.0 / math.sqrt(D))
             self.params[f"{l}.gate"] = torch.zeros(D, device=dev)
             for k in ("post", "pre"):
                 self.params[f"{l}.{k}_w"], self.params[f"{l}.{k}_b"] = torch.ones(D, device=dev), torch.zeros(D, device=dev)
@@ -65,6 +79,9 @@ class ResidualGCN:
         self.X, self.U, self.dX, self.dU = part(new()), part(new()), new(), part(new())
         self.dX_parts = part(self.dX)
         self.H, self.Z, self.dH, self.dZ = (part(new())[:L] for _ in range(4))
+        if ffn:
+            wide = torch.zeros(2, self.at[L], ffn, dtype=f32, device=dev)
+            self.A, self.dA = ([t[self.at[l]:self.at[l + 1]] for l in range(L)] for t in wide)
         self.logits = torch.zeros(batch, n_classes, dtype=f32, device=dev)
         self.table_rows, self.table_ids = torch.zeros(total, D, dtype=f32, device=dev), torch.zeros(total, dtype=torch.int32, device=dev)
         self.table_count, self.row_place = torch.zeros(1, dtype=torch.int32, device=dev), torch.arange(total, dtype=torch.int32, device=dev)
@@ -72,10 +89,17 @@ class ResidualGCN:
         # scratch of the gradient calls; they follow each other on one stream
         nbytes = max([csgs.csgs_embed_grad_scratch_bytes(total, dg.n_nodes, D), csgs.csgs_aggregate_grad_scratch_bytes(samples, self.lbs[0].adj_col.numel()),
                       csgs.csgs_layer_gemm_grad_w_scratch_bytes(n_max, D, max(D, n_classes)), csgs.csgs_layer_gemm_grad_w_scratch_bytes(n_max, D, n_classes)]
-                     + [csgs.csgs_norm_residual_grad_scratch_bytes(c, D) for c in self.caps])
+                     + [csgs.csgs_norm_residual_grad_scratch_bytes(c, D) for c in self.caps]
+                     + ([csgs.csgs_gated_grad_scratch_bytes(n_max, D, ffn, csgs.F32), csgs.csgs_linear_grad_scratch_bytes(n_max, ffn, D, csgs.F32)] if ffn else []))
         self.scratch = torch.empty(nbytes // 8 + 32, dtype=torch.int64, device=dev)
         names = list(self.grads)
         self.list = csgs.make_grad_list([self.grads[k] for k in names] + [self.table_rows], rows_dev=[None] * len(names) + [self.table_count])
+        if optimizer == "adamw":
+            self.steps_taken = torch.zeros(1, dtype=torch.int32, device=dev)
+            self.states = {k: csgs.adamw_states(v, state_bits if v.dim() == 2 else 32) for k, v in [*self.params.items(), ("table", self.table)]}
+            entries = [csgs.adamw_entry(self.params[k], self.grads[k], **self.states[k], weight_decay=weight_decay if self.params[k].dim() == 2 else 0.0) for k in names]
+            entries.append(csgs.adamw_entry(self.table, self.table_rows, **self.states["table"], ids=self.table_ids, n_dev=self.table_count))
+            self.adamw_list = csgs.make_adamw_list(entries)
 
     def rows_dev(self, l):
         """Device count of the rows of layer l (None: all of the batch)."""
@@ -102,7 +126,13 @@ class ResidualGCN:
             csgs.csgs_embed(self.table, self.ids[self.at[l]:self.at[l + 1]], self.X[l], scale=self.scale, n_dev=self.rows_dev(l))
         csgs.csgs_norm_residual(self.X[L], None, None, self.U[L], **self.norms(L))
         for l in range(L - 1, -1, -1):
-            pipeline.compute_step(lbs[l], self.caps[l], self.U[l + 1], None, False, True, self.params[f"{l}.w"], self.Z[l], self.H[l], nS_dev=self.rows_dev(l))
+            n = self.rows_dev(l)
+            if self.ffn:
+                csgs.csgs_aggregate(lbs[l].adj_rowptr, lbs[l].adj_col, lbs[l].adj_val, lbs[l].n_next, self.U[l + 1], None, None, True, self.Z[l], nS_dev=n, nS=self.caps[l])
+                csgs.csgs_gated(self.Z[l], self.params[f"{l}.wg"], self.params[f"{l}.wu"], self.A[l], M_dev=n)
+                csgs.csgs_linear(self.A[l], self.params[f"{l}.wd"], self.H[l], bias=self.params[f"{l}.bd"], M_dev=n)
+            else:
+                pipeline.compute_step(lbs[l], self.caps[l], self.U[l + 1], None, False, True, self.params[f"{l}.w"], self.Z[l], self.H[l], nS_dev=n)
             csgs.csgs_norm_residual(self.X[l], self.H[l], None, self.U[l], **self.norms(l))
         csgs.csgs_layer_gemm(self.U[0], self.params["w_out"], self.logits)
         return self.logits
@@ -116,8 +146,14 @@ class ResidualGCN:
             n = self.rows_dev(l)
             csgs.csgs_norm_residual_grad(self.X[l], self.H[l], None, self.dU[l], self.dX_parts[l], self.dH[l], g[f"{l}.gate"], g[f"{l}.post_w"], g[f"{l}.post_b"],
                                          g[f"{l}.pre_w"], g[f"{l}.pre_b"], self.scratch, **self.norms(l))
-            csgs.csgs_layer_gemm_grad_w(self.Z[l], self.dH[l], g[f"{l}.w"], self.scratch, M_dev=n)
-            csgs.csgs_layer_gemm_grad_z(self.dH[l], self.params[f"{l}.w"], self.dZ[l], M_dev=n)
+            if self.ffn:
+                csgs.csgs_linear_grad(self.A[l], self.params[f"{l}.wd"], self.dH[l], self.dA[l], g[f"{l}.wd"], g[f"{l}.bd"], None, self.scratch,
+                                      bias=self.params[f"{l}.bd"], M_dev=n)
+                csgs.csgs_gated_grad(self.Z[l], self.params[f"{l}.wg"], self.params[f"{l}.wu"], self.dA[l], self.dZ[l], g[f"{l}.wg"], g[f"{l}.wu"], None, None,
+                                     self.scratch, M_dev=n)
+            else:
+                csgs.csgs_layer_gemm_grad_w(self.Z[l], self.dH[l], g[f"{l}.w"], self.scratch, M_dev=n)
+                csgs.csgs_layer_gemm_grad_z(self.dH[l], self.params[f"{l}.w"], self.dZ[l], M_dev=n)
             csgs.csgs_aggregate_grad(lbs[l].adj_rowptr[:self.caps[l] + 1], lbs[l].adj_col, lbs[l].adj_val, lbs[l].n_next, self.dZ[l], self.U[l + 1], self.dU[l + 1],
                                      self.scratch, nS_dev=n)
         csgs.csgs_norm_residual_grad(self.X[L], None, None, self.dU[L], self.dX_parts[L], None, None, None, None, g["bottom.pre_w"], g["bottom.pre_b"], self.scratch,
@@ -125,12 +161,19 @@ class ResidualGCN:
         csgs.csgs_embed_grad_rows(self.ids, self.dX, self.dg.n_nodes, self.table_ids, self.table_count, self.table_rows, self.scratch, scale=self.scale)
 
     def clip(self):
+        """The gradients, cut to max_norm (AdamW leaves them and takes the factor in as it descends)."""
         self.status.zero_()      # (calls only set bits)
+        if self.optimizer == "adamw":
+            return
         csgs.csgs_grad_clip(self.list, csgs.GRAD_L2, self.max_norm, self.norm, self.status)
 
     def descend(self):
-        """A step of gradient descent on all parameters.  Clipping makes NaN of gradients whose norm is not finite: such a step changes nothing.  Decided on the
+        """A step on all parameters.  AdamW leaves out by itself what is not finite.  Gradient descent: clipping makes NaN of gradients whose norm is not finite: such a step changes nothing.  Decided on the
         device, from the status and not from the norm, which as a float may be infinite where the total is not."""
+        if self.optimizer == "adamw":
+            csgs.csgs_adamw(self.adamw_list, self.lr, self.steps_taken, clip=self.list, kind=csgs.GRAD_L2, max_norm=self.max_norm, norm=self.norm, status=self.status)
+            self.skipped += (self.status & csgs.ST_NONFINITE_GRAD) != 0
+            return
         finite = (self.status & csgs.ST_NONFINITE_GRAD) == 0
         self.skipped += ~finite
         for k, p in self.params.items():
@@ -156,12 +199,16 @@ def main():
     ap = argparse.ArgumentParser(description=__doc__, formatter_class=argparse.RawDescriptionHelpFormatter)
     ap.add_argument("--config", default="tiny", choices=list(synth.CONFIGS))
     ap.add_argument("--steps", type=int, default=20)
+    ap.add_argument("--ffn", type=int, default=0, help="width of the gated feed-forward block of a layer; 0: a product of the layer's width")
+    ap.add_argument("--optimizer", default="sgd", choices=["sgd", "adamw"])
+    ap.add_argument("--state-bits", type=int, default=32, choices=[32, 8])
     a = ap.parse_args()
     cfg = synth.CONFIGS[a.config]
     g = synth.make_graph(cfg)
     dg = pipeline.DeviceGraph(g)
     n_classes = cfg.n_classes or 4
-    net = ResidualGCN(dg, cfg.hidden, n_classes, cfg.n_layers, cfg.batch, cfg.samples, cfg.skew, min(g.nnz, 16_000_000))
+    net = ResidualGCN(dg, cfg.hidden, n_classes, cfg.n_layers, cfg.batch, cfg.samples, cfg.skew, min(g.nnz, 16_000_000),
+                      lr=0.1 if a.optimizer == "sgd" else 0.01, ffn=a.ffn, optimizer=a.optimizer, state_bits=a.state_bits)
     for it in range(a.steps):
         S0 = torch.from_numpy(synth.make_batch(g, cfg.batch, cfg.seed, it)).to(dg.device)
         labels = (S0.long() - g.local_lo) * n_classes // (g.local_hi - g.local_lo)
