@@ -82,8 +82,18 @@ __global__ __launch_bounds__(64 * JOIN_ROWS) void join_columns_k(const float *__
     const int lane = (int)threadIdx.x & 63, group = (int)threadIdx.x >> 6;
     const int64_t col = (int64_t)blockIdx.x * 64 + lane;
     double s = 0.0;
-    if (col < n)
-        for (int64_t p = group; p < parts; p += JOIN_ROWS) s += (double)part[p * n + col];
+    if (col < n) {
+        // (eight of a group's rows on their way at a time)
+        int64_t p = group;
+        for (; p + 7 * JOIN_ROWS < parts; p += 8 * JOIN_ROWS) {
+            float x[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[i] = part[(p + i * JOIN_ROWS) * n + col];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) s += (double)x[i];
+        }
+        for (; p < parts; p += JOIN_ROWS) s += (double)part[p * n + col];
+    }
     lds[group][lane] = s;
     __syncthreads();
     if (group == 0 && col < n) {
