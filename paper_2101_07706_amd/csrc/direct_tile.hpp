@@ -89,7 +89,7 @@ struct DirectTile : MatrixTile<uint16_t, BM, BN, WM, WN, A_ACROSS, B_ACROSS, NB,
     using LayoutA = typename Base::SideA;
     using LayoutB = typename Base::SideB;
     static constexpr int BUFFER = Base::TILE_BYTES, LDS_BYTES = BUFFERS * BUFFER > Base::OUT_BYTES ? BUFFERS * BUFFER : Base::OUT_BYTES, BK = Base::BK;
-    static constexpr int STEPS = Base::STEPS;
+    static constexpr int STEPS = Base::STEPS, WAVES = LDS_BYTES > 80 * 1024 ? NT / 256 : 2;     // (one block a compute unit, or two)
     using SideA = DirectSide<BM, A_ACROSS, NT, ROWB>;
     using SideB = DirectSide<BN, B_ACROSS, NT, ROWB>;
 

@@ -103,9 +103,11 @@ template <typename T, bool GRAD>
 static int launch_types(const GatedArgs &p, int64_t *parts, hipStream_t st)
 {
     const auto tiles = [&](int64_t m, int64_t n) { return (p.M + m - 1) / m * ((p.N + n - 1) / n); };
+    // Tiles of 256 rows by 128 columns of both matrices, one block a compute unit; for the gradient, which writes twice as much and reads dh, of 128 rows, two blocks: one forms
+    // products while the other writes (us, 65536 rows of 1024 by 4096: forward 1043 and 1092, gradient with its products 3182 and 3121).
     if constexpr (sizeof(T) == 2)
         if (tiles(256, 128) >= 200 && direct_operand(p.x, false, p.M, p.K, 256) && direct_operand(p.w[0], true, p.N, p.K, 128) && direct_operand(p.w[1], true, p.N, p.K, 128))
-            return launch_shape<DirectTile<256, 128, 2, 4, false, true, 2, 128, 2>, T, GRAD>(p, parts, st);
+            return launch_shape<std::conditional_t<GRAD, DirectTile<128, 128, 2, 2, false, true, 2, 64, 3>, DirectTile<256, 128, 2, 4, false, true, 2, 128, 2>>, T, GRAD>(p, parts, st);
     if (tiles(128, 64) >= 256) return launch_shape<AnyTile<T, 128, 64, 2, 2, false, true, 2>, T, GRAD>(p, parts, st);
     if (p.K >= 256 && p.M <= 32) return launch_shape<AnyTile<T, 32, 64, 1, 2, false, true, 2, sizeof(T) == 4 ? 4 : 8>, T, GRAD>(p, parts, st);
     if (p.K >= 256 && tiles(64, 64) <= 256) return launch_shape<AnyTile<T, 64, 64, 2, 2, false, true, 2, sizeof(T) == 4 ? 2 : 4>, T, GRAD>(p, parts, st);
