@@ -244,11 +244,12 @@ extern "C" int csgs_linear_grad(const csgs_linear_args *p, const void *dy, int64
     int64_t parts = 0;
     Operand t{s.t, p->N};
     float scale = 1.0f;
-    const bool plain = p->act == CSGS_ACT_NONE, direct = plain && p->dtype == p->y_dtype;
+    // (of an activation's derivative dr knows nothing)
+    const bool plain = p->act == CSGS_ACT_NONE || (!da && !dw && !dbias), direct = plain && p->dtype == p->y_dtype;
     if (direct) {                   // (t is dy itself, its factor that of the products)
         t = Operand{dy, lddy};
         scale = p->alpha;
-    } else if (!plain || da || dw || dbias || dr) {
+    } else {
         a.t = plain && !da && !dw ? nullptr : s.t;
         rc = plain ? launch_dy(a, p->dtype, p->y_dtype, &parts, st) : launch_linear<true>(a, p->dtype, p->y_dtype, &parts, st);
         if (rc != CSGS_OK) return rc;

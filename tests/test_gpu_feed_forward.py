@@ -53,12 +53,15 @@ class Maker:
         return torch.randn(n, generator=self.gen).to(self.dev)
 
 
+REFERENCE = {"device": "cpu"}      # (the largest sizes: in 64 bits on the device, plain products of two matrices)
+
+
 def cpu(t):
-    return None if t is None else t.detach().cpu().double()
+    return None if t is None else t.detach().to(REFERENCE["device"]).double()
 
 
 def within(got, want, tol, what):
-    got = got.detach().cpu()
+    got = got.detach().to(want.device)
     off = (got.double() - want).abs()
     tol = HALF_ULP[got.dtype] * want.abs() * 1.01 + tol * (1 + 2 * HALF_ULP[got.dtype]) + 1e-37
     assert bool(torch.isfinite(got).all()), f"{what}: not finite"
@@ -166,6 +169,31 @@ def test_linear_large(env, size, ts):
     csgs, dev = env
     for i, act in enumerate(("none", "gelu")):
         check_linear(csgs, dev, *size, ts, act, bias=True, residual=True, alpha=0.5, beta=1.0, count=[None, size[0] - 77][i], gap=[0, 1][i], seed=i)
+
+
+@pytest.fixture
+def on_device():
+    REFERENCE["device"] = "cuda"
+    yield
+    REFERENCE["device"] = "cpu"
+
+
+# tiles of 256 that go straight to LDS: more rows than whole tiles, k that ends inside a chunk, columns inside a tile and a piece, rows on multiples of 4 bytes
+@pytest.mark.parametrize("ts", [(B, B), (B, F)], ids=["bf16", "mixed"])
+@pytest.mark.parametrize("size", [(21_007, 520, 1032), (52_000, 72, 40), (51_200, 1000, 8), (300, 8, 52_002), (300, 2056, 20_050)], ids=str)
+def test_linear_straight_to_lds(env, size, ts, on_device):
+    csgs, dev = env
+    M = size[0]
+    for i, (act, count, gap, shift) in enumerate((("none", None, 0, 0), ("silu", M - 77, 6, 2), ("none", M // 3, 8, 2), ("gelu", 0, 0, 8))):
+        check_linear(csgs, dev, *size, ts, act, bias=i != 2, residual=i != 1, alpha=0.5, beta=-1.0, count=count, gap=gap, shift=shift, seed=i, in_place=i == 2)
+
+
+@pytest.mark.parametrize("size", [(21_007, 520, 1032), (51_300, 72, 40), (300, 8, 26_002), (700, 2056, 10_050)], ids=str)
+def test_gated_straight_to_lds(env, size, on_device):
+    csgs, dev = env
+    M = size[0]
+    for i, (act, count, gap, shift) in enumerate((("silu", None, 0, 0), ("gelu", M - 77, 6, 2), ("none", M // 3, 8, 2), ("relu", 0, 0, 8))):
+        check_gated(csgs, dev, *size, B, act, bias=i != 2, count=count, gap=gap, shift=shift, seed=i, halves=i == 2)
 
 
 def check_gated(csgs, dev, M, K, N, tb, act, bias, count=None, gap=0, shift=0, seed=0, halves=False):
