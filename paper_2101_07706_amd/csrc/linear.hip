@@ -135,7 +135,7 @@ static int launch_types(const LinearArgs &p, int64_t *parts, hipStream_t st)
     if constexpr (sizeof(T) == 2)
         if (tiles(256, 256) >= 200 && direct_operand(p.a, false, p.M, p.K, 256) && direct_operand(p.w, true, p.N, p.K, 256))
             return launch_shape<DirectTile<256, 256, 2, 4, false, true, 1, 128, 2>, T, TY, GRAD>(p, parts, st);
-    if (tiles(128, 128) >= 256) return launch_shape<AnyTile<T, 128, 128, 2, 2, false, true, 1>, T, TY, GRAD>(p, parts, st);
+    if (larger_tiles(tiles(128, 128), 128 * 128, tiles(64, 64), 64 * 64)) return launch_shape<AnyTile<T, 128, 128, 2, 2, false, true, 1>, T, TY, GRAD>(p, parts, st);
     if (p.K >= 256 && p.M <= 32) return launch_shape<AnyTile<T, 32, 64, 1, 2, false, true, 1, 8>, T, TY, GRAD>(p, parts, st);
     if (p.K >= 256 && tiles(64, 64) <= 256) return launch_shape<AnyTile<T, 64, 64, 2, 2, false, true, 1, 4>, T, TY, GRAD>(p, parts, st);
     return launch_shape<AnyTile<T, 64, 64, 2, 2, false, true, 1>, T, TY, GRAD>(p, parts, st);

@@ -93,7 +93,15 @@ __device__ CSGS_INLINE inline void form_sums(Tile &tile, char *lds, F sum)
     if (tile.settle(lds)) tile.again(lds, sum);
 }
 
-// ---------------------------------------------------------------- host side, matrix_grad.hip
+// ---------------------------------------------------------------- host side
+// Whether tiles of `large` entries are the quicker ones: a compute unit's share of them, against tiles of `small` entries, which read LDS twice as often for a product and take
+// 1 / 0.85 of the time where both fill the device (us, gated gradient in floats: 4001 rows of 602 by 1111, 576 and 1134 tiles, 300 and 275; 5224 rows of 224 by 760, 492 and 984, 28 and 33).
+inline bool larger_tiles(int64_t tiles_large, int64_t large, int64_t tiles_small, int64_t small)
+{
+    return 0.85 * (double)((tiles_large + 255) / 256 * large) <= (double)((tiles_small + 255) / 256 * small);
+}
+
+// matrix_grad.hip
 // Sums over rows that blocks left as parts [parts x n], joined in double in their order.
 int launch_join_columns(const float *part, int64_t parts, int32_t n, float *out, hipStream_t st);
 
