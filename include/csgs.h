@@ -672,8 +672,8 @@ int csgs_gated_grad(const csgs_gated_args *p /*host*/, const void *dh, int64_t l
  *
  * The tensors are described once, as those of csgs_grad_list.  A tensor may be a table of which the gradient holds rows alone
  * (csgs_embed_grad_rows): with ids, row j of g belongs to row ids[j] of p, and the rows that no id names are left untouched,
- * their states among them.  ids have to ascend strictly; ids outside [0, rows) are passed over; a row whose id does not ascend is left
- * untouched and sets CSGS_ST_BAD_NODE_ID.
+ * their states among them.  ids outside [0, rows) are passed over; the others have to ascend strictly: a row of g whose id is not above the
+ * one before it changes nothing and sets CSGS_ST_BAD_NODE_ID (further rows of g with one id may then leave a mix of their steps in its row).
  *
  * States in 8 bits.  A row's entries are cut into blocks of CSGS_STATE_BLOCK (the last one may be shorter); a block keeps one byte,
  * the exponent field E of its largest value's float (0: the block is zero; 255: the block holds a value that is not finite, all of it reads
@@ -727,8 +727,10 @@ typedef struct csgs_adamw_args {
 /* Bytes of device memory for a list of these tensors; 0 on bad input (n outside [1, 2^20], a tensor that csgs_adamw_list_init
  * would refuse). */
 size_t csgs_adamw_list_bytes(const csgs_adamw_tensor *t /*host*/, int32_t n);
-/* Writes the descriptions of the n tensors into l->base (kernels that carry them as arguments).  No two may share a parameter.
- * Host errors: CSGS_EINVAL, CSGS_EWORKSPACE, CSGS_EUNSUPPORTED (dtype, state, more than 2^40 entries, ids of more than 2^31 - 1 rows). */
+/* Writes the descriptions of the n tensors into l->base (kernels that carry them as arguments).  No two may share a parameter,
+ * a copy or a state.
+ * Host errors: CSGS_EINVAL (also: one address for two of those), CSGS_EWORKSPACE, CSGS_EUNSUPPORTED (dtype, state, more than 2^40 entries, ids
+ * of more than 2^31 - 1 rows). */
 int csgs_adamw_list_init(csgs_adamw_list *l /*host*/, const csgs_adamw_tensor *t /*host*/, int32_t n, void *stream);
 /* The step.  Two launches with clip, one without.  Where clip or total is given and the total is NaN or infinite, nothing is changed, *step
  * neither, and CSGS_ST_NONFINITE_GRAD is set.  Calls that share a list must be ordered on one stream.

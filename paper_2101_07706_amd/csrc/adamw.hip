@@ -10,6 +10,9 @@
 // those lanes.  g' = c g, m and v are formed in double (eight operations): which of two codes a state next to their border gets does then not
 // depend on how c g was rounded.
 #include <math.h>
+#include <algorithm>
+#include <new>
+#include <vector>
 #include "common.hpp"
 #include "grad_list.hpp"
 #include "row_pieces.hpp"
@@ -196,9 +199,13 @@ __device__ inline Place place_of(const AdamDesc &d, int64_t seg, int64_t live, i
         o.row = id;
         if (id < 0 || id >= d.rows) {
             o.row = -1;
-        } else if (j > 0 && d.ids[j - 1] >= id) {      // (two lanes that write one row would race)
-            o.row = -1;
-            if (status && lane == 0) atomicOr(status, CSGS_ST_BAD_NODE_ID);
+        } else {      // (two lanes that write one row would race)
+            int64_t k = j - 1;
+            while (k >= 0 && (d.ids[k] < 0 || d.ids[k] >= d.rows)) --k;
+            if (k >= 0 && d.ids[k] >= id) {
+                o.row = -1;
+                if (status && lane == 0) atomicOr(status, CSGS_ST_BAD_NODE_ID);
+            }
         }
     }
     *g_row = j;
@@ -437,17 +444,35 @@ static int describe(const csgs_adamw_tensor &t, int64_t *tiles, AdamDesc *d)
     return *tiles > ADAM_ENTRIES / CSGS_STATE_BLOCK ? CSGS_EUNSUPPORTED : CSGS_OK;
 }
 
+// Checks and counts all of a list's tensors.  What a step writes belongs to one of them: two that share an address would be written by two blocks at once.
+static int describe_all(const csgs_adamw_tensor *t, int32_t n, int64_t *tiles)
+{
+    *tiles = 0;
+    AdamDesc d;
+    try {
+        std::vector<const void *> written;
+        written.reserve((size_t)n * 6);
+        for (int32_t i = 0; i < n; ++i) {
+            const int rc = describe(t[i], tiles, &d);
+            if (rc != CSGS_OK) return rc;
+            for (const void *p : {(const void *)t[i].p, (const void *)t[i].copy, (const void *)t[i].m, (const void *)t[i].v, (const void *)t[i].m_exp, (const void *)t[i].v_exp})
+                if (p) written.push_back(p);
+        }
+        std::sort(written.begin(), written.end());
+        return std::adjacent_find(written.begin(), written.end()) == written.end() ? CSGS_OK : CSGS_EINVAL;
+    } catch (const std::bad_alloc &) {
+        return CSGS_EWORKSPACE;
+    }
+}
+
 }  // namespace csgs
 
 using namespace csgs;
 
 extern "C" size_t csgs_adamw_list_bytes(const csgs_adamw_tensor *t, int32_t n)
 {
-    if (!t || n < 1 || n > 1 << 20) return 0;
-    int64_t tiles = 0;
-    AdamDesc d;
-    for (int32_t i = 0; i < n; ++i)
-        if (describe(t[i], &tiles, &d) != CSGS_OK) return 0;
+    int64_t tiles;
+    if (!t || n < 1 || n > 1 << 20 || describe_all(t, n, &tiles) != CSGS_OK) return 0;
     return carve_adamw(nullptr, n, tiles).bytes;
 }
 
@@ -455,12 +480,9 @@ extern "C" int csgs_adamw_list_init(csgs_adamw_list *l, const csgs_adamw_tensor 
 {
     if (!l || !l->base || ((uintptr_t)l->base & 255) || !t || n < 1 || n > 1 << 20) return CSGS_EINVAL;
     l->ready = 0;
-    int64_t tiles = 0;
-    AdamDesc d;
-    for (int32_t i = 0; i < n; ++i) {
-        const int rc = describe(t[i], &tiles, &d);
-        if (rc != CSGS_OK) return rc;
-    }
+    int64_t tiles;
+    const int rc = describe_all(t, n, &tiles);
+    if (rc != CSGS_OK) return rc;
     const AdamMem m = carve_adamw(l->base, n, tiles);
     if (l->bytes < m.bytes) return CSGS_EWORKSPACE;
     int64_t at = 0;

@@ -167,6 +167,23 @@ def test_ids_that_do_not_ascend_are_left_out(env):
     p.check(before, 1, 1e-2, 0.9, 0.999, 1e-8)
 
 
+@pytest.mark.parametrize("bits", [32, 8])
+def test_an_id_named_again_behind_ids_that_are_passed_over(env, bits):
+    """The first row of g with an id is taken, whatever lies between it and the next one."""
+    csgs, dev = env
+    g = torch.randn(8, 40, generator=torch.Generator().manual_seed(1)).to(dev)
+    got = []
+    for ids, rows in (([5, -1, 5, 20, 7, 7, -1, 2_000_000_000], list(range(8))), ([5, 7], [0, 4])):
+        p, step, status = torch.ones(20, 40, device=dev), *(torch.zeros(1, dtype=torch.int32, device=dev) for _ in range(2))
+        state = csgs.adamw_states(p, bits)
+        l = csgs.make_adamw_list([csgs.adamw_entry(p, g[rows], **state, ids=torch.tensor(ids, dtype=torch.int32, device=dev))])
+        csgs.csgs_adamw(l, 1e-2, step, status=status)
+        got.append((p, *state.values()))
+        assert int(status) == (csgs.ST_BAD_NODE_ID if len(ids) == 8 else 0) and int(step) == 1
+    assert all(torch.equal(a, b) for a, b in zip(*got))
+    assert int((got[0][0] != 1).any(1).sum()) == 2
+
+
 @pytest.mark.parametrize("kind", ["l2", "l1", "max"])
 @pytest.mark.parametrize("bits", [32, 8])
 def test_clipped_by_the_norm_of_the_gradients(env, kind, bits):

@@ -48,6 +48,19 @@ def test_adamw_lists():
     assert L.csgs_adamw_list_init(None, one, 1, Z) == csgs.EINVAL
 
 
+@pytest.mark.parametrize("theirs", ["p", "copy", "m", "v", "m_exp", "v_exp"])
+def test_what_a_step_writes_belongs_to_one_tensor(theirs):
+    L = csgs.lib()
+    one = dict(p=1 << 20, copy=2 << 20, ldcopy=5, m=3 << 20, v=4 << 20, m_exp=5 << 20, v_exp=6 << 20, state=1)
+    other = {k: v if k in ("ldcopy", "state") else v + (8 << 20) for k, v in one.items()}
+    pair = lambda **kw: (csgs.AdamwTensor * 2)(adam(**one), adam(**{**other, **kw}))  # noqa: E731
+    assert L.csgs_adamw_list_bytes(pair(), 2) > 0
+    for mine in ("p", "copy", "m", "v", "m_exp", "v_exp"):
+        ts = pair(**{theirs: one[mine]})
+        l = csgs.AdamwList(4096, 1 << 40, 0, 0, 0)
+        assert L.csgs_adamw_list_bytes(ts, 2) == 0 and L.csgs_adamw_list_init(C.byref(l), ts, 2, Z) == csgs.EINVAL and l.ready == 0
+
+
 def test_adamw_step():
     L = csgs.lib()
     ready, raw = csgs.AdamwList(4096, 1 << 20, 1, 1, 1), csgs.AdamwList(4096, 1 << 20, 0, 0, 0)
