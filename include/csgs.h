@@ -604,7 +604,7 @@ int csgs_grad_clip(const csgs_grad_list *l /*host*/, int kind, float max_norm, f
  * act: the identity, max(z, 0), the logistic function s(z), z s(z), or z Phi(z) with the normal distribution's Phi.  One rounding per output.
  * y may be r (same address and leading dimension); other overlaps are not allowed.  A row of y depends on its own rows of a and r alone.
  * With M_dev only rows below the device count are computed and written; a's rows past it may be read, whatever they hold.
- * Host errors: CSGS_EINVAL, CSGS_EUNSUPPORTED (types).
+ * Host errors: CSGS_EINVAL, CSGS_EUNSUPPORTED (types; 2^24 tiles of 64 by 64 and more).
  */
 enum { CSGS_ACT_NONE = 0, CSGS_ACT_RELU = 1, CSGS_ACT_SIGMOID = 2, CSGS_ACT_SILU = 3, CSGS_ACT_GELU = 4 };
 

@@ -94,7 +94,7 @@ static int launch_shape(GatedArgs p, int64_t *parts, hipStream_t st)
     p.tiles_m = ((int64_t)p.M + BM - 1) / BM;
     p.tiles_n = ((int64_t)p.N + BN - 1) / BN;
     *parts = p.tiles_m * WM;
-    if (p.tiles_m * p.tiles_n > 1 << 30) return CSGS_EUNSUPPORTED;
+    if (p.tiles_m * p.tiles_n > MOST_BLOCKS) return CSGS_EUNSUPPORTED;
     CSGS_LAUNCH(K_GATED, (gated_k<Tile, T, GRAD>), dim3((unsigned)(p.tiles_m * p.tiles_n)), dim3(Tile::THREADS), st, p);
     CSGS_LAUNCH_CHECK();
     return CSGS_OK;
@@ -170,7 +170,7 @@ extern "C" int csgs_gated(const csgs_gated_args *p, void *h, int64_t ldh, void *
     GatedArgs a;
     const int rc = check(p, &a);
     if (rc != CSGS_OK) return rc;
-    if (!h || ldh < p->N || h == p->x || h == p->wg || h == p->wu) return CSGS_EINVAL;
+    if (!h || ldh < p->N || !outputs_apart({p->x, p->wg, p->wu, p->bg, p->bu}, {h})) return CSGS_EINVAL;
     a.h = h;
     a.ldh = ldh;
     int64_t parts;
@@ -190,7 +190,8 @@ extern "C" int csgs_gated_grad(const csgs_gated_args *p, const void *dh, int64_t
     int rc = check(p, &a);
     if (rc != CSGS_OK) return rc;
     if (!dh || lddh < p->N || (dx && lddx < p->K) || (dwg && lddwg < p->N) || (dwu && lddwu < p->N)) return CSGS_EINVAL;
-    if ((!dx && !dwg && !dwu && !dbg && !dbu) || (dbg && !p->bg) || (dbu && !p->bu) || dx == dh || dwg == dh || dwu == dh) return CSGS_EINVAL;
+    if ((!dx && !dwg && !dwu && !dbg && !dbu) || (dbg && !p->bg) || (dbu && !p->bu)) return CSGS_EINVAL;
+    if (!outputs_apart({p->x, p->wg, p->wu, p->bg, p->bu, dh}, {dx, dwg, dwu, dbg, dbu})) return CSGS_EINVAL;
     if (!scratch || ((uintptr_t)scratch & 255)) return CSGS_EINVAL;
     const GatedScratch s = carve_gated(scratch, p->M, p->K, p->N, p->dtype);
     if (scratch_bytes < s.bytes) return CSGS_EWORKSPACE;

@@ -123,7 +123,7 @@ static int launch_shape(LinearArgs p, int64_t *parts, hipStream_t st)
     p.tiles_m = ((int64_t)p.M + BM - 1) / BM;
     p.tiles_n = ((int64_t)p.N + BN - 1) / BN;
     *parts = p.tiles_m * WM;
-    if (p.tiles_m * p.tiles_n > 1 << 30) return CSGS_EUNSUPPORTED;
+    if (p.tiles_m * p.tiles_n > MOST_BLOCKS) return CSGS_EUNSUPPORTED;
     CSGS_LAUNCH(K_LINEAR, (linear_k<Tile, T, TY, GRAD>), dim3((unsigned)(p.tiles_m * p.tiles_n)), dim3(Tile::THREADS), st, p);
     CSGS_LAUNCH_CHECK();
     return CSGS_OK;
@@ -151,7 +151,7 @@ static int launch_dy(LinearArgs p, int dtype, int y_dtype, int64_t *parts, hipSt
 {
     *parts = ((int64_t)p.M + DY_ROWS - 1) / DY_ROWS;
     p.tiles_n = ((int64_t)p.N + 255) / 256;
-    if (*parts * p.tiles_n > 1 << 30) return CSGS_EUNSUPPORTED;
+    if (*parts * p.tiles_n > MOST_BLOCKS) return CSGS_EUNSUPPORTED;
     const dim3 grid((unsigned)(*parts * p.tiles_n)), block(256);
     if (dtype == CSGS_F32) CSGS_LAUNCH(K_LINEAR_DY, (linear_dy_k<float, float>), grid, block, st, p);
     else if (y_dtype == CSGS_F32) CSGS_LAUNCH(K_LINEAR_DY, (linear_dy_k<uint16_t, float>), grid, block, st, p);
@@ -210,7 +210,7 @@ extern "C" int csgs_linear(const csgs_linear_args *p, void *y, int64_t ldy, void
     LinearArgs a;
     const int rc = check(p, &a);
     if (rc != CSGS_OK) return rc;
-    if (!y || ldy < p->N || (y == p->r && ldy != p->ldr) || y == p->a || y == p->w) return CSGS_EINVAL;
+    if (!y || ldy < p->N || (y == p->r && ldy != p->ldr) || !outputs_apart({p->a, p->w, p->bias}, {y})) return CSGS_EINVAL;
     a.y = y;
     a.ldy = ldy;
     int64_t parts;
@@ -230,7 +230,8 @@ extern "C" int csgs_linear_grad(const csgs_linear_args *p, const void *dy, int64
     int rc = check(p, &a);
     if (rc != CSGS_OK) return rc;
     if (!dy || lddy < p->N || (da && ldda < p->K) || (dw && lddw < p->N) || (dr && lddr < p->N) || (!da && !dw && !dbias && !dr)) return CSGS_EINVAL;
-    if ((dbias && !p->bias) || (dr && !p->r) || (dr == dy && lddr != lddy) || da == dy || dw == dy) return CSGS_EINVAL;
+    if ((dbias && !p->bias) || (dr && !p->r) || (dr == dy && lddr != lddy)) return CSGS_EINVAL;
+    if (!outputs_apart({p->a, p->w, p->bias}, {da, dw, dbias, dr}) || !outputs_apart({dy}, {da, dw, dbias})) return CSGS_EINVAL;
     if (!scratch || ((uintptr_t)scratch & 255)) return CSGS_EINVAL;
     const LinearScratch s = carve_linear(scratch, p->M, p->K, p->N, p->dtype);
     if (scratch_bytes < s.bytes) return CSGS_EWORKSPACE;

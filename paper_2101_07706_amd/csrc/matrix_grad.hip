@@ -157,7 +157,7 @@ static int launch_shape(const OutProduct &p, float *parts, hipStream_t st)
     a.tiles_m = (p.rows + BM - 1) / BM;
     a.tiles_n = (p.cols + BN - 1) / BN;
     const int64_t blocks = a.tiles_m * a.tiles_n;
-    if (blocks > 1 << 30) return CSGS_EUNSUPPORTED;
+    if (blocks > MOST_BLOCKS) return CSGS_EUNSUPPORTED;
     constexpr int64_t BK = Tile::BK;
     constexpr int64_t SLOTS = 256 * (Tile::LDS_BYTES > 80 * 1024 ? 1 : 2);
     int64_t n = parts_of(p.rows, p.cols, p.red, p.outs, blocks * p.outs, SLOTS);

@@ -168,8 +168,8 @@ class ResidualGCN:
         csgs.csgs_grad_clip(self.list, csgs.GRAD_L2, self.max_norm, self.norm, self.status)
 
     def descend(self):
-        """A step on all parameters.  AdamW leaves out by itself what is not finite.  Gradient descent: clipping makes NaN of gradients whose norm is not finite: such a step changes nothing.  Decided on the
-        device, from the status and not from the norm, which as a float may be infinite where the total is not."""
+        """A step on all parameters.  Gradients whose norm is not finite change nothing: AdamW sees to that by itself, for gradient descent clipping makes NaN of
+        them, and it is decided here, on the device, from the status and not from the norm, which as a float may be infinite where the total is not."""
         if self.optimizer == "adamw":
             csgs.csgs_adamw(self.adamw_list, self.lr, self.steps_taken, clip=self.list, kind=csgs.GRAD_L2, max_norm=self.max_norm, norm=self.norm, status=self.status)
             self.skipped += (self.status & csgs.ST_NONFINITE_GRAD) != 0

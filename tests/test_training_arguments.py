@@ -216,6 +216,35 @@ def test_gated_gradient():
     assert call(gated(), nbytes=need - 1) == csgs.EWORKSPACE
 
 
+def test_products_whose_outputs_lie_on_inputs_or_each_other():
+    L = csgs.lib()
+    inputs, outputs = [4096, 8192, 12288, 1 << 20], [2 << 20, 3 << 20, 4 << 20, 5 << 20]
+
+    def linear_grad(out):
+        p = linear(r=24576)
+        return L.csgs_linear_grad(C.byref(p), ptr(1 << 20), 5, ptr(out[0]), 6, ptr(out[1]), 5, ptr(out[2]), ptr(out[3]), 5, ptr(6 << 20), 1, Z)
+
+    def gated_grad(out):
+        p = gated(bu=20480)
+        return L.csgs_gated_grad(C.byref(p), ptr(1 << 20), 5, ptr(out[0]), 6, ptr(out[1]), 5, ptr(out[2]), 5, ptr(out[3]), ptr(out[4]), ptr(6 << 20), 1, Z)
+    for call, ins, outs in ((linear_grad, inputs, outputs), (gated_grad, inputs + [16384, 20480], outputs + [7 << 20])):
+        assert call(outs) == csgs.EWORKSPACE        # (nothing else is wrong with it)
+        for i in range(len(outs)):
+            for other in ins + outs[:i]:
+                ok = call is linear_grad and i == 3 and other == 1 << 20       # (dr may be dy)
+                assert call([*outs[:i], other, *outs[i + 1:]]) == (csgs.EWORKSPACE if ok else csgs.EINVAL), (call, i, other)
+    assert L.csgs_linear(C.byref(linear()), ptr(12288), 5, Z) == csgs.EINVAL and L.csgs_gated(C.byref(gated()), ptr(16384), 5, Z) == csgs.EINVAL
+
+
+def test_products_of_more_blocks_than_a_launch_has():
+    L = csgs.lib()
+    big = 2 ** 31 - 1
+    assert L.csgs_linear(C.byref(linear(M=big, N=129, ldw=129, ldr=129)), ptr(1 << 20), 129, Z) == csgs.EUNSUPPORTED
+    assert L.csgs_gated(C.byref(gated(M=big, N=1000, ldwg=1000, ldwu=1000)), ptr(1 << 20), 1000, Z) == csgs.EUNSUPPORTED
+    p = linear(M=big, N=1, ldw=1, ldr=1, K=1 << 20, lda=1 << 20)
+    assert L.csgs_linear_grad(C.byref(p), ptr(1 << 20), 1, ptr(2 << 20), 1 << 20, Z, 1, Z, Z, 1, ptr(6 << 20), 1 << 62, Z) == csgs.EUNSUPPORTED
+
+
 @pytest.mark.parametrize("size", [csgs.csgs_linear_grad_scratch_bytes, csgs.csgs_gated_grad_scratch_bytes])
 def test_scratch_for_the_largest_product_serves_smaller_ones(size):
     assert size(0, 1, 1, 0) == 0 and size(1, 0, 1, 0) == 0 and size(1, 1, 0, 0) == 0 and size(1, 1, 1, 2) == 0 and size(-1, 1, 1, 0) == 0
