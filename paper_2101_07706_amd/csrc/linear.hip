@@ -1,4 +1,13 @@
 // csgs_linear: y = alpha act(a w + bias) + beta r, and its gradient.
+//
+// One product with its epilogue: a, w and r are read and y is written once, 2 M K N operations.  For wide layers the matrix cores bound it, and under them the clock, which falls to 1.6 -
+// 1.9 GHz as they fill (65536 rows of 4096 by 1024 in bfloat16: 523 us, 1051 TFLOP/s; matrix cores busy 45 - 65 % of the cycles); for narrow ones (K or N up to some hundred) the
+// rows' bytes, for few rows the launch and the way through a tile's sum (one row of 1024 by 1024: 8 us).
+//
+// Gradient, t = alpha dy .* act'(a w + bias): act' needs the product again (4 M K N are da and dw, 2 M K N this), which is cheaper than 4 bytes of each entry kept in the forward pass and leaves
+// the forward call nothing to keep.  t is written once, in the operands' type: for bfloat16 a rounding of half a step, 2^-8 relative, of each term of da and dw, which the
+// matrix cores ask for.  Column sums for dbias and dr come from the same registers, before that rounding.  Without an activation t is dy but for a factor: da and dw are formed from
+// dy itself where the types are the same, else linear_dy_k rounds it (65536 rows of 1024, float to bfloat16 with sums: 116 us with dr).
 #include "products.hpp"
 #include "direct_tile.hpp"
 #include "split_tile.hpp"
@@ -132,10 +141,14 @@ template <typename T, typename TY, bool GRAD>
 static int launch_types(const LinearArgs &p, int64_t *parts, hipStream_t st)
 {
     const auto tiles = [&](int64_t m, int64_t n) { return (p.M + m - 1) / m * ((p.N + n - 1) / n); };
+    // Tiles of 256 by 256 straight to LDS, one block a compute unit; those of 128 by 128 are held two a compute unit, 512 at once: the larger ones are taken where the smaller ones
+    // would need a second round (us, 1024 by 1024, large and small: 6400 rows 35 and 30, 9600 rows 36 and 43, 16384 rows 42 and 55; 12800 rows of 4096 by 1024 102 and 194).
     if constexpr (sizeof(T) == 2)
-        if (tiles(256, 256) >= 200 && direct_operand(p.a, false, p.M, p.K, 256) && direct_operand(p.w, true, p.N, p.K, 256))
+        if (tiles(256, 256) > 128 && direct_operand(p.a, false, p.M, p.K, 256) && direct_operand(p.w, true, p.N, p.K, 256))
             return launch_shape<DirectTile<256, 256, 2, 4, false, true, 1, 128, 2>, T, TY, GRAD>(p, parts, st);
     if (larger_tiles(tiles(128, 128), 128 * 128, tiles(64, 64), 64 * 64)) return launch_shape<AnyTile<T, 128, 128, 2, 2, false, true, 1>, T, TY, GRAD>(p, parts, st);
+    // Few tiles and long sums: groups of a block's wavefronts take a tile's chunks in turn (us, without and with: one row of 1024 by 1024 15 and 8, in floats 31 and 16; 128 rows of 4096 by
+    // 1024 34 and 22; 1024 rows of 1024 by 1024 11.6 and 9.8; 2048 rows, 512 tiles, 13.6 and 17.1).
     if (p.K >= 256 && p.M <= 32) return launch_shape<AnyTile<T, 32, 64, 1, 2, false, true, 1, 8>, T, TY, GRAD>(p, parts, st);
     if (p.K >= 256 && tiles(64, 64) <= 256) return launch_shape<AnyTile<T, 64, 64, 2, 2, false, true, 1, 4>, T, TY, GRAD>(p, parts, st);
     return launch_shape<AnyTile<T, 64, 64, 2, 2, false, true, 1>, T, TY, GRAD>(p, parts, st);

@@ -6,6 +6,8 @@
 // (each by the matrix cores without a rounding, summed in float): a product costs six times 32 cycles a step of 16 k instead of 8 times 64 on the float cores.  ah bh has sums of its own,
 // the others share one set, which is added at the end: the large sums are rounded once for 16 k.  (Products down to 2^-149 keep what floats keep: the matrix cores take and
 // give numbers below 2^-126.)
+// Bound by six products and by the splitting in front of LDS (4001 rows of 602 by 1111, gated, with all gradients: 453 us on the float cores, 316 so with the same tiles, now 272, 118
+// TFLOP/s as floats count; relative error against 64 bits 1.2e-6 on the float cores, 2.7e-7 so).
 //
 // x - h is NaN where x is not finite.  Sums that are not finite are formed again, by the float cores: those give what the inputs do.
 #pragma once
