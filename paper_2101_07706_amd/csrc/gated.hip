@@ -118,9 +118,9 @@ static int launch_types(const GatedArgs &p, int64_t *parts, hipStream_t st)
         if (tiles(256, 128) > 128 && direct_operand(p.x, false, p.M, p.K, 256) && direct_operand(p.w[0], true, p.N, p.K, 128) && direct_operand(p.w[1], true, p.N, p.K, 128))
             return launch_shape<std::conditional_t<GRAD, DirectTile<128, 128, 2, 2, false, true, 2, 64, 3>, DirectTile<256, 128, 2, 4, false, true, 2, 128, 2>>, T, GRAD>(p, parts, st);
     if (larger_tiles(tiles(128, 64), 128 * 64, tiles(64, 64), 64 * 64)) return launch_shape<AnyTile<T, 128, 64, 2, 2, false, true, 2>, T, GRAD>(p, parts, st);
-    // (groups of wavefronts as for csgs_linear; us, without and with: one row of 1024 by 4096 17.4 and 11.3, in floats 46 and 24; 128 rows of 1024 by 1024 in floats 49 and 34.  Two
-    // matrices' tiles in three planes leave LDS for fewer groups)
-    if (p.K >= 256 && p.M <= 32) return launch_shape<AnyTile<T, 32, 64, 1, 2, false, true, 2, sizeof(T) == 4 ? 4 : 8>, T, GRAD>(p, parts, st);
+    // (groups of wavefronts as for csgs_linear; us, without and with: one row of 1024 by 4096 17.4 and 11.3, in floats 46 and 24; 128 rows of 1024 by 1024 in floats 49 and 34, on half the
+    // rows 24.  Two matrices' tiles in three planes leave LDS for fewer groups)
+    if (p.K >= 256 && (p.M <= 32 || tiles(64, 64) <= 128)) return launch_shape<AnyTile<T, 32, 64, 1, 2, false, true, 2, sizeof(T) == 4 ? 4 : 8>, T, GRAD>(p, parts, st);
     if (p.K >= 256 && tiles(64, 64) <= 256) return launch_shape<AnyTile<T, 64, 64, 2, 2, false, true, 2, sizeof(T) == 4 ? 2 : 4>, T, GRAD>(p, parts, st);
     return launch_shape<AnyTile<T, 64, 64, 2, 2, false, true, 2>, T, GRAD>(p, parts, st);
 }

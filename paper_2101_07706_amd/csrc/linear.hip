@@ -147,9 +147,10 @@ static int launch_types(const LinearArgs &p, int64_t *parts, hipStream_t st)
         if (tiles(256, 256) > 128 && direct_operand(p.a, false, p.M, p.K, 256) && direct_operand(p.w, true, p.N, p.K, 256))
             return launch_shape<DirectTile<256, 256, 2, 4, false, true, 1, 128, 2>, T, TY, GRAD>(p, parts, st);
     if (larger_tiles(tiles(128, 128), 128 * 128, tiles(64, 64), 64 * 64)) return launch_shape<AnyTile<T, 128, 128, 2, 2, false, true, 1>, T, TY, GRAD>(p, parts, st);
-    // Few tiles and long sums: groups of a block's wavefronts take a tile's chunks in turn (us, without and with: one row of 1024 by 1024 15 and 8, in floats 31 and 16; 128 rows of 4096 by
-    // 1024 34 and 22; 1024 rows of 1024 by 1024 11.6 and 9.8; 2048 rows, 512 tiles, 13.6 and 17.1).
-    if (p.K >= 256 && p.M <= 32) return launch_shape<AnyTile<T, 32, 64, 1, 2, false, true, 1, 8>, T, TY, GRAD>(p, parts, st);
+    // Few tiles and long sums: groups of a block's wavefronts take a tile's chunks in turn (us, without and with: one row of 1024 by 1024 15 and 8, in floats 31 and 16; 1024 rows of 1024 by
+    // 1024, 256 tiles, 11.6 and 9.8; 2048 rows, 512 tiles, 13.6 and 17.1).  Eight groups on half the rows as long as those tiles have a unit each (us, four groups and eight: 128 rows of 4096
+    // by 1024 22 and 17; 1024 of 1024 by 512, 128 tiles, floats 21 and 18; 1024 of 1024 by 1024, floats 23 and 33).
+    if (p.K >= 256 && (p.M <= 32 || tiles(64, 64) <= 128)) return launch_shape<AnyTile<T, 32, 64, 1, 2, false, true, 1, 8>, T, TY, GRAD>(p, parts, st);
     if (p.K >= 256 && tiles(64, 64) <= 256) return launch_shape<AnyTile<T, 64, 64, 2, 2, false, true, 1, 4>, T, TY, GRAD>(p, parts, st);
     return launch_shape<AnyTile<T, 64, 64, 2, 2, false, true, 1>, T, TY, GRAD>(p, parts, st);
 }

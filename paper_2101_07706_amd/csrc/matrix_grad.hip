@@ -198,6 +198,9 @@ static int launch_sides(const OutProduct &p, float *parts, hipStream_t st)
     // (us, floats, 512 by 512, tiles of 128 and of 64: da of 8192 rows, 256 tiles, 41 and 35, dw of 16384 rows, 16 tiles and 32 possible parts, 68 and 79; gradient of 4001 rows of 602 by
     // 1111 with both matrices, da 160 tiles and 3 possible parts, 272 and 291)
     if (tiles(128, 128) * most >= 384) return launch_shape<AnyTile<T, 128, 128, 2, 2, ACROSS, ACROSS, 1>, T>(p, parts, st);
+    // (four groups of wavefronts take a tile's chunks in turn; us, without and with: da of 1024 rows, 256 columns, sums of 1024, floats 23 and 16, of 4096 rows, 512 tiles and parts, 29 and 23;
+    // dw of 1400 rows of 37 by 6 23 and 13; of 4096 rows of 256 by 256 in bfloat16 12.4 and 12.4)
+    if (tiles(64, 64) * most <= 512) return launch_shape<AnyTile<T, 64, 64, 2, 2, ACROSS, ACROSS, 1, 4>, T>(p, parts, st);
     return launch_shape<AnyTile<T, 64, 64, 2, 2, ACROSS, ACROSS, 1>, T>(p, parts, st);
 }
 

@@ -196,6 +196,27 @@ def test_gated_straight_to_lds(env, size, on_device):
         check_gated(csgs, dev, *size, B, act, bias=i != 2, count=count, gap=gap, shift=shift, seed=i, halves=i == 2)
 
 
+# tiles of 64 by one and by four groups of wavefronts, of 32 rows by eight; gradients' parts of one chunk and of many
+TILES = [(8200, 520, 260), (4064, 1000, 16), (1024, 300, 70), (1000, 257, 600), (96, 2048, 130)]
+
+
+@pytest.mark.parametrize("ts", [(F, F), (B, B), (B, F)], ids=["f32", "bf16", "mixed"])
+@pytest.mark.parametrize("size", TILES, ids=str)
+def test_linear_over_tiles(env, size, ts, on_device):
+    csgs, dev = env
+    M = size[0]
+    for i, (act, count, gap) in enumerate((("none", None, 0), ("silu", M - 33, 3), ("gelu", 40, 8))):
+        check_linear(csgs, dev, *size, ts, act, bias=i != 2, residual=i != 1, alpha=0.5, beta=-1.0, count=count, gap=gap, seed=i)
+
+
+@pytest.mark.parametrize("tb", [F, B], ids=["f32", "bf16"])
+@pytest.mark.parametrize("size", TILES, ids=str)
+def test_gated_over_tiles(env, size, tb, on_device):
+    csgs, dev = env
+    check_gated(csgs, dev, *size, tb, "silu", bias=True, gap=0, seed=1)
+    check_gated(csgs, dev, *size, tb, "gelu", bias=False, count=size[0] - 33, gap=1, seed=2)
+
+
 def check_gated(csgs, dev, M, K, N, tb, act, bias, count=None, gap=0, shift=0, seed=0, halves=False):
     mk = Maker(dev, seed, gap, shift)
     x = mk.matrix(M, K, tb)
