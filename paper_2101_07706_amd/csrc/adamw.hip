@@ -310,7 +310,7 @@ __global__ __launch_bounds__(256, 4) void adamw_k(AdamMem m, int64_t tiles, Adam
             if (a.status && !take) atomicOr(a.status, CSGS_ST_NONFINITE_GRAD);
         }
     }
-    // (the counter is advanced by the block that ends last: every block has read it by then)
+    // (the counter is advanced by the block that ends last, and a block ends behind a barrier of its wavefronts: each of them has read it by then)
     const int32_t before = __builtin_amdgcn_readfirstlane(*a.step);
     const double t = (double)(before < 0 ? 0 : before) + 1.0;
     const double r = sqrt(-expm1(t * a.log_beta2));
@@ -343,11 +343,13 @@ __global__ __launch_bounds__(256, 4) void adamw_k(AdamMem m, int64_t tiles, Adam
                 }
             }
         }
+    // Every wavefront has read the counter for itself: none is counted before all of its block have.
+    __syncthreads();
     if (threadIdx.x == 0) {
         const uint32_t blocks = gridDim.x, group = blockIdx.x % DONE_GROUPS, groups = blocks < DONE_GROUPS ? blocks : DONE_GROUPS;
         const auto last_of = [&](uint32_t place, uint32_t n) {
             uint32_t *at = m.done + place * DONE_STEP;
-            // (relaxed: nothing that the blocks have written is handed on, and the counter was read long before; a release would write back a die's cache)
+            // (relaxed: nothing that the blocks have written is handed on, and the counter was read in front of the barrier; a release would write back a die's cache)
             if (__hip_atomic_fetch_add(at, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) + 1 != n) return false;
             *at = 0;
             return true;

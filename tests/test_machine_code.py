@@ -239,3 +239,31 @@ def test_waiting_blocks_fit_together(tmp_path):
             assert 512 // (-(-regs // 8) * 8) >= blocks, f"{regs} registers"
             assert blocks * lds <= 160 << 10, f"{lds} bytes of LDS"
     assert seen == 1
+
+
+# The block of a step that ends last writes the counter that every wavefront has read: on every way to the place where a block is counted there is a
+# barrier behind the last load of any wavefront.
+def test_steps_are_counted_behind_a_barrier(functions):
+    seen = 0
+    for name, ins in functions:
+        if "7adamw_kE" not in name:
+            continue
+        at = {a: k for k, (a, _, _, _) in enumerate(ins)}
+        before = [[] for _ in ins]
+        for k, (_, op, _, target) in enumerate(ins):
+            if op not in ("s_branch", "s_endpgm") and k + 1 < len(ins):
+                before[k + 1].append(k)
+            if op.startswith(("s_branch", "s_cbranch")) and target in at:
+                before[at[target]].append(k)
+        count = next(k for k, (_, op, args, _) in enumerate(ins) if op == "global_atomic_add" and args.split()[-1] == "sc0")
+        todo, been = list(before[count]), set()
+        while todo:
+            k = todo.pop()
+            _, op, args, _ = ins[k]
+            if k in been or op == "s_barrier":
+                continue
+            been.add(k)
+            assert before[k] and not op.startswith(("global_load", "flat_load", "global_store")), f"{name} {ins[k][0]:#x}: {op} {args.strip()}"
+            todo += before[k]
+        seen += 1
+    assert seen == 1
