@@ -602,6 +602,7 @@ int csgs_grad_clip(const csgs_grad_list *l /*host*/, int kind, float max_norm, f
  *     y = alpha act(a w + bias) + beta r
  * with a [M x K], w [K x N] of `dtype`, bias [N] float, r and y [M x N] of `y_dtype`, all row-major, rows starting on any element.
  * act: the identity, max(z, 0), the logistic function s(z), z s(z), or z Phi(z) with the normal distribution's Phi.  One rounding per output.
+ * Floats are multiplied as three bfloat16 parts each, six of the nine products of these: of a product at most 1.001 2^-24 of it is left out, as much as a rounding, of either sign.
  * y may be r (same address and leading dimension); other overlaps are not allowed.  A row of y depends on its own rows of a and r alone.
  * With M_dev only rows below the device count are computed and written; a's rows past it may be read, whatever they hold.
  * Host errors: CSGS_EINVAL, CSGS_EUNSUPPORTED (types; 2^24 tiles of 64 by 64 and more).

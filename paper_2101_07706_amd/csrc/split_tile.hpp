@@ -1,11 +1,11 @@
 // A block's tile of a product of floats, on the bfloat16 matrix cores.
 //
-// A float is the sum of three bfloat16 numbers, exactly: its upper 16 bits h, the upper 16 bits m of x - h, and l = x - h - m, of which 8 bits are left.  Of the nine products of
-// two such sums the six with weights down to 2^-16 are formed,
-//     a b = ah bh + (ah bm + am bh) + (ah bl + am bm + al bh) + rest,     |rest| < 2^-23 |a b|, 2^-25 |a b| on average
-// (each by the matrix cores without a rounding, summed in float): a product costs six times 32 cycles a step of 16 k instead of 8 times 64 on the float cores.  ah bh has sums of its own,
-// the others share one set, which is added at the end: the large sums are rounded once for 16 k.  (Products down to 2^-149 keep what floats keep: the matrix cores take and
-// give numbers below 2^-126.)
+// A float is the sum of three bfloat16 numbers, exactly: itself rounded, h; what that leaves rounded, m; and l = x - h - m, of which 7 bits are left.  Rounded to nearest, for x in [1, 2)
+// |m| <= 2^-8 and |l| <= 2^-17.  Of the nine products of two such sums the six with weights down to 2^-16 are formed,
+//     a b = ah bh + (ah bm + am bh) + (ah bl + am bm + al bh) + rest,     |rest| = |am bl + al bm + al bl| <= 1.001 2^-24 |a b|, of either sign
+// (parts that are cut off, not rounded, leave up to 8 times as much, always of the product's sign; each product is formed by the matrix cores without a rounding and summed in float): a product
+// costs six times 32 cycles a step of 16 k instead of 8 times 64 on the float cores.  ah bh has sums of its own, the others share one set, which is added at the end: the large sums are
+// rounded once for 16 k.  (Products down to 2^-149 keep what floats keep: the matrix cores take and give numbers below 2^-126.)
 // Bound by six products and by the splitting in front of LDS (4001 rows of 602 by 1111, gated, with all gradients: 453 us on the float cores, 316 so with the same tiles, now 272, 118
 // TFLOP/s as floats count; relative error against 64 bits 1.2e-6 on the float cores, 2.7e-7 so).
 //
@@ -14,6 +14,8 @@
 #include "matrix_tile.hpp"
 
 namespace csgs {
+
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 
 template <int R, bool ACROSS, int NT>
 struct SplitSide {
@@ -48,16 +50,13 @@ struct SplitSide {
             u32x4 plane[3];
 #pragma unroll
             for (int e = 0; e < 8; e += 2) {
-                uint32_t part[2][3];
+                float x[2] = {held[i][e], held[i][e + 1]};
 #pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                    const float x = held[i][e + j], r = x - __uint_as_float(__float_as_uint(x) & 0xFFFF0000u);
-                    part[j][0] = __float_as_uint(x);
-                    part[j][1] = __float_as_uint(r);
-                    part[j][2] = __float_as_uint(r - __uint_as_float(__float_as_uint(r) & 0xFFFF0000u));
+                for (int q = 0; q < 3; ++q) {
+                    plane[q][e / 2] = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{x[0], x[1]}), bf16x2));
+                    x[0] -= __uint_as_float(plane[q][e / 2] << 16);
+                    x[1] -= __uint_as_float(plane[q][e / 2] & 0xFFFF0000u);
                 }
-#pragma unroll
-                for (int q = 0; q < 3; ++q) plane[q][e / 2] = __builtin_amdgcn_perm(part[1][q], part[0][q], 0x07060302u);      // (the upper halves)
             }
 #pragma unroll
             for (int q = 0; q < 3; ++q) *(u32x4 *)(lds + q * Layout::BYTES + (tid + i * NT) * 16) = plane[q];
