@@ -5,17 +5,20 @@
 //     a b = ah bh + (ah bm + am bh) + (ah bl + am bm + al bh) + rest,     |rest| = |am bl + al bm + al bl| <= 1.001 2^-24 |a b|, of either sign
 // (parts that are cut off, not rounded, leave up to 8 times as much, always of the product's sign; each product is formed by the matrix cores without a rounding and summed in float): a product
 // costs six times 32 cycles a step of 16 k instead of 8 times 64 on the float cores.  ah bh has sums of its own, the others share one set, which is added at the end: the large sums are
-// rounded once for 16 k.  (Products down to 2^-149 keep what floats keep: the matrix cores take and give numbers below 2^-126.)
+// rounded once for 16 k.  A bfloat16 number's lowest bit is 2^-133 at least, a float's 2^-149: operands are split 2^16 times as large, exactly, sums divided by 2^32 at the end, so that every
+// float has its parts, those below 2^-126 too (which the matrix cores take and give).
 // Bound by six products and by the splitting in front of LDS (4001 rows of 602 by 1111, gated, with all gradients: 453 us on the float cores, 316 so with the same tiles, now 272, 118
 // TFLOP/s as floats count; relative error against 64 bits 1.2e-6 on the float cores, 2.7e-7 so).
 //
-// x - h is NaN where x is not finite.  Sums that are not finite are formed again, by the float cores: those give what the inputs do.
+// The parts are not all finite where x is not, and from 2^112 on.  Sums that are not finite, as they are of such parts and from 2^96 on, are formed again, by the float cores: those give what
+// the inputs do.
 #pragma once
 #include "matrix_tile.hpp"
 
 namespace csgs {
 
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+constexpr float SPLIT_SCALE = 65536.0f, SPLIT_BACK = 1.0f / 65536.0f / 65536.0f;
 
 template <int R, bool ACROSS, int NT>
 struct SplitSide {
@@ -50,7 +53,7 @@ struct SplitSide {
             u32x4 plane[3];
 #pragma unroll
             for (int e = 0; e < 8; e += 2) {
-                float x[2] = {held[i][e], held[i][e + 1]};
+                float x[2] = {held[i][e] * SPLIT_SCALE, held[i][e + 1] * SPLIT_SCALE};
 #pragma unroll
                 for (int q = 0; q < 3; ++q) {
                     plane[q][e / 2] = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{x[0], x[1]}), bf16x2));
@@ -135,9 +138,12 @@ struct SplitTile : MatrixTile<float, BM, BN, WM, WN, A_ACROSS, B_ACROSS, NB, 128
         each_of<NB * TN * TM>([&](auto i) CSGS_INLINE { acc[i / (TN * TM)][i / TM % TN][i % TM] += second.acc[i / (TN * TM)][i / TM % TN][i % TM]; });
         Base::join(lds);
         each_of<NB * TN * TM>([&](auto i) CSGS_INLINE {
-            const f32x16 &x = acc[i / (TN * TM)][i / TM % TN][i % TM];
+            f32x16 &x = acc[i / (TN * TM)][i / TM % TN][i % TM];
 #pragma unroll
-            for (int r = 0; r < 16; ++r) bad |= !finite(x[r]);
+            for (int r = 0; r < 16; ++r) {
+                x[r] *= SPLIT_BACK;
+                bad |= !finite(x[r]);
+            }
         });
         return __syncthreads_or(bad);
     }

@@ -70,6 +70,25 @@ def test_gated_with_the_largest_parts(env):
         assert bool(((h.cpu().double() - want).abs() <= 2.01 * bound(K, K * x * x) * K * x * x + ULP * want).all()), hex(bits)
 
 
+# Operands near both ends of the range, whose products lie in it: every bit of every float counts, in numbers below 2^-126 as well.
+@pytest.mark.parametrize("size", [(3, 1, 5), (70, 40, 80), (5, 1024, 64), (2100, 40, 2060)], ids=str)
+@pytest.mark.parametrize("ends", [(1e-36, 1e3), (1e-38, 1e20), (3e-40, 1e30), (3e38, 1e-3), (1e34, 1e-34), (3.4e38, 0.0009), (2e-44, 3e38)], ids=str)
+def test_the_ends_of_the_range(env, size, ends):
+    csgs, dev = env
+    M, K, N = size
+    gen = torch.Generator().manual_seed(K)
+    near = lambda r, c, v: (v * (1 - 0.4 * torch.rand(r, c, generator=gen, dtype=torch.float64))).float()
+    for lo, hi in (ends, ends[::-1]):
+        A, W = near(M, K, lo), near(K, N, hi)
+        out = torch.zeros(M, N, device=dev)
+        csgs.csgs_linear(A.to(dev), W.to(dev), out)
+        want = A.double() @ W.double()
+        if float(want.max()) > 3.4e38:
+            continue
+        # (one more rounding for each product where they are formed by the float cores)
+        assert bool(((out.cpu().double() - want).abs() <= bound(K, want) + K * ULP * want).all())
+
+
 def test_the_largest_float_among_others(env):
     csgs, dev = env
     M, K, N = 70, 90, 40
