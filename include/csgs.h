@@ -675,6 +675,7 @@ int csgs_gated_grad(const csgs_gated_args *p /*host*/, const void *dh, int64_t l
  * (csgs_embed_grad_rows): with ids, row j of g belongs to row ids[j] of p, and the rows that no id names are left untouched,
  * their states among them.  ids outside [0, rows) are passed over; the others have to ascend strictly: a row of g whose id is not above the
  * one before it changes nothing and sets CSGS_ST_BAD_NODE_ID (further rows of g with one id may then leave a mix of their steps in its row).
+ * A run of ids that are passed over is looked at once more for the row behind it, about 500 of them in a microsecond; long ones are better left behind n_dev.
  *
  * States in 8 bits.  A row's entries are cut into blocks of CSGS_STATE_BLOCK (the last one may be shorter); a block keeps one byte,
  * the exponent field E of its largest value's float (0: the block is zero; 255: the block holds a value that is not finite, all of it reads

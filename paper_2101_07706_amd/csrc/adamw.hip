@@ -181,6 +181,48 @@ __device__ inline void store_codes(uint8_t *p, int n, uint32_t w)
     for (int i = 0; i < n; ++i) store_global<uint8_t>(p + i, (uint8_t)(w >> (8 * i)));
 }
 
+// The id in front of ids[j] that counts, the ones that are passed over left out, or -1: what ids[j] has to be above.  Usually its neighbour.  Behind a run of ids that are passed over a
+// lane looks at NEAR_IDS of them, then its whole wavefront at FAR_IDS at a time (us, 300 rows of 100 behind a million ids of -1: one by one
+// 116000, so 1800).  For all lanes of a wavefront.
+constexpr int NEAR_IDS = 8, FAR_STEPS = 4, FAR_IDS = FAR_STEPS * WAVE;
+__device__ inline int32_t id_before(const int32_t *ids, int64_t rows, int64_t j, bool ask)
+{
+    const auto counts = [&](int32_t id) { return id >= 0 && id < rows; };
+    int32_t before = -1;
+    int64_t k = ask ? j - 1 : -1;
+    for (int i = 0; i < NEAR_IDS && k >= 0; ++i, --k) {
+        const int32_t id = load_global<int32_t>(ids + k);
+        if (counts(id)) {
+            before = id;
+            k = -1;
+        }
+    }
+    for (uint64_t todo; (todo = __ballot(k >= 0)) != 0;) {
+        const int first = __builtin_ctzll(todo), lane = (int)threadIdx.x & (WAVE - 1);
+        const int64_t from = (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int32_t)k, first) |
+                                       (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int32_t)(k >> 32), first) << 32);
+        int32_t found = -1;
+        for (int64_t at = from; at >= 0 && found < 0; at -= FAR_IDS) {
+            int32_t id[FAR_STEPS];
+#pragma unroll
+            for (int i = 0; i < FAR_STEPS; ++i) {
+                const int64_t mine = at - i * WAVE - lane;
+                id[i] = mine >= 0 ? load_global<int32_t>(ids + mine) : -1;
+            }
+#pragma unroll
+            for (int i = 0; i < FAR_STEPS; ++i) {
+                const uint64_t some = __ballot(counts(id[i]));
+                if (found < 0 && some) found = __builtin_amdgcn_readlane(id[i], __builtin_ctzll(some));
+            }
+        }
+        if (k == from) {      // (all lanes of that row)
+            before = found;
+            k = -1;
+        }
+    }
+    return before;
+}
+
 // A lane's four entries of a segment.
 struct Place {
     int64_t row, block, state, at;    // row of p (-1: none), block of it; entry of the states and of the row
@@ -197,16 +239,13 @@ __device__ inline Place place_of(const AdamDesc &d, int64_t seg, int64_t live, i
         o.row = -1;
     } else if (d.ids) {
         const int32_t id = d.ids[j];
-        o.row = id;
-        if (id < 0 || id >= d.rows) {
+        o.row = id < d.rows ? id : -1;      // (below 0: none)
+    }
+    if (d.ids) {      // (two lanes that write one row would race)
+        const int32_t before = id_before(d.ids, d.rows, j, o.row >= 0);
+        if (o.row >= 0 && before >= o.row) {
             o.row = -1;
-        } else {      // (two lanes that write one row would race)
-            int64_t k = j - 1;
-            while (k >= 0 && (d.ids[k] < 0 || d.ids[k] >= d.rows)) --k;
-            if (k >= 0 && d.ids[k] >= id) {
-                o.row = -1;
-                if (status && lane == 0) atomicOr(status, CSGS_ST_BAD_NODE_ID);
-            }
+            if (status && lane == 0) atomicOr(status, CSGS_ST_BAD_NODE_ID);
         }
     }
     *g_row = j;

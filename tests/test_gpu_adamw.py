@@ -409,3 +409,54 @@ def test_two_lists_side_by_side(env):
     for ps, bs in zip(params, before):
         for p, b in zip(ps, bs):
             p.check(b, 1, 1e-2, 0.9, 0.999, 1e-8)
+
+
+def long_runs(gen, run, cols, dev):
+    """A table whose gradient's ids are passed over in runs of `run` and more, in front of and between rows that count, some of them named again behind a run."""
+    ids, keep = [-1] * run, []
+    for k, (id, again, gap) in enumerate([(3, False, run), (3, True, 9), (7, False, 8), (9, False, 1), (9, True, run + 1), (9, True, 0), (40, False, 300), (41, False, 255), (41, True, 256),
+                                          (60, False, run // 2), (50, True, 0), (400, False, run // 3)]):
+        if not again:
+            keep.append(len(ids))
+        ids += [id] + [[-1, 500, 2_000_000_000][k % 3]] * gap
+    p = torch.randn(500, cols, generator=gen).to(dev)
+    g = torch.randn(len(ids), cols, generator=gen).to(dev)
+    return p, g, torch.tensor(ids, dtype=torch.int32), keep
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("cols", [1, 4, 5, 64, 300])
+@pytest.mark.parametrize("run", [7, 64, 70, 300, 3000])
+def test_ids_behind_long_runs_that_are_passed_over(env, bits, cols, run):
+    """As the ids that count alone: whatever lies between them, each is taken once, and one that is not above the last of them is left out."""
+    csgs, dev = env
+    p, g, ids, keep = long_runs(torch.Generator().manual_seed(run), run, cols, dev)
+    got = []
+    for rows in (torch.arange(len(ids)), torch.tensor(keep)):
+        q, step, status = p.clone(), *(torch.zeros(1, dtype=torch.int32, device=dev) for _ in range(2))
+        state = csgs.adamw_states(q, bits)
+        csgs.csgs_adamw(csgs.make_adamw_list([csgs.adamw_entry(q, g[rows.to(dev)].contiguous(), **state, ids=ids[rows].to(dev))]), 1e-2, step, status=status)
+        got.append((q, *state.values()))
+        assert int(status) == (csgs.ST_BAD_NODE_ID if len(rows) == len(ids) else 0) and int(step) == 1
+    assert all(torch.equal(a, b) for a, b in zip(*got))
+    assert int((got[0][0] != p).any(1).sum()) == len(keep)
+
+
+def test_a_long_run_of_ids_costs_a_look_at_them(env):
+    """Rows behind a million ids that are passed over: the device looks at hundreds of them at a time (one by one they took 116 ms)."""
+    csgs, dev = env
+    run, rows, cols = 1_000_000, 300, 100
+    p, g = torch.zeros(500, cols, device=dev), torch.ones(1, cols, device=dev).expand(run + rows, cols).contiguous()
+    ids = torch.cat([torch.full((run,), -1, dtype=torch.int32), torch.arange(rows, dtype=torch.int32)]).to(dev)
+    step = torch.zeros(1, dtype=torch.int32, device=dev)
+    l = csgs.make_adamw_list([csgs.adamw_entry(p, g, **csgs.adamw_states(p), ids=ids)])
+    times = []
+    for _ in range(3):
+        e = [torch.cuda.Event(enable_timing=True) for _ in range(2)]
+        e[0].record()
+        csgs.csgs_adamw(l, 1e-2, step)
+        e[1].record()
+        torch.cuda.synchronize()
+        times.append(e[0].elapsed_time(e[1]))
+    assert int((p != 0).any(1).sum()) == rows
+    assert min(times) < 50.0, times
