@@ -603,9 +603,10 @@ int csgs_grad_clip(const csgs_grad_list *l /*host*/, int kind, float max_norm, f
  * with a [M x K], w [K x N] of `dtype`, bias [N] float, r and y [M x N] of `y_dtype`, all row-major, rows starting on any element.
  * act: the identity, max(z, 0), the logistic function s(z), z s(z), or z Phi(z) with the normal distribution's Phi.  One rounding per output.
  * Floats are multiplied as three bfloat16 parts each, six of the nine products of these: of a product at most 1.001 2^-24 of it is left out, as much as a rounding, of either sign.
- * y may be r (same address and leading dimension); other overlaps are not allowed.  A row of y depends on its own rows of a and r alone.
+ * y may be r (same address and leading dimension); other overlaps are refused, rows past the device count among them.  (Columns of one buffer lie apart.)  A row of y
+ * depends on its own rows of a and r alone.
  * With M_dev only rows below the device count are computed and written; a's rows past it may be read, whatever they hold.
- * Host errors: CSGS_EINVAL, CSGS_EUNSUPPORTED (types; 2^24 tiles of 64 by 64 and more).
+ * Host errors: CSGS_EINVAL, CSGS_EUNSUPPORTED (types; 2^24 tiles of 64 by 64 and more; a matrix that spans more than 2^40 bytes).
  */
 enum { CSGS_ACT_NONE = 0, CSGS_ACT_RELU = 1, CSGS_ACT_SIGMOID = 2, CSGS_ACT_SILU = 3, CSGS_ACT_GELU = 4 };
 
@@ -628,7 +629,7 @@ int csgs_linear(const csgs_linear_args *p /*host*/, void *y, int64_t ldy, void *
  *     da = t w^T [M x K], dw = a^T t [K x N] of dtype, dbias = column sums of t [N] float, dr = beta dy [M x N] of y_dtype
  * each nullable, not all of them.  Rows of a and dy past the device count add nothing, whatever they hold; those rows of da and dr are left untouched.
  * For dtype CSGS_BF16, t is rounded to bfloat16 between the products, dbias is summed from t before that.  Sums over rows are split into parts that
- * are added in a fixed order: two calls on the same input give the same bits.  dr may be dy (same leading dimension); other overlaps are not allowed.
+ * are added in a fixed order: two calls on the same input give the same bits.  dr may be dy (same leading dimension); other overlaps are refused.
  * scratch: device, 256-byte aligned, csgs_linear_grad_scratch_bytes(M, K, N, dtype) bytes (0 on bad input); nothing in it needs to be kept or
  * cleared between calls.  The size does not fall as M, K or N grow.
  * Host errors: CSGS_EINVAL (also: dbias or dr without the input it belongs to), CSGS_EWORKSPACE, CSGS_EUNSUPPORTED. */

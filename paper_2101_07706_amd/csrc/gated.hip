@@ -149,6 +149,16 @@ static int check(const csgs_gated_args *p, GatedArgs *a)
     return CSGS_OK;
 }
 
+// What both calls read, as memory.
+struct GatedMemory {
+    Memory x, wg, wu, bg, bu, count;
+    explicit GatedMemory(const csgs_gated_args *p)
+        : x(matrix_of(p->dtype, p->x, p->M, p->K, p->ldx)), wg(matrix_of(p->dtype, p->wg, p->K, p->N, p->ldwg)), wu(matrix_of(p->dtype, p->wu, p->K, p->N, p->ldwu)),
+          bg(vector_of(p->bg, p->N)), bu(vector_of(p->bu, p->N)), count(count_of(p->M_dev))
+    {
+    }
+};
+
 struct GatedScratch {
     void *t[2];
     float *columns[2], *parts;
@@ -181,7 +191,11 @@ extern "C" int csgs_gated(const csgs_gated_args *p, void *h, int64_t ldh, void *
     GatedArgs a;
     const int rc = check(p, &a);
     if (rc != CSGS_OK) return rc;
-    if (!h || ldh < p->N || !outputs_apart({p->x, p->wg, p->wu, p->bg, p->bu}, {h})) return CSGS_EINVAL;
+    if (!h || ldh < p->N) return CSGS_EINVAL;
+    const GatedMemory at(p);
+    const Memory out = matrix_of(p->dtype, h, p->M, p->N, ldh);
+    if (spans_too_much({at.x, at.wg, at.wu, out})) return CSGS_EUNSUPPORTED;
+    if (!outputs_apart({at.x, at.wg, at.wu, at.bg, at.bu, at.count}, {out})) return CSGS_EINVAL;
     a.h = h;
     a.ldh = ldh;
     int64_t parts;
@@ -202,10 +216,15 @@ extern "C" int csgs_gated_grad(const csgs_gated_args *p, const void *dh, int64_t
     if (rc != CSGS_OK) return rc;
     if (!dh || lddh < p->N || (dx && lddx < p->K) || (dwg && lddwg < p->N) || (dwu && lddwu < p->N)) return CSGS_EINVAL;
     if ((!dx && !dwg && !dwu && !dbg && !dbu) || (dbg && !p->bg) || (dbu && !p->bu)) return CSGS_EINVAL;
-    if (!outputs_apart({p->x, p->wg, p->wu, p->bg, p->bu, dh}, {dx, dwg, dwu, dbg, dbu})) return CSGS_EINVAL;
+    const GatedMemory at(p);
+    const Memory in = matrix_of(p->dtype, dh, p->M, p->N, lddh), out_x = matrix_of(p->dtype, dx, p->M, p->K, lddx), out_g = matrix_of(p->dtype, dwg, p->K, p->N, lddwg),
+                 out_u = matrix_of(p->dtype, dwu, p->K, p->N, lddwu), out_bg = vector_of(dbg, p->N), out_bu = vector_of(dbu, p->N);
+    if (spans_too_much({at.x, at.wg, at.wu, in, out_x, out_g, out_u})) return CSGS_EUNSUPPORTED;
+    if (!outputs_apart({at.x, at.wg, at.wu, at.bg, at.bu, at.count, in}, {out_x, out_g, out_u, out_bg, out_bu})) return CSGS_EINVAL;
     if (!scratch || ((uintptr_t)scratch & 255)) return CSGS_EINVAL;
     const GatedScratch s = carve_gated(scratch, p->M, p->K, p->N, p->dtype);
     if (scratch_bytes < s.bytes) return CSGS_EWORKSPACE;
+    if (!outputs_apart({at.x, at.wg, at.wu, at.bg, at.bu, at.count, in, out_x, out_g, out_u, out_bg, out_bu}, {Memory{scratch, 1, (int64_t)s.bytes, 0}})) return CSGS_EINVAL;
     hipStream_t st = (hipStream_t)stream;
     a.dh = dh;
     a.lddh = lddh;

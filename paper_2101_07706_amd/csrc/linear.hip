@@ -196,6 +196,15 @@ static int check(const csgs_linear_args *p, LinearArgs *a)
     return CSGS_OK;
 }
 
+// What both calls read, as memory.
+struct LinearMemory {
+    Memory a, w, bias, count;
+    explicit LinearMemory(const csgs_linear_args *p)
+        : a(matrix_of(p->dtype, p->a, p->M, p->K, p->lda)), w(matrix_of(p->dtype, p->w, p->K, p->N, p->ldw)), bias(vector_of(p->bias, p->N)), count(count_of(p->M_dev))
+    {
+    }
+};
+
 // Scratch of the gradient: t, rows of column sums, parts of the products.
 struct LinearScratch {
     void *t;
@@ -224,7 +233,12 @@ extern "C" int csgs_linear(const csgs_linear_args *p, void *y, int64_t ldy, void
     LinearArgs a;
     const int rc = check(p, &a);
     if (rc != CSGS_OK) return rc;
-    if (!y || ldy < p->N || (y == p->r && ldy != p->ldr) || !outputs_apart({p->a, p->w, p->bias}, {y})) return CSGS_EINVAL;
+    if (!y || ldy < p->N) return CSGS_EINVAL;
+    const LinearMemory at(p);
+    const Memory out = matrix_of(p->y_dtype, y, p->M, p->N, ldy), r = matrix_of(p->y_dtype, p->r, p->M, p->N, p->ldr);
+    if (y == p->r && ldy != p->ldr) return CSGS_EINVAL;
+    if (spans_too_much({at.a, at.w, out, r})) return CSGS_EUNSUPPORTED;
+    if (!outputs_apart({at.a, at.w, at.bias, at.count, y == p->r ? Memory{} : r}, {out})) return CSGS_EINVAL;
     a.y = y;
     a.ldy = ldy;
     int64_t parts;
@@ -245,10 +259,16 @@ extern "C" int csgs_linear_grad(const csgs_linear_args *p, const void *dy, int64
     if (rc != CSGS_OK) return rc;
     if (!dy || lddy < p->N || (da && ldda < p->K) || (dw && lddw < p->N) || (dr && lddr < p->N) || (!da && !dw && !dbias && !dr)) return CSGS_EINVAL;
     if ((dbias && !p->bias) || (dr && !p->r) || (dr == dy && lddr != lddy)) return CSGS_EINVAL;
-    if (!outputs_apart({p->a, p->w, p->bias}, {da, dw, dbias, dr}) || !outputs_apart({dy}, {da, dw, dbias})) return CSGS_EINVAL;
+    const LinearMemory at(p);
+    const Memory in = matrix_of(p->y_dtype, dy, p->M, p->N, lddy), out_a = matrix_of(p->dtype, da, p->M, p->K, ldda), out_w = matrix_of(p->dtype, dw, p->K, p->N, lddw),
+                 out_b = vector_of(dbias, p->N), out_r = matrix_of(p->y_dtype, dr, p->M, p->N, lddr);
+    if (spans_too_much({at.a, at.w, in, out_a, out_w, out_r})) return CSGS_EUNSUPPORTED;
+    const Memory dy_beside_dr = dr == dy ? Memory{} : in;
+    if (!outputs_apart({at.a, at.w, at.bias, at.count, dy_beside_dr}, {out_a, out_w, out_b, out_r})) return CSGS_EINVAL;
     if (!scratch || ((uintptr_t)scratch & 255)) return CSGS_EINVAL;
     const LinearScratch s = carve_linear(scratch, p->M, p->K, p->N, p->dtype);
     if (scratch_bytes < s.bytes) return CSGS_EWORKSPACE;
+    if (!outputs_apart({at.a, at.w, at.bias, at.count, in, out_a, out_w, out_b, out_r}, {Memory{scratch, 1, (int64_t)s.bytes, 0}})) return CSGS_EINVAL;
     hipStream_t st = (hipStream_t)stream;
     a.dy = dy;
     a.lddy = lddy;

@@ -1,5 +1,6 @@
 // Kernels of the feed-forward block's products: what they share (linear.hip, gated.hip, matrix_grad.hip).
 #pragma once
+#include "apart.hpp"
 #include "matrix_tile.hpp"
 
 namespace csgs {
@@ -96,18 +97,9 @@ __device__ CSGS_INLINE inline void form_sums(Tile &tile, char *lds, F sum)
 // ---------------------------------------------------------------- host side
 // Blocks of one launch: the device counts 32 bits of threads, of which a block has 256 where there are many.
 constexpr int64_t MOST_BLOCKS = (1 << 24) - 1;
-// Whether no output (null: not asked for) starts where an input or another output does.
-template <int NI, int NO>
-inline bool outputs_apart(const void *const (&in)[NI], const void *const (&out)[NO])
-{
-    for (int i = 0; i < NO; ++i) {
-        for (int j = 0; out[i] && j < NI; ++j)
-            if (out[i] == in[j]) return false;
-        for (int j = 0; out[i] && j < i; ++j)
-            if (out[i] == out[j]) return false;
-    }
-    return true;
-}
+inline Memory matrix_of(int dtype, const void *p, int64_t rows, int64_t cols, int64_t ld) { return matrix_memory(p, rows, cols, ld, dtype == CSGS_F32 ? 4 : 2); }
+inline Memory vector_of(const float *p, int64_t n) { return matrix_memory(p, 1, n, n, 4); }
+inline Memory count_of(const int32_t *p) { return matrix_memory(p, 1, 1, 1, 4); }
 // Whether tiles of `large` entries are the quicker ones: a compute unit's share of them, against tiles of `small` entries, which read LDS twice as often for a product and take
 // 1 / 0.85 of the time where both fill the device (us, gated gradient in floats: 4001 rows of 602 by 1111, 576 and 1134 tiles, 300 and 275; 5224 rows of 224 by 760, 492 and 984, 28 and 33).
 inline bool larger_tiles(int64_t tiles_large, int64_t large, int64_t tiles_small, int64_t small)

@@ -453,3 +453,31 @@ def test_other_stream_and_replayed_graphs_that_share_scratch(env):
         for name in got:
             assert torch.equal(got[name], want[name]), (i, name)
         assert float(want["dwg"].float().abs().sum()) > 0
+
+
+@pytest.mark.parametrize("tb", [F, B], ids=["f32", "bf16"])
+def test_matrices_in_the_columns_of_one_buffer(env, tb):
+    """Inputs and outputs side by side in each row of one buffer, as in buffers of their own."""
+    csgs, dev = env
+    M, K, N = 300, 72, 40
+    mk = Maker(dev, 9)
+    a, dy, w, w2, b = mk.matrix(M, K, tb), mk.matrix(M, N, tb), mk.matrix(K, N, tb, 0.1), mk.matrix(K, N, tb, 0.1), mk.vector(N)
+    scratch = torch.empty(csgs.csgs_gated_grad_scratch_bytes(M, K, N, elem(csgs, tb)), dtype=torch.uint8, device=dev)
+
+    def run(cut, both):
+        x, d, y, h, dx = cut
+        x.copy_(a)
+        d.copy_(dy)
+        dwg, dwu = both
+        csgs.csgs_linear(x, w, y, bias=b, r=d, act=csgs.ACT_SILU)
+        csgs.csgs_gated(x, w, w2, h)
+        csgs.csgs_gated_grad(x, w, w2, d, dx, dwg, dwu, None, None, scratch)
+        return [t.clone() for t in (y, h, dx, dwg, dwu)]
+    widths = [K, N, N, N, K]
+    one = torch.full((M, sum(widths) + 3), math.nan, dtype=tb, device=dev)
+    weights = torch.full((K, 2 * N), math.nan, dtype=tb, device=dev)
+    got = run(one[:, 1:-2].split(widths, 1), weights.split(N, 1))
+    want = run([torch.full((M, c), math.nan, dtype=tb, device=dev) for c in widths], [torch.zeros(K, N, dtype=tb, device=dev) for _ in range(2)])
+    for g, t in zip(got, want):
+        assert torch.equal(g, t)
+    assert bool(one[:, 0].isnan().all()) and bool(one[:, -2:].isnan().all())
