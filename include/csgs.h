@@ -730,10 +730,11 @@ typedef struct csgs_adamw_args {
 /* Bytes of device memory for a list of these tensors; 0 on bad input (n outside [1, 2^20], a tensor that csgs_adamw_list_init
  * would refuse). */
 size_t csgs_adamw_list_bytes(const csgs_adamw_tensor *t /*host*/, int32_t n);
-/* Writes the descriptions of the n tensors into l->base (kernels that carry them as arguments).  No two may share a parameter,
- * a copy or a state.
- * Host errors: CSGS_EINVAL (also: one address for two of those), CSGS_EWORKSPACE, CSGS_EUNSUPPORTED (dtype, state, more than 2^40 entries, ids
- * of more than 2^31 - 1 rows). */
+/* Writes the descriptions of the n tensors into l->base (kernels that carry them as arguments).  What a step writes of them (parameters, copies,
+ * states, exponents) lies apart from all else that the list names; gradients, ids and counts may be shared.  Columns of one buffer lie apart.
+ * Host errors: CSGS_EINVAL (also: memory of those that meets, but for a tensor's exponents and the rest of that tensor), CSGS_EWORKSPACE,
+ * CSGS_EUNSUPPORTED (dtype, state, more than 2^40 entries or bytes from one end to the other, ids of more than 2^31 - 1 rows, more than 2^26 pairs
+ * of matrices in each other's gaps). */
 int csgs_adamw_list_init(csgs_adamw_list *l /*host*/, const csgs_adamw_tensor *t /*host*/, int32_t n, void *stream);
 /* The step.  Two launches with clip, one without.  Where clip or total is given and the total is NaN or infinite, nothing is changed, *step
  * neither, and CSGS_ST_NONFINITE_GRAD is set.  Calls that share a list must be ordered on one stream.
@@ -742,7 +743,7 @@ int csgs_adamw(const csgs_adamw_list *l /*host*/, const csgs_adamw_args *a /*hos
 
 /* States in 8 bits, as values and back (checkpoints; a change of the kind): codes [rows x cols] with exps as above, `which` CSGS_STATE_FIRST (m)
  * or CSGS_STATE_SECOND (v; negative values and NaN in it read as: the former 0, the latter NaN), values [rows x cols] float with leading dimension ld.
- * Host errors: CSGS_EINVAL, CSGS_EUNSUPPORTED (more than 2^40 entries). */
+ * Host errors: CSGS_EINVAL (also: memory that meets), CSGS_EUNSUPPORTED (more than 2^40 entries). */
 int csgs_state_read(const uint8_t *codes, const uint8_t *exps, int which, int64_t rows, int64_t cols, float *values, int64_t ld, void *stream);
 int csgs_state_write(const float *values, int64_t ld, int which, int64_t rows, int64_t cols, uint8_t *codes, uint8_t *exps, void *stream);
 

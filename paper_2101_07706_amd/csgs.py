@@ -821,6 +821,12 @@ def adamw_states(p, bits=32):
     return {k: torch.zeros(rows, blocks if "exp" in k else cols, dtype=torch.uint8, device=p.device) for k in ("m", "v", "m_exp", "v_exp")}
 
 
+def _meet(a, b):
+    """Whether the memory that two tensors span meets."""
+    end = lambda t: t.data_ptr() + (sum((n - 1) * s for n, s in zip(t.shape, t.stride())) + 1) * t.element_size()  # noqa: E731
+    return a.data_ptr() < end(b) and b.data_ptr() < end(a)
+
+
 def adamw_entry(p, g, m, v, m_exp=None, v_exp=None, copy=None, ids=None, n_dev=None, weight_decay=0.0, lr_scale=1.0):
     """A parameter for make_adamw_list: p with its gradient g, states m and v (float32, or uint8 with exponents m_exp and v_exp: adamw_states), a bfloat16
     copy of p, for a table whose gradient holds rows alone their ids (strictly ascending), a device int32 with the number of rows of g that count."""
@@ -837,6 +843,7 @@ def adamw_entry(p, g, m, v, m_exp=None, v_exp=None, copy=None, ids=None, n_dev=N
     assert (m_exp is None) == (v_exp is None) == (not small), "exponents for states in 8 bits"
     for t in (m_exp, v_exp):
         assert t is None or (t.dtype is torch.uint8 and t.numel() == rows * blocks and t.is_contiguous()), f"uint8, {blocks} a row, contiguous"
+        assert t is None or not any(_meet(t, u) for u in (p, g, m, v, copy, m_exp if t is v_exp else v_exp) if u is not None), "exponents in memory of their own"
     ldcopy = 0
     if copy is not None:
         assert copy.dtype is torch.bfloat16 and copy.shape == p.shape, "a bfloat16 copy of the parameter's shape"

@@ -11,9 +11,8 @@
 // those lanes.  g' = c g, m and v are formed in double (eight operations): which of two codes a state next to their border gets does then not
 // depend on how c g was rounded.
 #include <math.h>
-#include <algorithm>
 #include <new>
-#include <vector>
+#include "apart.hpp"
 #include "common.hpp"
 #include "grad_list.hpp"
 #include "row_pieces.hpp"
@@ -486,22 +485,44 @@ static int describe(const csgs_adamw_tensor &t, int64_t *tiles, AdamDesc *d)
     return *tiles > ADAM_ENTRIES / CSGS_STATE_BLOCK ? CSGS_EUNSUPPORTED : CSGS_OK;
 }
 
-// Checks and counts all of a list's tensors.  What a step writes belongs to one of them: two that share an address would be written by two blocks at once.
+// What a step reads and writes of tensor i.  (A tensor's own exponents are not compared with the rest of it: whoever allocates them knows them from its entries.)
+static bool hold(const csgs_adamw_tensor &t, int32_t i, std::vector<Held> &all)
+{
+    const bool small = t.state == CSGS_STATE_8BIT;
+    const int64_t blocks = (t.cols + CSGS_STATE_BLOCK - 1) / CSGS_STATE_BLOCK, p = t.p_dtype == CSGS_F32 ? 4 : 2, g = t.g_dtype == CSGS_F32 ? 4 : 2, state = small ? 1 : 4;
+    const Held held[] = {
+        {matrix_memory(t.p, t.rows, t.cols, t.ldp, p), i, true, false},
+        {matrix_memory(t.copy, t.rows, t.cols, t.ldcopy, 2), i, true, false},
+        {matrix_memory(t.m, t.rows, t.cols, t.cols, state), i, true, false},
+        {matrix_memory(t.v, t.rows, t.cols, t.cols, state), i, true, false},
+        {matrix_memory(t.m_exp, t.rows, blocks, blocks, 1), i, true, true},
+        {matrix_memory(t.v_exp, t.rows, blocks, blocks, 1), i, true, true},
+        {matrix_memory(t.g, t.n, t.cols, t.ldg, g), i, false, false},
+        {matrix_memory(t.ids, 1, t.n, t.n, 4), i, false, false},
+        {matrix_memory(t.n_dev, 1, 1, 1, 4), i, false, false},
+    };
+    for (const Held &h : held) {
+        if (!h.at.p) continue;
+        if (spans_too_much(h.at)) return false;
+        all.push_back(h);
+    }
+    return true;
+}
+// Checks and counts all of a list's tensors.  What a step writes belongs to one of them and lies apart from what it reads: two blocks would write it at once, or one read it late.
 static int describe_all(const csgs_adamw_tensor *t, int32_t n, int64_t *tiles)
 {
     *tiles = 0;
     AdamDesc d;
     try {
-        std::vector<const void *> written;
-        written.reserve((size_t)n * 6);
+        std::vector<Held> all;
+        all.reserve((size_t)n * 9);
         for (int32_t i = 0; i < n; ++i) {
             const int rc = describe(t[i], tiles, &d);
             if (rc != CSGS_OK) return rc;
-            for (const void *p : {(const void *)t[i].p, (const void *)t[i].copy, (const void *)t[i].m, (const void *)t[i].v, (const void *)t[i].m_exp, (const void *)t[i].v_exp})
-                if (p) written.push_back(p);
+            if (!hold(t[i], i, all)) return CSGS_EUNSUPPORTED;
         }
-        std::sort(written.begin(), written.end());
-        return std::adjacent_find(written.begin(), written.end()) == written.end() ? CSGS_OK : CSGS_EINVAL;
+        const Lie lie = all_apart(all);
+        return lie == Lie::APART ? CSGS_OK : lie == Lie::MEET ? CSGS_EINVAL : CSGS_EUNSUPPORTED;
     } catch (const std::bad_alloc &) {
         return CSGS_EWORKSPACE;
     }
@@ -584,7 +605,11 @@ extern "C" int csgs_adamw(const csgs_adamw_list *l, const csgs_adamw_args *a, vo
 static int state_ok(const void *codes, const void *exps, const void *values, int which, int64_t rows, int64_t cols, int64_t ld)
 {
     if (!codes || !exps || !values || rows <= 0 || cols <= 0 || ld < cols || (which != CSGS_STATE_FIRST && which != CSGS_STATE_SECOND)) return CSGS_EINVAL;
-    return rows > ADAM_ENTRIES / cols ? CSGS_EUNSUPPORTED : CSGS_OK;
+    if (rows > ADAM_ENTRIES / cols) return CSGS_EUNSUPPORTED;
+    const int64_t blocks = (cols + CSGS_STATE_BLOCK - 1) / CSGS_STATE_BLOCK;
+    const Memory c = matrix_memory(codes, rows, cols, cols, 1), e = matrix_memory(exps, rows, blocks, blocks, 1), v = matrix_memory(values, rows, cols, ld, 4);
+    if (spans_too_much({c, e, v})) return CSGS_EUNSUPPORTED;
+    return outputs_apart({}, {c, e, v}) ? CSGS_OK : CSGS_EINVAL;
 }
 static dim3 state_grid(int64_t segs, int bits)
 {

@@ -3,6 +3,8 @@
 #include <stdint.h>
 #include <algorithm>
 #include <initializer_list>
+#include <tuple>
+#include <vector>
 
 namespace csgs {
 
@@ -65,6 +67,41 @@ inline bool spans_too_much(const std::initializer_list<Memory> &all)
     for (const Memory &m : all)
         if (spans_too_much(m)) return true;
     return false;
+}
+
+// Memory of one of many tensors.
+struct Held {
+    Memory at;
+    int32_t owner;
+    bool written, beside;      // beside: not compared with its owner's other memory
+};
+enum class Lie { APART, MEET, TOO_MANY };
+// Whether what is written lies apart from everything else; what is only read may be shared.  In the order of the first bytes, each is compared with those before it that have not ended: columns
+// of one buffer are compared in pairs, MOST_PAIRS of them at most.
+constexpr int64_t MOST_PAIRS = 1ll << 26;
+inline Lie all_apart(std::vector<Held> &all)
+{
+    const auto key = [](const Held &h) { return std::make_tuple((uintptr_t)h.at.p, h.written, h.at.rows, h.at.width, h.at.step); };
+    std::sort(all.begin(), all.end(), [&](const Held &a, const Held &b) { return key(a) < key(b); });
+    std::vector<const Held *> open[2];       // read, written
+    int64_t pairs = 0;
+    for (size_t i = 0; i < all.size(); ++i) {
+        const Held &h = all[i];
+        if (!h.written && i > 0 && key(h) == key(all[i - 1])) continue;
+        for (int w = h.written ? 0 : 1; w < 2; ++w) {
+            size_t kept = 0;
+            for (const Held *o : open[w]) {
+                if (memory_end(o->at) <= (uintptr_t)h.at.p) continue;
+                open[w][kept++] = o;
+                if (o->owner == h.owner && (o->beside || h.beside)) continue;
+                if (++pairs > MOST_PAIRS) return Lie::TOO_MANY;
+                if (memory_meets(o->at, h.at)) return Lie::MEET;
+            }
+            open[w].resize(kept);
+        }
+        open[h.written].push_back(&h);
+    }
+    return Lie::APART;
 }
 
 }  // namespace csgs

@@ -123,3 +123,86 @@ def test_memory_that_no_device_has():
         assert L.csgs_linear(C.byref(linear(M=40, **kw)), 1 << 20, 5, None) == csgs.EUNSUPPORTED, kw
     assert L.csgs_linear(C.byref(linear(M=40)), 1 << 20, 1 << 62, None) == csgs.EUNSUPPORTED
     assert L.csgs_gated(C.byref(gated(M=40, ldx=1 << 50)), 1 << 20, 5, None) == csgs.EUNSUPPORTED
+
+
+WRITTEN = ["p", "copy", "m", "v", "m_exp", "v_exp"]
+
+
+def tensor(base, **kw):
+    """A parameter of 40 x 300 bfloat16 with states in 8 bits, its memory 64 KB apart from `base` on."""
+    at = {k: base + 64 * KB * i for i, k in enumerate(WRITTEN + ["g", "ids", "n_dev"])}
+    t = dict(at, rows=40, cols=300, n=40, ldp=300, ldcopy=300, ldg=300, p_dtype=1, g_dtype=1, state=1, weight_decay=0.0, lr_scale=1.0, reserved=0)
+    t.update(kw)
+    return csgs.AdamwTensor(*[t[k] for k, _ in csgs.AdamwTensor._fields_])
+
+
+SPAN = dict(p=24_000, copy=24_000, m=12_000, v=12_000, m_exp=80, v_exp=80, g=24_000, ids=160, n_dev=4)
+
+
+def answer(*tensors):
+    L = csgs.lib()
+    ts = (csgs.AdamwTensor * len(tensors))(*tensors)
+    if L.csgs_adamw_list_bytes(ts, len(ts)) > 0:
+        return csgs.OK
+    l = csgs.AdamwList(4096, 1 << 40, 0, 0, 0)
+    rc = L.csgs_adamw_list_init(C.byref(l), ts, len(ts), None)
+    assert rc != csgs.OK and l.ready == 0
+    return rc
+
+
+@pytest.mark.parametrize("mine", list(SPAN))
+def test_lists_whose_tensors_share_part_of_their_memory(mine):
+    one, base = tensor(64 * KB), 1024 * KB
+    assert answer(one, tensor(base)) == csgs.OK
+    for theirs in SPAN:
+        at = getattr(one, theirs)
+        for address in (at, at + SPAN[theirs] - 4, at + 4 - SPAN[mine], at + (SPAN[theirs] - SPAN[mine]) // 8 * 4):
+            want = csgs.EINVAL if mine in WRITTEN or theirs in WRITTEN else csgs.OK
+            assert answer(one, tensor(base, **{mine: address})) == want and answer(tensor(base, **{mine: address}), one) == want, (theirs, address - at)
+        for address in (at + SPAN[theirs], at - SPAN[mine]):
+            assert answer(one, tensor(base, **{mine: address})) == csgs.OK, (theirs, address - at)
+
+
+def test_tensors_whose_own_memory_meets():
+    for a, b in (("p", "copy"), ("p", "m"), ("m", "v"), ("copy", "v"), ("p", "g"), ("m", "g"), ("p", "ids"), ("v", "n_dev")):
+        one = tensor(64 * KB)
+        assert answer(tensor(64 * KB, **{b: getattr(one, a) + 600})) == csgs.EINVAL, (a, b)
+
+
+def test_lists_over_the_columns_of_one_buffer():
+    """Parts of one matrix, of its copy and of its gradient; the same gradient and the same count for several."""
+    base, L = 1 << 30, csgs.lib()
+    cut = lambda i, first, **kw: tensor(base * (i + 2), p=base + 2 * first, ldp=900, g=4 * KB, n_dev=2 * KB, **kw)  # noqa: E731
+    assert answer(cut(0, 0), cut(1, 300), cut(2, 600)) == csgs.OK
+    assert answer(cut(0, 0), cut(1, 299), cut(2, 600)) == csgs.EINVAL
+    assert answer(cut(0, 0), cut(1, 300), cut(2, 601)) == csgs.EINVAL
+    assert answer(cut(0, 0), tensor(base * 9, g=base + 600, ldg=900)) == csgs.OK and answer(cut(0, 0), tensor(base * 9, g=base + 598, ldg=900)) == csgs.EINVAL
+    # many tensors with one count; more interleaved ones than are compared in pairs
+    n = 100_000
+    ts = (csgs.AdamwTensor * n)(*[tensor((i + 2) << 20, n_dev=4096) for i in range(n)])
+    assert L.csgs_adamw_list_bytes(ts, n) > 0
+    n = 12_000
+    ts = (csgs.AdamwTensor * n)(*[tensor((i + 2) << 40, p=base + 2 * i, cols=1, ldp=n, ldg=1, copy=0) for i in range(n)])
+    assert L.csgs_adamw_list_bytes(ts, n) == 0 and L.csgs_adamw_list_init(C.byref(csgs.AdamwList(4096, 1 << 40, 0, 0, 0)), ts, n, None) == csgs.EUNSUPPORTED
+    assert L.csgs_adamw_list_bytes(ts, 3000) > 0
+    assert answer(tensor(base, ldp=1 << 50)) == csgs.EUNSUPPORTED
+
+
+def test_states_on_their_values():
+    L = csgs.lib()
+    codes, exps, values = 64 * KB, 128 * KB, 256 * KB          # 40 x 300
+    for c, e, v in ((values + 47_996, exps, values), (values - 11_999, exps, values), (codes, values + 100, values), (codes, codes + 11_999, values), (codes, codes - 79, values)):
+        assert L.csgs_state_read(c, e, 0, 40, 300, v, 300, None) == csgs.EINVAL and L.csgs_state_write(v, 300, 0, 40, 300, c, e, None) == csgs.EINVAL
+    assert L.csgs_state_read(codes, exps, 0, 40, 300, values, 1 << 50, None) == csgs.EUNSUPPORTED
+
+
+def test_binding_sees_exponents_on_their_tensor():
+    import torch
+    p, both = torch.zeros(4, 300), torch.zeros(4 * 300 + 16, dtype=torch.uint8)
+    s = csgs.adamw_states(p, 8)
+    csgs.adamw_entry(p, p.clone(), **s)
+    for k in ("m_exp", "v_exp"):
+        for bad in (s["m"].view(-1)[8:16].view(4, 2), p.view(torch.uint8).view(-1)[100:108].view(4, 2), both[1196:1204].view(4, 2)):
+            with pytest.raises(AssertionError):
+                csgs.adamw_entry(p, p.clone(), **{**s, "v": both[:1200].view(4, 300), k: bad})
+    csgs.adamw_entry(p, p.clone(), **{**s, "v": both[:1200].view(4, 300), "m_exp": both[1200:1208].view(4, 2), "v_exp": both[1208:].view(4, 2)})
