@@ -628,7 +628,8 @@ int csgs_linear(const csgs_linear_args *p /*host*/, void *y, int64_t ldy, void *
  * t = alpha dy .* act'(a w + bias):
  *     da = t w^T [M x K], dw = a^T t [K x N] of dtype, dbias = column sums of t [N] float, dr = beta dy [M x N] of y_dtype
  * each nullable, not all of them.  Rows of a and dy past the device count add nothing, whatever they hold; those rows of da and dr are left untouched.
- * For dtype CSGS_BF16, t is rounded to bfloat16 between the products, dbias is summed from t before that.  Sums over rows are split into parts that
+ * For dtype CSGS_BF16, t is rounded to bfloat16 between the products, a float dy with it (who needs more of dy takes a and w as floats); dbias is
+ * summed from t before that.  Sums over rows are split into parts that
  * are added in a fixed order: two calls on the same input give the same bits.  dr may be dy (same leading dimension); other overlaps are refused.
  * scratch: device, 256-byte aligned, csgs_linear_grad_scratch_bytes(M, K, N, dtype) bytes (0 on bad input); nothing in it needs to be kept or
  * cleared between calls.  The size does not fall as M, K or N grow.

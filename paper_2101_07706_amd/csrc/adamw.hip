@@ -2,8 +2,8 @@
 //
 // Every entry is read and written once: p, g, m, v in, p, m, v (and a bfloat16 copy of p) out, 28 bytes an entry with float states and 16 with
 // states in 8 bits, and some 60 operations: bound by memory where the tensors are long, by one launch (two with clipping) and a chain of four
-// loads (tile, description, row, entries) where they are short.  (100 M entries with bfloat16 gradients and copies, clipped: 579 us with the pass for the norm, 4.9 TB/s; 51 M with states in 8
-// bits 255 us, 3.2 TB/s: their codes cost as many operations as the step; a toy network 11 us.)  Clipping costs no pass of its own: the blocks join what grad_norm_k left and
+// loads (tile, description, row, entries) where they are short.  (100 M entries with bfloat16 gradients and copies, clipped: 581 us with the pass for the norm, 4.9 TB/s; 51 M with
+// states in 8 bits 253 us, 3.2 TB/s: their codes cost as many operations as the step; a toy network 11 us, both launches.)  Clipping costs no pass of its own: the blocks join what grad_norm_k left and
 // multiply g by the factor here.
 //
 // A piece of work is a segment: up to 256 entries of a row, four a lane, by 1 << lane_bits lanes (the fewest that hold a row, at most a wavefront).
@@ -20,7 +20,7 @@
 namespace csgs {
 
 constexpr int ADAM_U = 2;              // segments of a thread in one tile, all asked for before the first is worked on
-constexpr int ADAM_BLOCKS = 1024;      // what the device holds at once (us, 51 M entries with 8-bit states: 1024 473, 2048 475, 8192 485)
+constexpr int ADAM_BLOCKS = 1024;      // what the device holds at once (us, the kernel alone, 1024, 2048 and 8192: 51 M entries with 8-bit states 253, 255 and 268, 120 K rows of a table 108, 110 and 124)
 constexpr int64_t ADAM_ENTRIES = 1ll << 40;
 
 struct AdamDesc {

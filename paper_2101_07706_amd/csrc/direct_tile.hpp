@@ -6,7 +6,7 @@
 // end of a row by an offset that is never inside.
 //
 // Bound by the matrix cores' rate at the clock that they leave (1.6 - 1.9 GHz) and by what of the copies is not hidden.  Measured on 65536 rows of 4096 by 1024: tiles of 128 by 128 by way of
-// registers 835 us; 256 by 256 copied straight, four wavefronts, 614; eight wavefronts, two on each of the unit's four cores, 523 (1051 TFLOP/s; a large library product of
+// registers 835 us; 256 by 256 copied straight, four wavefronts, 614; eight wavefronts, two on each of the unit's four cores, 521 (1056 TFLOP/s; a large library product of
 // these sizes reaches 1254).  Chunks of 32 k in three or four buffers, and two blocks of 128 rows a compute unit, were no faster.
 //
 // A chunk of 64 k is four steps.  A step's fragments are read from LDS while the products of the step before are formed; one wait and one barrier a chunk, in front of

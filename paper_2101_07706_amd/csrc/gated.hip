@@ -1,12 +1,12 @@
 // csgs_gated: h = act(x wg + bg) .* (x wu + bu), and its gradient.
 //
 // Both projections in one kernel: a tile of x serves both products, whose entries meet in one lane's registers, so that neither g nor u (8 M N bytes each way in floats) reaches memory.
-// 4 M K N operations, bound by the matrix cores and their clock (65536 rows of 1024 by 4096 in bfloat16: 1050 us, 1047 TFLOP/s); a single row is bound by the weights' bytes and the way through a
+// 4 M K N operations, bound as csgs_linear (65536 rows of 1024 by 4096 in bfloat16: 1117 us, 985 TFLOP/s, 1157 on a slower card; matrix cores busy 49 % of the cycles at 1.7 GHz); a single row is bound by the weights' bytes and the way through a
 // tile's sum (16.8 MB, 11.5 us).
 //
 // Gradient: g and u formed again (4 M K N beside the 8 M K N of dx, dwg and dwu), tg = dh .* u .* act'(g) and tu = dh .* act(g) written once in the operands' type (for bfloat16 a
 // rounding of half a step, 2^-8 relative, of each term, which the matrix cores ask for), their column sums from registers before that; dx as one sum over both pairs, dwg and dwu
-// by one launch (65536 rows: 3130 us, 1054 TFLOP/s).
+// by one launch (65536 rows: 3146 us, 1049 TFLOP/s, 3317 on a slower card).
 #include "products.hpp"
 #include "direct_tile.hpp"
 #include "split_tile.hpp"
@@ -113,7 +113,8 @@ static int launch_types(const GatedArgs &p, int64_t *parts, hipStream_t st)
     const auto tiles = [&](int64_t m, int64_t n) { return (p.M + m - 1) / m * ((p.N + n - 1) / n); };
     // Tiles of 256 rows by 128 columns of both matrices, one block a compute unit, where smaller ones would need a second round (us, 1024 by 1024, large and small: 3200 rows 29 and 25, 4800
     // rows 30 and 37, 8192 rows 37 and 50); for the gradient, which writes twice as much and reads dh, of 128 rows, two blocks: one forms
-    // products while the other writes (us, 65536 rows of 1024 by 4096: forward 1043 and 1092, gradient with its products 3182 and 3121).
+    // products while the other writes (us, 65536 rows of 1024 by 4096: forward 1043 and 1092, gradient with its products 3182 and 3121; on another card
+    // 1109 and 1101, 3205 and 3136).
     if constexpr (sizeof(T) == 2)
         if (tiles(256, 128) > 128 && direct_operand(p.x, false, p.M, p.K, 256) && direct_operand(p.w[0], true, p.N, p.K, 128) && direct_operand(p.w[1], true, p.N, p.K, 128))
             return launch_shape<std::conditional_t<GRAD, DirectTile<128, 128, 2, 2, false, true, 2, 64, 3>, DirectTile<256, 128, 2, 4, false, true, 2, 128, 2>>, T, GRAD>(p, parts, st);

@@ -1,8 +1,8 @@
 // csgs_linear: y = alpha act(a w + bias) + beta r, and its gradient.
 //
-// One product with its epilogue: a, w and r are read and y is written once, 2 M K N operations.  For wide layers the matrix cores bound it, and under them the clock, which falls to 1.6 -
-// 1.9 GHz as they fill (65536 rows of 4096 by 1024 in bfloat16: 523 us, 1051 TFLOP/s; matrix cores busy 45 - 65 % of the cycles); for narrow ones (K or N up to some hundred) the
-// rows' bytes, for few rows the launch and the way through a tile's sum (one row of 1024 by 1024: 8 us).
+// One product with its epilogue: a, w and r are read and y is written once, 2 M K N operations.  For wide layers bound by the matrix cores, by the clock under them, and by what of a
+// tile's copies and outputs nothing hides (65536 rows of 4096 by 1024 in bfloat16: 521 us, 1056 TFLOP/s, 542 on a slower card; matrix cores busy 54 % of the cycles at 1.6 GHz with the
+// counters on); for narrow ones (K or N up to some hundred) by the rows' bytes, for few rows by the launch and the way through a tile's sum (one row of 1024 by 1024: 8 us).
 //
 // Gradient, t = alpha dy .* act'(a w + bias): act' needs the product again (4 M K N are da and dw, 2 M K N this), which is cheaper than 4 bytes of each entry kept in the forward pass and leaves
 // the forward call nothing to keep.  t is written once, in the operands' type: for bfloat16 a rounding of half a step, 2^-8 relative, of each term of da and dw, which the

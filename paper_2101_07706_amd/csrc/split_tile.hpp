@@ -7,8 +7,10 @@
 // costs six times 32 cycles a step of 16 k instead of 8 times 64 on the float cores.  ah bh has sums of its own, the others share one set, which is added at the end: the large sums are
 // rounded once for 16 k.  A bfloat16 number's lowest bit is 2^-133 at least, a float's 2^-149: operands are split 2^16 times as large, exactly, sums divided by 2^32 at the end, so that every
 // float has its parts, those below 2^-126 too (which the matrix cores take and give).
-// Bound by six products and by the splitting in front of LDS (4001 rows of 602 by 1111, gated, with all gradients: 453 us on the float cores, 316 so with the same tiles, now 272, 118
-// TFLOP/s as floats count; relative error against 64 bits 1.2e-6 on the float cores, 2.7e-7 so).
+// Bound by six products and by the splitting in front of LDS, 13 operations for two entries, which each block does for itself between two barriers (4001 rows of 602 by 1111, gated, with all
+// gradients: 453 us on the float cores, 282 so, 114 TFLOP/s as floats count, 292 on a slower card; relative error against 64 bits 1.2e-6 on the float cores, 2.5e-7 so; 8192 rows of 1024 by
+// 256 41 us, 105 TFLOP/s; 32768 rows of 1024 by 1024 404 us, 170).  The scale costs 2 to 4 % of that.  Two sets of sums and the pieces on their way take 219 to 242 of the 256 registers that two
+// blocks a compute unit leave a lane; LDS would hold more (48 KB of 160 at 128 by 128).
 //
 // The parts are not all finite where x is not, and from 2^112 on.  Sums that are not finite, as they are of such parts and from 2^96 on, are formed again, by the float cores: those give what
 // the inputs do.
